@@ -79,6 +79,7 @@ typedef int32_t vt_status;
 #define VT_DEV_KV_OVERFLOW 1u     /* a kernel saw a KV length at or past capacity and skipped */
 #define VT_DEV_WAIT_TIMEOUT 2u    /* a kernel gave up waiting on an asynchronous copy */
 #define VT_DEV_BAD_TOKEN 4u       /* the embedding gather saw a token id outside [0, vocab) */
+#define VT_DEV_BAD_PAGE 8u        /* a page table holds an id outside [0, n_pages) where a page is needed */
 
 typedef void* vt_stream; /* a cudaStream_t; NULL is the legacy default stream */
 
@@ -557,6 +558,105 @@ VT_API vt_status vt_test_wait_limit(int32_t form, uint32_t* status, vt_stream st
  * in chunks of 1024.  Every shard must be fp16: VT_ERR_STATE when one is block-quantized. */
 VT_API vt_status vt_prefill_tokens(const vt_partition* part, vt_kv* kv, const void* x_in, int32_t n,
                             void* x_out, vt_stream stream);
+
+/* ---------------------------------------------------------------- paged KV cache ---------------
+ * Several sequences served at once from one pool of pages (Section 2.1, "LLM Inference": the KV
+ * cache that prefill fills and every decode step appends to; Section 3.2.1: a device's shard of the
+ * attention heads, whose K and V these calls hold).  A vt_kv holds one sequence in memory reserved
+ * for its longest length; here each sequence has as many pages as it needs, anywhere in the pool.
+ *
+ * The pool, the page tables, the lengths and all rows are the caller's device buffers, one pool per
+ * (layer, shard); tables, lengths and starts serve every layer.  The values, q, k, v and the outputs
+ * have the pool's dtype; sums, softmax statistics and the rotation are fp32.
+ *
+ * Sequence b holds lens[b] positions before a call.  Its new rows are rows starts[b] ..
+ * starts[b + 1] - 1 of the call's row arrays (starts NULL: the one row b) and sit at positions
+ * lens[b], lens[b] + 1, ...  Position p of sequence b is entry p % page_size of page
+ * tables[b][p / page_size].  The usual order in a layer is vt_paged_append, then vt_paged_decode or
+ * vt_paged_prefill with the same batch, whose rows attend to their own keys too; the caller adds the
+ * new rows to lens once per step, after the last layer.  lens[b] < 0 marks an idle slot of the batch:
+ * nothing of it is stored and its output rows are zeros.  Several tables may share pages (a common
+ * prefix), as long as no two sequences append to the same entry.
+ *
+ * Nothing about the lengths or tables is known on the host, so all three calls can be captured into
+ * a CUDA graph.  What only a kernel can see sets bits in the status word of the vt_paged
+ * (vt_paged_status), and the offending entry is skipped: VT_DEV_KV_OVERFLOW for a position at or past
+ * pages_per_seq * page_size (or past the rotation table), VT_DEV_BAD_PAGE for a page id outside
+ * [0, n_pages) where a page is needed.  starts outside [0, n_rows] are clamped into it.  Entries of
+ * a table past a sequence's last page, and pool entries that no sequence holds, are never used and
+ * may hold anything.
+ * Errors of all: VT_ERR_INVALID_ARG (null pointers, sizes out of range, a pointer that is not 16-byte
+ * aligned, a stride that is not a multiple of 8 elements), VT_ERR_SHAPE (unsupported dtype, d_head,
+ * page_size or heads), before anything is enqueued. */
+typedef enum { VT_F16 = 0, VT_BF16 = 1 } vt_dtype; /* IEEE binary16, bfloat16 */
+
+/* One layer's K and V of one shard.  Entry (page, head, position in the page) begins at element
+ * page * page_stride + head * head_stride + position * pos_stride of k and of v, d_head contiguous
+ * values; so pools [page][head][position][d_head] and [page][position][head][d_head] both serve. */
+typedef struct {
+    void *k, *v;
+    int32_t dtype;      /* vt_dtype */
+    int32_t n_pages;
+    int32_t page_size;  /* positions per page, a power of two in [1, 1024] */
+    int32_t n_kv_heads;
+    int32_t d_head;     /* 64 or 128 */
+    int64_t page_stride, head_stride, pos_stride; /* elements, multiples of 8 */
+} vt_paged_pool;
+
+typedef struct {
+    const int32_t* tables; /* device [n_seqs][pages_per_seq] page ids */
+    const int32_t* lens;   /* device [n_seqs] */
+    const int32_t* starts; /* device [n_seqs + 1], or NULL: one row per sequence */
+    int32_t n_seqs, pages_per_seq; /* pages_per_seq * page_size <= 2^30 */
+} vt_paged_batch;
+
+typedef struct vt_paged vt_paged;
+
+/* Library plumbing: the workspace (partial results of sequences that several CTAs share) and the
+ * status word of the paged calls, on the current device.  One vt_paged serves any pools and batches;
+ * calls that use it must be ordered (one stream, or events).  vt_paged_create synchronizes `stream`;
+ * vt_paged_status synchronizes the device, clear != 0 resets the word. */
+VT_API vt_status vt_paged_create(const vt_allocator* allocator, vt_stream stream, vt_paged** out);
+VT_API void vt_paged_destroy(vt_paged* paged);
+VT_API vt_status vt_paged_status(vt_paged* paged, uint32_t* flags, int32_t clear);
+
+/* Library plumbing for vt_paged_append: the rotation table of Section 2.1's rotary positions,
+ * table[p][i] = (cos, sin) of the angle p * theta^(-2 i / d_head), device fp32
+ * [max_seq][d_head / 2][2], computed in fp64.  A caller may fill such a table otherwise (scaled
+ * frequencies; (1, 0) for pairs that are not rotated). */
+VT_API vt_status vt_rope_table(float* table, int32_t max_seq, int32_t d_head, double theta, vt_stream stream);
+
+/* vt_paged_append (Section 2.1, decode and prefill phases: K/V written to the cache): row r of
+ * sequence b at position p:
+ *   k[r], rotated by row p of `rope`, and v[r] are written to their entry of the pool;
+ *   q_out[r] = q[r] rotated by row p of `rope`.
+ * The rotation pairs dimensions i and i + d_head / 2 of every head.  q [n_rows][n_heads][d_head],
+ * k and v [n_rows][n_kv_heads][d_head], each row contiguous and *_ld elements from the next (so that
+ * the three may lie in one projection's output); q_out likewise and may be q itself.  rope: device
+ * fp32 [rope_len][d_head / 2][2].  A row at a position that does not fit gets a zero q_out row; rows
+ * outside every sequence are left alone. */
+VT_API vt_status vt_paged_append(vt_paged* paged, const vt_paged_pool* pool, const vt_paged_batch* batch,
+                                 int32_t n_rows, int32_t n_heads, const void* q, int64_t q_ld, const void* k,
+                                 int64_t k_ld, const void* v, int64_t v_ld, const float* rope, int32_t rope_len,
+                                 void* q_out, int64_t q_out_ld, vt_stream stream);
+
+/* vt_paged_decode (Section 2.1, decode phase; Section 3.2.1, one device's heads): attention of one
+ * new row per sequence (batch->starts must be NULL; n_rows = n_seqs).  Query head h of row b attends
+ * over positions [max(0, p - window + 1), p], p = lens[b], of KV head h / (n_heads / n_kv_heads)
+ * (window 0: [0, p]):
+ *   out[b][h] = sum_j softmax_j(scale * q[b][h] . k_j) v_j.
+ * q, out [n_seqs][n_heads][d_head], rows q_ld / out_ld elements apart.  n_heads: a multiple of
+ * n_kv_heads, at most 128 times it. */
+VT_API vt_status vt_paged_decode(vt_paged* paged, const vt_paged_pool* pool, const vt_paged_batch* batch,
+                                 int32_t n_heads, const void* q, int64_t q_ld, float scale, int32_t window, void* out,
+                                 int64_t out_ld, vt_stream stream);
+
+/* vt_paged_prefill (Section 2.1, prefill phase): the same attention for any number of new rows per
+ * sequence; row i of sequence b attends over [max(0, p - window + 1), p], p = lens[b] + i.  Rows
+ * outside every sequence are left alone. */
+VT_API vt_status vt_paged_prefill(vt_paged* paged, const vt_paged_pool* pool, const vt_paged_batch* batch,
+                                  int32_t n_rows, int32_t n_heads, const void* q, int64_t q_ld, float scale,
+                                  int32_t window, void* out, int64_t out_ld, vt_stream stream);
 
 #ifdef __cplusplus
 }

@@ -2193,3 +2193,206 @@ extern "C" vt_status vt_prefill_tokens(const vt_partition* p, vt_kv* kv, const v
         for (int l = 0; l < s.n_layers; ++l) kv->h_len[l] += n;
     return ok();
 }
+
+// ================================================================== paged KV cache
+
+struct vt_paged {
+    Allocator alloc;
+    uint32_t* status = nullptr;
+};
+
+extern "C" void vt_paged_destroy(vt_paged* g) {
+    if (!g) return;
+    cudaDeviceSynchronize();
+    g->alloc.put(g->status);
+    delete g;
+}
+
+extern "C" vt_status vt_paged_create(const vt_allocator* allocator, vt_stream stream, vt_paged** out) {
+    if (!out) return fail(VT_ERR_INVALID_ARG, "out is NULL");
+    *out = nullptr;
+    if (allocator && (!allocator->alloc || !allocator->free))
+        return fail(VT_ERR_INVALID_ARG, "allocator callbacks must not be NULL");
+    VT_CUDA(init_library());
+    cudaStream_t st = (cudaStream_t)stream;
+    vt_paged* g = new vt_paged();
+    if (allocator) {
+        g->alloc.a = *allocator;
+        g->alloc.custom = true;
+    }
+    g->status = static_cast<uint32_t*>(g->alloc.get(256));
+    if (!g->status) {
+        vt_paged_destroy(g);
+        return fail(VT_ERR_ALLOC, "allocating the paged workspace failed");
+    }
+    cudaError_t e = cudaMemsetAsync(g->status, 0, 256, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (e != cudaSuccess) {
+        vt_paged_destroy(g);
+        return fail(VT_ERR_CUDA, "setting up the paged workspace failed: %s", cudaGetErrorString(e));
+    }
+    *out = g;
+    return ok();
+}
+
+extern "C" vt_status vt_paged_status(vt_paged* g, uint32_t* flags, int32_t clear) {
+    if (!g) return fail(VT_ERR_INVALID_ARG, "paged is NULL");
+    return read_status(g->status, flags, clear, nullptr);
+}
+
+extern "C" vt_status vt_rope_table(float* table, int32_t max_seq, int32_t dh, double theta, vt_stream stream) {
+    if (!table) return fail(VT_ERR_INVALID_ARG, "table is NULL");
+    if (!aligned16(table)) return fail(VT_ERR_INVALID_ARG, "table must be 16-byte aligned");
+    if (max_seq < 1 || !(theta > 0.0) || !std::isfinite(theta))
+        return fail(VT_ERR_INVALID_ARG, "max_seq must be >= 1 and theta finite and > 0");
+    if (dh != 64 && dh != 128) return fail(VT_ERR_SHAPE, "d_head must be 64 or 128");
+    VT_CUDA(launch_rope_table(reinterpret_cast<float2*>(table), max_seq, dh, theta, (cudaStream_t)stream));
+    return ok();
+}
+
+namespace {
+
+// Rules common to the paged calls; fills the view of the pool through the batch.
+vt_status paged_view(const vt_paged* g, const vt_paged_pool* p, const vt_paged_batch* b, PagedView* c) {
+    if (!g || !p || !b) return fail(VT_ERR_INVALID_ARG, "paged, pool and batch must not be NULL");
+    if (p->dtype != VT_F16 && p->dtype != VT_BF16) return fail(VT_ERR_SHAPE, "unknown dtype %d", p->dtype);
+    if (p->d_head != 64 && p->d_head != 128) return fail(VT_ERR_SHAPE, "d_head must be 64 or 128 (got %d)", p->d_head);
+    if (p->page_size < 1 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)))
+        return fail(VT_ERR_SHAPE, "page_size must be a power of two in [1, 1024] (got %d)", p->page_size);
+    if (p->n_kv_heads < 1 || p->n_kv_heads > 4096) return fail(VT_ERR_SHAPE, "n_kv_heads must be in [1, 4096]");
+    if (p->n_pages < 1) return fail(VT_ERR_INVALID_ARG, "n_pages must be >= 1");
+    if (!p->k || !p->v || !aligned16(p->k) || !aligned16(p->v))
+        return fail(VT_ERR_INVALID_ARG, "the pool's k and v must be 16-byte aligned and not NULL");
+    // a stride that only one entry has is not used
+    const struct { int64_t stride; bool used; const char* what; } strides[3] = {
+        {p->page_stride, p->n_pages > 1, "page"}, {p->head_stride, p->n_kv_heads > 1, "head"},
+        {p->pos_stride, p->page_size > 1, "pos"}};
+    for (const auto& s : strides)
+        if (s.used && (s.stride < p->d_head || s.stride % 8 || s.stride > ((int64_t)1 << 40)))
+            return fail(VT_ERR_INVALID_ARG, "%s_stride %lld must be a multiple of 8, at least d_head and at most 2^40", s.what,
+                        (long long)s.stride);
+    if (b->n_seqs < 0 || b->pages_per_seq < 1)
+        return fail(VT_ERR_INVALID_ARG, "n_seqs must be >= 0 and pages_per_seq >= 1");
+    if ((int64_t)b->pages_per_seq * p->page_size > ((int64_t)1 << 30))
+        return fail(VT_ERR_INVALID_ARG, "pages_per_seq * page_size must be at most 2^30");
+    if (b->n_seqs > 0 && (!b->tables || !b->lens)) return fail(VT_ERR_INVALID_ARG, "tables and lens must not be NULL");
+    c->page_stride = strides[0].used ? p->page_stride : 0;
+    c->head_stride = strides[1].used ? p->head_stride : 0;
+    c->pos_stride = strides[2].used ? p->pos_stride : 0;
+    c->n_pages = p->n_pages;
+    c->page_size = p->page_size;
+    c->page_shift = 0;
+    while ((1 << c->page_shift) < p->page_size) ++c->page_shift;
+    c->n_kv_heads = p->n_kv_heads;
+    c->tables = b->tables;
+    c->per_seq = b->pages_per_seq;
+    c->cap = b->pages_per_seq * p->page_size;
+    c->lens = b->lens;
+    c->starts = b->starts;
+    c->n_seqs = b->n_seqs;
+    c->status = g->status;
+    return VT_OK;
+}
+
+// Row arrays: n_rows rows of `heads` heads, ld elements apart.
+vt_status paged_rows(const char* what, const void* x, int64_t ld, int n_rows, int heads, int dh) {
+    if (!x || !aligned16(x)) return fail(VT_ERR_INVALID_ARG, "%s must be 16-byte aligned and not NULL", what);
+    if (n_rows > 1 && (ld < (int64_t)heads * dh || ld % 8 || ld > ((int64_t)1 << 31)))
+        return fail(VT_ERR_INVALID_ARG, "rows of %s: %lld elements apart must be a multiple of 8, at least %d and at most 2^31", what,
+                    (long long)ld, heads * dh);
+    return VT_OK;
+}
+
+vt_status paged_n_rows(const vt_paged_batch* b, int n_rows) {
+    if (n_rows < 0 || n_rows > (1 << 24)) return fail(VT_ERR_INVALID_ARG, "n_rows must be in [0, 2^24]");
+    if (!b->starts && n_rows != b->n_seqs)
+        return fail(VT_ERR_INVALID_ARG, "without starts every sequence has one row: %d rows, %d sequences", n_rows, b->n_seqs);
+    return VT_OK;
+}
+
+vt_status paged_heads(const vt_paged_pool* p, int n_heads) {
+    if (n_heads < 1 || n_heads % p->n_kv_heads || n_heads / p->n_kv_heads > 128)
+        return fail(VT_ERR_SHAPE, "n_heads %d must be a multiple of n_kv_heads %d, at most 128 times it", n_heads, p->n_kv_heads);
+    return VT_OK;
+}
+
+vt_status paged_attn(vt_paged* g, const vt_paged_pool* pool, const vt_paged_batch* batch, int n_rows, int n_heads,
+                     const void* q, int64_t q_ld, float scale, int window, void* out, int64_t out_ld, PagedAttnArgs* a) {
+    VT_TRY(paged_view(g, pool, batch, &a->c));
+    VT_TRY(paged_n_rows(batch, n_rows));
+    VT_TRY(paged_heads(pool, n_heads));
+    if (!std::isfinite(scale)) return fail(VT_ERR_INVALID_ARG, "scale must be finite");
+    if (window < 0) return fail(VT_ERR_INVALID_ARG, "window %d is negative", window);
+    a->n_rows = n_rows;
+    if (n_rows == 0 || batch->n_seqs == 0) return VT_OK;
+    VT_TRY(paged_rows("q", q, q_ld, n_rows, n_heads, pool->d_head));
+    VT_TRY(paged_rows("out", out, out_ld, n_rows, n_heads, pool->d_head));
+    a->n_heads = n_heads;
+    a->group = n_heads / pool->n_kv_heads;
+    a->q = static_cast<const uint16_t*>(q);
+    a->q_ld = n_rows > 1 ? q_ld : 0;
+    a->kpool = static_cast<const uint16_t*>(pool->k);
+    a->vpool = static_cast<const uint16_t*>(pool->v);
+    a->scale_log2 = scale * 1.4426950408889634f;
+    a->window = window;
+    a->out = static_cast<uint16_t*>(out);
+    a->out_ld = n_rows > 1 ? out_ld : 0;
+    return VT_OK;
+}
+
+}  // namespace
+
+extern "C" vt_status vt_paged_append(vt_paged* g, const vt_paged_pool* pool, const vt_paged_batch* batch, int32_t n_rows,
+                                     int32_t n_heads, const void* q, int64_t q_ld, const void* k, int64_t k_ld,
+                                     const void* v, int64_t v_ld, const float* rope, int32_t rope_len, void* q_out,
+                                     int64_t q_out_ld, vt_stream stream) {
+    PagedAppendArgs a{};
+    VT_TRY(paged_view(g, pool, batch, &a.c));
+    VT_TRY(paged_n_rows(batch, n_rows));
+    VT_TRY(paged_heads(pool, n_heads));
+    if (rope_len < 1) return fail(VT_ERR_INVALID_ARG, "rope_len must be >= 1");
+    if (!rope || !aligned16(rope)) return fail(VT_ERR_INVALID_ARG, "rope must be 16-byte aligned and not NULL");
+    if (n_rows == 0 || batch->n_seqs == 0) return ok();
+    const int dh = pool->d_head, hk = pool->n_kv_heads;
+    VT_TRY(paged_rows("q", q, q_ld, n_rows, n_heads, dh));
+    VT_TRY(paged_rows("k", k, k_ld, n_rows, hk, dh));
+    VT_TRY(paged_rows("v", v, v_ld, n_rows, hk, dh));
+    VT_TRY(paged_rows("q_out", q_out, q_out_ld, n_rows, n_heads, dh));
+    a.n_rows = n_rows;
+    a.n_heads = n_heads;
+    a.q = static_cast<const uint16_t*>(q);
+    a.k = static_cast<const uint16_t*>(k);
+    a.v = static_cast<const uint16_t*>(v);
+    a.q_ld = n_rows > 1 ? q_ld : 0;
+    a.k_ld = n_rows > 1 ? k_ld : 0;
+    a.v_ld = n_rows > 1 ? v_ld : 0;
+    a.rope = reinterpret_cast<const float2*>(rope);
+    a.rope_len = rope_len;
+    a.q_out = static_cast<uint16_t*>(q_out);
+    a.q_out_ld = n_rows > 1 ? q_out_ld : 0;
+    a.kpool = static_cast<uint16_t*>(pool->k);
+    a.vpool = static_cast<uint16_t*>(pool->v);
+    VT_CUDA(launch_paged_append(a, pool->dtype, dh, (cudaStream_t)stream));
+    return ok();
+}
+
+extern "C" vt_status vt_paged_decode(vt_paged* g, const vt_paged_pool* pool, const vt_paged_batch* batch, int32_t n_heads,
+                                     const void* q, int64_t q_ld, float scale, int32_t window, void* out,
+                                     int64_t out_ld, vt_stream stream) {
+    if (batch && batch->starts) return fail(VT_ERR_INVALID_ARG, "vt_paged_decode takes one row per sequence: starts must be NULL");
+    PagedAttnArgs a{};
+    VT_TRY(paged_attn(g, pool, batch, batch ? batch->n_seqs : 0, n_heads, q, q_ld, scale, window, out, out_ld, &a));
+    if (a.n_rows == 0) return ok();
+    VT_CUDA(launch_paged_attn(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
+    return ok();
+}
+
+extern "C" vt_status vt_paged_prefill(vt_paged* g, const vt_paged_pool* pool, const vt_paged_batch* batch, int32_t n_rows,
+                                      int32_t n_heads, const void* q, int64_t q_ld, float scale, int32_t window,
+                                      void* out, int64_t out_ld, vt_stream stream) {
+    PagedAttnArgs a{};
+    VT_TRY(paged_attn(g, pool, batch, n_rows, n_heads, q, q_ld, scale, window, out, out_ld, &a));
+    if (a.n_rows == 0 || batch->n_seqs == 0) return ok();
+    VT_CUDA(launch_paged_attn(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
+    return ok();
+}

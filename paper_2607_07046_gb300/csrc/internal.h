@@ -284,6 +284,43 @@ struct CombineTokenQArgs {               // a token's combine, partials travelli
 };
 cudaError_t launch_combine_token_q(const CombineTokenQArgs& a, cudaStream_t st);
 
+// ------------------------------------------------------------------ paged KV cache (paged.cu)
+// A pool seen through the page tables of a batch; strides in elements.
+struct PagedView {
+    int64_t page_stride, head_stride, pos_stride;
+    int n_pages, page_size, page_shift, n_kv_heads;
+    const int32_t* tables;  // [n_seqs][per_seq]
+    int per_seq, cap;       // cap: per_seq * page_size
+    const int32_t* lens;
+    const int32_t* starts;  // nullptr: row b is sequence b's
+    int n_seqs;
+    uint32_t* status;
+};
+struct PagedAppendArgs {
+    PagedView c;
+    int n_rows, n_heads;
+    const uint16_t *q, *k, *v;  // rows q_ld, k_ld, v_ld elements apart
+    int64_t q_ld, k_ld, v_ld;
+    const float2* rope;         // [rope_len][dh / 2]
+    int rope_len;
+    uint16_t* q_out;
+    int64_t q_out_ld;
+    uint16_t *kpool, *vpool;
+};
+struct PagedAttnArgs {
+    PagedView c;
+    int n_rows, n_heads, group;
+    const uint16_t* q;
+    int64_t q_ld;
+    const uint16_t *kpool, *vpool;
+    float scale_log2;           // scale * log2(e)
+    int window;
+    uint16_t* out;
+    int64_t out_ld;
+};
+cudaError_t launch_paged_append(const PagedAppendArgs& a, int dtype, int dh, cudaStream_t st);
+cudaError_t launch_paged_attn(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st);
+
 // ------------------------------------------------------------------ static scratch
 // (static_scratch.cu) the decode step whose intermediates are in one file-scope __device__ array.
 constexpr size_t kStaticScratchBytes = (size_t)1 << 20;  // 1 MiB

@@ -33,6 +33,9 @@ VT_MAX_DEVICES = 16
 VT_DEV_KV_OVERFLOW = 1
 VT_DEV_WAIT_TIMEOUT = 2
 VT_DEV_BAD_TOKEN = 4
+VT_DEV_BAD_PAGE = 8
+VT_F16 = 0
+VT_BF16 = 1
 VT_BLOCK_ATTN = 0
 VT_BLOCK_FFN = 1
 VT_PARTITION_PRUNE = 1
@@ -78,6 +81,16 @@ class vt_layer_weights(ctypes.Structure):
 
 class vt_shard(ctypes.Structure):
     _fields_ = [("layer", _I32), ("device", _I32), ("block", _I32)]
+
+
+class vt_paged_pool(ctypes.Structure):
+    _fields_ = [("k", _P), ("v", _P), ("dtype", _I32), ("n_pages", _I32), ("page_size", _I32),
+                ("n_kv_heads", _I32), ("d_head", _I32), ("page_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("pos_stride", ctypes.c_int64)]
+
+
+class vt_paged_batch(ctypes.Structure):
+    _fields_ = [("tables", _P), ("lens", _P), ("starts", _P), ("n_seqs", _I32), ("pages_per_seq", _I32)]
 
 
 _lib = None
@@ -160,6 +173,17 @@ def lib() -> ctypes.CDLL:
             "vt_token_partials_read": (S, [_P, _I32, _P]),
             "vt_token_test_barrier": (S, [_P, _I32, _U32, _P]),
             "vt_test_wait_limit": (S, [_I32, _P, _P]),
+            "vt_paged_create": (S, [ctypes.POINTER(vt_allocator), _P, ctypes.POINTER(_P)]),
+            "vt_paged_destroy": (None, [_P]),
+            "vt_paged_status": (S, [_P, ctypes.POINTER(ctypes.c_uint32), _I32]),
+            "vt_rope_table": (S, [_P, _I32, _I32, ctypes.c_double, _P]),
+            "vt_paged_append": (S, [_P, ctypes.POINTER(vt_paged_pool), ctypes.POINTER(vt_paged_batch), _I32, _I32,
+                                    _P, ctypes.c_int64, _P, ctypes.c_int64, _P, ctypes.c_int64, _P, _I32,
+                                    _P, ctypes.c_int64, _P]),
+            "vt_paged_decode": (S, [_P, ctypes.POINTER(vt_paged_pool), ctypes.POINTER(vt_paged_batch), _I32,
+                                    _P, ctypes.c_int64, ctypes.c_float, _I32, _P, ctypes.c_int64, _P]),
+            "vt_paged_prefill": (S, [_P, ctypes.POINTER(vt_paged_pool), ctypes.POINTER(vt_paged_batch), _I32, _I32,
+                                     _P, ctypes.c_int64, ctypes.c_float, _I32, _P, ctypes.c_int64, _P]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -642,3 +666,117 @@ def vt_prefill_tokens(part: int, kv: int, x_in, n: int, x_out, stream=None) -> N
     import torch
     _check(lib().vt_prefill_tokens(part, kv, _ptr(x_in, torch.float16), n,
                                    _ptr(x_out, torch.float16), _stream(stream)))
+
+
+# ------------------------------------------------------------------ paged KV cache
+
+def make_paged_pool(k, v) -> vt_paged_pool:
+    """One layer's K and V: fp16 or bf16 CUDA tensors seen as [pages, KV heads, positions in a page,
+    head dim] with equal strides (permute a pool that lies in another order), head dim contiguous.
+    The structure keeps the tensors alive."""
+    import torch
+    for t in (k, v):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 4:
+            raise ValueError("expected CUDA tensors [pages, KV heads, positions in a page, head dim]")
+    if k.dtype not in (torch.float16, torch.bfloat16) or v.dtype != k.dtype:
+        raise TypeError(f"expected float16 or bfloat16 K and V of one type, got {k.dtype} and {v.dtype}")
+    if k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1 or k.device != v.device:
+        raise ValueError("K and V need one shape, equal strides, one device and a contiguous head dim")
+    p = vt_paged_pool(k.data_ptr(), v.data_ptr(), VT_F16 if k.dtype == torch.float16 else VT_BF16, k.shape[0],
+                      k.shape[2], k.shape[1], k.shape[3], k.stride(0), k.stride(1), k.stride(2))
+    p.tensors = (k, v)
+    return p
+
+
+def make_paged_batch(tables, lens, starts=None) -> vt_paged_batch:
+    """tables int32 [sequences, pages per sequence], lens int32 [sequences] (positions held; < 0: idle
+    slot), starts int32 [sequences + 1] (first row of each sequence) or None for one row each; CUDA
+    tensors, read by the kernels of each call, so a program may update them in place between calls.
+    The structure keeps the tensors alive."""
+    import torch
+    if tables.dim() != 2 or lens.shape != tables.shape[:1] or (starts is not None and starts.numel() != lens.numel() + 1):
+        raise ValueError("expected tables [sequences, pages], lens [sequences] and starts [sequences + 1]")
+    if lens.device != tables.device or (starts is not None and starts.device != tables.device):
+        raise ValueError("tables, lens and starts need one device")
+    b = vt_paged_batch(_ptr(tables, torch.int32), _ptr(lens, torch.int32), _ptr(starts, torch.int32), tables.shape[0],
+                       tables.shape[1])
+    b.tensors = (tables, lens, starts)
+    return b
+
+
+def vt_paged_create(stream=None, allocator: str = "torch") -> int:
+    out = _P()
+    alloc = ctypes.byref(_TORCH_ALLOCATOR) if allocator == "torch" else None
+    _check(lib().vt_paged_create(alloc, _stream(stream), ctypes.byref(out)))
+    return out.value
+
+
+def vt_paged_destroy(paged: int) -> None:
+    if paged:
+        lib().vt_paged_destroy(paged)
+
+
+def vt_paged_status(paged: int, clear: bool = False) -> int:
+    f = ctypes.c_uint32()
+    _check(lib().vt_paged_status(paged, ctypes.byref(f), int(clear)))
+    return int(f.value)
+
+
+def vt_rope_table(table, theta: float, stream=None) -> None:
+    """Fills a float32 CUDA tensor [positions, head dim / 2, 2] with (cos, sin) of the angles."""
+    import torch
+    if table.dim() != 3 or table.shape[2] != 2:
+        raise ValueError("expected [positions, head dim / 2, 2]")
+    _check(lib().vt_rope_table(_ptr(table, torch.float32), table.shape[0], 2 * table.shape[1], float(theta),
+                               _stream(stream)))
+
+
+def _rows(t, pool, heads: Optional[int] = None) -> Tuple[int, int]:
+    """(data_ptr, elements between rows) of a CUDA tensor [rows, heads, head dim] of the pool's type and
+    device whose rows are contiguous."""
+    shape, stride, k = t.shape, t.stride(), pool.tensors[0]
+    if len(shape) != 3 or shape[2] != pool.d_head or (heads is not None and shape[1] != heads):
+        raise ValueError(f"expected [rows, {'heads' if heads is None else heads}, {pool.d_head}], got {tuple(shape)}")
+    if t.dtype != k.dtype:
+        raise TypeError(f"expected {k.dtype}, got {t.dtype}")
+    if t.device != k.device or stride[2] != 1 or (stride[1] != shape[2] and shape[1] != 1):
+        raise ValueError("expected rows of contiguous heads on the pool's device")
+    return t.data_ptr(), stride[0]
+
+
+def vt_paged_append(paged: int, pool: vt_paged_pool, batch: vt_paged_batch, q, k, v, rope, q_out, stream=None) -> None:
+    """q, q_out [rows, heads, head dim] and k, v [rows, KV heads, head dim] (views of one projection's
+    output will do); rope float32 [positions, head dim / 2, 2]."""
+    import torch
+    n, heads = q.shape[0], q.shape[1]
+    if k.shape[0] != n or v.shape[0] != n or q_out.shape[0] != n:
+        raise ValueError("q, k, v and q_out need one number of rows")
+    if rope.dim() != 3 or rope.shape[2] != 2 or 2 * rope.shape[1] != pool.d_head:
+        raise ValueError("expected rope [positions, head dim / 2, 2]")
+    (qp, ql), (kp, kl), (vp, vl), (op, ol) = (_rows(q, pool), _rows(k, pool, pool.n_kv_heads),
+                                             _rows(v, pool, pool.n_kv_heads), _rows(q_out, pool, heads))
+    _check(lib().vt_paged_append(paged, pool, batch, n, heads, qp, ql, kp, kl, vp, vl, _ptr(rope, torch.float32),
+                                 rope.shape[0], op, ol, _stream(stream)))
+
+
+def vt_paged_decode(paged: int, pool: vt_paged_pool, batch: vt_paged_batch, q, out, scale: Optional[float] = None,
+                    window: int = 0, stream=None) -> None:
+    """Attention of one new row per sequence: q, out [sequences, heads, head dim]; scale: None for
+    1 / sqrt(head dim)."""
+    heads = q.shape[1]
+    if q.shape[0] != batch.n_seqs or out.shape[0] != batch.n_seqs:
+        raise ValueError("one row of q and out per sequence")
+    (qp, ql), (op, ol) = _rows(q, pool), _rows(out, pool, heads)
+    _check(lib().vt_paged_decode(paged, pool, batch, heads, qp, ql, pool.d_head ** -0.5 if scale is None else scale,
+                                 window, op, ol, _stream(stream)))
+
+
+def vt_paged_prefill(paged: int, pool: vt_paged_pool, batch: vt_paged_batch, q, out, scale: Optional[float] = None,
+                     window: int = 0, stream=None) -> None:
+    """Causal attention of the new rows of every sequence: q, out [rows, heads, head dim]."""
+    n, heads = q.shape[0], q.shape[1]
+    if out.shape[0] != n:
+        raise ValueError("q and out need one number of rows")
+    (qp, ql), (op, ol) = _rows(q, pool), _rows(out, pool, heads)
+    _check(lib().vt_paged_prefill(paged, pool, batch, n, heads, qp, ql, pool.d_head ** -0.5 if scale is None else scale,
+                                  window, op, ol, _stream(stream)))
