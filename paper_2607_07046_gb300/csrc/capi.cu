@@ -119,6 +119,8 @@ cudaError_t init_library() {
         g_init_err = init_token_kernels();
         if (g_init_err != cudaSuccess) return;
         g_init_err = init_quant_kernels();
+        if (g_init_err != cudaSuccess) return;
+        g_init_err = init_paged_decode();
     });
     return g_init_err;
 }
@@ -2198,13 +2200,16 @@ extern "C" vt_status vt_prefill_tokens(const vt_partition* p, vt_kv* kv, const v
 
 struct vt_paged {
     Allocator alloc;
+    uint8_t* base = nullptr;     // status word, arrival counters, slots
     uint32_t* status = nullptr;
+    int* arrived = nullptr;      // [kPagedMaxGrid]
+    float* work = nullptr;       // [2 kPagedMaxGrid][kPagedSlotFloats]
 };
 
 extern "C" void vt_paged_destroy(vt_paged* g) {
     if (!g) return;
     cudaDeviceSynchronize();
-    g->alloc.put(g->status);
+    g->alloc.put(g->base);
     delete g;
 }
 
@@ -2220,12 +2225,16 @@ extern "C" vt_status vt_paged_create(const vt_allocator* allocator, vt_stream st
         g->alloc.a = *allocator;
         g->alloc.custom = true;
     }
-    g->status = static_cast<uint32_t*>(g->alloc.get(256));
-    if (!g->status) {
+    const size_t head = 256 + kPagedMaxGrid * sizeof(int);
+    g->base = static_cast<uint8_t*>(g->alloc.get(head + (size_t)2 * kPagedMaxGrid * kPagedSlotFloats * sizeof(float)));
+    if (!g->base) {
         vt_paged_destroy(g);
         return fail(VT_ERR_ALLOC, "allocating the paged workspace failed");
     }
-    cudaError_t e = cudaMemsetAsync(g->status, 0, 256, st);
+    g->status = reinterpret_cast<uint32_t*>(g->base);
+    g->arrived = reinterpret_cast<int*>(g->base + 256);
+    g->work = reinterpret_cast<float*>(g->base + head);
+    cudaError_t e = cudaMemsetAsync(g->base, 0, head, st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     if (e != cudaSuccess) {
         vt_paged_destroy(g);
@@ -2337,6 +2346,9 @@ vt_status paged_attn(vt_paged* g, const vt_paged_pool* pool, const vt_paged_batc
     a->window = window;
     a->out = static_cast<uint16_t*>(out);
     a->out_ld = n_rows > 1 ? out_ld : 0;
+    a->work = g->work;
+    a->slot_floats = kPagedSlotFloats;
+    a->arrived = g->arrived;
     return VT_OK;
 }
 
@@ -2383,7 +2395,7 @@ extern "C" vt_status vt_paged_decode(vt_paged* g, const vt_paged_pool* pool, con
     PagedAttnArgs a{};
     VT_TRY(paged_attn(g, pool, batch, batch ? batch->n_seqs : 0, n_heads, q, q_ld, scale, window, out, out_ld, &a));
     if (a.n_rows == 0) return ok();
-    VT_CUDA(launch_paged_attn(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
+    VT_CUDA(launch_paged_decode(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
     return ok();
 }
 

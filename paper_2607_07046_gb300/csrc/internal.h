@@ -317,9 +317,18 @@ struct PagedAttnArgs {
     int window;
     uint16_t* out;
     int64_t out_ld;
+    // workspace: two slots a CTA for parts of a unit that several CTAs share, and for each CTA the
+    // number of them that have stored their part (zero between calls)
+    float* work;
+    int64_t slot_floats;
+    int* arrived;
 };
+constexpr int kPagedSlotFloats = 32 + 16 * 128;
+constexpr int kPagedMaxGrid = 1024;
 cudaError_t launch_paged_append(const PagedAppendArgs& a, int dtype, int dh, cudaStream_t st);
 cudaError_t launch_paged_attn(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st);
+cudaError_t launch_paged_decode(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st);
+cudaError_t init_paged_decode();
 
 // ------------------------------------------------------------------ static scratch
 // (static_scratch.cu) the decode step whose intermediates are in one file-scope __device__ array.

@@ -2,31 +2,13 @@
 // sequences in pages of one pool).
 //
 //   k_paged_append   rotates q and k to their positions, writes k and v to the pages
-//   k_paged_attn     attention of each new row over the pages of its sequence
+//   k_paged_attn     attention of several new rows of a sequence over its pages
 #include <cuda_runtime.h>
 #include <math.h>
-
-#include <utility>
 
 #include "paged.cuh"
 
 namespace vt {
-
-template <typename Args>
-static cudaError_t launch_paged_k(void (*kern)(Args), unsigned grid, int threads, size_t smem, cudaStream_t st,
-                                  const Args& a) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = g_use_pdl ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kern, a);
-}
 
 // ================================================================== append
 //

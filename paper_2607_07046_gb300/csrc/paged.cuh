@@ -6,10 +6,29 @@
 #include <cuda_fp16.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "device.cuh"
 #include "internal.h"
 
 namespace vt {
+
+// A launch that may set up while the preceding kernel of the stream finishes.
+template <typename Args>
+static cudaError_t launch_paged_k(void (*kern)(Args), unsigned grid, int threads, size_t smem, cudaStream_t st,
+                                  const Args& a) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = g_use_pdl ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kern, a);
+}
 
 // Two 16-bit elements of a word as floats, and back (round to nearest even).
 template <class T>

@@ -1,0 +1,472 @@
+// Attention of one new row per sequence over the paged KV cache (Voltron Section 2.1, decode phase).
+//
+//   o_h = sum_j softmax_j(scale q_h . k_j) v_j over the row's positions, one pass over K and V with a
+//   running maximum m (log2 units), sum l and o per query head.
+//
+// What bounds it: every K and V byte is read once and meets `group` query heads (group FLOPs a byte), so
+// HBM.  The work of a unit (a sequence's KV head and up to 8 NT of its query heads) is cut into steps of
+// 16 positions; the steps of all units form one line, and CTA c takes its c-th equal part, whatever the
+// sequences' lengths are.  They are known on the device only, so that a captured launch serves any
+// lengths.  Inside a CTA step i goes to warp i % 4, each with its own ring of asynchronous 16-byte copies
+// (K and V rows gathered through the page table), so no barrier stands in the stream; 128 KB or more a SM
+// are in flight.  A unit that several CTAs share is joined by the last of them to finish: partial (m, l,
+// o) in a workspace, added in CTA order, so a result does not depend on timing.
+//
+// Products run on mma.sync m16n8k16 (tcgen05 would need 64 or more rows where there are 1 to 16):
+//   S [16 heads x 8 keys] = Q . K^T      A: Q from registers, B: K rows by ldmatrix
+//   O^T [16 dims x 8 heads] += V^T . P^T  A: V by ldmatrix.trans, B: P as S leaves it in registers
+// P is cut into two 16-bit terms, hi = round(p) and lo = round(p - hi), two products each: the weights
+// then carry 16 (bf16) or 22 (fp16) bits and the output's own rounding is the only one that counts.
+#include <cuda_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "paged.cuh"
+
+namespace vt {
+
+constexpr int kPdWarps = 4, kPdThreads = kPdWarps * 32;
+constexpr int kPdKeys = 16;                  // positions of a step
+constexpr int kPdRing = 96 * 1024;           // bytes of the four warps' rings
+constexpr int kPdCtasPerSm = 2;
+// steps a CTA takes at least: fewer CTAs, each with work for all its warps, and fewer parts to join
+constexpr int kPdMinSteps = 8;
+
+template <int DH>
+struct PdGeom {
+    static constexpr int kRow = DH * 2;                            // bytes of a K or V row
+    static constexpr int kStage = 2 * kPdKeys * kRow;              // K rows, then V rows
+    static constexpr int kStages = kPdRing / (kPdWarps * kStage);  // 3 (dh 128) or 6 (dh 64)
+    static constexpr size_t kSmem = kPdRing + (size_t)kPdWarps * 8 * DH * 4;
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool full) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(full ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+template <class T>
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if constexpr (std::is_same<T, __half>::value)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Attended positions [beg, end) of the row of sequence b (end 0: none).
+__device__ __forceinline__ void pd_range(const PagedAttnArgs& a, int b, int& beg, int& end) {
+    const int len = paged_len(a.c, b);
+    end = len < 0 ? 0 : min(len + 1, a.c.cap);
+    beg = a.window > 0 ? max(0, len + 1 - a.window) : 0;
+    if (beg >= end) beg = end = 0;  // a length past the table may leave the window nothing
+}
+__device__ __forceinline__ int pd_steps(int beg, int end) { return (end + kPdKeys - 1) / kPdKeys - beg / kPdKeys; }
+
+// Where a walk over the steps of the units stands.
+struct PdCursor {
+    int b, u, i, steps, beg, end;
+    __device__ __forceinline__ void open(const PagedAttnArgs& a, int seq) {
+        b = seq;
+        steps = 0;
+        if (b < a.c.n_seqs) {
+            pd_range(a, b, beg, end);
+            steps = pd_steps(beg, end);
+        }
+    }
+    // n steps further (units: units of a sequence); sequences without positions have none
+    __device__ __forceinline__ void move(const PagedAttnArgs& a, int n, int units) {
+        i += n;
+        while (b < a.c.n_seqs && i >= steps) {
+            i -= steps;
+            if (steps == 0 || ++u == units) {
+                u = 0;
+                open(a, b + 1);
+            }
+        }
+    }
+};
+
+template <class T, int DH, int NT>
+__global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const __grid_constant__ PagedAttnArgs a) {
+    using E = Elem<T>;
+    using G = PdGeom<DH>;
+    constexpr int S = G::kStages, CPR = DH / 8, RPI = 32 / CPR;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ int64_t s_sum[kPdWarps], s_before;
+    __shared__ int s_seq, s_last;
+    __shared__ float s_ml[2][kPdWarps][8 * NT];
+    __shared__ uint32_t s_mask[kPdWarps][S];
+    const PagedView& c = a.c;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const int tiles = (a.group + 8 * NT - 1) / (8 * NT), units = c.n_kv_heads * tiles;
+    pdl_wait();
+    pdl_launch_dependents();
+
+    // ---- this CTA's part of the line of steps: thread t sums the sequences [t ch, (t + 1) ch)
+    const int ch = (c.n_seqs + kPdThreads - 1) / kPdThreads;
+    int64_t mine = 0;
+    bool idle = false;
+    for (int b = tid * ch; b < min(c.n_seqs, (tid + 1) * ch); ++b) {
+        int beg, end;
+        pd_range(a, b, beg, end);
+        if (blockIdx.x == 0 && c.lens[b] >= c.cap) set_status(c.status, VT_DEV_KV_OVERFLOW);
+        idle |= end == 0;
+        mine += pd_steps(beg, end);
+    }
+    int64_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+    }
+    if (lane == 31) s_sum[warp] = upto;
+    const bool any_idle = __syncthreads_or(idle);
+    int64_t total = 0;
+    for (int w = 0; w < kPdWarps; ++w) {
+        if (w < warp) upto += s_sum[w];
+        total += s_sum[w];
+    }
+    if (any_idle)
+        for (int b = blockIdx.x; b < c.n_seqs; b += gridDim.x) {
+            int beg, end;
+            pd_range(a, b, beg, end);
+            if (end == 0)
+                for (int e = tid; e < a.n_heads * DH / 8; e += kPdThreads)
+                    reinterpret_cast<uint4*>(a.out + b * a.out_ld)[e] = make_uint4(0u, 0u, 0u, 0u);
+        }
+    const int64_t line = total * units;
+    const int64_t per = max((line + gridDim.x - 1) / gridDim.x, (int64_t)kPdMinSteps);
+    const int64_t t0 = blockIdx.x * per, t1 = min(line, t0 + per);
+    if (t0 >= t1) return;
+    if (upto - mine <= t0 / units && t0 / units < upto) {  // the thread whose sequences hold step t0
+        int64_t before = upto - mine;
+        int b = tid * ch;
+        for (;; ++b) {
+            int beg, end;
+            pd_range(a, b, beg, end);
+            const int n = pd_steps(beg, end);
+            if (t0 / units < before + n) break;
+            before += n;
+        }
+        s_seq = b;
+        s_before = before;
+    }
+    __syncthreads();
+
+    // ---- the copies: this warp's steps t0 + warp, t0 + warp + 4, ...
+    PdCursor at;  // of the whole CTA
+    at.open(a, s_seq);
+    {
+        const int64_t r = t0 - s_before * units;
+        at.u = (int)(r / at.steps);
+        at.i = (int)(r - (int64_t)at.u * at.steps);
+    }
+    const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * S * G::kStage);
+    PdCursor ld = at;
+    ld.move(a, warp, units);
+    int64_t to_load = (t1 - t0 - warp + kPdWarps - 1) / kPdWarps;
+    int page = -1;  // lane r < 16: the page of row r of the next step to load (-1: not attended to)
+    auto look_up = [&]() {
+        page = -1;
+        if (to_load > 0 && lane < kPdKeys) {
+            const int p = (ld.beg / kPdKeys + ld.i) * kPdKeys + lane;
+            if (p >= ld.beg && p < ld.end) page = c.tables[(int64_t)ld.b * c.per_seq + (p >> c.page_shift)];
+            else page = -2;
+        }
+    };
+    look_up();
+    int st_load = 0;
+    auto load_step = [&]() {
+        if (to_load > 0) {
+            const bool on = lane < kPdKeys && (unsigned)page < (unsigned)c.n_pages;
+            if (lane < kPdKeys && !on && page != -2) set_status(c.status, VT_DEV_BAD_PAGE);
+            const int p = (ld.beg / kPdKeys + ld.i) * kPdKeys + lane;
+            const int64_t off = on ? page * c.page_stride + (ld.u / tiles) * c.head_stride + (p & (c.page_size - 1)) * c.pos_stride
+                                   : -1;
+            const uint32_t mask = __ballot_sync(0xffffffffu, on);
+            if (lane == 0) s_mask[warp][st_load] = mask;
+            const uint32_t dst = ring + (uint32_t)(st_load * G::kStage);
+            const int chunk = lane % CPR;
+#pragma unroll
+            for (int r0 = 0; r0 < kPdKeys; r0 += RPI) {
+                const int r = r0 + lane / CPR;
+                const int64_t o = __shfl_sync(0xffffffffu, off, r);
+                const uint32_t d = dst + (uint32_t)(r * G::kRow + ((chunk ^ (r & 7)) << 4));
+                const int64_t src = (o < 0 ? 0 : o) + chunk * 8;  // rows without a position are filled with zeros
+                cp_async16(d, a.kpool + src, o >= 0);
+                cp_async16(d + kPdKeys * G::kRow, a.vpool + src, o >= 0);
+            }
+            ld.move(a, kPdWarps, units);
+            --to_load;
+            look_up();
+        }
+        cp_async_commit();
+        st_load = st_load + 1 == S ? 0 : st_load + 1;
+    };
+#pragma unroll
+    for (int s = 0; s < S - 1; ++s) load_step();
+
+    // ---- the steps, unit by unit
+    int st = 0, skip = warp;  // skip: steps until this warp's next
+    float* so = reinterpret_cast<float*>(smem + kPdRing);
+    for (int64_t now = t0; now < t1;) {
+        const int n = (int)min((int64_t)(at.steps - at.i), t1 - now);  // steps of this unit here
+        const int kvh = at.u / tiles, h0 = (at.u - kvh * tiles) * 8 * NT, nh = min(8 * NT, a.group - h0);
+        const int64_t row = (int64_t)at.b * a.q_ld + (int64_t)(kvh * a.group + h0) * DH;
+        uint32_t q[DH / 16][4];
+#pragma unroll
+        for (int k = 0; k < DH / 16; ++k) {
+            const uint16_t* src = a.q + row + k * 16 + 2 * t;
+            q[k][0] = g < nh ? *reinterpret_cast<const uint32_t*>(src + g * DH) : 0u;
+            q[k][2] = g < nh ? *reinterpret_cast<const uint32_t*>(src + g * DH + 8) : 0u;
+            q[k][1] = NT > 1 && g + 8 < nh ? *reinterpret_cast<const uint32_t*>(src + (g + 8) * DH) : 0u;
+            q[k][3] = NT > 1 && g + 8 < nh ? *reinterpret_cast<const uint32_t*>(src + (g + 8) * DH + 8) : 0u;
+        }
+        float m[NT], l[NT], o[DH / 16][NT][4];
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            m[x] = -INFINITY;
+            l[x] = 0.f;
+#pragma unroll
+            for (int i = 0; i < DH / 16; ++i) o[i][x][0] = o[i][x][1] = o[i][x][2] = o[i][x][3] = 0.f;
+        }
+        int k0 = skip;
+        for (; k0 < n; k0 += kPdWarps) {
+            load_step();
+            cp_async_wait<S - 1>();
+            __syncwarp();
+            const uint32_t ks = ring + (uint32_t)(st * G::kStage), vs = ks + kPdKeys * G::kRow;
+            const uint32_t mask = s_mask[warp][st];
+            const int lr = ((lane >> 4) << 3) + (lane & 7), lc = (lane >> 3) & 1;  // ldmatrix: row, chunk of a pair
+            float s[2][4] = {};
+#pragma unroll
+            for (int k = 0; k < DH / 16; ++k) {
+                uint32_t kb[4];
+                ldsm4(ks + (uint32_t)(lr * G::kRow + (((2 * k + lc) ^ (lr & 7)) << 4)), kb);
+                mma16816<T>(s[0], q[k], kb[0], kb[1]);
+                mma16816<T>(s[1], q[k], kb[2], kb[3]);
+            }
+            uint32_t hi[NT][2], lo[NT][2];
+            float al[NT];
+            bool moved = false;
+#pragma unroll
+            for (int x = 0; x < NT; ++x) {
+                float v[4], mx = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {  // keys 2t, 2t + 1, 2t + 8, 2t + 9 of head g + 8x
+                    const int key = 8 * (e >> 1) + 2 * t + (e & 1);
+                    v[e] = (mask >> key) & 1u ? s[e >> 1][2 * x + (e & 1)] * a.scale_log2 : -INFINITY;
+                    mx = fmaxf(mx, v[e]);
+                }
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                const float mn = fmaxf(m[x], mx), ref = mn == -INFINITY ? 0.f : mn;
+                al[x] = exp2f(m[x] - ref);
+                moved |= mn != m[x];
+                m[x] = mn;
+                float p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[e] = exp2f(v[e] - ref);
+                l[x] = l[x] * al[x] + ((p[0] + p[1]) + (p[2] + p[3]));
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    hi[x][e] = E::pack(p[2 * e], p[2 * e + 1]);
+                    const float2 f = E::unpack(hi[x][e]);
+                    lo[x][e] = E::pack(p[2 * e] - f.x, p[2 * e + 1] - f.y);
+                }
+            }
+            if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+                for (int x = 0; x < NT; ++x) {  // heads 2t and 2t + 1 of o's columns
+                    const float a0 = __shfl_sync(0xffffffffu, al[x], 8 * t), a1 = __shfl_sync(0xffffffffu, al[x], 8 * t + 4);
+#pragma unroll
+                    for (int i = 0; i < DH / 16; ++i) {
+                        o[i][x][0] *= a0;
+                        o[i][x][1] *= a1;
+                        o[i][x][2] *= a0;
+                        o[i][x][3] *= a1;
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < DH / 16; ++i) {
+                uint32_t va[4], vt[4];
+                ldsm4_t(vs + (uint32_t)(lr * G::kRow + (((2 * i + lc) ^ (lr & 7)) << 4)), va);
+                vt[0] = va[0], vt[1] = va[1], vt[2] = va[2], vt[3] = va[3];
+#pragma unroll
+                for (int x = 0; x < NT; ++x) {
+                    mma16816<T>(o[i][x], vt, hi[x][0], hi[x][1]);
+                    mma16816<T>(o[i][x], vt, lo[x][0], lo[x][1]);
+                }
+            }
+            __syncwarp();
+            st = st + 1 == S ? 0 : st + 1;
+        }
+        skip = k0 - n;
+
+        // ---- the unit's end here: the four warps' (m, l, o) into one
+        const bool whole = at.i == 0 && n == at.steps;
+        int64_t first = 0, last = 0;  // the CTAs that share the unit
+        if (!whole) {
+            const int64_t u0 = now - at.i;
+            first = u0 / per;
+            last = (u0 + at.steps - 1) / per;
+        }
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            l[x] += __shfl_xor_sync(0xffffffffu, l[x], 1);
+            l[x] += __shfl_xor_sync(0xffffffffu, l[x], 2);
+            if (t == 0) {
+                s_ml[0][warp][8 * x + g] = m[x];
+                s_ml[1][warp][8 * x + g] = l[x];
+            }
+        }
+        __syncthreads();
+        const int slot = (int)(2 * blockIdx.x + (first == blockIdx.x ? 1 : 0));
+        float* part = a.work + (int64_t)slot * a.slot_floats;
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            float f[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int h = 8 * x + 2 * t + e;
+                float mm = s_ml[0][0][h];
+                for (int w = 1; w < kPdWarps; ++w) mm = fmaxf(mm, s_ml[0][w][h]);
+                f[e] = exp2f(s_ml[0][warp][h] - (mm == -INFINITY ? 0.f : mm));
+            }
+            if (x > 0) __syncthreads();  // the buffer holds 8 heads
+#pragma unroll
+            for (int i = 0; i < DH / 16; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int h = 2 * t + (e & 1), d = (16 * i + g + 8 * (e >> 1)) ^ (8 * t);
+                    so[(warp * 8 + h) * DH + d] = o[i][x][e] * f[e & 1];
+                }
+            __syncthreads();
+            for (int e = tid; e < 8 * DH / 8; e += kPdThreads) {  // 8 dims of a head
+                const int h = e / (DH / 8), d = (e % (DH / 8)) * 8, ds = d ^ (8 * (h >> 1));
+                if (8 * x + h >= nh) continue;
+                float sum[8] = {};
+                float mm = s_ml[0][0][8 * x + h], ll = 0.f;
+                for (int w = 1; w < kPdWarps; ++w) mm = fmaxf(mm, s_ml[0][w][8 * x + h]);
+                const float ref = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+                for (int w = 0; w < kPdWarps; ++w) {
+                    ll += s_ml[1][w][8 * x + h] * exp2f(s_ml[0][w][8 * x + h] - ref);
+                    const float4* v = reinterpret_cast<const float4*>(so + (w * 8 + h) * DH + ds);
+                    const float4 v0 = v[0], v1 = v[1];
+                    sum[0] += v0.x, sum[1] += v0.y, sum[2] += v0.z, sum[3] += v0.w;
+                    sum[4] += v1.x, sum[5] += v1.y, sum[6] += v1.z, sum[7] += v1.w;
+                }
+                if (whole) {
+                    const float inv = ll == 0.f ? 0.f : 1.f / ll;
+                    uint16_t* dst = a.out + (int64_t)at.b * a.out_ld + (int64_t)(kvh * a.group + h0 + 8 * x + h) * DH + d;
+                    *reinterpret_cast<uint4*>(dst) = make_uint4(E::pack(sum[0] * inv, sum[1] * inv), E::pack(sum[2] * inv, sum[3] * inv),
+                                                                E::pack(sum[4] * inv, sum[5] * inv), E::pack(sum[6] * inv, sum[7] * inv));
+                } else {
+                    float* po = part + 16 * NT + (8 * x + h) * DH + d;
+                    reinterpret_cast<float4*>(po)[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+                    reinterpret_cast<float4*>(po)[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+                    if (d == 0) {
+                        part[8 * x + h] = mm;
+                        part[8 * NT + 8 * x + h] = ll;
+                    }
+                }
+            }
+        }
+        if (!whole) {
+            // ---- the last CTA of the unit to get here joins the parts, in CTA order
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                const int parts = (int)(last - first) + 1;
+                s_last = atomicAdd(&a.arrived[first], 1) == parts - 1;
+                if (s_last) a.arrived[first] = 0;  // ready for the next call
+            }
+            __syncthreads();
+            if (s_last) {
+                __threadfence();
+                for (int e = tid; e < nh * (DH / 8); e += kPdThreads) {
+                    const int h = e / (DH / 8), d = (e % (DH / 8)) * 8;
+                    float sum[8] = {}, mm = -INFINITY, ll = 0.f;
+#pragma unroll 4
+                    for (int64_t p = first; p <= last; ++p) {
+                        const float* src = a.work + (2 * p + (p == first ? 1 : 0)) * a.slot_floats;
+                        const float pm = __ldcg(src + h), pl = __ldcg(src + 8 * NT + h);
+                        const float4* v = reinterpret_cast<const float4*>(src + 16 * NT + h * DH + d);
+                        const float4 v0 = __ldcg(v), v1 = __ldcg(v + 1);
+                        const float mn = fmaxf(mm, pm), ref = mn == -INFINITY ? 0.f : mn;
+                        const float fa = exp2f(mm - ref), fb = exp2f(pm - ref);
+                        mm = mn;
+                        ll = ll * fa + pl * fb;
+                        sum[0] = sum[0] * fa + v0.x * fb, sum[1] = sum[1] * fa + v0.y * fb;
+                        sum[2] = sum[2] * fa + v0.z * fb, sum[3] = sum[3] * fa + v0.w * fb;
+                        sum[4] = sum[4] * fa + v1.x * fb, sum[5] = sum[5] * fa + v1.y * fb;
+                        sum[6] = sum[6] * fa + v1.z * fb, sum[7] = sum[7] * fa + v1.w * fb;
+                    }
+                    const float inv = ll == 0.f ? 0.f : 1.f / ll;
+                    uint16_t* dst = a.out + (int64_t)at.b * a.out_ld + (int64_t)(kvh * a.group + h0 + h) * DH + d;
+                    *reinterpret_cast<uint4*>(dst) = make_uint4(E::pack(sum[0] * inv, sum[1] * inv), E::pack(sum[2] * inv, sum[3] * inv),
+                                                                E::pack(sum[4] * inv, sum[5] * inv), E::pack(sum[6] * inv, sum[7] * inv));
+                }
+            }
+        }
+        __syncthreads();  // so and s_ml are free for the next unit
+        now += n;
+        at.move(a, n, units);
+    }
+    cp_async_wait<0>();
+}
+
+template <class T, int DH, int NT>
+static cudaError_t decode_nt(const PagedAttnArgs& a, cudaStream_t st) {
+    const int units = a.c.n_kv_heads * ((a.group + 8 * NT - 1) / (8 * NT));
+    const int64_t span = a.window > 0 ? std::min<int64_t>(a.window + kPdKeys, a.c.cap) : a.c.cap;
+    const int64_t most = (int64_t)a.c.n_seqs * units * ((span + kPdKeys - 1) / kPdKeys + 1);  // steps at the longest lengths
+    const int64_t grid = std::min<int64_t>(std::min(kPagedMaxGrid, kPdCtasPerSm * g_num_sms), (most + kPdMinSteps - 1) / kPdMinSteps);
+    return launch_paged_k(k_paged_decode<T, DH, NT>, (unsigned)grid, kPdThreads, PdGeom<DH>::kSmem, st, a);
+}
+template <class T>
+static cudaError_t decode_t(const PagedAttnArgs& a, int dh, cudaStream_t st) {
+    if (dh == 128) return a.group <= 8 ? decode_nt<T, 128, 1>(a, st) : decode_nt<T, 128, 2>(a, st);
+    return a.group <= 8 ? decode_nt<T, 64, 1>(a, st) : decode_nt<T, 64, 2>(a, st);
+}
+cudaError_t launch_paged_decode(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st) {
+    return dtype == VT_F16 ? decode_t<__half>(a, dh, st) : decode_t<__nv_bfloat16>(a, dh, st);
+}
+
+template <class T, int DH, int NT>
+static cudaError_t init_one() {
+    return cudaFuncSetAttribute(k_paged_decode<T, DH, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                (int)PdGeom<DH>::kSmem);
+}
+cudaError_t init_paged_decode() {
+    cudaError_t e[8] = {init_one<__half, 64, 1>(),        init_one<__half, 64, 2>(),        init_one<__half, 128, 1>(),
+                        init_one<__half, 128, 2>(),       init_one<__nv_bfloat16, 64, 1>(), init_one<__nv_bfloat16, 64, 2>(),
+                        init_one<__nv_bfloat16, 128, 1>(), init_one<__nv_bfloat16, 128, 2>()};
+    for (cudaError_t x : e)
+        if (x != cudaSuccess) return x;
+    return cudaSuccess;
+}
+
+}  // namespace vt
