@@ -607,7 +607,8 @@ typedef struct {
     const int32_t* tables; /* device [n_seqs][pages_per_seq] page ids */
     const int32_t* lens;   /* device [n_seqs] */
     const int32_t* starts; /* device [n_seqs + 1], or NULL: one row per sequence */
-    int32_t n_seqs, pages_per_seq; /* pages_per_seq * page_size <= 2^30 */
+    int32_t n_seqs;        /* at most 16384 */
+    int32_t pages_per_seq; /* pages_per_seq * page_size <= 2^30 */
 } vt_paged_batch;
 
 typedef struct vt_paged vt_paged;
@@ -646,7 +647,7 @@ VT_API vt_status vt_paged_append(vt_paged* paged, const vt_paged_pool* pool, con
  * (window 0: [0, p]):
  *   out[b][h] = sum_j softmax_j(scale * q[b][h] . k_j) v_j.
  * q, out [n_seqs][n_heads][d_head], rows q_ld / out_ld elements apart.  n_heads: a multiple of
- * n_kv_heads, at most 128 times it. */
+ * n_kv_heads, at most 128 times it.  scale: finite, >= 0. */
 VT_API vt_status vt_paged_decode(vt_paged* paged, const vt_paged_pool* pool, const vt_paged_batch* batch,
                                  int32_t n_heads, const void* q, int64_t q_ld, float scale, int32_t window, void* out,
                                  int64_t out_ld, vt_stream stream);

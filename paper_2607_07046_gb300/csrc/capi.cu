@@ -121,6 +121,8 @@ cudaError_t init_library() {
         g_init_err = init_quant_kernels();
         if (g_init_err != cudaSuccess) return;
         g_init_err = init_paged_decode();
+        if (g_init_err != cudaSuccess) return;
+        g_init_err = init_paged_prefill();
     });
     return g_init_err;
 }
@@ -2203,7 +2205,7 @@ struct vt_paged {
     uint8_t* base = nullptr;     // status word, arrival counters, slots
     uint32_t* status = nullptr;
     int* arrived = nullptr;      // [kPagedMaxGrid]
-    float* work = nullptr;       // [2 kPagedMaxGrid][kPagedSlotFloats]
+    float* work = nullptr;       // [paged_work_floats()]
 };
 
 extern "C" void vt_paged_destroy(vt_paged* g) {
@@ -2226,7 +2228,7 @@ extern "C" vt_status vt_paged_create(const vt_allocator* allocator, vt_stream st
         g->alloc.custom = true;
     }
     const size_t head = 256 + kPagedMaxGrid * sizeof(int);
-    g->base = static_cast<uint8_t*>(g->alloc.get(head + (size_t)2 * kPagedMaxGrid * kPagedSlotFloats * sizeof(float)));
+    g->base = static_cast<uint8_t*>(g->alloc.get(head + paged_work_floats() * sizeof(float)));
     if (!g->base) {
         vt_paged_destroy(g);
         return fail(VT_ERR_ALLOC, "allocating the paged workspace failed");
@@ -2280,8 +2282,8 @@ vt_status paged_view(const vt_paged* g, const vt_paged_pool* p, const vt_paged_b
         if (s.used && (s.stride < p->d_head || s.stride % 8 || s.stride > ((int64_t)1 << 40)))
             return fail(VT_ERR_INVALID_ARG, "%s_stride %lld must be a multiple of 8, at least d_head and at most 2^40", s.what,
                         (long long)s.stride);
-    if (b->n_seqs < 0 || b->pages_per_seq < 1)
-        return fail(VT_ERR_INVALID_ARG, "n_seqs must be >= 0 and pages_per_seq >= 1");
+    if (b->n_seqs < 0 || b->n_seqs > kPagedMaxSeqs || b->pages_per_seq < 1)
+        return fail(VT_ERR_INVALID_ARG, "n_seqs must be in [0, %d] and pages_per_seq >= 1", kPagedMaxSeqs);
     if ((int64_t)b->pages_per_seq * p->page_size > ((int64_t)1 << 30))
         return fail(VT_ERR_INVALID_ARG, "pages_per_seq * page_size must be at most 2^30");
     if (b->n_seqs > 0 && (!b->tables || !b->lens)) return fail(VT_ERR_INVALID_ARG, "tables and lens must not be NULL");
@@ -2330,7 +2332,7 @@ vt_status paged_attn(vt_paged* g, const vt_paged_pool* pool, const vt_paged_batc
     VT_TRY(paged_view(g, pool, batch, &a->c));
     VT_TRY(paged_n_rows(batch, n_rows));
     VT_TRY(paged_heads(pool, n_heads));
-    if (!std::isfinite(scale)) return fail(VT_ERR_INVALID_ARG, "scale must be finite");
+    if (!std::isfinite(scale) || scale < 0.f) return fail(VT_ERR_INVALID_ARG, "scale must be finite and >= 0");
     if (window < 0) return fail(VT_ERR_INVALID_ARG, "window %d is negative", window);
     a->n_rows = n_rows;
     if (n_rows == 0 || batch->n_seqs == 0) return VT_OK;
@@ -2347,7 +2349,6 @@ vt_status paged_attn(vt_paged* g, const vt_paged_pool* pool, const vt_paged_batc
     a->out = static_cast<uint16_t*>(out);
     a->out_ld = n_rows > 1 ? out_ld : 0;
     a->work = g->work;
-    a->slot_floats = kPagedSlotFloats;
     a->arrived = g->arrived;
     return VT_OK;
 }
@@ -2405,6 +2406,6 @@ extern "C" vt_status vt_paged_prefill(vt_paged* g, const vt_paged_pool* pool, co
     PagedAttnArgs a{};
     VT_TRY(paged_attn(g, pool, batch, n_rows, n_heads, q, q_ld, scale, window, out, out_ld, &a));
     if (a.n_rows == 0 || batch->n_seqs == 0) return ok();
-    VT_CUDA(launch_paged_attn(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
+    VT_CUDA(launch_paged_prefill(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
     return ok();
 }

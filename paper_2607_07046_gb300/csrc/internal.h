@@ -317,18 +317,21 @@ struct PagedAttnArgs {
     int window;
     uint16_t* out;
     int64_t out_ld;
-    // workspace: two slots a CTA for parts of a unit that several CTAs share, and for each CTA the
-    // number of them that have stored their part (zero between calls)
+    // workspace: slots for the parts of a unit that several CTAs share, and for the first CTA of each
+    // such unit the number of parts that are there (zero between calls)
     float* work;
-    int64_t slot_floats;
     int* arrived;
 };
-constexpr int kPagedSlotFloats = 32 + 16 * 128;
-constexpr int kPagedMaxGrid = 1024;
+constexpr int kPagedMaxGrid = 1024;                          // CTAs of an attention launch, at most
+constexpr int64_t kPagedDecodeSlot = 32 + 16 * 128;          // floats: (m, l) and o of 16 heads; two a CTA
+constexpr int64_t kPagedPrefillSlot = 2 * 128 + 128 * 128;   // floats: (m, l) and O of 128 rows; four a CTA
+constexpr int kPagedMaxSeqs = 16384;                         // sequences of a batch
+size_t paged_work_floats();
 cudaError_t launch_paged_append(const PagedAppendArgs& a, int dtype, int dh, cudaStream_t st);
-cudaError_t launch_paged_attn(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st);
 cudaError_t launch_paged_decode(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st);
+cudaError_t launch_paged_prefill(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st);
 cudaError_t init_paged_decode();
+cudaError_t init_paged_prefill();
 
 // ------------------------------------------------------------------ static scratch
 // (static_scratch.cu) the decode step whose intermediates are in one file-scope __device__ array.

@@ -1,10 +1,6 @@
-// Kernels of the paged KV cache (Voltron Section 2.1, the KV cache of prefill and decode, for several
-// sequences in pages of one pool).
-//
-//   k_paged_append   rotates q and k to their positions, writes k and v to the pages
-//   k_paged_attn     attention of several new rows of a sequence over its pages
+// Rotation and append of the paged KV cache (Voltron Section 2.1, the KV cache of prefill and decode, for
+// several sequences in pages of one pool).
 #include <cuda_runtime.h>
-#include <math.h>
 
 #include "paged.cuh"
 
@@ -108,81 +104,6 @@ static cudaError_t append_dh(const PagedAppendArgs& a, cudaStream_t st) {
 cudaError_t launch_paged_append(const PagedAppendArgs& a, int dtype, int dh, cudaStream_t st) {
     if (dtype == VT_F16) return dh == 128 ? append_dh<__half, 128>(a, st) : append_dh<__half, 64>(a, st);
     return dh == 128 ? append_dh<__nv_bfloat16, 128>(a, st) : append_dh<__nv_bfloat16, 64>(a, st);
-}
-
-// ================================================================== attention
-//
-// One warp per (row, query head): o = sum_j softmax_j(q . k_j) v_j over the row's positions, with a
-// running maximum m and sum l.  A lane holds dh / 32 neighbouring dimensions.
-constexpr int kAttnRowWarps = 4;
-
-template <class T, int DH>
-__global__ void __launch_bounds__(kAttnRowWarps * 32) k_paged_attn(const __grid_constant__ PagedAttnArgs a) {
-    constexpr int W = DH / 64;  // words a lane
-    using E = Elem<T>;
-    pdl_wait();
-    pdl_launch_dependents();
-    const PagedView& c = a.c;
-    const int lane = threadIdx.x & 31;
-    const int64_t gw = (int64_t)blockIdx.x * kAttnRowWarps + (threadIdx.x >> 5);
-    const int row = (int)(gw / a.n_heads), h = (int)(gw - (int64_t)row * a.n_heads);
-    if (row >= a.n_rows) return;
-    const int b = paged_seq_of_row(c, row, lane);
-    if (b < 0) return;
-    const int len = paged_len(c, b);
-    int end = 0, beg = 0;
-    if (len >= 0) {
-        const int p = len + (row - paged_start(c, b, a.n_rows));
-        if (p >= c.cap && lane == 0) set_status(c.status, VT_DEV_KV_OVERFLOW);
-        end = min(p + 1, c.cap);
-        if (a.window > 0) beg = max(0, p - a.window + 1);
-    }
-    float q[2 * W], o[2 * W], m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int e = 0; e < W; ++e) {
-        const float2 f = E::unpack(reinterpret_cast<const uint32_t*>(a.q + row * a.q_ld + (int64_t)h * DH)[lane * W + e]);
-        q[2 * e] = f.x * a.scale_log2;
-        q[2 * e + 1] = f.y * a.scale_log2;
-        o[2 * e] = o[2 * e + 1] = 0.f;
-    }
-    for (int j = beg; j < end; ++j) {
-        const int64_t at = paged_entry(c, b, h / a.group, j);
-        if (at < 0) continue;
-        float s = 0.f;
-        float2 v[W];
-#pragma unroll
-        for (int e = 0; e < W; ++e) {
-            const float2 k = E::unpack(reinterpret_cast<const uint32_t*>(a.kpool + at)[lane * W + e]);
-            v[e] = E::unpack(reinterpret_cast<const uint32_t*>(a.vpool + at)[lane * W + e]);
-            s += q[2 * e] * k.x + q[2 * e + 1] * k.y;
-        }
-        s = warp_sum(s);
-        const float mn = fmaxf(m, s), al = m == mn ? 1.f : exp2f(m - mn), p = mn == -INFINITY ? 0.f : exp2f(s - mn);
-        m = mn;
-        l = l * al + p;
-#pragma unroll
-        for (int e = 0; e < W; ++e) {
-            o[2 * e] = o[2 * e] * al + p * v[e].x;
-            o[2 * e + 1] = o[2 * e + 1] * al + p * v[e].y;
-        }
-    }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-    for (int e = 0; e < W; ++e)
-        reinterpret_cast<uint32_t*>(a.out + row * a.out_ld + (int64_t)h * DH)[lane * W + e] =
-            E::pack(o[2 * e] * inv, o[2 * e + 1] * inv);
-}
-
-template <class T, int DH>
-static cudaError_t attn_dh(const PagedAttnArgs& a, cudaStream_t st) {
-    const int64_t warps = (int64_t)a.n_rows * a.n_heads;
-    return launch_paged_k(k_paged_attn<T, DH>, (unsigned)((warps + kAttnRowWarps - 1) / kAttnRowWarps),
-                          kAttnRowWarps * 32, 0, st, a);
-}
-
-cudaError_t launch_paged_attn(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st) {
-    if (dtype == VT_F16) return dh == 128 ? attn_dh<__half, 128>(a, st) : attn_dh<__half, 64>(a, st);
-    return dh == 128 ? attn_dh<__nv_bfloat16, 128>(a, st) : attn_dh<__nv_bfloat16, 64>(a, st);
 }
 
 }  // namespace vt

@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
         }
         __syncthreads();
         const int slot = (int)(2 * blockIdx.x + (first == blockIdx.x ? 1 : 0));
-        float* part = a.work + (int64_t)slot * a.slot_floats;
+        float* part = a.work + (int64_t)slot * kPagedDecodeSlot;
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
             float f[2];
@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
                     float sum[8] = {}, mm = -INFINITY, ll = 0.f;
 #pragma unroll 4
                     for (int64_t p = first; p <= last; ++p) {
-                        const float* src = a.work + (2 * p + (p == first ? 1 : 0)) * a.slot_floats;
+                        const float* src = a.work + (2 * p + (p == first ? 1 : 0)) * kPagedDecodeSlot;
                         const float pm = __ldcg(src + h), pl = __ldcg(src + 8 * NT + h);
                         const float4* v = reinterpret_cast<const float4*>(src + 16 * NT + h * DH + d);
                         const float4 v0 = __ldcg(v), v1 = __ldcg(v + 1);

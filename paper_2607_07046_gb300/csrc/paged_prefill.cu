@@ -1,0 +1,727 @@
+// Causal attention of several new rows per sequence over the paged KV cache, on the 5th-generation tensor
+// cores (Voltron Section 2.1, prefill phase, for several sequences).
+//
+// A unit of work is a sequence's KV head and two tiles of query rows: row r of a tile is query head
+// r % group of the KV head and token r / group, so the group's heads share the K and V blocks and a few
+// new tokens still fill a tile.  Both tiles walk the unit's positions in blocks of 128 keys:
+//   S_x = Q_x . K_j^T       tcgen05, M 128, N 128, K dh, operands in shared memory, S in tensor memory
+//   P_x = 2^(S_x scale log2(e) - m), masked, 16 bits, written over S_x in tensor memory
+//   O_x += P_x . V_j        tcgen05, M 128, N dh, K 128, P from tensor memory, V as it lies in the pages
+// While the softmax of one tile runs, the tensor core has the other tile's products.  A block pair costs
+// 4 x 512 cycles of tensor work, as long as the 2 x 128 x 128 exponentials take on the SM's special-function
+// units, and K and V pass through shared memory once for both tiles.
+//
+//   warps 0-3, 4-7  softmax of tile 0 and 1, one thread a row (its lane of the tensor memory): no exchange
+//                   between threads.  m is a reference maximum; O and l are rescaled only when a block's
+//                   maximum exceeds it by more than 8 (log2), so P stays below 2^8.
+//   warps 8-10      copies: rows of K and V through the page table, and Q, by 16-byte asynchronous copies in
+//                   the swizzled operand layout (a tensor copy cannot follow pages smaller than its box, nor
+//                   leave out the positions past a sequence's end, which are filled with zeros here)
+//   warp 11         tensor memory and the MMAs
+//
+// The blocks of all units form one line, and CTA c (one an SM) takes its c-th equal part, so neither few
+// long histories nor ragged prompts leave SMs idle; lengths are known on the device only.  A unit that
+// several CTAs share is joined by the last of them to finish, in CTA order.  Every mbarrier wait is
+// bounded; on a timeout a warp sets VT_DEV_WAIT_TIMEOUT, issues and stores nothing more, and still passes
+// every named barrier.
+#include <cuda_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+#include <climits>
+
+#include "paged.cuh"
+#include "tcgen05.cuh"
+
+namespace vt {
+
+constexpr int kPfRows = 128, kPfKeys = 128;  // rows of a tile, keys of a block
+constexpr int kPfThreads = 384;
+constexpr int kPfCopyWarps = 3;
+// registers a thread: at launch 65536 / 384, rounded down to 8; then 2 x 128 threads of softmax and 128 of
+// copies and MMAs
+constexpr int kPfLaunchRegs = 168, kPfSoftmaxRegs = 208, kPfCopyRegs = 88;
+static_assert(256 * kPfSoftmaxRegs + 128 * kPfCopyRegs <= kPfThreads * kPfLaunchRegs,
+              "the register split must fit in the registers the block is launched with");
+constexpr int kPfMaskRing = 8;   // validity words of the last blocks (the copies lead by fewer blocks)
+constexpr int kPfMinBlocks = 2;  // blocks a CTA takes at least
+constexpr int kPfLag = 2;        // copy groups in flight behind the one just issued
+
+template <int DH>
+struct PfGeom {
+    static constexpr int kTile = kPfRows * DH * 2;         // bytes of a Q tile, of a K or V block
+    static constexpr int kAtom = kPfRows * 128;            // its 64-column box
+    static constexpr int kSlots = DH == 128 ? 5 : 10;      // K and V blocks of the ring, in turn
+    static constexpr size_t kSmem = 1024 + (size_t)(2 + kSlots) * kTile + 512;
+};
+
+// The units in order: sequence, KV head, tile pair.
+struct PfCursor {
+    int b, kvh, pt;        // unit
+    int i, n, kb0;         // next block, blocks of the unit, its first block's number
+    int len, row0, rows;   // the sequence (rows 0: idle)
+    int kbeg, kend;        // attended positions of the unit
+    __device__ __forceinline__ void seq(const PagedAttnArgs& a, int at) {
+        b = at;
+        kvh = pt = 0;
+        rows = 0;
+        if (b < a.c.n_seqs) {
+            len = paged_len(a.c, b);
+            row0 = paged_start(a.c, b, a.n_rows);
+            rows = len < 0 ? 0 : max(0, paged_start(a.c, b + 1, a.n_rows) - row0);
+        }
+    }
+    // attended positions of tokens [t0, t1) of the sequence
+    __device__ __forceinline__ void range(const PagedAttnArgs& a, int t0, int t1, int& beg, int& end) const {
+        end = min(len + t1, a.c.cap);
+        beg = a.window > 0 ? max(0, len + t0 + 1 - a.window) : 0;
+        if (beg >= end) beg = end = 0;
+    }
+    __device__ __forceinline__ static int blocks(int beg, int end) { return (end + kPfKeys - 1) / kPfKeys - beg / kPfKeys; }
+    __device__ __forceinline__ void unit(const PagedAttnArgs& a, int tr) {
+        const int t0 = pt * 2 * tr;
+        range(a, t0, min(t0 + 2 * tr, rows), kbeg, kend);
+        kb0 = kbeg / kPfKeys;
+        n = blocks(kbeg, kend);
+        i = 0;
+    }
+    // on to the next unit that has blocks
+    __device__ __forceinline__ void next(const PagedAttnArgs& a, int tr) {
+        do {
+            if ((pt + 1) * 2 * tr < rows)
+                ++pt;
+            else if (rows > 0 && kvh + 1 < a.c.n_kv_heads)
+                ++kvh, pt = 0;
+            else {
+                do seq(a, b + 1);
+                while (rows == 0 && b < a.c.n_seqs);
+                if (b >= a.c.n_seqs) return;
+            }
+            unit(a, tr);
+        } while (n == 0);
+    }
+    __device__ __forceinline__ void move(const PagedAttnArgs& a, int tr, int blocks_done) {
+        i += blocks_done;
+        if (i >= n) next(a, tr);
+    }
+    // blocks [lo, hi) of those numbered j0 .. j1 - 1 that tile x attends to; false: the tile has no tokens
+    __device__ __forceinline__ bool tile(const PagedAttnArgs& a, int tr, int x, int j0, int j1, int& lo, int& hi) const {
+        const int t0 = (2 * pt + x) * tr, t1 = min(t0 + tr, rows);
+        lo = hi = j0;
+        if (t0 >= t1) return false;
+        int beg, end;
+        range(a, t0, t1, beg, end);
+        if (end > beg) {
+            lo = max(j0, beg / kPfKeys);
+            hi = max(lo, min(j1, (end + kPfKeys - 1) / kPfKeys));
+        }
+        return true;
+    }
+};
+
+__device__ __forceinline__ void pf_copy16(uint32_t dst, const void* src, bool full) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(full ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void pf_zero_row(const PagedAttnArgs& a, int row, int words, int lane) {
+    for (int e = lane; e < words; e += 32) reinterpret_cast<uint4*>(a.out + row * a.out_ld)[e] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+template <class T, int DH>
+__global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_constant__ PagedAttnArgs a) {
+    using E = Elem<T>;
+    using G = PfGeom<DH>;
+    constexpr int S = G::kSlots;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t* Qs = smem;                      // [2][kTile]
+    uint8_t* Rs = Qs + 2 * G::kTile;         // [S][kTile]
+    uint32_t* valid = reinterpret_cast<uint32_t*>(Rs + S * G::kTile);  // [kPfMaskRing][4]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(valid + kPfMaskRing * 4);
+    uint64_t* full = bars;                   // [S]
+    uint64_t* empty = full + S;              // [S]
+    uint64_t* q_full = empty + S;
+    uint64_t* q_empty = q_full + 1;
+    uint64_t* s_full = q_empty + 1;          // [2] S_x is there (and O_x holds every earlier block)
+    uint64_t* p_full = s_full + 2;           // [2]
+    uint64_t* o_full = p_full + 2;           // [2] the unit's last block is in O_x
+    uint64_t* o_free = o_full + 2;           // [2] O_x has been read
+    uint64_t* done = o_free + 2;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+    volatile int* s_err = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    volatile int* s_last = s_err + 1;        // [2]
+    int64_t* s_at = reinterpret_cast<int64_t*>(tmem_slot + 4);  // [2]: blocks of all units; blocks before the first unit's
+    int* s_unit = reinterpret_cast<int*>(s_at + 2);             // [4]
+
+    const PagedView& c = a.c;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tr = kPfRows / a.group;  // tokens of a tile
+    if (tid == 0) {
+        for (int s = 0; s < S; ++s) {
+            mbar_init(&full[s], kPfCopyWarps);
+            mbar_init(&empty[s], 1);
+        }
+        mbar_init(q_full, kPfCopyWarps);
+        mbar_init(q_empty, 1);
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(&s_full[x], 1);
+            mbar_init(&p_full[x], 4);
+            mbar_init(&o_full[x], 1);
+            mbar_init(&o_free[x], 4);
+        }
+        mbar_init(done, 1);
+        *s_err = 0;
+        fence_mbar_init();
+    }
+    pdl_wait();
+    pdl_launch_dependents();
+
+    // ---- blocks of each sequence for one KV head (a warp a sequence, a lane a tile pair); rows that
+    // attend to nothing get zeros
+    int64_t* tot = reinterpret_cast<int64_t*>(smem);
+    PfCursor at;
+    for (int b = warp; b < c.n_seqs; b += kPfThreads / 32) {
+        at.seq(a, b);
+        int64_t sum = 0;
+        if (at.len < 0) {
+            const int end = paged_start(c, b + 1, a.n_rows);
+            for (int r = at.row0; r < end; ++r)
+                if (r % gridDim.x == blockIdx.x) pf_zero_row(a, r, a.n_heads * DH / 8, lane);
+        } else {
+            if (blockIdx.x == 0 && lane == 0 && at.len + at.rows > c.cap) set_status(c.status, VT_DEV_KV_OVERFLOW);
+            for (int p0 = 0; p0 * 2 * tr < at.rows; p0 += 32) {
+                const int t0 = (p0 + lane) * 2 * tr;
+                int n = 0;
+                if (t0 < at.rows) {
+                    int beg, end;
+                    at.range(a, t0, min(t0 + 2 * tr, at.rows), beg, end);
+                    n = PfCursor::blocks(beg, end);
+                }
+                for (unsigned none = __ballot_sync(0xffffffffu, t0 < at.rows && n == 0); none; none &= none - 1) {
+                    const int z0 = (p0 + __ffs(none) - 1) * 2 * tr;
+                    for (int r = z0; r < min(z0 + 2 * tr, at.rows); ++r)
+                        if ((at.row0 + r) % gridDim.x == blockIdx.x) pf_zero_row(a, at.row0 + r, a.n_heads * DH / 8, lane);
+                }
+                sum += n;
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        }
+        if (lane == 0) tot[b] = sum;
+    }
+    __syncthreads();
+    // ---- where this CTA's part of the line begins
+    if (warp == 0) {
+        int64_t sum = 0;
+        for (int b = lane; b < c.n_seqs; b += 32) sum += tot[b];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        const int64_t line = sum * c.n_kv_heads;
+        const int64_t per = max((line + gridDim.x - 1) / gridDim.x, (int64_t)kPfMinBlocks);
+        const int64_t t0 = blockIdx.x * per;
+        if (lane == 0) s_at[0] = line;
+        if (t0 < line) {
+            int64_t before = 0;  // blocks of the sequences before b0, one KV head
+            int b = 0;
+            for (int b0 = 0;; b0 += 32) {
+                const int64_t v = b0 + lane < c.n_seqs ? tot[b0 + lane] : 0;
+                int64_t upto = v;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int64_t w = __shfl_up_sync(0xffffffffu, upto, o);
+                    if (lane >= o) upto += w;
+                }
+                const unsigned m = __ballot_sync(0xffffffffu, (before + upto) * c.n_kv_heads > t0);
+                if (m) {
+                    const int k = __ffs(m) - 1;
+                    b = b0 + k;
+                    before += __shfl_sync(0xffffffffu, upto - v, k);
+                    break;
+                }
+                before += __shfl_sync(0xffffffffu, upto, 31);
+            }
+            int64_t r = t0 - before * c.n_kv_heads;
+            const int kvh = (int)(r / tot[b]);
+            r -= (int64_t)kvh * tot[b];
+            at.seq(a, b);
+            for (int p0 = 0;; p0 += 32) {  // the tile pair
+                const int q0 = (p0 + lane) * 2 * tr;
+                int n = 0;
+                if (q0 < at.rows) {
+                    int beg, end;
+                    at.range(a, q0, min(q0 + 2 * tr, at.rows), beg, end);
+                    n = PfCursor::blocks(beg, end);
+                }
+                int64_t upto = n;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int64_t w = __shfl_up_sync(0xffffffffu, upto, o);
+                    if (lane >= o) upto += w;
+                }
+                const unsigned m = __ballot_sync(0xffffffffu, upto > r);
+                if (m) {
+                    const int k = __ffs(m) - 1;
+                    const int64_t skip = __shfl_sync(0xffffffffu, upto - n, k);
+                    if (lane == 0) {
+                        s_unit[0] = b;
+                        s_unit[1] = kvh;
+                        s_unit[2] = p0 + k;
+                        s_unit[3] = (int)(r - skip);
+                    }
+                    break;
+                }
+                r -= __shfl_sync(0xffffffffu, upto, 31);
+            }
+        }
+    }
+    __syncthreads();
+    const int64_t line = s_at[0];
+    const int64_t per = max((line + gridDim.x - 1) / gridDim.x, (int64_t)kPfMinBlocks);
+    const int64_t t0 = blockIdx.x * per, t1 = min(line, t0 + per);
+    if (t0 >= t1) return;
+    at.seq(a, s_unit[0]);
+    at.kvh = s_unit[1];
+    at.pt = s_unit[2];
+    at.unit(a, tr);
+    at.i = s_unit[3];
+    if (warp == 11) {
+        tc::tmem_alloc(tmem_slot, 512);
+        tc::tmem_relinquish();
+    }
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    const uint32_t tmem = *tmem_slot;  // S_0, S_1 (128 columns each, P over them), O_0, O_1
+    constexpr uint32_t kOCol = 2 * kPfKeys;
+
+    if (warp >= 8)  // a whole warpgroup
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPfCopyRegs));
+    if (warp >= 8 && warp < 11) {
+        // ================================================================ copies
+        const int w = warp - 8;
+        bool ok = true;
+        uint64_t *sent1 = nullptr, *sent2 = nullptr;  // the last two groups, not yet announced
+        auto announce = [&](uint64_t* bar) {
+            fence_proxy_async_smem();  // the copies wrote as threads do; the MMA reads as the copy engine does
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+        };
+        auto sent = [&](uint64_t* bar) {
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            if (sent2) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(kPfLag) : "memory");
+                announce(sent2);
+            }
+            sent2 = sent1;
+            sent1 = bar;
+        };
+        // 128 rows of which this warp copies every third group of 8: row 32 q + l starts at element off[q] of
+        // lane l (-1: zeros)
+        auto rows = [&](uint8_t* dst, const uint16_t* src, const int64_t (&off)[4]) {
+            constexpr int CPR = DH / 8, RPI = 32 / CPR;
+            const int chunk = lane % CPR, sub = lane / CPR;
+            const uint32_t d0 = smem_u32(dst) + (uint32_t)((chunk >> 3) * G::kAtom);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    if ((4 * q + g) % kPfCopyWarps != w) continue;
+#pragma unroll
+                    for (int r0 = 0; r0 < 8; r0 += RPI) {
+                        const int r = 8 * g + r0 + sub, row = 32 * q + r;
+                        const int64_t o = __shfl_sync(0xffffffffu, off[q], r);
+                        pf_copy16(d0 + (uint32_t)(row * 128 + (((chunk & 7) ^ (row & 7)) << 4)), src + (o < 0 ? 0 : o) + chunk * 8, o >= 0);
+                    }
+                }
+        };
+        int slot = 0, round = 0, blk = 0, nq = 0;
+        auto block = [&](const uint16_t* pool, const int64_t (&off)[4]) {
+            if (ok && round > 0) ok = mbar_wait_warp(&empty[slot], (round - 1) & 1);
+            if (ok) {
+                rows(Rs + slot * G::kTile, pool, off);
+                sent(&full[slot]);
+            }
+            if (++slot == S) slot = 0, ++round;
+        };
+        for (int64_t now = t0; ok && now < t1;) {
+            const int n = (int)min((int64_t)(at.n - at.i), t1 - now);
+            for (int j = at.kb0 + at.i, j0 = j; ok && j < j0 + n; ++j) {
+                int64_t off[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int p = j * kPfKeys + 32 * q + lane;
+                    off[q] = p >= at.kbeg && p < at.kend ? paged_entry(c, at.b, at.kvh, p) : -1;
+                    const uint32_t m = __ballot_sync(0xffffffffu, off[q] >= 0);
+                    if (w == 0 && lane == 0) valid[(blk % kPfMaskRing) * 4 + q] = m;
+                }
+                ++blk;
+                block(a.kpool, off);
+                if (j == j0 && ok) {  // the unit's queries, once the last unit's products with its own are done
+                    if (nq > 0) ok = mbar_wait_warp(q_empty, (nq - 1) & 1);
+                    ++nq;
+                    for (int x = 0; ok && x < 2; ++x) {
+                        int64_t qo[4];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int r = 32 * q + lane, tok = (2 * at.pt + x) * tr + r / a.group;
+                            qo[q] = r < tr * a.group && tok < at.rows
+                                        ? (at.row0 + tok) * a.q_ld + (int64_t)(at.kvh * a.group + r % a.group) * DH
+                                        : -1;
+                        }
+                        if ((2 * at.pt + x) * tr < at.rows) rows(Qs + x * G::kTile, a.q, qo);
+                    }
+                    if (ok) sent(q_full);
+                }
+                block(a.vpool, off);
+            }
+            now += n;
+            at.move(a, tr, n);
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        if (ok) {
+            if (sent2) announce(sent2);
+            if (sent1) announce(sent1);
+        } else if (lane == 0) {
+            *s_err = 1;
+            set_status(c.status, VT_DEV_WAIT_TIMEOUT);
+        }
+    } else if (warp == 11) {
+        // ================================================================ MMAs
+        constexpr uint32_t kType = std::is_same<T, __half>::value ? 0u : tc::kIdescBf16;
+        constexpr uint32_t idesc_s = tc::idesc_f16(kPfRows, kPfKeys) | kType, idesc_o = tc::idesc_f16_bmn(kPfRows, DH) | kType;
+        const uint32_t qd = tc::desc_sw128_lo(smem_u32(Qs)), kd = tc::desc_sw128_lo(smem_u32(Rs));
+        const uint64_t vd = tc::desc_sw128_mn(smem_u32(Rs), G::kAtom);
+        const uint32_t vd_hi = (uint32_t)(vd >> 32), vd_lo = (uint32_t)vd;
+        constexpr uint32_t kStep = G::kTile >> 4;
+        bool ok = true;
+        int slot = 0, par = 0, nq = 0;
+        int np[2] = {0, 0}, no[2] = {0, 0};
+        for (int64_t now = t0; ok && now < t1;) {
+            const int n = (int)min((int64_t)(at.n - at.i), t1 - now);
+            const int j0 = at.kb0 + at.i, j1 = j0 + n;
+            int lo[2], hi[2];
+            at.tile(a, tr, 0, j0, j1, lo[0], hi[0]);
+            at.tile(a, tr, 1, j0, j1, lo[1], hi[1]);
+            ok = mbar_wait_warp(q_full, nq & 1);
+            ++nq;
+            for (int j = j0 - 1; ok && j < j1; ++j) {
+                int vs = 0, ks = 0, kpar = 0;
+                if (j >= j0) {
+                    vs = slot;
+                    ok = mbar_wait_warp(&full[vs], par);
+                    if (++slot == S) slot = 0, par ^= 1;
+                }
+                const bool more = j + 1 < j1;
+                if (more) {
+                    ks = slot;
+                    kpar = par;
+                    if (++slot == S) slot = 0, par ^= 1;
+                }
+                bool have_k = false;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (ok && j >= lo[x] && j < hi[x]) {
+                        ok = mbar_wait_warp(&p_full[x], np[x] & 1);
+                        ++np[x];
+                        if (ok && j == lo[x]) {
+                            if (no[x] > 0) ok = mbar_wait_warp(&o_free[x], (no[x] - 1) & 1);
+                            ++no[x];
+                        }
+                        if (!ok) break;
+                        tc::fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int kk = 0; kk < kPfKeys / 16; ++kk)
+                                tc::mma_f16_ts(tmem + kOCol + (uint32_t)(x * DH), tmem + (uint32_t)(x * kPfKeys + kk * 8),
+                                               tc::desc_of(vd_hi, vd_lo + (uint32_t)vs * kStep + (uint32_t)kk * (2048 >> 4)), idesc_o,
+                                               (j > lo[x] || kk > 0) ? 1u : 0u);
+                            if (j == hi[x] - 1) tc::mma_commit(&o_full[x]);
+                        }
+                        __syncwarp();
+                    }
+                    if (x == 1 && ok && j >= j0) {
+                        if (elect_one()) tc::mma_commit(&empty[vs]);
+                        __syncwarp();
+                    }
+                    if (ok && more && !have_k) {
+                        ok = mbar_wait_warp(&full[ks], kpar);
+                        have_k = true;
+                    }
+                    if (ok && more && j + 1 >= lo[x] && j + 1 < hi[x]) {
+                        tc::fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int kk = 0; kk < DH / 16; ++kk) {
+                                const uint32_t off = (uint32_t)(kk >> 2) * (G::kAtom >> 4) + (uint32_t)(kk & 3) * 2;
+                                tc::mma_f16(tmem + (uint32_t)(x * kPfKeys), tc::desc_of(tc::kDescSw128Hi, qd + (uint32_t)x * kStep + off),
+                                            tc::desc_of(tc::kDescSw128Hi, kd + (uint32_t)ks * kStep + off), idesc_s, kk > 0);
+                            }
+                            tc::mma_commit(&s_full[x]);
+                        }
+                        __syncwarp();
+                    }
+                }
+                if (ok && more) {
+                    if (elect_one()) {
+                        tc::mma_commit(&empty[ks]);
+                        if (j + 1 == j1 - 1) tc::mma_commit(q_empty);
+                    }
+                    __syncwarp();
+                }
+                if (*s_err) ok = false;
+            }
+            now += n;
+            at.move(a, tr, n);
+        }
+        if (!ok && lane == 0) {
+            *s_err = 1;
+            set_status(c.status, VT_DEV_WAIT_TIMEOUT);
+        }
+        // tensor memory is freed only after every MMA issued has completed
+        if (elect_one()) tc::mma_commit(done);
+        __syncwarp();
+        if (!mbar_wait_warp(done, 0) && lane == 0) set_status(c.status, VT_DEV_WAIT_TIMEOUT);
+    } else {
+        // ================================================================ softmax of tile x
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPfSoftmaxRegs));
+        const int x = warp >> 2, row = tid & 127;
+        const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t s_at_col = tmem + lane_off + (uint32_t)(x * kPfKeys), o_at_col = tmem + lane_off + kOCol + (uint32_t)(x * DH);
+        const float sl2 = a.scale_log2;
+        bool ok = true;
+        int ns = 0, no = 0, blk = 0;
+        for (int64_t now = t0; now < t1;) {
+            const int n = (int)min((int64_t)(at.n - at.i), t1 - now);
+            const int j0 = at.kb0 + at.i, j1 = j0 + n;
+            int lo, hi;
+            const bool has = at.tile(a, tr, x, j0, j1, lo, hi);
+            const int tok = (2 * at.pt + x) * tr + row / a.group;
+            const bool live = row < tr * a.group && tok < at.rows;
+            const int qp = live ? at.len + tok : -1;  // position of this row (-1: it attends to nothing)
+            const int first_key = a.window > 0 ? qp - a.window + 1 : 0;
+            float m_use = -INFINITY, l = 0.f;
+            for (int j = lo; j < hi; ++j) {
+                if (ok && *s_err) ok = false;
+                if (ok) ok = mbar_wait_warp(&s_full[x], ns & 1);
+                ++ns;
+                if (!ok) continue;
+                tc::fence_after();
+                uint32_t sv[4][32];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tc::tmem_ld32(s_at_col + 32 * q, sv[q]);
+                const uint32_t* vw = valid + ((blk + j - j0) % kPfMaskRing) * 4;
+                const int kp0 = j * kPfKeys, cb = first_key - kp0, ce = qp + 1 - kp0;
+                uint32_t mw[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) mw[q] = fa_range_bits(cb - 32 * q, ce - 32 * q) & vw[q];
+                const bool plain = __all_sync(0xffffffffu, (mw[0] & mw[1] & mw[2] & mw[3]) == 0xffffffffu);
+                float pm = -INFINITY;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    tc::tmem_ld_wait_on(sv[q]);
+                    if (!plain)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (!((mw[q] >> e) & 1u)) sv[q][e] = 0xff800000u;  // -inf
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) pm = fa_max3(pm, __uint_as_float(sv[q][e]), __uint_as_float(sv[q][e + 1]));
+                }
+                const float bms = pm == -INFINITY ? pm : pm * sl2;
+                float alpha = 1.f;
+                bool resc = false;
+                if (bms > m_use + 8.f) {
+                    if (m_use != -INFINITY) {
+                        alpha = fa_ex2(m_use - bms);
+                        resc = true;
+                    }
+                    m_use = bms;
+                }
+                if (__any_sync(0xffffffffu, resc)) {  // O_x holds every earlier block (s_full)
+#pragma unroll
+                    for (int q = 0; q < DH / 32; ++q) {
+                        uint32_t o[32];
+                        tc::tmem_ld32(o_at_col + 32 * q, o);
+                        tc::tmem_ld_wait_on(o);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                        tc::tmem_st32(o_at_col + 32 * q, o);
+                    }
+                    l *= alpha;
+                }
+                // P is rounded to the type of V, as the product needs it: half a unit in its last place, of the
+                // same size as the output's own rounding
+                const float nm = m_use == -INFINITY ? 0.f : -m_use;
+                float ls[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    uint32_t w[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const uint32_t* s2 = &sv[2 * q + (e >> 4)][2 * (e & 15)];
+                        const float p0 = fa_ex2(fmaf(__uint_as_float(s2[0]), sl2, nm)), p1 = fa_ex2(fmaf(__uint_as_float(s2[1]), sl2, nm));
+                        ls[(2 * e) & 3] += p0;
+                        ls[(2 * e + 1) & 3] += p1;
+                        w[e] = E::pack(p0, p1);
+                    }
+                    tc::tmem_st32(s_at_col + 32 * q, w);
+                }
+                l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+                tc::tmem_st_wait();
+                tc::fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[x]);
+            }
+            blk += n;
+            // ---- the tile's end here
+            const bool any = hi > lo, whole = at.i == 0 && n == at.n;
+            if (any) {
+                if (ok) ok = mbar_wait_warp(&o_full[x], no & 1);
+                ++no;
+                if (ok) tc::fence_after();
+            }
+            if (!ok && lane == 0) {
+                *s_err = 1;
+                set_status(c.status, VT_DEV_WAIT_TIMEOUT);
+            }
+            uint16_t* dst = a.out + (at.row0 + tok) * a.out_ld + (int64_t)(at.kvh * a.group + row % a.group) * DH;
+            if (whole) {
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+                for (int q = 0; q < DH / 32; ++q) {
+                    uint32_t o[32];
+                    if (any && ok) {
+                        tc::tmem_ld32(o_at_col + 32 * q, o);
+                        tc::tmem_ld_wait_on(o);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = 0u;
+                    }
+                    if (live && ok)
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                w[e] = E::pack(__uint_as_float(o[8 * u + 2 * e]) * inv, __uint_as_float(o[8 * u + 2 * e + 1]) * inv);
+                            reinterpret_cast<uint4*>(dst)[4 * q + u] = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                }
+            } else if (has) {
+                // a part: (m, l) and O by four columns, all rows side by side
+                const int64_t u0 = now - at.i;
+                const int first = (int)(u0 / per), last = (int)((u0 + at.n - 1) / per);
+                auto slot_of = [&](int cta) { return a.work + (int64_t)(4 * cta + (cta == first ? 2 : 0) + x) * kPagedPrefillSlot; };
+                float* part = slot_of((int)blockIdx.x);
+                reinterpret_cast<float2*>(part)[row] = make_float2(m_use, l);
+                if (any) {
+#pragma unroll
+                    for (int q = 0; q < DH / 32; ++q) {
+                        uint32_t o[32];
+                        tc::tmem_ld32(o_at_col + 32 * q, o);
+                        tc::tmem_ld_wait_on(o);
+                        if (live)
+#pragma unroll
+                            for (int u = 0; u < 8; ++u)
+                                reinterpret_cast<uint4*>(part + 2 * kPfRows)[(8 * q + u) * kPfRows + row] =
+                                    make_uint4(o[4 * u], o[4 * u + 1], o[4 * u + 2], o[4 * u + 3]);
+                    }
+                }
+                __threadfence();
+                consumer_bar(1 + x, 128);
+                if (row == 0) {
+                    const int mine = atomicAdd(&a.arrived[2 * first + x], 1);
+                    s_last[x] = mine == last - first;
+                    if (mine == last - first) a.arrived[2 * first + x] = 0;  // ready for the next call
+                }
+                consumer_bar(1 + x, 128);
+                if (s_last[x] && live && ok) {  // the last to get here joins the parts, in CTA order
+                    __threadfence();
+                    float mm = -INFINITY, ll = 0.f;
+                    for (int p = first; p <= last; ++p) mm = fmaxf(mm, __ldcg(reinterpret_cast<const float2*>(slot_of(p)) + row).x);
+                    const float ref = mm == -INFINITY ? 0.f : mm;
+                    for (int p = first; p <= last; ++p) {
+                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(slot_of(p)) + row);
+                        ll += ml.y * fa_ex2(ml.x - ref);
+                    }
+                    const float inv = ll == 0.f ? 0.f : 1.f / ll;
+#pragma unroll
+                    for (int q = 0; q < DH / 32; ++q) {
+                        float o[32];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = 0.f;
+                        for (int p = first; p <= last; ++p) {
+                            const float* src = slot_of(p);
+                            const float2 ml = __ldcg(reinterpret_cast<const float2*>(src) + row);
+                            if (ml.y == 0.f) continue;  // nothing attended to there, nothing stored
+                            const float f = fa_ex2(ml.x - ref) * inv;
+#pragma unroll
+                            for (int u = 0; u < 8; ++u) {
+                                const float4 v = __ldcg(reinterpret_cast<const float4*>(src + 2 * kPfRows) + (8 * q + u) * kPfRows + row);
+                                o[4 * u] += f * v.x;
+                                o[4 * u + 1] += f * v.y;
+                                o[4 * u + 2] += f * v.z;
+                                o[4 * u + 3] += f * v.w;
+                            }
+                        }
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+                            reinterpret_cast<uint4*>(dst)[4 * q + u] =
+                                make_uint4(E::pack(o[8 * u], o[8 * u + 1]), E::pack(o[8 * u + 2], o[8 * u + 3]),
+                                           E::pack(o[8 * u + 4], o[8 * u + 5]), E::pack(o[8 * u + 6], o[8 * u + 7]));
+                    }
+                }
+                consumer_bar(1 + x, 128);  // s_last is free
+            }
+            if (any) {
+                tc::fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&o_free[x]);
+            }
+            now += n;
+            at.move(a, tr, n);
+        }
+    }
+    tc::fence_before();
+    __syncthreads();
+    if (warp == 11) {
+        tc::fence_after();
+        tc::tmem_dealloc(tmem, 512);
+    }
+}
+
+// Workspace of both attention kernels.
+size_t paged_work_floats() {
+    return (size_t)std::max(2 * kPagedMaxGrid * kPagedDecodeSlot, 4 * g_num_sms * kPagedPrefillSlot);
+}
+
+template <class T, int DH>
+static cudaError_t prefill_dh(const PagedAttnArgs& a, cudaStream_t st) {
+    // blocks at the longest lengths
+    const int64_t pairs = (int64_t)a.n_rows / (2 * (kPfRows / a.group)) + a.c.n_seqs;
+    const int64_t span = a.window > 0 ? std::min<int64_t>((int64_t)a.window + 2 * kPfRows, a.c.cap) : a.c.cap;
+    const int64_t most = pairs * a.c.n_kv_heads * (span / kPfKeys + 2);
+    const int64_t grid = std::min<int64_t>(std::min(kPagedMaxGrid / 2, g_num_sms), (most + kPfMinBlocks - 1) / kPfMinBlocks);
+    return launch_paged_k(k_paged_prefill<T, DH>, (unsigned)grid, kPfThreads, PfGeom<DH>::kSmem, st, a);
+}
+
+cudaError_t launch_paged_prefill(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st) {
+    if (dtype == VT_F16) return dh == 128 ? prefill_dh<__half, 128>(a, st) : prefill_dh<__half, 64>(a, st);
+    return dh == 128 ? prefill_dh<__nv_bfloat16, 128>(a, st) : prefill_dh<__nv_bfloat16, 64>(a, st);
+}
+
+template <class T, int DH>
+static cudaError_t init_one() {
+    cudaFuncAttributes f;
+    cudaError_t e = cudaFuncGetAttributes(&f, k_paged_prefill<T, DH>);
+    if (e != cudaSuccess) return e;
+    if (f.numRegs != kPfLaunchRegs) return cudaErrorInvalidConfiguration;  // the register split needs exactly these
+    return cudaFuncSetAttribute(k_paged_prefill<T, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PfGeom<DH>::kSmem);
+}
+cudaError_t init_paged_prefill() {
+    const cudaError_t e[4] = {init_one<__half, 64>(), init_one<__half, 128>(), init_one<__nv_bfloat16, 64>(),
+                              init_one<__nv_bfloat16, 128>()};
+    for (cudaError_t x : e)
+        if (x != cudaSuccess) return x;
+    return cudaSuccess;
+}
+
+}  // namespace vt

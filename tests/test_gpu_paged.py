@@ -492,7 +492,7 @@ def test_refusals(vtlib, paged):
     cases = [
         (dict(g=None), inv), (dict(p=None), inv), (dict(b=None), inv), (dict(qp=None), inv), (dict(o=None), inv),
         (dict(qp=q.data_ptr() + 2), inv), (dict(ol=252), inv), (dict(ql=128), inv), (dict(ql=260), inv),
-        (dict(scale=float("nan")), inv), (dict(scale=float("inf")), inv), (dict(window=-1), inv),
+        (dict(scale=float("nan")), inv), (dict(scale=float("inf")), inv), (dict(scale=-0.1), inv), (dict(window=-1), inv),
         (dict(heads=3), shape), (dict(heads=0), shape), (dict(heads=2 * 129), shape),
         (dict(b=c.batch(vt)), inv),
     ]
@@ -501,7 +501,7 @@ def test_refusals(vtlib, paged):
                      ({"v": pool.v + 8}, inv), ({"page_stride": 100}, inv), ({"head_stride": 32}, inv), ({"pos_stride": 0}, inv),
                      ({"page_stride": -2048}, inv)):
         cases.append((dict(p=change(pool, **kw)), want))
-    for kw in ({"tables": None}, {"lens": None}, {"n_seqs": -1}, {"pages_per_seq": 0}, {"pages_per_seq": 1 << 27}):
+    for kw in ({"tables": None}, {"lens": None}, {"n_seqs": -1}, {"n_seqs": 16385}, {"pages_per_seq": 0}, {"pages_per_seq": 1 << 27}):
         cases.append((dict(b=change(batch, **kw)), inv))
     for kw, want in cases:
         assert decode(**kw) == want, kw
