@@ -14,9 +14,10 @@
 //   warps 0-3, 4-7  softmax of tile 0 and 1, one thread a row (its lane of the tensor memory): no exchange
 //                   between threads.  m is a reference maximum; O and l are rescaled only when a block's
 //                   maximum exceeds it by more than 8 (log2), so P stays below 2^8.
-//   warps 8-10      copies: rows of K and V through the page table, and Q, by 16-byte asynchronous copies in
-//                   the swizzled operand layout (a tensor copy cannot follow pages smaller than its box, nor
-//                   leave out the positions past a sequence's end, which are filled with zeros here)
+//   warps 8-10      copies: Q, and K and V through the page table, by tensor copies of a page's rows; blocks that
+//                   hold positions outside the unit's range (whatever lies there must not reach V: they are
+//                   filled with zeros), bad pages or pages of fewer than 16 positions by 16-byte asynchronous
+//                   copies into the same swizzled layout
 //   warp 11         tensor memory and the MMAs
 //
 // The blocks of all units form one line, and CTA c (one an SM) takes its c-th equal part, so neither few
@@ -122,12 +123,27 @@ struct PfCursor {
 __device__ __forceinline__ void pf_copy16(uint32_t dst, const void* src, bool full) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(full ? 16 : 0) : "memory");
 }
+// The wait of a whole warp, polled by one lane: polls of 32 lanes are 32 accesses of shared memory, and ten
+// polling warps would keep the copies from it.
+__device__ __forceinline__ bool pf_wait(uint64_t* bar, uint32_t parity) {
+    int ok = 1;
+    if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity) ? 1 : 0;
+    return __shfl_sync(0xffffffffu, ok, 0) != 0;
+}
 __device__ __forceinline__ void pf_zero_row(const PagedAttnArgs& a, int row, int words, int lane) {
     for (int e = lane; e < words; e += 32) reinterpret_cast<uint4*>(a.out + row * a.out_ld)[e] = make_uint4(0u, 0u, 0u, 0u);
 }
 
+struct PfParams {
+    PagedAttnArgs a;
+    int tma;              // blocks that are whole come by tensor copies
+    CUtensorMap tq;       // [rows][heads][dh], boxes of a tile's rows by 64 columns
+    CUtensorMap tk, tv;   // [pages][KV heads][positions][dh], boxes of a page's positions (128 at most) by 64 columns
+};
+
 template <class T, int DH>
-__global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_constant__ PagedAttnArgs a) {
+__global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_constant__ PfParams P) {
+    const PagedAttnArgs& a = P.a;
     using E = Elem<T>;
     using G = PfGeom<DH>;
     constexpr int S = G::kSlots;
@@ -160,7 +176,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
             mbar_init(&full[s], kPfCopyWarps);
             mbar_init(&empty[s], 1);
         }
-        mbar_init(q_full, kPfCopyWarps);
+        mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
         for (int x = 0; x < 2; ++x) {
             mbar_init(&s_full[x], 1);
@@ -299,90 +315,158 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
         // ================================================================ copies
         const int w = warp - 8;
         bool ok = true;
-        uint64_t *sent1 = nullptr, *sent2 = nullptr;  // the last two groups, not yet announced
+        const int box_rows = min(c.page_size, kPfKeys), pages = kPfKeys / box_rows;  // of a block
+        constexpr int HALVES = DH / 64;
+        auto page_of = [&](int p) { return c.tables[(int64_t)at.b * c.per_seq + (p >> c.page_shift)]; };
+        // By tensor copies: lane i holds the page of rows i box_rows .. of block j, requested a block ahead.
+        auto request = [&](int j) {
+            const int p = j * kPfKeys + lane * box_rows;
+            return P.tma && lane < pages && p >= at.kbeg && p < at.kend ? page_of(p) : -1;
+        };
+        // By asynchronous copies: a pass of a warp covers RPI rows, CPR 16-byte chunks each; lane (sub, chunk) copies its
+        // chunk of rows sub, sub + RPI, ... of 8-row group g.  Groups go to the three warps in turn.
+        constexpr int CPR = DH / 8, RPI = 32 / CPR, GROUPS = (16 + kPfCopyWarps - 1) / kPfCopyWarps;
+        const int chunk = lane % CPR, sub = lane / CPR;
+        const uint32_t lane_dst = (uint32_t)((chunk >> 3) * G::kAtom + sub * 128);
+        auto copy_row = [&](uint32_t dst, int g, int k, const uint16_t* src, bool on) {
+            pf_copy16(dst + lane_dst + (uint32_t)((8 * g + k) * 128 + (((chunk & 7) ^ (sub + k)) << 4)), src, on);
+        };
+        uint64_t *sent1 = nullptr, *sent2 = nullptr;  // the last two groups of asynchronous copies, not yet announced
         auto announce = [&](uint64_t* bar) {
             fence_proxy_async_smem();  // the copies wrote as threads do; the MMA reads as the copy engine does
             __syncwarp();
             if (lane == 0) mbar_arrive(bar);
         };
-        auto sent = [&](uint64_t* bar) {
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            if (sent2) {
-                asm volatile("cp.async.wait_group %0;" ::"n"(kPfLag) : "memory");
-                announce(sent2);
-            }
-            sent2 = sent1;
-            sent1 = bar;
-        };
-        // 128 rows of which this warp copies every third group of 8: row 32 q + l starts at element off[q] of
-        // lane l (-1: zeros)
-        auto rows = [&](uint8_t* dst, const uint16_t* src, const int64_t (&off)[4]) {
-            constexpr int CPR = DH / 8, RPI = 32 / CPR;
-            const int chunk = lane % CPR, sub = lane / CPR;
-            const uint32_t d0 = smem_u32(dst) + (uint32_t)((chunk >> 3) * G::kAtom);
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    if ((4 * q + g) % kPfCopyWarps != w) continue;
-#pragma unroll
-                    for (int r0 = 0; r0 < 8; r0 += RPI) {
-                        const int r = 8 * g + r0 + sub, row = 32 * q + r;
-                        const int64_t o = __shfl_sync(0xffffffffu, off[q], r);
-                        pf_copy16(d0 + (uint32_t)(row * 128 + (((chunk & 7) ^ (row & 7)) << 4)), src + (o < 0 ? 0 : o) + chunk * 8, o >= 0);
-                    }
-                }
+        auto flush = [&]() {
+            if (!sent1) return;
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            if (sent2) announce(sent2);
+            announce(sent1);
+            sent1 = sent2 = nullptr;
         };
         int slot = 0, round = 0, blk = 0, nq = 0;
-        auto block = [&](const uint16_t* pool, const int64_t (&off)[4]) {
-            if (ok && round > 0) ok = mbar_wait_warp(&empty[slot], (round - 1) & 1);
-            if (ok) {
-                rows(Rs + slot * G::kTile, pool, off);
-                sent(&full[slot]);
-            }
-            if (++slot == S) slot = 0, ++round;
-        };
         for (int64_t now = t0; ok && now < t1;) {
             const int n = (int)min((int64_t)(at.n - at.i), t1 - now);
-            for (int j = at.kb0 + at.i, j0 = j; ok && j < j0 + n; ++j) {
-                int64_t off[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int p = j * kPfKeys + 32 * q + lane;
-                    off[q] = p >= at.kbeg && p < at.kend ? paged_entry(c, at.b, at.kvh, p) : -1;
-                    const uint32_t m = __ballot_sync(0xffffffffu, off[q] >= 0);
-                    if (w == 0 && lane == 0) valid[(blk % kPfMaskRing) * 4 + q] = m;
-                }
-                ++blk;
-                block(a.kpool, off);
-                if (j == j0 && ok) {  // the unit's queries, once the last unit's products with its own are done
-                    if (nq > 0) ok = mbar_wait_warp(q_empty, (nq - 1) & 1);
-                    ++nq;
-                    for (int x = 0; ok && x < 2; ++x) {
-                        int64_t qo[4];
+            const int j0 = at.kb0 + at.i;
+            int next_page = request(j0);
+            for (int j = j0; ok && j < j0 + n; ++j, ++blk) {
+                const int p0 = j * kPfKeys, lo = at.kbeg - p0, hi = at.kend - p0;  // attended rows [lo, hi)
+                const int page = next_page;
+                if (j + 1 < j0 + n) next_page = request(j + 1);
+                const bool clean = P.tma && __all_sync(0xffffffffu, lo <= 0 && hi >= kPfKeys &&
+                                                                        (lane >= pages || (unsigned)page < (unsigned)c.n_pages));
+                int64_t off[GROUPS];  // asynchronous copies: the lane's element in the first row of each group; -1: bad page
+                if (clean) {
+                    if (w == 0 && lane < 4) valid[(blk % kPfMaskRing) * 4 + lane] = 0xffffffffu;
+                    flush();
+                } else {
+                    if (w == 0)
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
-                            const int r = 32 * q + lane, tok = (2 * at.pt + x) * tr + r / a.group;
-                            qo[q] = r < tr * a.group && tok < at.rows
-                                        ? (at.row0 + tok) * a.q_ld + (int64_t)(at.kvh * a.group + r % a.group) * DH
-                                        : -1;
+                            const int r = 32 * q + lane;
+                            bool on = r >= lo && r < hi;
+                            if (on && (unsigned)page_of(p0 + r) >= (unsigned)c.n_pages) {
+                                on = false;
+                                set_status(c.status, VT_DEV_BAD_PAGE);
+                            }
+                            const uint32_t m = __ballot_sync(0xffffffffu, on);
+                            if (lane == 0) valid[(blk % kPfMaskRing) * 4 + q] = m;
                         }
-                        if ((2 * at.pt + x) * tr < at.rows) rows(Qs + x * G::kTile, a.q, qo);
-                    }
-                    if (ok) sent(q_full);
+                    if (c.page_size >= 8)  // 8 rows that begin at a multiple of 8 lie in one page
+#pragma unroll
+                        for (int i = 0; i < GROUPS; ++i) {
+                            const int r = 8 * (w + i * kPfCopyWarps), p = p0 + r;
+                            const int pg = r < hi && r + 8 > lo && r < kPfKeys ? page_of(p) : 0;
+                            off[i] = (unsigned)pg < (unsigned)c.n_pages
+                                         ? pg * c.page_stride + at.kvh * c.head_stride +
+                                               ((p & (c.page_size - 1)) + sub) * c.pos_stride + chunk * 8
+                                         : -1;
+                        }
                 }
-                block(a.vpool, off);
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    if (ok && round > 0) ok = pf_wait(&empty[slot], (round - 1) & 1);
+                    if (!ok) break;
+                    const uint32_t dst = smem_u32(Rs + slot * G::kTile);
+                    if (clean) {
+                        const CUtensorMap* map = kv == 0 ? &P.tk : &P.tv;
+                        const int boxes = (pages * HALVES - w + kPfCopyWarps - 1) / kPfCopyWarps;  // of this warp
+                        if (elect_one()) mbar_arrive_expect_tx(&full[slot], (uint32_t)(boxes * box_rows * 128));
+                        for (int x = w; x < pages * HALVES; x += kPfCopyWarps) {
+                            const int i = x / HALVES, h = x % HALVES;
+                            const int pg = __shfl_sync(0xffffffffu, page, i);
+                            if (elect_one())
+                                tc::tma_load_4d(dst + (uint32_t)(h * G::kAtom + i * box_rows * 128), map, 64 * h,
+                                                (p0 + i * box_rows) & (c.page_size - 1), at.kvh, pg, &full[slot]);
+                            __syncwarp();
+                        }
+                    } else {
+                        const uint16_t* pool = kv == 0 ? a.kpool : a.vpool;
+                        if (c.page_size >= 8) {
+#pragma unroll
+                            for (int i = 0; i < GROUPS; ++i) {
+                                const int g = w + i * kPfCopyWarps;
+                                if (g >= 16) break;
+                                const uint16_t* src = pool + (off[i] < 0 ? 0 : off[i]);
+                                const int end = off[i] < 0 ? 0 : hi;
+#pragma unroll
+                                for (int k = 0; k < 8; k += RPI) {
+                                    const int r = 8 * g + k + sub;
+                                    copy_row(dst, g, k, src + k * c.pos_stride, r >= lo && r < end);
+                                }
+                            }
+                        } else {
+#pragma unroll 1
+                            for (int g = w; g < 16; g += kPfCopyWarps)
+#pragma unroll 1
+                                for (int k = 0; k < 8; k += RPI) {
+                                    const int r = 8 * g + k + sub, p = p0 + r;
+                                    const int pg = r >= lo && r < hi ? page_of(p) : -1;
+                                    const bool on = (unsigned)pg < (unsigned)c.n_pages;
+                                    const int64_t o = on ? pg * c.page_stride + at.kvh * c.head_stride + (p & (c.page_size - 1)) * c.pos_stride : 0;
+                                    copy_row(dst, g, k, pool + o + chunk * 8, on);
+                                }
+                        }
+                        asm volatile("cp.async.commit_group;" ::: "memory");
+                        if (sent2) {
+                            asm volatile("cp.async.wait_group %0;" ::"n"(kPfLag) : "memory");
+                            announce(sent2);
+                        }
+                        sent2 = sent1;
+                        sent1 = &full[slot];
+                    }
+                    if (++slot == S) slot = 0, ++round;
+                    if (kv == 0 && j == j0 && w == 0) {  // the unit's queries, once the last unit's products with its own are done
+                        if (nq > 0) ok = pf_wait(q_empty, (nq - 1) & 1);
+                        ++nq;
+                        const int tiles = (2 * at.pt + 1) * tr < at.rows ? 2 : 1;
+                        if (ok && elect_one()) {
+                            mbar_arrive_expect_tx(q_full, (uint32_t)(tiles * HALVES * tr * a.group * 128));
+                            for (int x = 0; x < tiles; ++x)
+                                for (int h = 0; h < HALVES; ++h)
+                                    tc::tma_load_3d(Qs + x * G::kTile + h * G::kAtom, &P.tq, 64 * h, at.kvh * a.group,
+                                                    at.row0 + (2 * at.pt + x) * tr, smem_u32(q_full));
+                        }
+                        __syncwarp();
+                    }
+                }
             }
             now += n;
             at.move(a, tr, n);
         }
+        if (ok) flush();
         asm volatile("cp.async.wait_group 0;" ::: "memory");
-        if (ok) {
-            if (sent2) announce(sent2);
-            if (sent1) announce(sent1);
-        } else if (lane == 0) {
-            *s_err = 1;
-            set_status(c.status, VT_DEV_WAIT_TIMEOUT);
+        if (!ok) {
+            if (lane == 0) {
+                *s_err = 1;
+                set_status(c.status, VT_DEV_WAIT_TIMEOUT);
+            }
+            // no tensor copy may still be in flight when the CTA ends
+            for (int s = 0; s < S; ++s) {
+                const int fills = round + (s < slot ? 1 : 0);
+                if (fills > 0) pf_wait(&full[s], (fills - 1) & 1);
+            }
+            if (w == 0 && nq > 0) pf_wait(q_full, (nq - 1) & 1);
         }
     } else if (warp == 11) {
         // ================================================================ MMAs
@@ -401,13 +485,13 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
             int lo[2], hi[2];
             at.tile(a, tr, 0, j0, j1, lo[0], hi[0]);
             at.tile(a, tr, 1, j0, j1, lo[1], hi[1]);
-            ok = mbar_wait_warp(q_full, nq & 1);
+            ok = pf_wait(q_full, nq & 1);
             ++nq;
             for (int j = j0 - 1; ok && j < j1; ++j) {
                 int vs = 0, ks = 0, kpar = 0;
                 if (j >= j0) {
                     vs = slot;
-                    ok = mbar_wait_warp(&full[vs], par);
+                    ok = pf_wait(&full[vs], par);
                     if (++slot == S) slot = 0, par ^= 1;
                 }
                 const bool more = j + 1 < j1;
@@ -420,10 +504,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     if (ok && j >= lo[x] && j < hi[x]) {
-                        ok = mbar_wait_warp(&p_full[x], np[x] & 1);
+                        ok = pf_wait(&p_full[x], np[x] & 1);
                         ++np[x];
                         if (ok && j == lo[x]) {
-                            if (no[x] > 0) ok = mbar_wait_warp(&o_free[x], (no[x] - 1) & 1);
+                            if (no[x] > 0) ok = pf_wait(&o_free[x], (no[x] - 1) & 1);
                             ++no[x];
                         }
                         if (!ok) break;
@@ -443,7 +527,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                         __syncwarp();
                     }
                     if (ok && more && !have_k) {
-                        ok = mbar_wait_warp(&full[ks], kpar);
+                        ok = pf_wait(&full[ks], kpar);
                         have_k = true;
                     }
                     if (ok && more && j + 1 >= lo[x] && j + 1 < hi[x]) {
@@ -479,7 +563,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
         // tensor memory is freed only after every MMA issued has completed
         if (elect_one()) tc::mma_commit(done);
         __syncwarp();
-        if (!mbar_wait_warp(done, 0) && lane == 0) set_status(c.status, VT_DEV_WAIT_TIMEOUT);
+        if (!pf_wait(done, 0) && lane == 0) set_status(c.status, VT_DEV_WAIT_TIMEOUT);
     } else {
         // ================================================================ softmax of tile x
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPfSoftmaxRegs));
@@ -501,7 +585,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
             float m_use = -INFINITY, l = 0.f;
             for (int j = lo; j < hi; ++j) {
                 if (ok && *s_err) ok = false;
-                if (ok) ok = mbar_wait_warp(&s_full[x], ns & 1);
+                if (ok) ok = pf_wait(&s_full[x], ns & 1);
                 ++ns;
                 if (!ok) continue;
                 tc::fence_after();
@@ -574,7 +658,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
             // ---- the tile's end here
             const bool any = hi > lo, whole = at.i == 0 && n == at.n;
             if (any) {
-                if (ok) ok = mbar_wait_warp(&o_full[x], no & 1);
+                if (ok) ok = pf_wait(&o_full[x], no & 1);
                 ++no;
                 if (ok) tc::fence_after();
             }
@@ -700,7 +784,24 @@ static cudaError_t prefill_dh(const PagedAttnArgs& a, cudaStream_t st) {
     const int64_t span = a.window > 0 ? std::min<int64_t>((int64_t)a.window + 2 * kPfRows, a.c.cap) : a.c.cap;
     const int64_t most = pairs * a.c.n_kv_heads * (span / kPfKeys + 2);
     const int64_t grid = std::min<int64_t>(std::min(kPagedMaxGrid / 2, g_num_sms), (most + kPfMinBlocks - 1) / kPfMinBlocks);
-    return launch_paged_k(k_paged_prefill<T, DH>, (unsigned)grid, kPfThreads, PfGeom<DH>::kSmem, st, a);
+    PfParams P{};
+    P.a = a;
+    const PagedView& c = a.c;
+    const bool bf16 = !std::is_same<T, __half>::value;
+    const uint64_t qd[3] = {DH, (uint64_t)a.n_heads, (uint64_t)a.n_rows};
+    const uint64_t qs[2] = {DH * 2, (uint64_t)(a.q_ld ? a.q_ld : (int64_t)a.n_heads * DH) * 2};
+    const uint32_t qb[3] = {64, (uint32_t)a.group, (uint32_t)(kPfRows / a.group)};
+    if (!make_tensor_map(&P.tq, bf16, 3, a.q, qd, qs, qb)) return cudaErrorInvalidValue;
+    // Boxes of fewer than 16 rows would cost more than the copies of 16 bytes (2 KB boxes: 1160 cycles a block of 32 KB,
+    // 16 KB boxes 680, asynchronous copies 1210 to 1310, all of them measured with every SM copying from the L2).
+    if (c.page_size >= 16) {
+        const uint64_t kd[4] = {DH, (uint64_t)c.page_size, (uint64_t)c.n_kv_heads, (uint64_t)c.n_pages};
+        const uint64_t ks[3] = {(uint64_t)c.pos_stride * 2, (uint64_t)(c.head_stride ? c.head_stride : DH) * 2,
+                                (uint64_t)(c.page_stride ? c.page_stride : DH) * 2};
+        const uint32_t kb[4] = {64, (uint32_t)std::min(c.page_size, kPfKeys), 1, 1};
+        P.tma = make_tensor_map(&P.tk, bf16, 4, a.kpool, kd, ks, kb) && make_tensor_map(&P.tv, bf16, 4, a.vpool, kd, ks, kb);
+    }
+    return launch_paged_k(k_paged_prefill<T, DH>, (unsigned)grid, kPfThreads, PfGeom<DH>::kSmem, st, P);
 }
 
 cudaError_t launch_paged_prefill(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st) {

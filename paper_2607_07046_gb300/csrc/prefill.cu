@@ -1284,6 +1284,21 @@ static bool make_map_k2(CUtensorMap* map, const void* base, int64_t inner, int64
     return true;
 }
 
+bool make_tensor_map(CUtensorMap* map, bool bf16, int rank, const void* base, const uint64_t* dims, const uint64_t* strides,
+                     const uint32_t* box) {
+    cuuint64_t d[5], s[4];
+    cuuint32_t b[5], one[5];
+    for (int i = 0; i < rank; ++i) {
+        d[i] = dims[i];
+        b[i] = box[i];
+        one[i] = 1;
+        if (i + 1 < rank) s[i] = strides[i];
+    }
+    return g_encode && g_encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank,
+                                const_cast<void*>(base), d, s, b, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // One GEMM of a grouped launch: C_g = A_g . B_g^T with m rows (shared by the group), n_g columns
 // and k_g inner elements; `base` carries the epilogue's pointers.
 struct GemmSpec {
