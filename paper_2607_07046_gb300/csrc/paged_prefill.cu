@@ -53,7 +53,7 @@ struct PfGeom {
     static constexpr int kTile = kPfRows * DH * 2;         // bytes of a Q tile, of a K or V block
     static constexpr int kAtom = kPfRows * 128;            // its 64-column box
     static constexpr int kSlots = DH == 128 ? 5 : 10;      // K and V blocks of the ring, in turn
-    static constexpr size_t kSmem = 1024 + (size_t)(2 + kSlots) * kTile + 512;
+    static constexpr size_t kSmem = 1024 + (size_t)(2 + kSlots) * kTile + 512 + kPfThreads / 32 * 64;
 };
 
 // The units in order: sequence, KV head, tile pair.
@@ -158,8 +158,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
     uint64_t* q_full = empty + S;
     uint64_t* q_empty = q_full + 1;
     uint64_t* s_full = q_empty + 1;          // [2] S_x is there (and O_x holds every earlier block)
-    uint64_t* p_full = s_full + 2;           // [2]
-    uint64_t* o_full = p_full + 2;           // [2] the unit's last block is in O_x
+    uint64_t* p_full = s_full + 2;           // [2][2] halves of P_x, 64 keys each
+    uint64_t* o_full = p_full + 4;           // [2] the unit's last block is in O_x
     uint64_t* o_free = o_full + 2;           // [2] O_x has been read
     uint64_t* done = o_free + 2;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
@@ -167,6 +167,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
     volatile int* s_last = s_err + 1;        // [2]
     int64_t* s_at = reinterpret_cast<int64_t*>(tmem_slot + 4);  // [2]: blocks of all units; blocks before the first unit's
     int* s_unit = reinterpret_cast<int*>(s_at + 2);             // [4]
+    // where each warp stands between units: in shared memory, as the registers hold S meanwhile
+    PfCursor* cursor = reinterpret_cast<PfCursor*>(s_unit + 4) + (threadIdx.x >> 5);
 
     const PagedView& c = a.c;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -180,7 +182,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
         mbar_init(q_empty, 1);
         for (int x = 0; x < 2; ++x) {
             mbar_init(&s_full[x], 1);
-            mbar_init(&p_full[x], 4);
+            mbar_init(&p_full[2 * x], 4);
+            mbar_init(&p_full[2 * x + 1], 4);
             mbar_init(&o_full[x], 1);
             mbar_init(&o_free[x], 4);
         }
@@ -299,6 +302,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
     at.pt = s_unit[2];
     at.unit(a, tr);
     at.i = s_unit[3];
+    if (lane == 0) *cursor = at;
     if (warp == 11) {
         tc::tmem_alloc(tmem_slot, 512);
         tc::tmem_relinquish();
@@ -315,6 +319,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
         // ================================================================ copies
         const int w = warp - 8;
         bool ok = true;
+        PfCursor at = *cursor;
         const int box_rows = min(c.page_size, kPfKeys), pages = kPfKeys / box_rows;  // of a block
         constexpr int HALVES = DH / 64;
         auto page_of = [&](int p) { return c.tables[(int64_t)at.b * c.per_seq + (p >> c.page_shift)]; };
@@ -479,12 +484,21 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
         bool ok = true;
         int slot = 0, par = 0, nq = 0;
         int np[2] = {0, 0}, no[2] = {0, 0};
-        for (int64_t now = t0; ok && now < t1;) {
-            const int n = (int)min((int64_t)(at.n - at.i), t1 - now);
-            const int j0 = at.kb0 + at.i, j1 = j0 + n;
-            int lo[2], hi[2];
-            at.tile(a, tr, 0, j0, j1, lo[0], hi[0]);
-            at.tile(a, tr, 1, j0, j1, lo[1], hi[1]);
+        for (int64_t left = t1 - t0; ok && left > 0;) {
+            int n, j0, j1, lo[2], hi[2];
+            {
+                PfCursor at = *cursor;
+                n = (int)min((int64_t)(at.n - at.i), left);
+                j0 = at.kb0 + at.i;
+                j1 = j0 + n;
+                at.tile(a, tr, 0, j0, j1, lo[0], hi[0]);
+                at.tile(a, tr, 1, j0, j1, lo[1], hi[1]);
+                at.move(a, tr, n);
+                __syncwarp();  // every lane has read the cursor
+                if (lane == 0) *cursor = at;
+                __syncwarp();
+            }
+            left -= n;
             ok = pf_wait(q_full, nq & 1);
             ++nq;
             for (int j = j0 - 1; ok && j < j1; ++j) {
@@ -504,20 +518,26 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     if (ok && j >= lo[x] && j < hi[x]) {
-                        ok = pf_wait(&p_full[x], np[x] & 1);
-                        ++np[x];
-                        if (ok && j == lo[x]) {
+                        if (j == lo[x]) {
                             if (no[x] > 0) ok = pf_wait(&o_free[x], (no[x] - 1) & 1);
                             ++no[x];
                         }
-                        if (!ok) break;
-                        tc::fence_after();
-                        if (elect_one()) {
 #pragma unroll
-                            for (int kk = 0; kk < kPfKeys / 16; ++kk)
-                                tc::mma_f16_ts(tmem + kOCol + (uint32_t)(x * DH), tmem + (uint32_t)(x * kPfKeys + kk * 8),
-                                               tc::desc_of(vd_hi, vd_lo + (uint32_t)vs * kStep + (uint32_t)kk * (2048 >> 4)), idesc_o,
-                                               (j > lo[x] || kk > 0) ? 1u : 0u);
+                        for (int half = 0; half < 2; ++half) {
+                            ok = ok && pf_wait(&p_full[2 * x + half], np[x] & 1);
+                            if (!ok) break;
+                            tc::fence_after();
+                            if (elect_one())
+#pragma unroll
+                                for (int kk = 4 * half; kk < 4 * half + 4; ++kk)
+                                    tc::mma_f16_ts(tmem + kOCol + (uint32_t)(x * DH), tmem + (uint32_t)(x * kPfKeys + kk * 8),
+                                                   tc::desc_of(vd_hi, vd_lo + (uint32_t)vs * kStep + (uint32_t)kk * (2048 >> 4)), idesc_o,
+                                                   (j > lo[x] || kk > 0) ? 1u : 0u);
+                            __syncwarp();
+                        }
+                        ++np[x];
+                        if (!ok) break;
+                        if (elect_one()) {
                             if (j == hi[x] - 1) tc::mma_commit(&o_full[x]);
                         }
                         __syncwarp();
@@ -553,8 +573,6 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                 }
                 if (*s_err) ok = false;
             }
-            now += n;
-            at.move(a, tr, n);
         }
         if (!ok && lane == 0) {
             *s_err = 1;
@@ -573,14 +591,18 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
         const float sl2 = a.scale_log2;
         bool ok = true;
         int ns = 0, no = 0, blk = 0;
-        for (int64_t now = t0; now < t1;) {
-            const int n = (int)min((int64_t)(at.n - at.i), t1 - now);
-            const int j0 = at.kb0 + at.i, j1 = j0 + n;
-            int lo, hi;
-            const bool has = at.tile(a, tr, x, j0, j1, lo, hi);
-            const int tok = (2 * at.pt + x) * tr + row / a.group;
-            const bool live = row < tr * a.group && tok < at.rows;
-            const int qp = live ? at.len + tok : -1;  // position of this row (-1: it attends to nothing)
+        for (int64_t left = t1 - t0; left > 0;) {
+            int n, j0, lo, hi, qp;
+            bool has, live;
+            {
+                const PfCursor at = *cursor;
+                n = (int)min((int64_t)(at.n - at.i), left);
+                j0 = at.kb0 + at.i;
+                has = at.tile(a, tr, x, j0, j0 + n, lo, hi);
+                const int tok = (2 * at.pt + x) * tr + row / a.group;
+                live = row < tr * a.group && tok < at.rows;
+                qp = live ? at.len + tok : -1;  // position of this row (-1: it attends to nothing)
+            }
             const int first_key = a.window > 0 ? qp - a.window + 1 : 0;
             float m_use = -INFINITY, l = 0.f;
             for (int j = lo; j < hi; ++j) {
@@ -632,30 +654,38 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                     l *= alpha;
                 }
                 // P is rounded to the type of V, as the product needs it: half a unit in its last place, of the
-                // same size as the output's own rounding
+                // same size as the output's own rounding.  Its first 64 keys are announced while the others are
+                // worked out.
                 const float nm = m_use == -INFINITY ? 0.f : -m_use;
-                float ls[4] = {0.f, 0.f, 0.f, 0.f};
+                const uint64_t sl2x2 = f2_pack(sl2, sl2), nmx2 = f2_pack(nm, nm);
+                uint64_t ls[2] = {0ull, 0ull};
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
                     uint32_t w[32];
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
                         const uint32_t* s2 = &sv[2 * q + (e >> 4)][2 * (e & 15)];
-                        const float p0 = fa_ex2(fmaf(__uint_as_float(s2[0]), sl2, nm)), p1 = fa_ex2(fmaf(__uint_as_float(s2[1]), sl2, nm));
-                        ls[(2 * e) & 3] += p0;
-                        ls[(2 * e + 1) & 3] += p1;
+                        float p0, p1;
+                        f2_unpack(f2_fma(f2_pack(__uint_as_float(s2[0]), __uint_as_float(s2[1])), sl2x2, nmx2), p0, p1);
+                        p0 = fa_ex2(p0);
+                        p1 = fa_ex2(p1);
+                        ls[e & 1] = f2_add(ls[e & 1], f2_pack(p0, p1));
                         w[e] = E::pack(p0, p1);
                     }
                     tc::tmem_st32(s_at_col + 32 * q, w);
+                    tc::tmem_st_wait();
+                    tc::fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_full[2 * x + q]);
                 }
-                l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
-                tc::tmem_st_wait();
-                tc::fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[x]);
+                float l0, l1;
+                f2_unpack(f2_add(ls[0], ls[1]), l0, l1);
+                l += l0 + l1;
             }
             blk += n;
             // ---- the tile's end here
+            PfCursor at = *cursor;
+            const int tok = (2 * at.pt + x) * tr + row / a.group;
             const bool any = hi > lo, whole = at.i == 0 && n == at.n;
             if (any) {
                 if (ok) ok = pf_wait(&o_full[x], no & 1);
@@ -691,7 +721,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                 }
             } else if (has) {
                 // a part: (m, l) and O by four columns, all rows side by side
-                const int64_t u0 = now - at.i;
+                const int64_t per = max((s_at[0] + gridDim.x - 1) / gridDim.x, (int64_t)kPfMinBlocks);
+                const int64_t u0 = min(s_at[0], (blockIdx.x + 1) * per) - left - at.i;
                 const int first = (int)(u0 / per), last = (int)((u0 + at.n - 1) / per);
                 auto slot_of = [&](int cta) { return a.work + (int64_t)(4 * cta + (cta == first ? 2 : 0) + x) * kPagedPrefillSlot; };
                 float* part = slot_of((int)blockIdx.x);
@@ -760,8 +791,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&o_free[x]);
             }
-            now += n;
+            left -= n;
             at.move(a, tr, n);
+            __syncwarp();  // every lane has read the cursor
+            if (lane == 0) *cursor = at;
+            __syncwarp();
         }
     }
     tc::fence_before();
