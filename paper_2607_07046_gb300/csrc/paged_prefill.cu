@@ -123,9 +123,14 @@ struct PfCursor {
 __device__ __forceinline__ void pf_copy16(uint32_t dst, const void* src, bool full) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(full ? 16 : 0) : "memory");
 }
-// The wait of a whole warp, polled by one lane: polls of 32 lanes are 32 accesses of shared memory, and ten
-// polling warps would keep the copies from it.
+// The wait of a whole warp.  A phase that is there or about to be is seen by plain tests (15 cycles each, where
+// a bounded wait takes 150 to 240 although the phase is complete); after kPfTests of them one lane waits, so that
+// a dozen waiting warps do not keep shared memory busy.
+constexpr int kPfTests = 64;
 __device__ __forceinline__ bool pf_wait(uint64_t* bar, uint32_t parity) {
+#pragma unroll 1
+    for (int i = 0; i < kPfTests; ++i)
+        if (__all_sync(0xffffffffu, fa_test(bar, parity))) return true;
     int ok = 1;
     if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity) ? 1 : 0;
     return __shfl_sync(0xffffffffu, ok, 0) != 0;
@@ -191,8 +196,12 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
         *s_err = 0;
         fence_mbar_init();
     }
-    pdl_wait();
+    pdl_wait();  // a preceding kernel may hold tensor memory
     pdl_launch_dependents();
+    if (warp == 11) {
+        tc::tmem_alloc(tmem_slot, 512);
+        tc::tmem_relinquish();
+    }
 
     // ---- blocks of each sequence for one KV head (a warp a sequence, a lane a tile pair); rows that
     // attend to nothing get zeros
@@ -296,17 +305,16 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
     const int64_t line = s_at[0];
     const int64_t per = max((line + gridDim.x - 1) / gridDim.x, (int64_t)kPfMinBlocks);
     const int64_t t0 = blockIdx.x * per, t1 = min(line, t0 + per);
-    if (t0 >= t1) return;
+    if (t0 >= t1) {
+        if (warp == 11) tc::tmem_dealloc(*tmem_slot, 512);
+        return;
+    }
     at.seq(a, s_unit[0]);
     at.kvh = s_unit[1];
     at.pt = s_unit[2];
     at.unit(a, tr);
     at.i = s_unit[3];
     if (lane == 0) *cursor = at;
-    if (warp == 11) {
-        tc::tmem_alloc(tmem_slot, 512);
-        tc::tmem_relinquish();
-    }
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
@@ -699,26 +707,29 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
             uint16_t* dst = a.out + (at.row0 + tok) * a.out_ld + (int64_t)(at.kvh * a.group + row % a.group) * DH;
             if (whole) {
                 const float inv = l == 0.f ? 0.f : 1.f / l;
+                uint32_t o[DH / 32][32];
+                if (any && ok) {
 #pragma unroll
-                for (int q = 0; q < DH / 32; ++q) {
-                    uint32_t o[32];
-                    if (any && ok) {
-                        tc::tmem_ld32(o_at_col + 32 * q, o);
-                        tc::tmem_ld_wait_on(o);
-                    } else {
+                    for (int q = 0; q < DH / 32; ++q) tc::tmem_ld32(o_at_col + 32 * q, o[q]);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = 0u;
-                    }
-                    if (live && ok)
+                    for (int q = 0; q < DH / 32; ++q) tc::tmem_ld_wait_on(o[q]);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < DH / 32; ++q)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[q][e] = 0u;
+                }
+                if (live && ok)
+#pragma unroll
+                    for (int q = 0; q < DH / 32; ++q)
 #pragma unroll
                         for (int u = 0; u < 4; ++u) {
                             uint32_t w[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                w[e] = E::pack(__uint_as_float(o[8 * u + 2 * e]) * inv, __uint_as_float(o[8 * u + 2 * e + 1]) * inv);
+                                w[e] = E::pack(__uint_as_float(o[q][8 * u + 2 * e]) * inv, __uint_as_float(o[q][8 * u + 2 * e + 1]) * inv);
                             reinterpret_cast<uint4*>(dst)[4 * q + u] = make_uint4(w[0], w[1], w[2], w[3]);
                         }
-                }
             } else if (has) {
                 // a part: (m, l) and O by four columns, all rows side by side
                 const int64_t per = max((s_at[0] + gridDim.x - 1) / gridDim.x, (int64_t)kPfMinBlocks);
@@ -728,17 +739,18 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                 float* part = slot_of((int)blockIdx.x);
                 reinterpret_cast<float2*>(part)[row] = make_float2(m_use, l);
                 if (any) {
+                    uint32_t o[DH / 32][32];
 #pragma unroll
-                    for (int q = 0; q < DH / 32; ++q) {
-                        uint32_t o[32];
-                        tc::tmem_ld32(o_at_col + 32 * q, o);
-                        tc::tmem_ld_wait_on(o);
-                        if (live)
+                    for (int q = 0; q < DH / 32; ++q) tc::tmem_ld32(o_at_col + 32 * q, o[q]);
+#pragma unroll
+                    for (int q = 0; q < DH / 32; ++q) tc::tmem_ld_wait_on(o[q]);
+                    if (live)
+#pragma unroll
+                        for (int q = 0; q < DH / 32; ++q)
 #pragma unroll
                             for (int u = 0; u < 8; ++u)
                                 reinterpret_cast<uint4*>(part + 2 * kPfRows)[(8 * q + u) * kPfRows + row] =
-                                    make_uint4(o[4 * u], o[4 * u + 1], o[4 * u + 2], o[4 * u + 3]);
-                    }
+                                    make_uint4(o[q][4 * u], o[q][4 * u + 1], o[q][4 * u + 2], o[q][4 * u + 3]);
                 }
                 __threadfence();
                 consumer_bar(1 + x, 128);
@@ -758,24 +770,34 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                         ll += ml.y * fa_ex2(ml.x - ref);
                     }
                     const float inv = ll == 0.f ? 0.f : 1.f / ll;
-#pragma unroll
+#pragma unroll 1
                     for (int q = 0; q < DH / 32; ++q) {
                         float o[32];
 #pragma unroll
                         for (int e = 0; e < 32; ++e) o[e] = 0.f;
-                        for (int p = first; p <= last; ++p) {
-                            const float* src = slot_of(p);
-                            const float2 ml = __ldcg(reinterpret_cast<const float2*>(src) + row);
-                            if (ml.y == 0.f) continue;  // nothing attended to there, nothing stored
-                            const float f = fa_ex2(ml.x - ref) * inv;
+#pragma unroll 1
+                        for (int p0 = first; p0 <= last; p0 += 4) {  // four parts' loads in flight
+                            float4 v[4][8];
+                            float f[4];
 #pragma unroll
-                            for (int u = 0; u < 8; ++u) {
-                                const float4 v = __ldcg(reinterpret_cast<const float4*>(src + 2 * kPfRows) + (8 * q + u) * kPfRows + row);
-                                o[4 * u] += f * v.x;
-                                o[4 * u + 1] += f * v.y;
-                                o[4 * u + 2] += f * v.z;
-                                o[4 * u + 3] += f * v.w;
+                            for (int k = 0; k < 4; ++k) {
+                                const float* src = slot_of(min(p0 + k, last));
+                                const float2 ml = __ldcg(reinterpret_cast<const float2*>(src) + row);
+                                f[k] = p0 + k <= last && ml.y != 0.f ? fa_ex2(ml.x - ref) * inv : 0.f;
+#pragma unroll
+                                for (int u = 0; u < 8; ++u)
+                                    v[k][u] = __ldcg(reinterpret_cast<const float4*>(src + 2 * kPfRows) + (8 * q + u) * kPfRows + row);
                             }
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                if (f[k] != 0.f)  // else nothing attended to there, and nothing stored
+#pragma unroll
+                                    for (int u = 0; u < 8; ++u) {
+                                        o[4 * u] += f[k] * v[k][u].x;
+                                        o[4 * u + 1] += f[k] * v[k][u].y;
+                                        o[4 * u + 2] += f[k] * v[k][u].z;
+                                        o[4 * u + 3] += f[k] * v[k][u].w;
+                                    }
                         }
 #pragma unroll
                         for (int u = 0; u < 4; ++u)

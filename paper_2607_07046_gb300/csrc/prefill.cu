@@ -769,16 +769,6 @@ __device__ __forceinline__ bool fa_wait_warp(uint64_t* bar, uint32_t parity) {
     if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity) ? 1 : 0;
     return __shfl_sync(0xffffffffu, ok, 0) != 0;
 }
-// one non-blocking test of a phase
-__device__ __forceinline__ bool fa_test(uint64_t* bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
 __device__ __forceinline__ void fa_pair_sync(uint32_t id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
 
 // Test hook: one warp in each form of the kernels' waits, for a phase that nothing completes.

@@ -226,6 +226,17 @@ __host__ __device__ constexpr uint32_t idesc_f16_bmn(int m, int n) { return ides
 
 }  // namespace tc
 
+// one non-blocking test of a phase
+__device__ __forceinline__ bool fa_test(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+
 // ------------------------------------------------------------------ softmax steps
 // 2^x on the special-function unit (inputs far below -126 and -inf give 0)
 __device__ __forceinline__ float fa_ex2(float x) {
