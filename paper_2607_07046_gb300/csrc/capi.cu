@@ -2406,6 +2406,9 @@ extern "C" vt_status vt_paged_prefill(vt_paged* g, const vt_paged_pool* pool, co
     PagedAttnArgs a{};
     VT_TRY(paged_attn(g, pool, batch, n_rows, n_heads, q, q_ld, scale, window, out, out_ld, &a));
     if (a.n_rows == 0 || batch->n_seqs == 0) return ok();
-    VT_CUDA(launch_paged_prefill(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
+    // A few columns (rows times query heads of a group) per sequence: the kernel of single tokens, which streams K and V
+    // once for 16 of them; the tensor cores' tiles take 128.
+    const bool few = (int64_t)n_rows * a.group <= (int64_t)16 * batch->n_seqs;
+    VT_CUDA((few ? launch_paged_decode : launch_paged_prefill)(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
     return ok();
 }

@@ -1,20 +1,22 @@
-// Attention of one new row per sequence over the paged KV cache (Voltron Section 2.1, decode phase).
+// Attention of one or a few new rows per sequence over the paged KV cache (Voltron Section 2.1, decode
+// phase).
 //
-//   o_h = sum_j softmax_j(scale q_h . k_j) v_j over the row's positions, one pass over K and V with a
-//   running maximum m (log2 units), sum l and o per query head.
+//   o_c = sum_j softmax_j(scale q_c . k_j) v_j over the positions of column c, one pass over K and V with a
+//   running maximum m (log2 units), sum l and o per column.  The columns of a sequence's KV head are its new
+//   rows times the query heads of the group (column i group + h: row i, head h).
 //
-// What bounds it: every K and V byte is read once and meets `group` query heads (group FLOPs a byte), so
-// HBM.  The work of a unit (a sequence's KV head and up to 8 NT of its query heads) is cut into steps of
-// 16 positions; the steps of all units form one line, and CTA c takes its c-th equal part, whatever the
+// What bounds it: every K and V byte is read once and meets a few columns (one FLOP a byte and column), so
+// HBM.  The work of a unit (a sequence's KV head and up to 8 NT of its columns) is cut into steps of 16
+// positions; the steps of all units form one line, and CTA c takes its c-th equal part, whatever the
 // sequences' lengths are.  They are known on the device only, so that a captured launch serves any
-// lengths.  Inside a CTA step i goes to warp i % 4, each with its own ring of asynchronous 16-byte copies
+// lengths.  A unit counts kPdUnitCost steps more than it has, as its queries and its result take that time.  Inside a CTA step i goes to warp i % 4, each with its own ring of asynchronous 16-byte copies
 // (K and V rows gathered through the page table), so no barrier stands in the stream; 128 KB or more a SM
 // are in flight.  A unit that several CTAs share is joined by the last of them to finish: partial (m, l,
 // o) in a workspace, added in CTA order, so a result does not depend on timing.
 //
 // Products run on mma.sync m16n8k16 (tcgen05 would need 64 or more rows where there are 1 to 16):
-//   S [16 heads x 8 keys] = Q . K^T      A: Q from registers, B: K rows by ldmatrix
-//   O^T [16 dims x 8 heads] += V^T . P^T  A: V by ldmatrix.trans, B: P as S leaves it in registers
+//   S [16 columns x 8 keys] = Q . K^T       A: Q from registers, B: K rows by ldmatrix
+//   O^T [16 dims x 8 columns] += V^T . P^T  A: V by ldmatrix.trans, B: P as S leaves it in registers
 // P is cut into two 16-bit terms, hi = round(p) and lo = round(p - hi), two products each: the weights
 // then carry 16 (bf16) or 22 (fp16) bits and the output's own rounding is the only one that counts.
 #include <cuda_runtime.h>
@@ -32,6 +34,7 @@ constexpr int kPdRing = 96 * 1024;           // bytes of the four warps' rings
 constexpr int kPdCtasPerSm = 2;
 // steps a CTA takes at least: fewer CTAs, each with work for all its warps, and fewer parts to join
 constexpr int kPdMinSteps = 8;
+constexpr int kPdUnitCost = 4;
 
 template <int DH>
 struct PdGeom {
@@ -73,40 +76,50 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Attended positions [beg, end) of the row of sequence b (end 0: none).
-__device__ __forceinline__ void pd_range(const PagedAttnArgs& a, int b, int& beg, int& end) {
-    const int len = paged_len(a.c, b);
-    end = len < 0 ? 0 : min(len + 1, a.c.cap);
-    beg = a.window > 0 ? max(0, len + 1 - a.window) : 0;
-    if (beg >= end) beg = end = 0;  // a length past the table may leave the window nothing
-}
-__device__ __forceinline__ int pd_steps(int beg, int end) { return (end + kPdKeys - 1) / kPdKeys - beg / kPdKeys; }
+// A sequence's new rows, and the positions [beg, end) that they attend to (end 0: none).
+struct PdSeq {
+    int row0, rows, len, beg, end, tiles, steps;
+    // tiles: units of a KV head, of `cols` columns
+    template <bool ROWS>
+    __device__ __forceinline__ void open(const PagedAttnArgs& a, int b, int cols) {
+        len = paged_len(a.c, b);
+        row0 = b;
+        rows = 1;
+        if (ROWS) {
+            row0 = paged_start(a.c, b, a.n_rows);
+            rows = max(0, paged_start(a.c, b + 1, a.n_rows) - row0);
+        }
+        end = len < 0 || rows == 0 ? 0 : min(len + rows, a.c.cap);
+        beg = a.window > 0 ? max(0, len + 1 - a.window) : 0;
+        if (beg >= end) beg = end = 0;  // a length past the table may leave the window nothing
+        steps = (end + kPdKeys - 1) / kPdKeys - beg / kPdKeys;
+        tiles = (rows * a.group + cols - 1) / cols;
+    }
+    // its share of the line, for one KV head
+    __device__ __forceinline__ int64_t cost() const { return steps > 0 ? (int64_t)tiles * (steps + kPdUnitCost) : 0; }
+};
 
-// Where a walk over the steps of the units stands.
+// Where a walk over the steps of the units stands: unit u of sequence b (KV head u / tiles), step i - kPdUnitCost.
+template <bool ROWS, int COLS>
 struct PdCursor {
-    int b, u, i, steps, beg, end;
+    int b, u, i;
+    PdSeq s;
     __device__ __forceinline__ void open(const PagedAttnArgs& a, int seq) {
         b = seq;
-        steps = 0;
-        if (b < a.c.n_seqs) {
-            pd_range(a, b, beg, end);
-            steps = pd_steps(beg, end);
-        }
+        s.steps = 0;
+        if (b < a.c.n_seqs) s.template open<ROWS>(a, b, COLS);
     }
-    // n steps further (units: units of a sequence); sequences without positions have none
-    __device__ __forceinline__ void move(const PagedAttnArgs& a, int n, int units) {
-        i += n;
-        while (b < a.c.n_seqs && i >= steps) {
-            i -= steps;
-            if (steps == 0 || ++u == units) {
-                u = 0;
-                open(a, b + 1);
-            }
-        }
+    // on to the next unit that has steps
+    __device__ __forceinline__ void next(const PagedAttnArgs& a) {
+        i = 0;
+        if (s.steps > 0 && ++u < a.c.n_kv_heads * s.tiles) return;
+        u = 0;
+        do open(a, b + 1);
+        while (s.steps == 0 && b < a.c.n_seqs);
     }
 };
 
-template <class T, int DH, int NT>
+template <class T, int DH, int NT, bool ROWS>
 __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const __grid_constant__ PagedAttnArgs a) {
     using E = Elem<T>;
     using G = PdGeom<DH>;
@@ -118,20 +131,20 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
     __shared__ uint32_t s_mask[kPdWarps][S];
     const PagedView& c = a.c;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    const int tiles = (a.group + 8 * NT - 1) / (8 * NT), units = c.n_kv_heads * tiles;
+    constexpr int COLS = 8 * NT;
     pdl_wait();
     pdl_launch_dependents();
 
-    // ---- this CTA's part of the line of steps: thread t sums the sequences [t ch, (t + 1) ch)
+    // ---- this CTA's part of the line: thread t sums the sequences [t ch, (t + 1) ch)
     const int ch = (c.n_seqs + kPdThreads - 1) / kPdThreads;
     int64_t mine = 0;
     bool idle = false;
     for (int b = tid * ch; b < min(c.n_seqs, (tid + 1) * ch); ++b) {
-        int beg, end;
-        pd_range(a, b, beg, end);
-        if (blockIdx.x == 0 && c.lens[b] >= c.cap) set_status(c.status, VT_DEV_KV_OVERFLOW);
-        idle |= end == 0;
-        mine += pd_steps(beg, end);
+        PdSeq s;
+        s.open<ROWS>(a, b, COLS);
+        if (blockIdx.x == 0 && (s.len + s.rows > c.cap || c.lens[b] > c.cap)) set_status(c.status, VT_DEV_KV_OVERFLOW);
+        idle |= s.steps == 0;
+        mine += s.cost();
     }
     int64_t upto = mine;
 #pragma unroll
@@ -146,62 +159,82 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
         if (w < warp) upto += s_sum[w];
         total += s_sum[w];
     }
-    if (any_idle)
+    if (any_idle)  // rows that attend to nothing get zeros
         for (int b = blockIdx.x; b < c.n_seqs; b += gridDim.x) {
-            int beg, end;
-            pd_range(a, b, beg, end);
-            if (end == 0)
-                for (int e = tid; e < a.n_heads * DH / 8; e += kPdThreads)
-                    reinterpret_cast<uint4*>(a.out + b * a.out_ld)[e] = make_uint4(0u, 0u, 0u, 0u);
+            PdSeq s;
+            s.open<ROWS>(a, b, COLS);
+            if (s.steps == 0)
+                for (int r = s.row0; r < s.row0 + s.rows; ++r)
+                    for (int e = tid; e < a.n_heads * DH / 8; e += kPdThreads)
+                        reinterpret_cast<uint4*>(a.out + r * a.out_ld)[e] = make_uint4(0u, 0u, 0u, 0u);
         }
-    const int64_t line = total * units;
+    const int64_t line = total * c.n_kv_heads;
     const int64_t per = max((line + gridDim.x - 1) / gridDim.x, (int64_t)kPdMinSteps);
     const int64_t t0 = blockIdx.x * per, t1 = min(line, t0 + per);
     if (t0 >= t1) return;
-    if (upto - mine <= t0 / units && t0 / units < upto) {  // the thread whose sequences hold step t0
+    if (upto - mine <= t0 / c.n_kv_heads && t0 / c.n_kv_heads < upto) {  // the thread whose sequences hold t0
         int64_t before = upto - mine;
         int b = tid * ch;
         for (;; ++b) {
-            int beg, end;
-            pd_range(a, b, beg, end);
-            const int n = pd_steps(beg, end);
-            if (t0 / units < before + n) break;
-            before += n;
+            PdSeq s;
+            s.open<ROWS>(a, b, COLS);
+            if (t0 / c.n_kv_heads < before + s.cost()) break;
+            before += s.cost();
         }
         s_seq = b;
         s_before = before;
     }
     __syncthreads();
 
-    // ---- the copies: this warp's steps t0 + warp, t0 + warp + 4, ...
-    PdCursor at;  // of the whole CTA
+    // ---- the copies.  Step k of the CTA's part (unit costs left out) is warp k % 4's.
+    PdCursor<ROWS, COLS> at;  // of the whole CTA
     at.open(a, s_seq);
     {
-        const int64_t r = t0 - s_before * units;
-        at.u = (int)(r / at.steps);
-        at.i = (int)(r - (int64_t)at.u * at.steps);
+        const int64_t r = t0 - s_before * c.n_kv_heads;
+        at.u = (int)(r / (at.s.steps + kPdUnitCost));
+        at.i = (int)(r - (int64_t)at.u * (at.s.steps + kPdUnitCost));
     }
+    PdCursor<ROWS, COLS> ld = at;  // of this warp's copies: the unit of its next step
+    int64_t ld_now = t0;           // where that unit's part begins in the line
+    int ld_i, ld_n, ld_skip = warp;  // next step of the unit, steps of it here, steps until this warp's next
+    auto ld_unit = [&]() {           // the steps [first, n) of the unit that lie in this part
+        const int first = max(0, ld.i - kPdUnitCost);
+        ld_n = (int)min((int64_t)ld.s.steps, t1 - ld_now + ld.i - kPdUnitCost);
+        ld_i = first;
+    };
+    // moves to this warp's next step; false: none
+    auto ld_seek = [&]() -> bool {
+        while (ld_i + ld_skip >= ld_n) {
+            if (ld_n > ld_i) ld_skip -= ld_n - ld_i;
+            ld_now += ld.s.steps + kPdUnitCost - ld.i;
+            if (ld_now >= t1) return false;
+            ld.next(a);
+            ld_unit();
+        }
+        ld_i += ld_skip;
+        ld_skip = 0;
+        return true;
+    };
+    ld_unit();
+    bool more = ld_seek();
     const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * S * G::kStage);
-    PdCursor ld = at;
-    ld.move(a, warp, units);
-    int64_t to_load = (t1 - t0 - warp + kPdWarps - 1) / kPdWarps;
     int page = -1;  // lane r < 16: the page of row r of the next step to load (-1: not attended to)
     auto look_up = [&]() {
         page = -1;
-        if (to_load > 0 && lane < kPdKeys) {
-            const int p = (ld.beg / kPdKeys + ld.i) * kPdKeys + lane;
-            if (p >= ld.beg && p < ld.end) page = c.tables[(int64_t)ld.b * c.per_seq + (p >> c.page_shift)];
+        if (more && lane < kPdKeys) {
+            const int p = (ld.s.beg / kPdKeys + ld_i) * kPdKeys + lane;
+            if (p >= ld.s.beg && p < ld.s.end) page = c.tables[(int64_t)ld.b * c.per_seq + (p >> c.page_shift)];
             else page = -2;
         }
     };
     look_up();
     int st_load = 0;
     auto load_step = [&]() {
-        if (to_load > 0) {
+        if (more) {
             const bool on = lane < kPdKeys && (unsigned)page < (unsigned)c.n_pages;
             if (lane < kPdKeys && !on && page != -2) set_status(c.status, VT_DEV_BAD_PAGE);
-            const int p = (ld.beg / kPdKeys + ld.i) * kPdKeys + lane;
-            const int64_t off = on ? page * c.page_stride + (ld.u / tiles) * c.head_stride + (p & (c.page_size - 1)) * c.pos_stride
+            const int p = (ld.s.beg / kPdKeys + ld_i) * kPdKeys + lane;
+            const int64_t off = on ? page * c.page_stride + (ld.u / ld.s.tiles) * c.head_stride + (p & (c.page_size - 1)) * c.pos_stride
                                    : -1;
             const uint32_t mask = __ballot_sync(0xffffffffu, on);
             if (lane == 0) s_mask[warp][st_load] = mask;
@@ -216,8 +249,8 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
                 cp_async16(d, a.kpool + src, o >= 0);
                 cp_async16(d + kPdKeys * G::kRow, a.vpool + src, o >= 0);
             }
-            ld.move(a, kPdWarps, units);
-            --to_load;
+            ld_skip = kPdWarps;
+            more = ld_seek();
             look_up();
         }
         cp_async_commit();
@@ -230,17 +263,32 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
     int st = 0, skip = warp;  // skip: steps until this warp's next
     float* so = reinterpret_cast<float*>(smem + kPdRing);
     for (int64_t now = t0; now < t1;) {
-        const int n = (int)min((int64_t)(at.steps - at.i), t1 - now);  // steps of this unit here
-        const int kvh = at.u / tiles, h0 = (at.u - kvh * tiles) * 8 * NT, nh = min(8 * NT, a.group - h0);
-        const int64_t row = (int64_t)at.b * a.q_ld + (int64_t)(kvh * a.group + h0) * DH;
+        // steps [i0, i0 + n) of the unit are in this part
+        const int i0 = max(0, at.i - kPdUnitCost), n = (int)min((int64_t)at.s.steps, t1 - now + at.i - kPdUnitCost) - i0;
+        const int64_t u0 = now - at.i + kPdUnitCost;  // where its steps begin in the line
+        now += at.s.steps + kPdUnitCost - at.i;
+        if (n <= 0) {
+            at.next(a);
+            continue;
+        }
+        const int kvh = at.u / at.s.tiles, c0 = (at.u - kvh * at.s.tiles) * COLS, nc = min(COLS, at.s.rows * a.group - c0);
+        // column c0 + c: its element offset in q and out
+        auto col_at = [&](int c, int64_t ld) {
+            const int row = ROWS ? (c0 + c) / a.group : 0;
+            return (at.s.row0 + row) * ld + (int64_t)(kvh * a.group + c0 + c - row * a.group) * DH;
+        };
         uint32_t q[DH / 16][4];
+        int last_key[NT];  // of this lane's columns, in the steps' keys
 #pragma unroll
-        for (int k = 0; k < DH / 16; ++k) {
-            const uint16_t* src = a.q + row + k * 16 + 2 * t;
-            q[k][0] = g < nh ? *reinterpret_cast<const uint32_t*>(src + g * DH) : 0u;
-            q[k][2] = g < nh ? *reinterpret_cast<const uint32_t*>(src + g * DH + 8) : 0u;
-            q[k][1] = NT > 1 && g + 8 < nh ? *reinterpret_cast<const uint32_t*>(src + (g + 8) * DH) : 0u;
-            q[k][3] = NT > 1 && g + 8 < nh ? *reinterpret_cast<const uint32_t*>(src + (g + 8) * DH + 8) : 0u;
+        for (int x = 0; x < 2; ++x) {
+            const bool on = x < NT && g + 8 * x < nc;
+            const uint16_t* src = a.q + (on ? col_at(g + 8 * x, a.q_ld) : 0) + 2 * t;
+#pragma unroll
+            for (int k = 0; k < DH / 16; ++k) {
+                q[k][x] = on ? *reinterpret_cast<const uint32_t*>(src + k * 16) : 0u;
+                q[k][2 + x] = on ? *reinterpret_cast<const uint32_t*>(src + k * 16 + 8) : 0u;
+            }
+            if (x < NT) last_key[x] = ROWS ? at.s.len + (c0 + g + 8 * x) / a.group : 0;
         }
         float m[NT], l[NT], o[DH / 16][NT][4];
 #pragma unroll
@@ -252,6 +300,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
         }
         int k0 = skip;
         for (; k0 < n; k0 += kPdWarps) {
+            const int p0 = ROWS ? (at.s.beg / kPdKeys + i0 + k0) * kPdKeys : 0;  // the step's first position
             load_step();
             cp_async_wait<S - 1>();
             __syncwarp();
@@ -273,9 +322,11 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
             for (int x = 0; x < NT; ++x) {
                 float v[4], mx = -INFINITY;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {  // keys 2t, 2t + 1, 2t + 8, 2t + 9 of head g + 8x
+                for (int e = 0; e < 4; ++e) {  // keys 2t, 2t + 1, 2t + 8, 2t + 9 of column g + 8x
                     const int key = 8 * (e >> 1) + 2 * t + (e & 1);
-                    v[e] = (mask >> key) & 1u ? s[e >> 1][2 * x + (e & 1)] * a.scale_log2 : -INFINITY;
+                    bool on = (mask >> key) & 1u;
+                    if (ROWS) on = on && p0 + key <= last_key[x] && (a.window == 0 || p0 + key > last_key[x] - a.window);
+                    v[e] = on ? s[e >> 1][2 * x + (e & 1)] * a.scale_log2 : -INFINITY;
                     mx = fmaxf(mx, v[e]);
                 }
                 mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
@@ -325,13 +376,8 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
         skip = k0 - n;
 
         // ---- the unit's end here: the four warps' (m, l, o) into one
-        const bool whole = at.i == 0 && n == at.steps;
-        int64_t first = 0, last = 0;  // the CTAs that share the unit
-        if (!whole) {
-            const int64_t u0 = now - at.i;
-            first = u0 / per;
-            last = (u0 + at.steps - 1) / per;
-        }
+        const bool whole = n == at.s.steps;
+        const int64_t first = u0 / per, last = (u0 + at.s.steps - 1) / per;  // the CTAs that share the unit
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
             l[x] += __shfl_xor_sync(0xffffffffu, l[x], 1);
@@ -365,7 +411,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
             __syncthreads();
             for (int e = tid; e < 8 * DH / 8; e += kPdThreads) {  // 8 dims of a head
                 const int h = e / (DH / 8), d = (e % (DH / 8)) * 8, ds = d ^ (8 * (h >> 1));
-                if (8 * x + h >= nh) continue;
+                if (8 * x + h >= nc) continue;
                 float sum[8] = {};
                 float mm = s_ml[0][0][8 * x + h], ll = 0.f;
                 for (int w = 1; w < kPdWarps; ++w) mm = fmaxf(mm, s_ml[0][w][8 * x + h]);
@@ -380,7 +426,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
                 }
                 if (whole) {
                     const float inv = ll == 0.f ? 0.f : 1.f / ll;
-                    uint16_t* dst = a.out + (int64_t)at.b * a.out_ld + (int64_t)(kvh * a.group + h0 + 8 * x + h) * DH + d;
+                    uint16_t* dst = a.out + col_at(8 * x + h, a.out_ld) + d;
                     *reinterpret_cast<uint4*>(dst) = make_uint4(E::pack(sum[0] * inv, sum[1] * inv), E::pack(sum[2] * inv, sum[3] * inv),
                                                                 E::pack(sum[4] * inv, sum[5] * inv), E::pack(sum[6] * inv, sum[7] * inv));
                 } else {
@@ -406,7 +452,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
             __syncthreads();
             if (s_last) {
                 __threadfence();
-                for (int e = tid; e < nh * (DH / 8); e += kPdThreads) {
+                for (int e = tid; e < nc * (DH / 8); e += kPdThreads) {
                     const int h = e / (DH / 8), d = (e % (DH / 8)) * 8;
                     float sum[8] = {}, mm = -INFINITY, ll = 0.f;
 #pragma unroll 4
@@ -425,40 +471,46 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
                         sum[6] = sum[6] * fa + v1.z * fb, sum[7] = sum[7] * fa + v1.w * fb;
                     }
                     const float inv = ll == 0.f ? 0.f : 1.f / ll;
-                    uint16_t* dst = a.out + (int64_t)at.b * a.out_ld + (int64_t)(kvh * a.group + h0 + h) * DH + d;
+                    uint16_t* dst = a.out + col_at(h, a.out_ld) + d;
                     *reinterpret_cast<uint4*>(dst) = make_uint4(E::pack(sum[0] * inv, sum[1] * inv), E::pack(sum[2] * inv, sum[3] * inv),
                                                                 E::pack(sum[4] * inv, sum[5] * inv), E::pack(sum[6] * inv, sum[7] * inv));
                 }
             }
         }
         __syncthreads();  // so and s_ml are free for the next unit
-        now += n;
-        at.move(a, n, units);
+        at.next(a);
     }
     cp_async_wait<0>();
 }
 
-template <class T, int DH, int NT>
+template <class T, int DH, int NT, bool ROWS>
 static cudaError_t decode_nt(const PagedAttnArgs& a, cudaStream_t st) {
-    const int units = a.c.n_kv_heads * ((a.group + 8 * NT - 1) / (8 * NT));
-    const int64_t span = a.window > 0 ? std::min<int64_t>(a.window + kPdKeys, a.c.cap) : a.c.cap;
-    const int64_t most = (int64_t)a.c.n_seqs * units * ((span + kPdKeys - 1) / kPdKeys + 1);  // steps at the longest lengths
+    // steps at the longest lengths
+    const int64_t tiles = (int64_t)a.n_rows * a.group / (8 * NT) + a.c.n_seqs;
+    const int64_t span = a.window > 0 ? std::min<int64_t>((int64_t)a.window + a.n_rows, a.c.cap) : a.c.cap;
+    const int64_t most = tiles * a.c.n_kv_heads * (span / kPdKeys + 2 + kPdUnitCost);
     const int64_t grid = std::min<int64_t>(std::min(kPagedMaxGrid, kPdCtasPerSm * g_num_sms), (most + kPdMinSteps - 1) / kPdMinSteps);
-    return launch_paged_k(k_paged_decode<T, DH, NT>, (unsigned)grid, kPdThreads, PdGeom<DH>::kSmem, st, a);
+    return launch_paged_k(k_paged_decode<T, DH, NT, ROWS>, (unsigned)grid, kPdThreads, PdGeom<DH>::kSmem, st, a);
 }
-template <class T>
+template <class T, bool ROWS>
 static cudaError_t decode_t(const PagedAttnArgs& a, int dh, cudaStream_t st) {
-    if (dh == 128) return a.group <= 8 ? decode_nt<T, 128, 1>(a, st) : decode_nt<T, 128, 2>(a, st);
-    return a.group <= 8 ? decode_nt<T, 64, 1>(a, st) : decode_nt<T, 64, 2>(a, st);
+    // columns that the sequences have on average; more than 8 share a pass over K and V in tiles of 16
+    const bool wide = (int64_t)a.n_rows * a.group > (int64_t)8 * a.c.n_seqs;
+    if (dh == 128) return wide ? decode_nt<T, 128, 2, ROWS>(a, st) : decode_nt<T, 128, 1, ROWS>(a, st);
+    return wide ? decode_nt<T, 64, 2, ROWS>(a, st) : decode_nt<T, 64, 1, ROWS>(a, st);
 }
 cudaError_t launch_paged_decode(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st) {
-    return dtype == VT_F16 ? decode_t<__half>(a, dh, st) : decode_t<__nv_bfloat16>(a, dh, st);
+    if (a.c.starts) return dtype == VT_F16 ? decode_t<__half, true>(a, dh, st) : decode_t<__nv_bfloat16, true>(a, dh, st);
+    return dtype == VT_F16 ? decode_t<__half, false>(a, dh, st) : decode_t<__nv_bfloat16, false>(a, dh, st);
 }
 
 template <class T, int DH, int NT>
 static cudaError_t init_one() {
-    return cudaFuncSetAttribute(k_paged_decode<T, DH, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                (int)PdGeom<DH>::kSmem);
+    const cudaError_t e = cudaFuncSetAttribute(k_paged_decode<T, DH, NT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               (int)PdGeom<DH>::kSmem);
+    return e != cudaSuccess ? e
+                            : cudaFuncSetAttribute(k_paged_decode<T, DH, NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                   (int)PdGeom<DH>::kSmem);
 }
 cudaError_t init_paged_decode() {
     cudaError_t e[8] = {init_one<__half, 64, 1>(),        init_one<__half, 64, 2>(),        init_one<__half, 128, 1>(),
