@@ -32,9 +32,13 @@ constexpr int kPdWarps = 4, kPdThreads = kPdWarps * 32;
 constexpr int kPdKeys = 16;                  // positions of a step
 constexpr int kPdRing = 96 * 1024;           // bytes of the four warps' rings
 constexpr int kPdCtasPerSm = 2;
-// steps a CTA takes at least: fewer CTAs, each with work for all its warps, and fewer parts to join
-constexpr int kPdMinSteps = 8;
-constexpr int kPdUnitCost = 4;
+// A unit's queries, merge and result cost as much as this many steps (measured: 64 ragged sequences 75 us at 0, 56 at
+// 4, 47 at 8 to 24, 50 at 32).
+constexpr int kPdUnitCost = 16;
+// What a CTA takes at least: where the largest unit costs no more than kPdWhole (12 steps), that much, so that none is
+// split and joined (8 heads of 128 positions: 5.4 us, split 6.7; at 48, units of 20 to 30 steps lost up to 2 us);
+// otherwise kPdMinSteps.
+constexpr int kPdMinSteps = 16, kPdWhole = 28;
 
 template <int DH>
 struct PdGeom {
@@ -126,7 +130,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
     constexpr int S = G::kStages, CPR = DH / 8, RPI = 32 / CPR;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ int64_t s_sum[kPdWarps], s_before;
-    __shared__ int s_seq, s_last;
+    __shared__ int s_seq, s_last, s_max[kPdWarps];
     __shared__ float s_ml[2][kPdWarps][8 * NT];
     __shared__ uint32_t s_mask[kPdWarps][S];
     const PagedView& c = a.c;
@@ -138,27 +142,35 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
     // ---- this CTA's part of the line: thread t sums the sequences [t ch, (t + 1) ch)
     const int ch = (c.n_seqs + kPdThreads - 1) / kPdThreads;
     int64_t mine = 0;
+    int largest = 0;
     bool idle = false;
     for (int b = tid * ch; b < min(c.n_seqs, (tid + 1) * ch); ++b) {
         PdSeq s;
         s.open<ROWS>(a, b, COLS);
         if (blockIdx.x == 0 && (s.len + s.rows > c.cap || c.lens[b] > c.cap)) set_status(c.status, VT_DEV_KV_OVERFLOW);
         idle |= s.steps == 0;
+        largest = max(largest, s.steps);
         mine += s.cost();
     }
+    largest = __reduce_max_sync(0xffffffffu, largest);
     int64_t upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
         if (lane >= o) upto += v;
     }
-    if (lane == 31) s_sum[warp] = upto;
+    if (lane == 31) {
+        s_sum[warp] = upto;
+        s_max[warp] = largest;
+    }
     const bool any_idle = __syncthreads_or(idle);
     int64_t total = 0;
     for (int w = 0; w < kPdWarps; ++w) {
         if (w < warp) upto += s_sum[w];
         total += s_sum[w];
+        largest = max(largest, s_max[w]);
     }
+    largest += kPdUnitCost;
     if (any_idle)  // rows that attend to nothing get zeros
         for (int b = blockIdx.x; b < c.n_seqs; b += gridDim.x) {
             PdSeq s;
@@ -169,7 +181,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
                         reinterpret_cast<uint4*>(a.out + r * a.out_ld)[e] = make_uint4(0u, 0u, 0u, 0u);
         }
     const int64_t line = total * c.n_kv_heads;
-    const int64_t per = max((line + gridDim.x - 1) / gridDim.x, (int64_t)kPdMinSteps);
+    const int64_t per = max((line + gridDim.x - 1) / gridDim.x, (int64_t)(largest <= kPdWhole ? largest : kPdMinSteps));
     const int64_t t0 = blockIdx.x * per, t1 = min(line, t0 + per);
     if (t0 >= t1) return;
     if (upto - mine <= t0 / c.n_kv_heads && t0 / c.n_kv_heads < upto) {  // the thread whose sequences hold t0
@@ -485,10 +497,9 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
 
 template <class T, int DH, int NT, bool ROWS>
 static cudaError_t decode_nt(const PagedAttnArgs& a, cudaStream_t st) {
-    // steps at the longest lengths
     const int64_t tiles = (int64_t)a.n_rows * a.group / (8 * NT) + a.c.n_seqs;
     const int64_t span = a.window > 0 ? std::min<int64_t>((int64_t)a.window + a.n_rows, a.c.cap) : a.c.cap;
-    const int64_t most = tiles * a.c.n_kv_heads * (span / kPdKeys + 2 + kPdUnitCost);
+    const int64_t most = tiles * a.c.n_kv_heads * (span / kPdKeys + 2 + kPdUnitCost);  // of cost, at the longest lengths
     const int64_t grid = std::min<int64_t>(std::min(kPagedMaxGrid, kPdCtasPerSm * g_num_sms), (most + kPdMinSteps - 1) / kPdMinSteps);
     return launch_paged_k(k_paged_decode<T, DH, NT, ROWS>, (unsigned)grid, kPdThreads, PdGeom<DH>::kSmem, st, a);
 }

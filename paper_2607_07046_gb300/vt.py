@@ -209,6 +209,9 @@ def _check(status: int) -> None:
 def _stream(stream) -> int:
     if stream is None:
         import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # the handle without a Stream object: 0.1 us, not 3
+        if raw is not None and torch.cuda.is_initialized():
+            return raw(torch._C._cuda_getDevice())
         return torch.cuda.current_stream().cuda_stream
     if hasattr(stream, "cuda_stream"):
         return stream.cuda_stream
@@ -684,7 +687,7 @@ def make_paged_pool(k, v) -> vt_paged_pool:
         raise ValueError("K and V need one shape, equal strides, one device and a contiguous head dim")
     p = vt_paged_pool(k.data_ptr(), v.data_ptr(), VT_F16 if k.dtype == torch.float16 else VT_BF16, k.shape[0],
                       k.shape[2], k.shape[1], k.shape[3], k.stride(0), k.stride(1), k.stride(2))
-    p.tensors = (k, v)
+    p.tensors, p.torch_dtype, p.device = (k, v), k.dtype, k.get_device()
     return p
 
 
@@ -734,12 +737,12 @@ def vt_rope_table(table, theta: float, stream=None) -> None:
 def _rows(t, pool, heads: Optional[int] = None) -> Tuple[int, int]:
     """(data_ptr, elements between rows) of a CUDA tensor [rows, heads, head dim] of the pool's type and
     device whose rows are contiguous."""
-    shape, stride, k = t.shape, t.stride(), pool.tensors[0]
+    shape, stride = t.shape, t.stride()
     if len(shape) != 3 or shape[2] != pool.d_head or (heads is not None and shape[1] != heads):
         raise ValueError(f"expected [rows, {'heads' if heads is None else heads}, {pool.d_head}], got {tuple(shape)}")
-    if t.dtype != k.dtype:
-        raise TypeError(f"expected {k.dtype}, got {t.dtype}")
-    if t.device != k.device or stride[2] != 1 or (stride[1] != shape[2] and shape[1] != 1):
+    if t.dtype is not pool.torch_dtype:
+        raise TypeError(f"expected {pool.torch_dtype}, got {t.dtype}")
+    if t.get_device() != pool.device or stride[2] != 1 or (stride[1] != shape[2] and shape[1] != 1):
         raise ValueError("expected rows of contiguous heads on the pool's device")
     return t.data_ptr(), stride[0]
 
