@@ -66,6 +66,11 @@ __device__ __forceinline__ int64_t paged_entry(const PagedView& c, int b, int h,
     return page * c.page_stride + h * c.head_stride + (p & (c.page_size - 1)) * c.pos_stride;
 }
 
+// a / b for a, b >= 0; the 64-bit division takes about four times as long as the 32-bit one.
+__device__ __forceinline__ int64_t paged_div(int64_t a, int64_t b) {
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 // First row of sequence b, and the row past its last, inside [0, n_rows].
 __device__ __forceinline__ int paged_start(const PagedView& c, int b, int n_rows) {
     return c.starts ? max(0, min(n_rows, c.starts[b])) : b;

@@ -181,16 +181,17 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
                         reinterpret_cast<uint4*>(a.out + r * a.out_ld)[e] = make_uint4(0u, 0u, 0u, 0u);
         }
     const int64_t line = total * c.n_kv_heads;
-    const int64_t per = max((line + gridDim.x - 1) / gridDim.x, (int64_t)(largest <= kPdWhole ? largest : kPdMinSteps));
+    const int64_t per = max(paged_div(line + gridDim.x - 1, gridDim.x), (int64_t)(largest <= kPdWhole ? largest : kPdMinSteps));
     const int64_t t0 = blockIdx.x * per, t1 = min(line, t0 + per);
     if (t0 >= t1) return;
-    if (upto - mine <= t0 / c.n_kv_heads && t0 / c.n_kv_heads < upto) {  // the thread whose sequences hold t0
+    const int64_t at_head = paged_div(t0, c.n_kv_heads);
+    if (upto - mine <= at_head && at_head < upto) {  // the thread whose sequences hold t0
         int64_t before = upto - mine;
         int b = tid * ch;
         for (;; ++b) {
             PdSeq s;
             s.open<ROWS>(a, b, COLS);
-            if (t0 / c.n_kv_heads < before + s.cost()) break;
+            if (at_head < before + s.cost()) break;
             before += s.cost();
         }
         s_seq = b;
@@ -203,7 +204,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
     at.open(a, s_seq);
     {
         const int64_t r = t0 - s_before * c.n_kv_heads;
-        at.u = (int)(r / (at.s.steps + kPdUnitCost));
+        at.u = (int)paged_div(r, at.s.steps + kPdUnitCost);
         at.i = (int)(r - (int64_t)at.u * (at.s.steps + kPdUnitCost));
     }
     PdCursor<ROWS, COLS> ld = at;  // of this warp's copies: the unit of its next step
@@ -389,7 +390,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
 
         // ---- the unit's end here: the four warps' (m, l, o) into one
         const bool whole = n == at.s.steps;
-        const int64_t first = u0 / per, last = (u0 + at.s.steps - 1) / per;  // the CTAs that share the unit
+        const int64_t first = paged_div(u0, per), last = paged_div(u0 + at.s.steps - 1, per);  // the CTAs that share the unit
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
             l[x] += __shfl_xor_sync(0xffffffffu, l[x], 1);

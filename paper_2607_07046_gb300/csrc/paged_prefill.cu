@@ -45,7 +45,11 @@ constexpr int kPfLaunchRegs = 168, kPfSoftmaxRegs = 208, kPfCopyRegs = 88;
 static_assert(256 * kPfSoftmaxRegs + 128 * kPfCopyRegs <= kPfThreads * kPfLaunchRegs,
               "the register split must fit in the registers the block is launched with");
 constexpr int kPfMaskRing = 8;   // validity words of the last blocks (the copies lead by fewer blocks)
-constexpr int kPfMinBlocks = 2;  // blocks a CTA takes at least
+// The start and end of a unit cost as much as this many blocks.
+constexpr int kPfUnitCost = 2;
+// What a CTA takes at least: where the largest unit costs no more than kPfWhole, that much, so that none is split and
+// joined; otherwise kPfMinBlocks.
+constexpr int kPfMinBlocks = 4, kPfWhole = 8;
 constexpr int kPfLag = 2;        // copy groups in flight behind the one just issued
 
 template <int DH>
@@ -59,7 +63,7 @@ struct PfGeom {
 // The units in order: sequence, KV head, tile pair.
 struct PfCursor {
     int b, kvh, pt;        // unit
-    int i, n, kb0;         // next block, blocks of the unit, its first block's number
+    int i, n, kb0;         // place in the unit (block i - kPfUnitCost), blocks of the unit, its first block's number
     int len, row0, rows;   // the sequence (rows 0: idle)
     int kbeg, kend;        // attended positions of the unit
     __device__ __forceinline__ void seq(const PagedAttnArgs& a, int at) {
@@ -101,10 +105,13 @@ struct PfCursor {
             unit(a, tr);
         } while (n == 0);
     }
-    __device__ __forceinline__ void move(const PagedAttnArgs& a, int tr, int blocks_done) {
-        i += blocks_done;
-        if (i >= n) next(a, tr);
+    // The unit's blocks [i0, i0 + n_here) of the `left` that the CTA still has; none: the unit's start lies here only.
+    __device__ __forceinline__ int part(int64_t left, int& n_here) const {
+        const int i0 = max(0, i - kPfUnitCost);
+        n_here = (int)min((int64_t)n, left + i - kPfUnitCost) - i0;
+        return i0;
     }
+    __device__ __forceinline__ int rest() const { return n + kPfUnitCost - i; }  // of the unit, in the line
     // blocks [lo, hi) of those numbered j0 .. j1 - 1 that tile x attends to; false: the tile has no tokens
     __device__ __forceinline__ bool tile(const PagedAttnArgs& a, int tr, int x, int j0, int j1, int& lo, int& hi) const {
         const int t0 = (2 * pt + x) * tr, t1 = min(t0 + tr, rows);
@@ -170,8 +177,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
     volatile int* s_err = reinterpret_cast<volatile int*>(tmem_slot + 1);
     volatile int* s_last = s_err + 1;        // [2]
-    int64_t* s_at = reinterpret_cast<int64_t*>(tmem_slot + 4);  // [2]: blocks of all units; blocks before the first unit's
+    int64_t* s_at = reinterpret_cast<int64_t*>(tmem_slot + 4);  // length of the line
     int* s_unit = reinterpret_cast<int*>(s_at + 2);             // [4]
+    int* s_largest = reinterpret_cast<int*>(s_at + 1);          // blocks of the largest unit
     // where each warp stands between units: in shared memory, as the registers hold S meanwhile
     PfCursor* cursor = reinterpret_cast<PfCursor*>(s_unit + 4) + (threadIdx.x >> 5);
 
@@ -194,6 +202,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
         }
         mbar_init(done, 1);
         *s_err = 0;
+        *s_largest = 0;
         fence_mbar_init();
     }
     pdl_wait();  // a preceding kernel may hold tensor memory
@@ -203,10 +212,12 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
         tc::tmem_relinquish();
     }
 
+    __syncthreads();
     // ---- blocks of each sequence for one KV head (a warp a sequence, a lane a tile pair); rows that
     // attend to nothing get zeros
     int64_t* tot = reinterpret_cast<int64_t*>(smem);
     PfCursor at;
+    int largest = 0;
     for (int b = warp; b < c.n_seqs; b += kPfThreads / 32) {
         at.seq(a, b);
         int64_t sum = 0;
@@ -224,19 +235,24 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                     at.range(a, t0, min(t0 + 2 * tr, at.rows), beg, end);
                     n = PfCursor::blocks(beg, end);
                 }
+                largest = max(largest, n);
                 for (unsigned none = __ballot_sync(0xffffffffu, t0 < at.rows && n == 0); none; none &= none - 1) {
                     const int z0 = (p0 + __ffs(none) - 1) * 2 * tr;
                     for (int r = z0; r < min(z0 + 2 * tr, at.rows); ++r)
                         if ((at.row0 + r) % gridDim.x == blockIdx.x) pf_zero_row(a, at.row0 + r, a.n_heads * DH / 8, lane);
                 }
-                sum += n;
+                sum += n > 0 ? n + kPfUnitCost : 0;
             }
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         }
         if (lane == 0) tot[b] = sum;
     }
+    largest = __reduce_max_sync(0xffffffffu, largest);
+    if (lane == 0 && largest > 0) atomicMax(s_largest, largest);
     __syncthreads();
+    largest = *s_largest + kPfUnitCost;
+    const int least = largest <= kPfWhole ? largest : kPfMinBlocks;
     // ---- where this CTA's part of the line begins
     if (warp == 0) {
         int64_t sum = 0;
@@ -244,7 +260,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         const int64_t line = sum * c.n_kv_heads;
-        const int64_t per = max((line + gridDim.x - 1) / gridDim.x, (int64_t)kPfMinBlocks);
+        const int64_t per = max(paged_div(line + gridDim.x - 1, gridDim.x), (int64_t)least);
         const int64_t t0 = blockIdx.x * per;
         if (lane == 0) s_at[0] = line;
         if (t0 < line) {
@@ -268,7 +284,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                 before += __shfl_sync(0xffffffffu, upto, 31);
             }
             int64_t r = t0 - before * c.n_kv_heads;
-            const int kvh = (int)(r / tot[b]);
+            const int kvh = (int)paged_div(r, tot[b]);
             r -= (int64_t)kvh * tot[b];
             at.seq(a, b);
             for (int p0 = 0;; p0 += 32) {  // the tile pair
@@ -278,6 +294,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                     int beg, end;
                     at.range(a, q0, min(q0 + 2 * tr, at.rows), beg, end);
                     n = PfCursor::blocks(beg, end);
+                    if (n > 0) n += kPfUnitCost;
                 }
                 int64_t upto = n;
 #pragma unroll
@@ -303,7 +320,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
     }
     __syncthreads();
     const int64_t line = s_at[0];
-    const int64_t per = max((line + gridDim.x - 1) / gridDim.x, (int64_t)kPfMinBlocks);
+    const int64_t per = max(paged_div(line + gridDim.x - 1, gridDim.x), (int64_t)least);
     const int64_t t0 = blockIdx.x * per, t1 = min(line, t0 + per);
     if (t0 >= t1) {
         if (warp == 11) tc::tmem_dealloc(*tmem_slot, 512);
@@ -358,10 +375,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
             sent1 = sent2 = nullptr;
         };
         int slot = 0, round = 0, blk = 0, nq = 0;
-        for (int64_t now = t0; ok && now < t1;) {
-            const int n = (int)min((int64_t)(at.n - at.i), t1 - now);
-            const int j0 = at.kb0 + at.i;
-            int next_page = request(j0);
+        for (int64_t left = t1 - t0; ok && left > 0;) {
+            int n;
+            const int j0 = at.kb0 + at.part(left, n);
+            left -= at.rest();
+            int next_page = n > 0 ? request(j0) : 0;
             for (int j = j0; ok && j < j0 + n; ++j, ++blk) {
                 const int p0 = j * kPfKeys, lo = at.kbeg - p0, hi = at.kend - p0;  // attended rows [lo, hi)
                 const int page = next_page;
@@ -464,8 +482,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                     }
                 }
             }
-            now += n;
-            at.move(a, tr, n);
+            at.next(a, tr);
         }
         if (ok) flush();
         asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -496,17 +513,17 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
             int n, j0, j1, lo[2], hi[2];
             {
                 PfCursor at = *cursor;
-                n = (int)min((int64_t)(at.n - at.i), left);
-                j0 = at.kb0 + at.i;
+                j0 = at.kb0 + at.part(left, n);
                 j1 = j0 + n;
                 at.tile(a, tr, 0, j0, j1, lo[0], hi[0]);
                 at.tile(a, tr, 1, j0, j1, lo[1], hi[1]);
-                at.move(a, tr, n);
+                left -= at.rest();
+                at.next(a, tr);
                 __syncwarp();  // every lane has read the cursor
                 if (lane == 0) *cursor = at;
                 __syncwarp();
             }
-            left -= n;
+            if (n <= 0) continue;
             ok = pf_wait(q_full, nq & 1);
             ++nq;
             for (int j = j0 - 1; ok && j < j1; ++j) {
@@ -603,9 +620,16 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
             int n, j0, lo, hi, qp;
             bool has, live;
             {
-                const PfCursor at = *cursor;
-                n = (int)min((int64_t)(at.n - at.i), left);
-                j0 = at.kb0 + at.i;
+                PfCursor at = *cursor;
+                j0 = at.kb0 + at.part(left, n);
+                if (n <= 0) {
+                    left -= at.rest();
+                    at.next(a, tr);
+                    __syncwarp();  // every lane has read the cursor
+                    if (lane == 0) *cursor = at;
+                    __syncwarp();
+                    continue;
+                }
                 has = at.tile(a, tr, x, j0, j0 + n, lo, hi);
                 const int tok = (2 * at.pt + x) * tr + row / a.group;
                 live = row < tr * a.group && tok < at.rows;
@@ -628,7 +652,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
 #pragma unroll
                 for (int q = 0; q < 4; ++q) mw[q] = fa_range_bits(cb - 32 * q, ce - 32 * q) & vw[q];
                 const bool plain = __all_sync(0xffffffffu, (mw[0] & mw[1] & mw[2] & mw[3]) == 0xffffffffu);
-                float pm = -INFINITY;
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     tc::tmem_ld_wait_on(sv[q]);
@@ -636,9 +660,12 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
                             if (!((mw[q] >> e) & 1u)) sv[q][e] = 0xff800000u;  // -inf
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) pm = fa_max3(pm, __uint_as_float(sv[q][e]), __uint_as_float(sv[q][e + 1]));
                 }
+#pragma unroll
+                for (int e = 0; e < 32; e += 2)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) mx[q] = fa_max3(mx[q], __uint_as_float(sv[q][e]), __uint_as_float(sv[q][e + 1]));
+                const float pm = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                 const float bms = pm == -INFINITY ? pm : pm * sl2;
                 float alpha = 1.f;
                 bool resc = false;
@@ -694,7 +721,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
             // ---- the tile's end here
             PfCursor at = *cursor;
             const int tok = (2 * at.pt + x) * tr + row / a.group;
-            const bool any = hi > lo, whole = at.i == 0 && n == at.n;
+            const bool any = hi > lo, whole = n == at.n;
             if (any) {
                 if (ok) ok = pf_wait(&o_full[x], no & 1);
                 ++no;
@@ -732,9 +759,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                         }
             } else if (has) {
                 // a part: (m, l) and O by four columns, all rows side by side
-                const int64_t per = max((s_at[0] + gridDim.x - 1) / gridDim.x, (int64_t)kPfMinBlocks);
-                const int64_t u0 = min(s_at[0], (blockIdx.x + 1) * per) - left - at.i;
-                const int first = (int)(u0 / per), last = (int)((u0 + at.n - 1) / per);
+                const int64_t u0 = t1 - left - at.i + kPfUnitCost;  // where the unit's blocks begin in the line
+                const int first = (int)paged_div(u0, per), last = (int)paged_div(u0 + at.n - 1, per);
                 auto slot_of = [&](int cta) { return a.work + (int64_t)(4 * cta + (cta == first ? 2 : 0) + x) * kPagedPrefillSlot; };
                 float* part = slot_of((int)blockIdx.x);
                 reinterpret_cast<float2*>(part)[row] = make_float2(m_use, l);
@@ -762,12 +788,20 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                 consumer_bar(1 + x, 128);
                 if (s_last[x] && live && ok) {  // the last to get here joins the parts, in CTA order
                     __threadfence();
-                    float mm = -INFINITY, ll = 0.f;
-                    for (int p = first; p <= last; ++p) mm = fmaxf(mm, __ldcg(reinterpret_cast<const float2*>(slot_of(p)) + row).x);
-                    const float ref = mm == -INFINITY ? 0.f : mm;
-                    for (int p = first; p <= last; ++p) {
-                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(slot_of(p)) + row);
-                        ll += ml.y * fa_ex2(ml.x - ref);
+                    float mm = -INFINITY, ll = 0.f, ref = 0.f;
+                    for (int p0 = first; p0 <= last; p0 += 4) {
+                        float2 ml[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) ml[k] = __ldcg(reinterpret_cast<const float2*>(slot_of(min(p0 + k, last))) + row);
+                        float mn = mm;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) mn = fmaxf(mn, ml[k].x);
+                        ref = mn == -INFINITY ? 0.f : mn;
+                        ll *= fa_ex2(mm - ref);
+                        mm = mn;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (p0 + k <= last) ll += ml[k].y * fa_ex2(ml[k].x - ref);
                     }
                     const float inv = ll == 0.f ? 0.f : 1.f / ll;
 #pragma unroll 1
@@ -813,8 +847,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&o_free[x]);
             }
-            left -= n;
-            at.move(a, tr, n);
+            left -= at.rest();
+            at.next(a, tr);
             __syncwarp();  // every lane has read the cursor
             if (lane == 0) *cursor = at;
             __syncwarp();
@@ -835,10 +869,10 @@ size_t paged_work_floats() {
 
 template <class T, int DH>
 static cudaError_t prefill_dh(const PagedAttnArgs& a, cudaStream_t st) {
-    // blocks at the longest lengths
+    // the line at the longest lengths
     const int64_t pairs = (int64_t)a.n_rows / (2 * (kPfRows / a.group)) + a.c.n_seqs;
     const int64_t span = a.window > 0 ? std::min<int64_t>((int64_t)a.window + 2 * kPfRows, a.c.cap) : a.c.cap;
-    const int64_t most = pairs * a.c.n_kv_heads * (span / kPfKeys + 2);
+    const int64_t most = pairs * a.c.n_kv_heads * (span / kPfKeys + 2 + kPfUnitCost);
     const int64_t grid = std::min<int64_t>(std::min(kPagedMaxGrid / 2, g_num_sms), (most + kPfMinBlocks - 1) / kPfMinBlocks);
     PfParams P{};
     P.a = a;
