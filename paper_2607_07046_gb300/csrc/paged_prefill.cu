@@ -14,11 +14,12 @@
 //   warps 0-3, 4-7  softmax of tile 0 and 1, one thread a row (its lane of the tensor memory): no exchange
 //                   between threads.  m is a reference maximum; O and l are rescaled only when a block's
 //                   maximum exceeds it by more than 8 (log2), so P stays below 2^8.
-//   warps 8-10      copies: Q, and K and V through the page table, by tensor copies of a page's rows; blocks that
+//   warps 8, 9      copies: Q, and K and V through the page table, by tensor copies of a page's rows; blocks that
 //                   hold positions outside the unit's range (whatever lies there must not reach V: they are
 //                   filled with zeros), bad pages or pages of fewer than 16 positions by 16-byte asynchronous
 //                   copies into the same swizzled layout
-//   warp 11         tensor memory and the MMAs
+//   warps 10, 11    the MMAs of tile 0 and 1: the waits and the issue of one fall into the other's products (one warp
+//                   for both took 4700 cycles for two blocks)
 //
 // The blocks of all units form one line, and CTA c (one an SM) takes its c-th equal part, so neither few
 // long histories nor ragged prompts leave SMs idle; lengths are known on the device only.  A unit that
@@ -38,7 +39,7 @@ namespace vt {
 
 constexpr int kPfRows = 128, kPfKeys = 128;  // rows of a tile, keys of a block
 constexpr int kPfThreads = 384;
-constexpr int kPfCopyWarps = 3;
+constexpr int kPfCopyWarps = 2, kPfMma = 8 + kPfCopyWarps;  // then one MMA warp a tile
 // registers a thread: at launch 65536 / 384, rounded down to 8; then 2 x 128 threads of softmax and 128 of
 // copies and MMAs
 constexpr int kPfLaunchRegs = 168, kPfSoftmaxRegs = 208, kPfCopyRegs = 88;
@@ -142,6 +143,15 @@ __device__ __forceinline__ bool pf_wait(uint64_t* bar, uint32_t parity) {
     if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity) ? 1 : 0;
     return __shfl_sync(0xffffffffu, ok, 0) != 0;
 }
+// Two at once: their tests overlap.
+__device__ __forceinline__ bool pf_wait2(uint64_t* bar0, uint32_t parity0, uint64_t* bar1, uint32_t parity1) {
+#pragma unroll 1
+    for (int i = 0; i < kPfTests; ++i) {
+        const bool p = fa_test(bar0, parity0), q = fa_test(bar1, parity1);
+        if (__all_sync(0xffffffffu, p && q)) return true;
+    }
+    return pf_wait(bar0, parity0) && pf_wait(bar1, parity1);
+}
 __device__ __forceinline__ void pf_zero_row(const PagedAttnArgs& a, int row, int words, int lane) {
     for (int e = lane; e < words; e += 32) reinterpret_cast<uint4*>(a.out + row * a.out_ld)[e] = make_uint4(0u, 0u, 0u, 0u);
 }
@@ -171,10 +181,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
     uint64_t* q_empty = q_full + 1;
     uint64_t* s_full = q_empty + 1;          // [2] S_x is there (and O_x holds every earlier block)
     uint64_t* p_full = s_full + 2;           // [2][2] halves of P_x, 64 keys each
-    uint64_t* o_full = p_full + 4;           // [2] the unit's last block is in O_x
+    uint64_t* pv_done = p_full + 4;          // [2] one more block is in O_x, and P_x has been read
+    uint64_t* o_full = pv_done + 2;          // [2] the unit's last block is in O_x
     uint64_t* o_free = o_full + 2;           // [2] O_x has been read
-    uint64_t* done = o_free + 2;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+    uint64_t* done = o_free + 2;             // [2]
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 2);
     volatile int* s_err = reinterpret_cast<volatile int*>(tmem_slot + 1);
     volatile int* s_last = s_err + 1;        // [2]
     int64_t* s_at = reinterpret_cast<int64_t*>(tmem_slot + 4);  // length of the line
@@ -189,25 +200,27 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
     if (tid == 0) {
         for (int s = 0; s < S; ++s) {
             mbar_init(&full[s], kPfCopyWarps);
-            mbar_init(&empty[s], 1);
+            mbar_init(&empty[s], 2);
         }
         mbar_init(q_full, 1);
-        mbar_init(q_empty, 1);
+        mbar_init(q_empty, 2);
         for (int x = 0; x < 2; ++x) {
             mbar_init(&s_full[x], 1);
             mbar_init(&p_full[2 * x], 4);
             mbar_init(&p_full[2 * x + 1], 4);
+            mbar_init(&pv_done[x], 1);
             mbar_init(&o_full[x], 1);
             mbar_init(&o_free[x], 4);
         }
-        mbar_init(done, 1);
+        mbar_init(&done[0], 1);
+        mbar_init(&done[1], 1);
         *s_err = 0;
         *s_largest = 0;
         fence_mbar_init();
     }
     pdl_wait();  // a preceding kernel may hold tensor memory
     pdl_launch_dependents();
-    if (warp == 11) {
+    if (warp == kPfMma) {
         tc::tmem_alloc(tmem_slot, 512);
         tc::tmem_relinquish();
     }
@@ -323,7 +336,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
     const int64_t per = max(paged_div(line + gridDim.x - 1, gridDim.x), (int64_t)least);
     const int64_t t0 = blockIdx.x * per, t1 = min(line, t0 + per);
     if (t0 >= t1) {
-        if (warp == 11) tc::tmem_dealloc(*tmem_slot, 512);
+        if (warp == kPfMma) tc::tmem_dealloc(*tmem_slot, 512);
         return;
     }
     at.seq(a, s_unit[0]);
@@ -340,7 +353,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
 
     if (warp >= 8)  // a whole warpgroup
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPfCopyRegs));
-    if (warp >= 8 && warp < 11) {
+    if (warp >= 8 && warp < kPfMma) {
         // ================================================================ copies
         const int w = warp - 8;
         bool ok = true;
@@ -354,7 +367,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
             return P.tma && lane < pages && p >= at.kbeg && p < at.kend ? page_of(p) : -1;
         };
         // By asynchronous copies: a pass of a warp covers RPI rows, CPR 16-byte chunks each; lane (sub, chunk) copies its
-        // chunk of rows sub, sub + RPI, ... of 8-row group g.  Groups go to the three warps in turn.
+        // chunk of rows sub, sub + RPI, ... of 8-row group g.  Groups go to the copy warps in turn.
         constexpr int CPR = DH / 8, RPI = 32 / CPR, GROUPS = (16 + kPfCopyWarps - 1) / kPfCopyWarps;
         const int chunk = lane % CPR, sub = lane / CPR;
         const uint32_t lane_dst = (uint32_t)((chunk >> 3) * G::kAtom + sub * 128);
@@ -486,6 +499,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
         }
         if (ok) flush();
         asm volatile("cp.async.wait_group 0;" ::: "memory");
+        // nor may the CTA end while a commit that releases a slot is on its way
+        for (int s = 0; ok && s < S; ++s) {
+            const int fills = round + (s < slot ? 1 : 0);
+            if (fills > 0) ok = pf_wait(&empty[s], (fills - 1) & 1);
+        }
         if (!ok) {
             if (lane == 0) {
                 *s_err = 1;
@@ -498,25 +516,25 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
             }
             if (w == 0 && nq > 0) pf_wait(q_full, (nq - 1) & 1);
         }
-    } else if (warp == 11) {
-        // ================================================================ MMAs
+    } else if (warp >= kPfMma) {
+        // ================================================================ MMAs of tile x
         constexpr uint32_t kType = std::is_same<T, __half>::value ? 0u : tc::kIdescBf16;
         constexpr uint32_t idesc_s = tc::idesc_f16(kPfRows, kPfKeys) | kType, idesc_o = tc::idesc_f16_bmn(kPfRows, DH) | kType;
-        const uint32_t qd = tc::desc_sw128_lo(smem_u32(Qs)), kd = tc::desc_sw128_lo(smem_u32(Rs));
+        constexpr uint32_t kStep = G::kTile >> 4;
+        const int x = warp - kPfMma;
+        const uint32_t qd = tc::desc_sw128_lo(smem_u32(Qs + x * G::kTile)), kd = tc::desc_sw128_lo(smem_u32(Rs));
         const uint64_t vd = tc::desc_sw128_mn(smem_u32(Rs), G::kAtom);
         const uint32_t vd_hi = (uint32_t)(vd >> 32), vd_lo = (uint32_t)vd;
-        constexpr uint32_t kStep = G::kTile >> 4;
+        const uint32_t s_tmem = tmem + (uint32_t)(x * kPfKeys), o_tmem = tmem + kOCol + (uint32_t)(x * DH);
         bool ok = true;
-        int slot = 0, par = 0, nq = 0;
-        int np[2] = {0, 0}, no[2] = {0, 0};
+        int slot = 0, par = 0, nq = 0, npv = 0, seen = 0, no = 0;  // npv, seen: products with V issued, and known to be done
         for (int64_t left = t1 - t0; ok && left > 0;) {
-            int n, j0, j1, lo[2], hi[2];
+            int n, j0, j1, lo, hi;
             {
                 PfCursor at = *cursor;
                 j0 = at.kb0 + at.part(left, n);
                 j1 = j0 + n;
-                at.tile(a, tr, 0, j0, j1, lo[0], hi[0]);
-                at.tile(a, tr, 1, j0, j1, lo[1], hi[1]);
+                at.tile(a, tr, x, j0, j1, lo, hi);
                 left -= at.rest();
                 at.next(a, tr);
                 __syncwarp();  // every lane has read the cursor
@@ -527,74 +545,60 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
             ok = pf_wait(q_full, nq & 1);
             ++nq;
             for (int j = j0 - 1; ok && j < j1; ++j) {
-                int vs = 0, ks = 0, kpar = 0;
-                if (j >= j0) {
-                    vs = slot;
-                    ok = pf_wait(&full[vs], par);
-                    if (++slot == S) slot = 0, par ^= 1;
-                }
-                const bool more = j + 1 < j1;
-                if (more) {
-                    ks = slot;
-                    kpar = par;
-                    if (++slot == S) slot = 0, par ^= 1;
-                }
-                bool have_k = false;
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    if (ok && j >= lo[x] && j < hi[x]) {
-                        if (j == lo[x]) {
-                            if (no[x] > 0) ok = pf_wait(&o_free[x], (no[x] - 1) & 1);
-                            ++no[x];
+                if (j >= j0) {  // O_x += P_x . V_j
+                    if (j >= lo && j < hi) {
+                        if (j == lo) {
+                            if (no > 0) ok = pf_wait(&o_free[x], (no - 1) & 1);
+                            ++no;
                         }
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
-                            ok = ok && pf_wait(&p_full[2 * x + half], np[x] & 1);
+                            ok = ok && (half == 0 ? pf_wait2(&full[slot], par, &p_full[2 * x], npv & 1) : pf_wait(&p_full[2 * x + 1], npv & 1));
                             if (!ok) break;
                             tc::fence_after();
-                            if (elect_one())
+                            if (elect_one()) {
 #pragma unroll
                                 for (int kk = 4 * half; kk < 4 * half + 4; ++kk)
-                                    tc::mma_f16_ts(tmem + kOCol + (uint32_t)(x * DH), tmem + (uint32_t)(x * kPfKeys + kk * 8),
-                                                   tc::desc_of(vd_hi, vd_lo + (uint32_t)vs * kStep + (uint32_t)kk * (2048 >> 4)), idesc_o,
-                                                   (j > lo[x] || kk > 0) ? 1u : 0u);
+                                    tc::mma_f16_ts(o_tmem, s_tmem + (uint32_t)(kk * 8),
+                                                   tc::desc_of(vd_hi, vd_lo + (uint32_t)slot * kStep + (uint32_t)kk * (2048 >> 4)), idesc_o,
+                                                   (j > lo || kk > 0) ? 1u : 0u);
+                                if (half == 1) {
+                                    tc::mma_commit(&pv_done[x]);
+                                    if (j == hi - 1) tc::mma_commit(&o_full[x]);
+                                    tc::mma_commit(&empty[slot]);
+                                }
+                            }
                             __syncwarp();
                         }
-                        ++np[x];
-                        if (!ok) break;
-                        if (elect_one()) {
-                            if (j == hi[x] - 1) tc::mma_commit(&o_full[x]);
-                        }
+                        ++npv;
+                    } else {
+                        ok = pf_wait(&full[slot], par);
+                        if (ok && elect_one()) tc::mma_commit(&empty[slot]);
                         __syncwarp();
                     }
-                    if (x == 1 && ok && j >= j0) {
-                        if (elect_one()) tc::mma_commit(&empty[vs]);
-                        __syncwarp();
-                    }
-                    if (ok && more && !have_k) {
-                        ok = pf_wait(&full[ks], kpar);
-                        have_k = true;
-                    }
-                    if (ok && more && j + 1 >= lo[x] && j + 1 < hi[x]) {
-                        tc::fence_after();
-                        if (elect_one()) {
+                    if (++slot == S) slot = 0, par ^= 1;
+                }
+                if (ok && j + 1 < j1) {  // S_x = Q_x . K_{j+1}^T, over P_x: nothing but this wait orders it behind the last product
+                    const bool on = j + 1 >= lo && j + 1 < hi;
+                    ok = on && seen < npv ? pf_wait2(&full[slot], par, &pv_done[x], seen & 1) : pf_wait(&full[slot], par);
+                    if (on) seen = npv;
+                    if (!ok) break;
+                    tc::fence_after();
+                    if (elect_one()) {
+                        if (on) {
 #pragma unroll
                             for (int kk = 0; kk < DH / 16; ++kk) {
                                 const uint32_t off = (uint32_t)(kk >> 2) * (G::kAtom >> 4) + (uint32_t)(kk & 3) * 2;
-                                tc::mma_f16(tmem + (uint32_t)(x * kPfKeys), tc::desc_of(tc::kDescSw128Hi, qd + (uint32_t)x * kStep + off),
-                                            tc::desc_of(tc::kDescSw128Hi, kd + (uint32_t)ks * kStep + off), idesc_s, kk > 0);
+                                tc::mma_f16(s_tmem, tc::desc_of(tc::kDescSw128Hi, qd + off),
+                                            tc::desc_of(tc::kDescSw128Hi, kd + (uint32_t)slot * kStep + off), idesc_s, kk > 0);
                             }
                             tc::mma_commit(&s_full[x]);
                         }
-                        __syncwarp();
-                    }
-                }
-                if (ok && more) {
-                    if (elect_one()) {
-                        tc::mma_commit(&empty[ks]);
+                        tc::mma_commit(&empty[slot]);
                         if (j + 1 == j1 - 1) tc::mma_commit(q_empty);
                     }
                     __syncwarp();
+                    if (++slot == S) slot = 0, par ^= 1;
                 }
                 if (*s_err) ok = false;
             }
@@ -604,9 +608,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
             set_status(c.status, VT_DEV_WAIT_TIMEOUT);
         }
         // tensor memory is freed only after every MMA issued has completed
-        if (elect_one()) tc::mma_commit(done);
+        if (elect_one()) tc::mma_commit(&done[x]);
         __syncwarp();
-        if (!pf_wait(done, 0) && lane == 0) set_status(c.status, VT_DEV_WAIT_TIMEOUT);
+        if (!pf_wait(&done[x], 0) && lane == 0) set_status(c.status, VT_DEV_WAIT_TIMEOUT);
     } else {
         // ================================================================ softmax of tile x
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPfSoftmaxRegs));
@@ -856,7 +860,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
     }
     tc::fence_before();
     __syncthreads();
-    if (warp == 11) {
+    if (warp == kPfMma) {
         tc::fence_after();
         tc::tmem_dealloc(tmem, 512);
     }
