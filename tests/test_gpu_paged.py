@@ -528,3 +528,39 @@ def test_refusals(vtlib, paged):
         vt.make_paged_batch(c.tables, c.lens, c.starts[:2])
     torch.cuda.synchronize()
     assert (out == 7.0).all() and vt.vt_paged_status(paged) == 0
+
+
+def test_serving_example(vtlib):
+    """The example serves five sequences; two layers of fp16 projections and activations leave each sequence's
+    hidden states within 2^-8 of the sequence alone in 64 bits (about ten roundings of 2^-11 a layer)."""
+    from examples.paged_serving import serve
+    err, n = serve()
+    assert n == 5 and err <= 2.0 ** -8, err
+
+
+@pytest.mark.parametrize("window", [0, 37])
+@pytest.mark.parametrize("dtype,d_head,group", [("f16", 128, 4), ("bf16", 64, 1), ("f16", 64, 16), ("bf16", 128, 3)])
+def test_few_rows_beside_many(vtlib, paged, dtype, d_head, group, window):
+    """Sequences of one to a few rows, and one whose rows fill many tiles of the kernel for few."""
+    lens = [(i * 7919) % 300 if i % 7 else -1 for i in range(120)]
+    rows = [1 + i % 3 if i % 5 else 0 for i in range(120)]
+    lens[60], rows[60] = 200, 60
+    c = Cache(vtlib, lens, rows, dtype, 2, d_head, 16, "pos")
+    check_attention(vtlib, paged, c, "prefill", 2 * group, window)
+
+
+@pytest.mark.parametrize("call", ["decode", "prefill"])
+def test_scale_zero_and_large(vtlib, paged, call):
+    """scale 0: every attended value weighs the same; a large scale: the highest score takes everything."""
+    c = Cache(vtlib, [0, 77, 200], [1] * 3 if call == "decode" else [150, 3, 40], "f16", 2, 64, 16)
+    check_attention(vtlib, paged, c, call, 4, scale=0.0)
+    c = Cache(vtlib, [0, 77, 200], [1] * 3 if call == "decode" else [150, 3, 40], "bf16", 2, 64, 16, seed=1)
+    check_attention(vtlib, paged, c, call, 4, scale=16.0)
+
+
+def test_many_sequences_of_one_block(vtlib, paged):
+    """More units than CTAs, most of a single block: the ends of units dominate."""
+    n = 400
+    lens = [(i * 613) % 90 for i in range(n)]
+    rows = [20 + i % 23 for i in range(n)]
+    check_attention(vtlib, paged, Cache(vtlib, lens, rows, "f16", 1, 64, 32), "prefill", 1)
