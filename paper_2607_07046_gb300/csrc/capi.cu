@@ -2408,8 +2408,10 @@ extern "C" vt_status vt_paged_prefill(vt_paged* g, const vt_paged_pool* pool, co
     VT_TRY(paged_attn(g, pool, batch, n_rows, n_heads, q, q_ld, scale, window, out, out_ld, &a));
     if (a.n_rows == 0 || batch->n_seqs == 0) return ok();
     // A few columns (rows times query heads of a group) per sequence: the kernel of single tokens, which streams K and V
-    // once for 16 of them; the tensor cores' tiles take 128.
-    const bool few = (int64_t)n_rows * a.group <= (int64_t)16 * batch->n_seqs;
+    // once for 16 of them; the tensor cores' tiles take 128.  (24 rows of 32 heads behind 300, 16 sequences: 48 us this
+    // way, 67 on the tiles; 32 rows of 20 heads behind 6000, 4 sequences: 81 and 72.)
+    constexpr int kFewColumns = 24;
+    const bool few = (int64_t)n_rows * a.group <= (int64_t)kFewColumns * batch->n_seqs;
     VT_CUDA((few ? launch_paged_decode : launch_paged_prefill)(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
     return ok();
 }
