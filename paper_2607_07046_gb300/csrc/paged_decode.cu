@@ -9,10 +9,11 @@
 // HBM.  The work of a unit (a sequence's KV head and up to 8 NT of its columns) is cut into steps of 16
 // positions; the steps of all units form one line, and CTA c takes its c-th equal part, whatever the
 // sequences' lengths are.  They are known on the device only, so that a captured launch serves any
-// lengths.  A unit counts kPdUnitCost steps more than it has, as its queries and its result take that time.  Inside a CTA step i goes to warp i % 4, each with its own ring of asynchronous 16-byte copies
-// (K and V rows gathered through the page table), so no barrier stands in the stream; 128 KB or more a SM
-// are in flight.  A unit that several CTAs share is joined by the last of them to finish: partial (m, l,
-// o) in a workspace, added in CTA order, so a result does not depend on timing.
+// lengths.  A unit counts kPdUnitCost steps more than it has, as its queries and its result take that time.
+// Inside a CTA step i goes to warp i % 4 (short units: whole units to a warp), each with its own ring of
+// asynchronous 16-byte copies (K and V rows gathered through the page table), so no barrier stands in the
+// stream; 128 KB or more a SM are in flight.  A unit that several CTAs share is joined by the last of them
+// to finish: partial (m, l, o) in a workspace, added in CTA order, so a result does not depend on timing.
 //
 // Products run on mma.sync m16n8k16 (tcgen05 would need 64 or more rows where there are 1 to 16):
 //   S [16 columns x 8 keys] = Q . K^T       A: Q from registers, B: K rows by ldmatrix
@@ -39,6 +40,12 @@ constexpr int kPdUnitCost = 16;
 // split and joined (8 heads of 128 positions: 5.4 us, split 6.7; at 48, units of 20 to 30 steps lost up to 2 us);
 // otherwise kPdMinSteps.
 constexpr int kPdMinSteps = 16, kPdWhole = 28;
+
+// Where the largest unit has no more steps than kPdSoloSteps and there are kPdSoloUnits or more such units for every CTA,
+// each warp has units of its own: merging four warps would cost more than the steps.  Measured, merged and alone: 168
+// sequences of 1 to 3 positions, 32 heads, 38 and 15 us; 1024 sequences of 61 to 65 positions, 8 KV heads, 87 and 56;
+// 24 sequences of 201 to 251, 32 heads, 24 and 22.  At 32 steps 300 sequences of 21 to 501 positions lost (51 to 63).
+constexpr int kPdSoloSteps = 16, kPdSoloUnits = 2;
 
 template <int DH>
 struct PdGeom {
@@ -129,8 +136,8 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
     using G = PdGeom<DH>;
     constexpr int S = G::kStages, CPR = DH / 8, RPI = 32 / CPR;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ int64_t s_sum[kPdWarps], s_before;
-    __shared__ int s_seq, s_last, s_max[kPdWarps];
+    __shared__ int64_t s_sum[kPdWarps], s_before[kPdWarps + 1];
+    __shared__ int s_seq[kPdWarps + 1], s_last, s_max[kPdWarps];
     __shared__ float s_ml[2][kPdWarps][8 * NT];
     __shared__ uint32_t s_mask[kPdWarps][S];
     const PagedView& c = a.c;
@@ -170,7 +177,6 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
         total += s_sum[w];
         largest = max(largest, s_max[w]);
     }
-    largest += kPdUnitCost;
     if (any_idle)  // rows that attend to nothing get zeros
         for (int b = blockIdx.x; b < c.n_seqs; b += gridDim.x) {
             PdSeq s;
@@ -181,36 +187,63 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
                         reinterpret_cast<uint4*>(a.out + r * a.out_ld)[e] = make_uint4(0u, 0u, 0u, 0u);
         }
     const int64_t line = total * c.n_kv_heads;
-    const int64_t per = max(paged_div(line + gridDim.x - 1, gridDim.x), (int64_t)(largest <= kPdWhole ? largest : kPdMinSteps));
-    const int64_t t0 = blockIdx.x * per, t1 = min(line, t0 + per);
+    const bool solo = largest <= kPdSoloSteps && line >= (int64_t)kPdSoloUnits * gridDim.x * (largest + kPdUnitCost);
+    const int64_t per = max(paged_div(line + gridDim.x - 1, gridDim.x),
+                            (int64_t)(largest + kPdUnitCost <= kPdWhole ? largest + kPdUnitCost : kPdMinSteps));
+    int64_t t0 = blockIdx.x * per, t1 = min(line, t0 + per);
     if (t0 >= t1) return;
-    const int64_t at_head = paged_div(t0, c.n_kv_heads);
-    if (upto - mine <= at_head && at_head < upto) {  // the thread whose sequences hold t0
-        int64_t before = upto - mine;
-        int b = tid * ch;
-        for (;; ++b) {
-            PdSeq s;
-            s.open<ROWS>(a, b, COLS);
-            if (at_head < before + s.cost()) break;
-            before += s.cost();
+    // the sequences that hold t0 and, for warps with units of their own, the beginnings of their parts and the last one's end
+    const int64_t per_warp = solo ? paged_div(t1 - t0 + kPdWarps - 1, kPdWarps) : 0;
+    for (int k = 0; k <= (solo ? kPdWarps : 0); ++k) {
+        const int64_t head = paged_div(min(t1, t0 + k * per_warp), c.n_kv_heads);
+        if (upto - mine <= head && head < upto) {  // the thread whose sequences hold it
+            int64_t before = upto - mine;
+            int b = tid * ch;
+            for (;; ++b) {
+                PdSeq s;
+                s.open<ROWS>(a, b, COLS);
+                if (head < before + s.cost()) break;
+                before += s.cost();
+            }
+            s_seq[k] = b;
+            s_before[k] = before;
         }
-        s_seq = b;
-        s_before = before;
     }
     __syncthreads();
 
-    // ---- the copies.  Step k of the CTA's part (unit costs left out) is warp k % 4's.
-    PdCursor<ROWS, COLS> at;  // of the whole CTA
-    at.open(a, s_seq);
-    {
-        const int64_t r = t0 - s_before * c.n_kv_heads;
+    // ---- the copies.  Step k of the CTA's part (unit costs left out) is warp k % 4's, or each warp has its own part, from
+    // the first unit that begins in it to the first that begins in the next.
+    const int stride = solo ? 1 : kPdWarps;
+    PdCursor<ROWS, COLS> at;  // of the whole CTA, or of the warp
+    if (solo) {
+        auto unit_start = [&](int64_t pos, int k) {  // of the first unit that begins at pos or after it
+            if (pos >= line) return line;
+            PdSeq s;
+            s.open<ROWS>(a, s_seq[k], COLS);
+            const int64_t r = pos - s_before[k] * c.n_kv_heads, cost = s.steps + kPdUnitCost;
+            return pos + (cost - 1 - (r + cost - 1 - paged_div(r + cost - 1, cost) * cost));
+        };
+        const int64_t w0 = unit_start(min(t1, t0 + warp * per_warp), warp);
+        const int64_t w1 = unit_start(min(t1, t0 + (warp + 1) * per_warp), warp + 1);
+        if (w0 >= w1) return;  // (no barrier of the whole CTA follows)
+        at.open(a, s_seq[warp]);
+        const int64_t r = w0 - s_before[warp] * c.n_kv_heads, cost = at.s.steps + kPdUnitCost;
+        at.u = (int)paged_div(r, cost) - 1;  // the unit before it, unless it is the sequence's first
+        at.i = 0;
+        if (at.u < 0) at.u = 0;
+        else at.next(a);
+        t0 = w0;
+        t1 = w1;
+    } else {
+        at.open(a, s_seq[0]);
+        const int64_t r = t0 - s_before[0] * c.n_kv_heads;
         at.u = (int)paged_div(r, at.s.steps + kPdUnitCost);
         at.i = (int)(r - (int64_t)at.u * (at.s.steps + kPdUnitCost));
     }
-    PdCursor<ROWS, COLS> ld = at;  // of this warp's copies: the unit of its next step
-    int64_t ld_now = t0;           // where that unit's part begins in the line
-    int ld_i, ld_n, ld_skip = warp;  // next step of the unit, steps of it here, steps until this warp's next
-    auto ld_unit = [&]() {           // the steps [first, n) of the unit that lie in this part
+    PdCursor<ROWS, COLS> ld = at;               // of this warp's copies: the unit of its next step
+    int64_t ld_now = t0;                        // where that unit's part begins in the line
+    int ld_i, ld_n, ld_skip = solo ? 0 : warp;  // next step of the unit, steps of it here, steps until this warp's next
+    auto ld_unit = [&]() {                      // the steps [first, n) of the unit that lie in this part
         const int first = max(0, ld.i - kPdUnitCost);
         ld_n = (int)min((int64_t)ld.s.steps, t1 - ld_now + ld.i - kPdUnitCost);
         ld_i = first;
@@ -262,7 +295,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
                 cp_async16(d, a.kpool + src, o >= 0);
                 cp_async16(d + kPdKeys * G::kRow, a.vpool + src, o >= 0);
             }
-            ld_skip = kPdWarps;
+            ld_skip = stride;
             more = ld_seek();
             look_up();
         }
@@ -273,7 +306,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
     for (int s = 0; s < S - 1; ++s) load_step();
 
     // ---- the steps, unit by unit
-    int st = 0, skip = warp;  // skip: steps until this warp's next
+    int st = 0, skip = solo ? 0 : warp;  // skip: steps until this warp's next
     float* so = reinterpret_cast<float*>(smem + kPdRing);
     for (int64_t now = t0; now < t1;) {
         // steps [i0, i0 + n) of the unit are in this part
@@ -312,7 +345,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
             for (int i = 0; i < DH / 16; ++i) o[i][x][0] = o[i][x][1] = o[i][x][2] = o[i][x][3] = 0.f;
         }
         int k0 = skip;
-        for (; k0 < n; k0 += kPdWarps) {
+        for (; k0 < n; k0 += stride) {
             const int p0 = ROWS ? (at.s.beg / kPdKeys + i0 + k0) * kPdKeys : 0;  // the step's first position
             load_step();
             cp_async_wait<S - 1>();
@@ -387,6 +420,34 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
             st = st + 1 == S ? 0 : st + 1;
         }
         skip = k0 - n;
+
+        if (solo) {  // ---- the unit's end: one warp's (m, l, o)
+            float* ws = so + warp * 8 * DH;
+#pragma unroll
+            for (int x = 0; x < NT; ++x) {
+                l[x] += __shfl_xor_sync(0xffffffffu, l[x], 1);
+                l[x] += __shfl_xor_sync(0xffffffffu, l[x], 2);
+                const float inv = l[x] == 0.f ? 0.f : 1.f / l[x];  // of column g + 8x; o's columns are 2t and 2t + 1
+                const float f[2] = {__shfl_sync(0xffffffffu, inv, 8 * t), __shfl_sync(0xffffffffu, inv, 8 * t + 4)};
+#pragma unroll
+                for (int i = 0; i < DH / 16; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        ws[(2 * t + (e & 1)) * DH + ((16 * i + g + 8 * (e >> 1)) ^ (8 * t))] = o[i][x][e] * f[e & 1];
+                __syncwarp();
+                for (int e = lane; e < 8 * DH / 8; e += 32) {  // 8 dims of a column
+                    const int h = e / (DH / 8), d = (e % (DH / 8)) * 8;
+                    if (8 * x + h >= nc) continue;
+                    const float4* v = reinterpret_cast<const float4*>(ws + h * DH + (d ^ (8 * (h >> 1))));
+                    const float4 v0 = v[0], v1 = v[1];
+                    *reinterpret_cast<uint4*>(a.out + col_at(8 * x + h, a.out_ld) + d) =
+                        make_uint4(E::pack(v0.x, v0.y), E::pack(v0.z, v0.w), E::pack(v1.x, v1.y), E::pack(v1.z, v1.w));
+                }
+                __syncwarp();
+            }
+            at.next(a);
+            continue;
+        }
 
         // ---- the unit's end here: the four warps' (m, l, o) into one
         const bool whole = n == at.s.steps;

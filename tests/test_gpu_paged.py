@@ -564,3 +564,15 @@ def test_many_sequences_of_one_block(vtlib, paged):
     lens = [(i * 613) % 90 for i in range(n)]
     rows = [20 + i % 23 for i in range(n)]
     check_attention(vtlib, paged, Cache(vtlib, lens, rows, "f16", 1, 64, 32), "prefill", 1)
+
+
+@pytest.mark.parametrize("window", [0, 20])
+@pytest.mark.parametrize("call", ["decode", "prefill"])
+@pytest.mark.parametrize("dtype,d_head,group,longest", [("f16", 64, 1, 3), ("bf16", 128, 2, 40), ("f16", 128, 7, 126), ("bf16", 64, 12, 70),
+                                                       ("f16", 128, 1, 200)])
+def test_many_short_sequences(vtlib, paged, call, dtype, d_head, group, longest, window):
+    """Many times more units than the GPU holds, of a few positions each, idle slots among them."""
+    n = 230
+    lens = [(i * 7919) % longest if i % 9 else -1 for i in range(n)]
+    rows = [1 if call == "decode" else (0 if i % 13 == 5 else 1 + (i % 17 == 0) * 2) for i in range(n)]
+    check_attention(vtlib, paged, Cache(vtlib, lens, rows, dtype, 8, d_head, 16, "pos"), call, 8 * group, window)
