@@ -51,6 +51,10 @@ constexpr int kPfUnitCost = 2;
 // What a CTA takes at least: where the largest unit costs no more than kPfWhole, that much, so that none is split and
 // joined; otherwise kPfMinBlocks.
 constexpr int kPfMinBlocks = 4, kPfWhole = 8;
+// Units of this many parts or more on average are joined by a kernel of its own.  Measured, by the last CTA and by a
+// kernel: 38 parts 63 and 47 us (32 rows behind 30000, 2 sequences of 2 KV heads), 9 parts 35 and 26, 5 parts 38 and 40,
+// 2 parts 156 and 162.
+constexpr int kPfJoinParts = 5;
 constexpr int kPfLag = 2;        // copy groups in flight behind the one just issued
 
 template <int DH>
@@ -156,14 +160,25 @@ __device__ __forceinline__ void pf_zero_row(const PagedAttnArgs& a, int row, int
     for (int e = lane; e < words; e += 32) reinterpret_cast<uint4*>(a.out + row * a.out_ld)[e] = make_uint4(0u, 0u, 0u, 0u);
 }
 
+// A unit that several CTAs share: the first of them leaves this, all of them their parts.
+struct PfSplit {
+    int parts, kvh, row0, tokens;  // parts 0: none begins in the CTA; of both tiles
+};
+__device__ __forceinline__ float* pf_slot(const PagedAttnArgs& a, int cta, int first, int x) {
+    return a.work + (int64_t)(4 * cta + (cta == first ? 2 : 0) + x) * kPagedPrefillSlot;
+}
+
 struct PfParams {
     PagedAttnArgs a;
+    PfSplit* split;       // [CTAs]
     int tma;              // blocks that are whole come by tensor copies
     CUtensorMap tq;       // [rows][heads][dh], boxes of a tile's rows by 64 columns
     CUtensorMap tk, tv;   // [pages][KV heads][positions][dh], boxes of a page's positions (128 at most) by 64 columns
 };
 
-template <class T, int DH>
+// JOIN: the parts of units that several CTAs share are left to k_paged_join; otherwise the last of a unit's CTAs to finish
+// joins them.
+template <class T, int DH, bool JOIN>
 __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_constant__ PfParams P) {
     const PagedAttnArgs& a = P.a;
     using E = Elem<T>;
@@ -220,6 +235,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
     }
     pdl_wait();  // a preceding kernel may hold tensor memory
     pdl_launch_dependents();
+    if (JOIN && tid == 0) P.split[blockIdx.x].parts = 0;
     if (warp == kPfMma) {
         tc::tmem_alloc(tmem_slot, 512);
         tc::tmem_relinquish();
@@ -765,10 +781,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                 // a part: (m, l) and O by four columns, all rows side by side
                 const int64_t u0 = t1 - left - at.i + kPfUnitCost;  // where the unit's blocks begin in the line
                 const int first = (int)paged_div(u0, per), last = (int)paged_div(u0 + at.n - 1, per);
-                auto slot_of = [&](int cta) { return a.work + (int64_t)(4 * cta + (cta == first ? 2 : 0) + x) * kPagedPrefillSlot; };
-                float* part = slot_of((int)blockIdx.x);
-                reinterpret_cast<float2*>(part)[row] = make_float2(m_use, l);
-                if (any) {
+                float* part = pf_slot(a, (int)blockIdx.x, first, x);
+                reinterpret_cast<float2*>(part)[row] = ok ? make_float2(m_use, l) : make_float2(-INFINITY, 0.f);
+                if (any && ok) {
                     uint32_t o[DH / 32][32];
 #pragma unroll
                     for (int q = 0; q < DH / 32; ++q) tc::tmem_ld32(o_at_col + 32 * q, o[q]);
@@ -782,69 +797,74 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                                 reinterpret_cast<uint4*>(part + 2 * kPfRows)[(8 * q + u) * kPfRows + row] =
                                     make_uint4(o[q][4 * u], o[q][4 * u + 1], o[q][4 * u + 2], o[q][4 * u + 3]);
                 }
-                __threadfence();
-                consumer_bar(1 + x, 128);
-                if (row == 0) {
-                    const int mine = atomicAdd(&a.arrived[2 * first + x], 1);
-                    s_last[x] = mine == last - first;
-                    if (mine == last - first) a.arrived[2 * first + x] = 0;  // ready for the next call
-                }
-                consumer_bar(1 + x, 128);
-                if (s_last[x] && live && ok) {  // the last to get here joins the parts, in CTA order
+                if (JOIN) {
+                    if (tid == 0 && first == (int)blockIdx.x)
+                        P.split[first] = {last - first + 1, at.kvh, at.row0 + 2 * at.pt * tr, min(2 * tr, at.rows - 2 * at.pt * tr)};
+                } else {
                     __threadfence();
-                    float mm = -INFINITY, ll = 0.f, ref = 0.f;
-                    for (int p0 = first; p0 <= last; p0 += 4) {
-                        float2 ml[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) ml[k] = __ldcg(reinterpret_cast<const float2*>(slot_of(min(p0 + k, last))) + row);
-                        float mn = mm;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) mn = fmaxf(mn, ml[k].x);
-                        ref = mn == -INFINITY ? 0.f : mn;
-                        ll *= fa_ex2(mm - ref);
-                        mm = mn;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (p0 + k <= last) ll += ml[k].y * fa_ex2(ml[k].x - ref);
+                    consumer_bar(1 + x, 128);
+                    if (row == 0) {
+                        const int mine = atomicAdd(&a.arrived[2 * first + x], 1);
+                        s_last[x] = mine == last - first;
+                        if (mine == last - first) a.arrived[2 * first + x] = 0;  // ready for the next call
                     }
-                    const float inv = ll == 0.f ? 0.f : 1.f / ll;
-#pragma unroll 1
-                    for (int q = 0; q < DH / 32; ++q) {
-                        float o[32];
+                    consumer_bar(1 + x, 128);
+                    if (s_last[x] && live && ok) {  // the last to get here joins the parts, in CTA order
+                        __threadfence();
+                        float mm = -INFINITY, ll = 0.f, ref = 0.f;
+                        for (int p0 = first; p0 <= last; p0 += 4) {
+                            float2 ml[4];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = 0.f;
-#pragma unroll 1
-                        for (int p0 = first; p0 <= last; p0 += 4) {  // four parts' loads in flight
-                            float4 v[4][8];
-                            float f[4];
+                            for (int k = 0; k < 4; ++k) ml[k] = __ldcg(reinterpret_cast<const float2*>(pf_slot(a, min(p0 + k, last), first, x)) + row);
+                            float mn = mm;
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const float* src = slot_of(min(p0 + k, last));
-                                const float2 ml = __ldcg(reinterpret_cast<const float2*>(src) + row);
-                                f[k] = p0 + k <= last && ml.y != 0.f ? fa_ex2(ml.x - ref) * inv : 0.f;
-#pragma unroll
-                                for (int u = 0; u < 8; ++u)
-                                    v[k][u] = __ldcg(reinterpret_cast<const float4*>(src + 2 * kPfRows) + (8 * q + u) * kPfRows + row);
-                            }
+                            for (int k = 0; k < 4; ++k) mn = fmaxf(mn, ml[k].x);
+                            ref = mn == -INFINITY ? 0.f : mn;
+                            ll *= fa_ex2(mm - ref);
+                            mm = mn;
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
-                                if (f[k] != 0.f)  // else nothing attended to there, and nothing stored
-#pragma unroll
-                                    for (int u = 0; u < 8; ++u) {
-                                        o[4 * u] += f[k] * v[k][u].x;
-                                        o[4 * u + 1] += f[k] * v[k][u].y;
-                                        o[4 * u + 2] += f[k] * v[k][u].z;
-                                        o[4 * u + 3] += f[k] * v[k][u].w;
-                                    }
+                                if (p0 + k <= last) ll += ml[k].y * fa_ex2(ml[k].x - ref);
                         }
+                        const float inv = ll == 0.f ? 0.f : 1.f / ll;
+#pragma unroll 1
+                        for (int q = 0; q < DH / 32; ++q) {
+                            float o[32];
 #pragma unroll
-                        for (int u = 0; u < 4; ++u)
-                            reinterpret_cast<uint4*>(dst)[4 * q + u] =
-                                make_uint4(E::pack(o[8 * u], o[8 * u + 1]), E::pack(o[8 * u + 2], o[8 * u + 3]),
-                                           E::pack(o[8 * u + 4], o[8 * u + 5]), E::pack(o[8 * u + 6], o[8 * u + 7]));
+                            for (int e = 0; e < 32; ++e) o[e] = 0.f;
+#pragma unroll 1
+                            for (int p0 = first; p0 <= last; p0 += 4) {  // four parts' loads in flight
+                                float4 v[4][8];
+                                float f[4];
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) {
+                                    const float* src = pf_slot(a, min(p0 + k, last), first, x);
+                                    const float2 ml = __ldcg(reinterpret_cast<const float2*>(src) + row);
+                                    f[k] = p0 + k <= last && ml.y != 0.f ? fa_ex2(ml.x - ref) * inv : 0.f;
+#pragma unroll
+                                    for (int u = 0; u < 8; ++u)
+                                        v[k][u] = __ldcg(reinterpret_cast<const float4*>(src + 2 * kPfRows) + (8 * q + u) * kPfRows + row);
+                                }
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    if (f[k] != 0.f)  // else nothing attended to there, and nothing stored
+#pragma unroll
+                                        for (int u = 0; u < 8; ++u) {
+                                            o[4 * u] += f[k] * v[k][u].x;
+                                            o[4 * u + 1] += f[k] * v[k][u].y;
+                                            o[4 * u + 2] += f[k] * v[k][u].z;
+                                            o[4 * u + 3] += f[k] * v[k][u].w;
+                                        }
+                            }
+#pragma unroll
+                            for (int u = 0; u < 4; ++u)
+                                reinterpret_cast<uint4*>(dst)[4 * q + u] =
+                                    make_uint4(E::pack(o[8 * u], o[8 * u + 1]), E::pack(o[8 * u + 2], o[8 * u + 3]),
+                                               E::pack(o[8 * u + 4], o[8 * u + 5]), E::pack(o[8 * u + 6], o[8 * u + 7]));
+                        }
                     }
+                    consumer_bar(1 + x, 128);  // s_last is free
                 }
-                consumer_bar(1 + x, 128);  // s_last is free
             }
             if (any) {
                 tc::fence_before();
@@ -866,9 +886,71 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
     }
 }
 
+// The units that several CTAs share: out = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) l_p over the parts in CTA order,
+// so a result does not depend on timing.  All CTAs take the items (unit, tile, 16 dims) in turn; a thread has 8 dims of
+// a row.  Bytes of the parts bound it, which lie in the L2.
+struct PfJoin {
+    PagedAttnArgs a;
+    const PfSplit* split;
+    int ctas;  // of the attention kernel
+};
+constexpr int kPfJoinThreads = 256;
+template <class T, int DH>
+__global__ void __launch_bounds__(kPfJoinThreads) k_paged_join(const __grid_constant__ PfJoin J) {
+    using E = Elem<T>;
+    const PagedAttnArgs& a = J.a;
+    constexpr int ITEMS = 2 * (DH / 16);  // of a unit
+    __shared__ int s_unit[kPagedMaxGrid / 2], s_n;
+    const int tid = threadIdx.x, tr = kPfRows / a.group;
+    pdl_wait();
+    pdl_launch_dependents();
+    if (tid < 32) {  // the units, in order
+        int n = 0;
+        for (int c0 = 0; c0 < J.ctas; c0 += 32) {
+            const bool on = c0 + tid < J.ctas && __ldcg(&J.split[c0 + tid].parts) > 0;
+            const unsigned m = __ballot_sync(0xffffffffu, on);
+            if (on) s_unit[n + __popc(m & ((1u << tid) - 1u))] = c0 + tid;
+            n += __popc(m);
+        }
+        if (tid == 0) s_n = n;
+    }
+    __syncthreads();
+    const int row = tid & (kPfRows - 1);
+    for (int e = blockIdx.x; e < s_n * ITEMS; e += gridDim.x) {
+        const int first = s_unit[e / ITEMS], x = e % ITEMS / (ITEMS / 2), g = (e % (ITEMS / 2)) * 2 + tid / kPfRows;
+        const int4 d = __ldcg(reinterpret_cast<const int4*>(J.split + first));
+        const PfSplit u = {d.x, d.y, d.z, d.w};
+        const int tok = x * tr + row / a.group;
+        if (row >= tr * a.group || tok >= u.tokens) continue;
+        auto ml_of = [&](int p) { return __ldcg(reinterpret_cast<const float2*>(pf_slot(a, first + p, first, x)) + row); };
+        float mm = -INFINITY, ll = 0.f;
+#pragma unroll 8
+        for (int p = 0; p < u.parts; ++p) mm = fmaxf(mm, ml_of(p).x);
+        const float ref = mm == -INFINITY ? 0.f : mm;
+        float o[8] = {};
+#pragma unroll 4
+        for (int p = 0; p < u.parts; ++p) {
+            const float2 ml = ml_of(p);
+            const float4* src = reinterpret_cast<const float4*>(pf_slot(a, first + p, first, x) + 2 * kPfRows) + 2 * g * kPfRows + row;
+            const float4 v0 = __ldcg(src), v1 = __ldcg(src + kPfRows);
+            const float f = fa_ex2(ml.x - ref);
+            ll += ml.y * f;
+            if (ml.y != 0.f) {  // else nothing attended to there, and nothing stored
+                o[0] += f * v0.x, o[1] += f * v0.y, o[2] += f * v0.z, o[3] += f * v0.w;
+                o[4] += f * v1.x, o[5] += f * v1.y, o[6] += f * v1.z, o[7] += f * v1.w;
+            }
+        }
+        const float inv = ll == 0.f ? 0.f : 1.f / ll;
+        uint16_t* dst = a.out + (int64_t)(u.row0 + tok) * a.out_ld + (int64_t)(u.kvh * a.group + row % a.group) * DH + 8 * g;
+        *reinterpret_cast<uint4*>(dst) = make_uint4(E::pack(o[0] * inv, o[1] * inv), E::pack(o[2] * inv, o[3] * inv),
+                                                    E::pack(o[4] * inv, o[5] * inv), E::pack(o[6] * inv, o[7] * inv));
+    }
+}
+
 // Workspace of both attention kernels.
+static size_t part_floats() { return (size_t)(4 * g_num_sms * kPagedPrefillSlot); }
 size_t paged_work_floats() {
-    return (size_t)std::max(2 * kPagedMaxGrid * kPagedDecodeSlot, 4 * g_num_sms * kPagedPrefillSlot);
+    return std::max((size_t)(2 * kPagedMaxGrid * kPagedDecodeSlot), part_floats() + kPagedMaxGrid / 2 * sizeof(PfSplit) / sizeof(float));
 }
 
 template <class T, int DH>
@@ -880,6 +962,9 @@ static cudaError_t prefill_dh(const PagedAttnArgs& a, cudaStream_t st) {
     const int64_t grid = std::min<int64_t>(std::min(kPagedMaxGrid / 2, g_num_sms), (most + kPfMinBlocks - 1) / kPfMinBlocks);
     PfParams P{};
     P.a = a;
+    // Where a long unit has many parts, joining them by one CTA takes longer than a second kernel, in which all SMs join.
+    const bool join = pairs * a.c.n_kv_heads * kPfJoinParts <= grid && span / kPfKeys + 2 + kPfUnitCost > kPfWhole;
+    P.split = reinterpret_cast<PfSplit*>(a.work + part_floats());
     const PagedView& c = a.c;
     const bool bf16 = !std::is_same<T, __half>::value;
     const uint64_t qd[3] = {DH, (uint64_t)a.n_heads, (uint64_t)a.n_rows};
@@ -895,7 +980,10 @@ static cudaError_t prefill_dh(const PagedAttnArgs& a, cudaStream_t st) {
         const uint32_t kb[4] = {64, (uint32_t)std::min(c.page_size, kPfKeys), 1, 1};
         P.tma = make_tensor_map(&P.tk, bf16, 4, a.kpool, kd, ks, kb) && make_tensor_map(&P.tv, bf16, 4, a.vpool, kd, ks, kb);
     }
-    return launch_paged_k(k_paged_prefill<T, DH>, (unsigned)grid, kPfThreads, PfGeom<DH>::kSmem, st, P);
+    if (!join) return launch_paged_k(k_paged_prefill<T, DH, false>, (unsigned)grid, kPfThreads, PfGeom<DH>::kSmem, st, P);
+    const cudaError_t e = launch_paged_k(k_paged_prefill<T, DH, true>, (unsigned)grid, kPfThreads, PfGeom<DH>::kSmem, st, P);
+    if (e != cudaSuccess) return e;
+    return launch_paged_k(k_paged_join<T, DH>, (unsigned)(2 * g_num_sms), kPfJoinThreads, 0, st, PfJoin{a, P.split, (int)grid});
 }
 
 cudaError_t launch_paged_prefill(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st) {
@@ -903,17 +991,22 @@ cudaError_t launch_paged_prefill(const PagedAttnArgs& a, int dtype, int dh, cuda
     return dh == 128 ? prefill_dh<__nv_bfloat16, 128>(a, st) : prefill_dh<__nv_bfloat16, 64>(a, st);
 }
 
-template <class T, int DH>
+template <class T, int DH, bool JOIN>
 static cudaError_t init_one() {
     cudaFuncAttributes f;
-    cudaError_t e = cudaFuncGetAttributes(&f, k_paged_prefill<T, DH>);
+    cudaError_t e = cudaFuncGetAttributes(&f, k_paged_prefill<T, DH, JOIN>);
     if (e != cudaSuccess) return e;
     if (f.numRegs != kPfLaunchRegs) return cudaErrorInvalidConfiguration;  // the register split needs exactly these
-    return cudaFuncSetAttribute(k_paged_prefill<T, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PfGeom<DH>::kSmem);
+    return cudaFuncSetAttribute(k_paged_prefill<T, DH, JOIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PfGeom<DH>::kSmem);
+}
+template <class T, int DH>
+static cudaError_t init_both() {
+    const cudaError_t e = init_one<T, DH, false>();
+    return e != cudaSuccess ? e : init_one<T, DH, true>();
 }
 cudaError_t init_paged_prefill() {
-    const cudaError_t e[4] = {init_one<__half, 64>(), init_one<__half, 128>(), init_one<__nv_bfloat16, 64>(),
-                              init_one<__nv_bfloat16, 128>()};
+    const cudaError_t e[4] = {init_both<__half, 64>(), init_both<__half, 128>(), init_both<__nv_bfloat16, 64>(),
+                              init_both<__nv_bfloat16, 128>()};
     for (cudaError_t x : e)
         if (x != cudaSuccess) return x;
     return cudaSuccess;

@@ -576,3 +576,11 @@ def test_many_short_sequences(vtlib, paged, call, dtype, d_head, group, longest,
     lens = [(i * 7919) % longest if i % 9 else -1 for i in range(n)]
     rows = [1 if call == "decode" else (0 if i % 13 == 5 else 1 + (i % 17 == 0) * 2) for i in range(n)]
     check_attention(vtlib, paged, Cache(vtlib, lens, rows, dtype, 8, d_head, 16, "pos"), call, 8 * group, window)
+
+
+@pytest.mark.parametrize("dtype,d_head,kv_heads,group,window,rows", [
+    ("f16", 64, 1, 5, 0, 77), ("bf16", 128, 2, 1, 3000, 129), ("f16", 128, 1, 128, 0, 9), ("bf16", 64, 3, 8, 6100, 33)])
+def test_prefill_of_many_parts(vtlib, paged, dtype, d_head, kv_heads, group, window, rows):
+    """A few long units, each shared by many SMs; a sequence with nothing to join and an idle one beside them."""
+    c = Cache(vtlib, [9999, 0, -1, 12345], [rows, 2, 5, 40], dtype, kv_heads, d_head, 32)
+    check_attention(vtlib, paged, c, "prefill", kv_heads * group, window)
