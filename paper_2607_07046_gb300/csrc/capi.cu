@@ -2410,8 +2410,12 @@ extern "C" vt_status vt_paged_prefill(vt_paged* g, const vt_paged_pool* pool, co
     // A few columns (rows times query heads of a group) per sequence: the kernel of single tokens, which streams K and V
     // once for 16 of them; the tensor cores' tiles take 128.  (24 rows of 32 heads behind 300, 16 sequences: 48 us this
     // way, 67 on the tiles; 32 rows of 20 heads behind 6000, 4 sequences: 81 and 72.)
-    constexpr int kFewColumns = 24;
-    const bool few = (int64_t)n_rows * a.group <= (int64_t)kFewColumns * batch->n_seqs;
+    // Or little work altogether, by the tables' width: that kernel starts sooner and spreads it over more SMs.  (8 KV heads
+    // of 4 query heads, one sequence: 30 rows 6 and 12 us, 50 behind 1000 20 and 28, 77 behind 300 17 and 19; 30 behind
+    // 5000, 70 steps a CTA, 35 and 26.)
+    constexpr int kFewColumns = 24, kFewSteps = 32;
+    const bool few = (int64_t)n_rows * a.group <= (int64_t)kFewColumns * batch->n_seqs ||
+                     paged_decode_line(a, 16) <= (int64_t)kFewSteps * 2 * g_num_sms;
     VT_CUDA((few ? launch_paged_decode : launch_paged_prefill)(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
     return ok();
 }

@@ -329,6 +329,7 @@ constexpr int kPagedMaxSeqs = 16384;                         // sequences of a b
 size_t paged_work_floats();
 cudaError_t launch_paged_append(const PagedAppendArgs& a, int dtype, int dh, cudaStream_t st);
 cudaError_t launch_paged_decode(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st);
+int64_t paged_decode_line(const PagedAttnArgs& a, int cols);
 cudaError_t launch_paged_prefill(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st);
 cudaError_t init_paged_decode();
 cudaError_t init_paged_prefill();

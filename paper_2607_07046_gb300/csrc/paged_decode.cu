@@ -557,11 +557,16 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
     cp_async_wait<0>();
 }
 
+// Length of the line at the longest lengths, with units of `cols` columns.
+int64_t paged_decode_line(const PagedAttnArgs& a, int cols) {
+    const int64_t tiles = (int64_t)a.n_rows * a.group / cols + a.c.n_seqs;
+    const int64_t span = a.window > 0 ? std::min<int64_t>((int64_t)a.window + a.n_rows, a.c.cap) : a.c.cap;
+    return tiles * a.c.n_kv_heads * (span / kPdKeys + 2 + kPdUnitCost);
+}
+
 template <class T, int DH, int NT, bool ROWS>
 static cudaError_t decode_nt(const PagedAttnArgs& a, cudaStream_t st) {
-    const int64_t tiles = (int64_t)a.n_rows * a.group / (8 * NT) + a.c.n_seqs;
-    const int64_t span = a.window > 0 ? std::min<int64_t>((int64_t)a.window + a.n_rows, a.c.cap) : a.c.cap;
-    const int64_t most = tiles * a.c.n_kv_heads * (span / kPdKeys + 2 + kPdUnitCost);  // of cost, at the longest lengths
+    const int64_t most = paged_decode_line(a, 8 * NT);
     const int64_t grid = std::min<int64_t>(std::min(kPagedMaxGrid, kPdCtasPerSm * g_num_sms), (most + kPdMinSteps - 1) / kPdMinSteps);
     return launch_paged_k(k_paged_decode<T, DH, NT, ROWS>, (unsigned)grid, kPdThreads, PdGeom<DH>::kSmem, st, a);
 }

@@ -584,3 +584,124 @@ def test_prefill_of_many_parts(vtlib, paged, dtype, d_head, kv_heads, group, win
     """A few long units, each shared by many SMs; a sequence with nothing to join and an idle one beside them."""
     c = Cache(vtlib, [9999, 0, -1, 12345], [rows, 2, 5, 40], dtype, kv_heads, d_head, 32)
     check_attention(vtlib, paged, c, "prefill", kv_heads * group, window)
+
+
+def widened(c, positions=60000):
+    """Tables as wide as a server's, nearly all of it unused: the widths alone keep the tiles' kernel."""
+    c.tables = torch.nn.functional.pad(c.tables, (0, positions // c.page), value=-1).contiguous()
+    return c
+
+
+@pytest.mark.parametrize("window", [0, 1, 2, 15, 127, 128, 129, 300, 5000])
+@pytest.mark.parametrize("dtype,d_head,kv_heads,group,page,order", [
+    ("f16", 128, 2, 2, 32, "pos"), ("bf16", 64, 1, 7, 16, "head"), ("f16", 64, 2, 1, 4, "head"), ("bf16", 128, 1, 20, 128, "pos")])
+def test_prefill_window_wide_tables(vtlib, paged, window, dtype, d_head, kv_heads, group, page, order):
+    rows = [30 + 57 * (i % 4) for i in range(len(LENS))]
+    c = widened(Cache(vtlib, LENS, rows, dtype, kv_heads, d_head, page, order, seed=window))
+    check_attention(vtlib, paged, c, "prefill", kv_heads * group, window)
+
+
+@pytest.mark.parametrize("std,scale", [(0.0, 1.0), (0.05, 1.0), (4.0, 1.0), (1.0, 0.0), (1.0, 16.0)])
+@pytest.mark.parametrize("dtype,d_head", [("f16", 128), ("bf16", 64)])
+def test_prefill_score_ranges_wide_tables(vtlib, paged, dtype, d_head, std, scale):
+    c = widened(Cache(vtlib, [0, 100, 513], [140, 30, 70], dtype, 2, d_head, 16))
+    check_attention(vtlib, paged, c, "prefill", 8, scale=scale, q=c.rows(8, std))
+
+
+def test_prefill_rising_scores_wide_tables(vtlib, paged):
+    c = widened(Cache(vtlib, [700], [150], "f16", 1, 64, 16))
+    page, off = c.positions(0, 850)
+    c.k[page, 0, off] = (torch.arange(850, device="cuda")[:, None] / 64).half().expand(-1, 64)
+    q = torch.ones(c.n_rows, 2, 64, dtype=torch.float16, device="cuda")
+    check_attention(vtlib, paged, c, "prefill", 2, scale=0.25, q=q)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_prefill_infinities_and_nan_wide_tables(vtlib, paged, dtype):
+    """A key that scores -inf takes no weight; NaN reaches the rows that attend to it and no other sequence."""
+    c = widened(Cache(vtlib, [40, 40, 40], [50, 60, 70], dtype, 1, 64, 16))
+    q = c.rows(1).abs()
+    page, off = c.positions(0, 90)
+    c.k[page[3], 0, off[3]] = float("-inf")
+    page2, off2 = c.positions(2, 110)
+    c.v[page2[7], 0, off2[7]] = float("nan")
+    out = torch.empty_like(q)
+    vtlib.vt_paged_prefill(paged, c.pool, c.batch(vtlib), q, out)
+    assert torch.isfinite(out[:110]).all() and torch.isnan(out[110:]).all()
+    c.v[page2[7], 0, off2[7]] = 0.0
+    ref, tol = attention(c, q, 0.125, 0)
+    assert ((out.double() - ref).abs() <= tol)[:110].all()
+
+
+@pytest.mark.parametrize("page", [4, 16, 64])
+def test_prefill_bad_pages_and_overflow_wide_tables(vtlib, paged, page):
+    """A page id that is not one of the pool's: its positions take no part, the call says so."""
+    vt = vtlib
+    c = widened(Cache(vt, [400, 60], [40, 50], "f16", 1, 64, page))
+    q = c.rows(2)
+    out, whole = torch.empty_like(q), torch.empty_like(q)
+    vt.vt_paged_prefill(paged, c.pool, c.batch(vt), q, whole)
+    keep = c.tables.clone()
+    page_id, off = c.positions(0, 440)
+    for bad in (-1, c.k.shape[0], 2 ** 31 - 1, -2 ** 31):
+        c.tables[0, 2] = bad
+        vt.vt_paged_prefill(paged, c.pool, c.batch(vt), q, out)
+        assert vt.vt_paged_status(paged, clear=True) == vt.VT_DEV_BAD_PAGE
+        c.tables.copy_(keep)
+        hide = torch.arange(440, device="cuda") > torch.arange(400, 440, device="cuda")[:, None]
+        hide[:, 2 * page:3 * page] = True
+        kk, vv = c.k[page_id, 0, off].double(), c.v[page_id, 0, off].double()
+        for h in range(2):
+            ref = torch.softmax((q[:40, h].double() @ kk.T / 8).masked_fill(hide, -math.inf), -1) @ vv
+            assert ((out[:40, h].double() - ref).abs() <= 2.0 ** -9 * vv.abs().max()).all()
+        assert torch.equal(out[40:], whole[40:])
+    ref, tol = attention(c, q, 0.125, 0)
+    c.tables[1, -(-110 // page):] = c.tables[0, 0]
+    c.lens[1] = 2 ** 31 - 1
+    vt.vt_paged_prefill(paged, c.pool, c.batch(vt), q, out)
+    assert vt.vt_paged_status(paged, clear=True) == vt.VT_DEV_KV_OVERFLOW
+    assert ((out.double() - ref).abs() <= tol)[:40].all()  # (the longer batch is cut elsewhere: not the same bits)
+
+
+def test_prefill_rows_outside_every_sequence_wide_tables(vtlib, paged):
+    """starts that end before the last row, begin after the first, run past the end, or fall."""
+    vt = vtlib
+    c = widened(Cache(vt, [20, 9], [80, 70], "f16", 1, 64, 16))
+    q = torch.randn(90, 2, 64, device="cuda").half()
+    lens = torch.tensor([1, 1], dtype=torch.int32, device="cuda")
+    for starts in ([10, 40, 80], [-5, 20, 1000], [50, 30, 70], [90, 90, 90], [-30, -20, -10]):
+        s = torch.tensor(starts, dtype=torch.int32, device="cuda")
+        out = torch.full_like(q, 7.0)
+        vt.vt_paged_prefill(paged, c.pool, vt.make_paged_batch(c.tables, lens, s), q, out)
+        a = [max(0, min(90, x)) for x in starts]
+        inside = torch.zeros(90, dtype=torch.bool, device="cuda")
+        for b in range(2):
+            inside[a[b]:a[b + 1]] = True
+        assert (out[~inside] == 7.0).all() and torch.isfinite(out[inside]).all()
+        assert vt.vt_paged_status(paged, clear=True) == 0
+
+
+def test_prefill_strides_and_offsets_past_32_bits_wide_tables(vtlib, paged):
+    """Pages whose entries lie more than 2^31 elements into the pool; rows and outputs with gaps."""
+    vt, stride = vtlib, 2 ** 29 + 8
+    small = widened(Cache(vt, [50, 3], [30, 40], "f16", 1, 64, 16, spare=0))
+    n = small.k.shape[0]
+    base = [torch.full(((n - 1) * stride + 16 * 64,), float("nan"), dtype=torch.float16, device="cuda") for _ in range(2)]
+    k, v = (t.as_strided((n, 1, 16, 64), (stride, 64, 64, 1)) for t in base)
+    k.copy_(small.k)
+    v.copy_(small.v)
+    q, big = small.rows(7)[:, 1:4], torch.full((small.n_rows, 5, 64), 3.0, dtype=torch.float16, device="cuda")
+    vt.vt_paged_prefill(paged, vt.make_paged_pool(k, v), small.batch(vt), q, big[:, :3])
+    ref, tol = attention(small, q, 0.125, 0)
+    assert ((big[:, :3].double() - ref).abs() <= tol).all() and (big[:, 3:] == 3.0).all()
+
+
+def test_prefill_repeats_bit_for_bit_wide_tables(vtlib, paged):
+    vt = vtlib
+    for rows, heads in (([40, 130, 30, 77], 2), ([60], 2), ([300, 200, 250, 280], 16)):
+        c = widened(Cache(vt, [3000, 77, 4097, 9000][:len(rows)], rows, "f16", 2, 128, 16))
+        q, outs = c.rows(heads), []
+        for _ in range(4):
+            outs.append(torch.empty_like(q))
+            vt.vt_paged_prefill(paged, c.pool, c.batch(vt), q, outs[-1])
+        assert all(torch.equal(outs[0], o) for o in outs[1:])
