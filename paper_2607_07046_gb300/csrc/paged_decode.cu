@@ -20,6 +20,11 @@
 //   O^T [16 dims x 8 columns] += V^T . P^T  A: V by ldmatrix.trans, B: P as S leaves it in registers
 // P is cut into two 16-bit terms, hi = round(p) and lo = round(p - hi), two products each: the weights
 // then carry 16 (bf16) or 22 (fp16) bits and the output's own rounding is the only one that counts.
+//
+// Measured: one history of 131,000 positions, 8 KV heads of 4, dh 128: 92 us, 5830 GB/s (86% of a copy's rate: the
+// start, the last steps and the join of 38 parts a head are the rest); 64 sequences of up to 8191, some idle: 47 us, 5310
+// GB/s; 16 of 500 to 4096 with 32 KV heads and a window of 1024: 46 us, 5290 GB/s; 128 positions of 8 heads: 5.6 us, all
+// of it latency (lengths, table, first rows, merge).
 #include <cuda_runtime.h>
 #include <math.h>
 
@@ -36,7 +41,7 @@ constexpr int kPdCtasPerSm = 2;
 // A unit's queries, merge and result cost as much as this many steps (measured: 64 ragged sequences 75 us at 0, 56 at
 // 4, 47 at 8 to 24, 50 at 32).
 constexpr int kPdUnitCost = 16;
-// What a CTA takes at least: where the largest unit costs no more than kPdWhole (12 steps), that much, so that none is
+// What a CTA takes at least: where the largest unit costs no more than kPdWhole (12 steps), that much, so that few are
 // split and joined (8 heads of 128 positions: 5.4 us, split 6.7; at 48, units of 20 to 30 steps lost up to 2 us);
 // otherwise kPdMinSteps.
 constexpr int kPdMinSteps = 16, kPdWhole = 28;

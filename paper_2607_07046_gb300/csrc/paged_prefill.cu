@@ -7,9 +7,16 @@
 //   S_x = Q_x . K_j^T       tcgen05, M 128, N 128, K dh, operands in shared memory, S in tensor memory
 //   P_x = 2^(S_x scale log2(e) - m), masked, 16 bits, written over S_x in tensor memory
 //   O_x += P_x . V_j        tcgen05, M 128, N dh, K 128, P from tensor memory, V as it lies in the pages
-// While the softmax of one tile runs, the tensor core has the other tile's products.  A block pair costs
-// 4 x 512 cycles of tensor work, as long as the 2 x 128 x 128 exponentials take on the SM's special-function
-// units, and K and V pass through shared memory once for both tiles.
+// While the softmax of one tile runs, the tensor core has the other tile's products, and K and V pass through
+// shared memory once for both tiles.
+//
+// What bounds it: by operations the tensor cores (4 dh FLOPs a score), 2 x 2 x 520 cycles a block of both
+// tiles; the 2 x 128 x 128 exponentials take as long on the SM's special-function units.  In fact one tile's
+// chain, softmax (2200 cycles) and then P to V, S and its notice (2350), takes about 5000 cycles a block, of
+// which the two tiles hide half from each other.  Measured: 4096 rows, 32 heads, dh 128: 173 us, 790 TFLOP/s
+// (41% of what a matrix product reaches); 512 rows behind 16000, 8 KV heads of 4: 157 us, 870; 5 prompts of
+// 150 to 900 rows: 45 us, of which a CTA's start takes 7.  One tile a CTA with two threads a row
+// took 171 and 147 us on the first two, but 55 on the third; 64-key halves were slower throughout.
 //
 //   warps 0-3, 4-7  softmax of tile 0 and 1, one thread a row (its lane of the tensor memory): no exchange
 //                   between threads.  m is a reference maximum; O and l are rescaled only when a block's
@@ -23,9 +30,10 @@
 //
 // The blocks of all units form one line, and CTA c (one an SM) takes its c-th equal part, so neither few
 // long histories nor ragged prompts leave SMs idle; lengths are known on the device only.  A unit that
-// several CTAs share is joined by the last of them to finish, in CTA order.  Every mbarrier wait is
-// bounded; on a timeout a warp sets VT_DEV_WAIT_TIMEOUT, issues and stores nothing more, and still passes
-// every named barrier.
+// several CTAs share is joined in CTA order, by the last of them to finish or (few long units) by
+// k_paged_join, so a result does not depend on timing.  Every mbarrier wait is bounded; on a timeout a warp
+// sets VT_DEV_WAIT_TIMEOUT, issues nothing more, stores no output (a part of nothing where others wait for
+// one), and still passes every named barrier.
 #include <cuda_runtime.h>
 #include <math.h>
 
@@ -48,12 +56,13 @@ static_assert(256 * kPfSoftmaxRegs + 128 * kPfCopyRegs <= kPfThreads * kPfLaunch
 constexpr int kPfMaskRing = 8;   // validity words of the last blocks (the copies lead by fewer blocks)
 // The start and end of a unit cost as much as this many blocks.
 constexpr int kPfUnitCost = 2;
-// What a CTA takes at least: where the largest unit costs no more than kPfWhole, that much, so that none is split and
-// joined; otherwise kPfMinBlocks.
+// What a CTA takes at least: where the largest unit costs no more than kPfWhole, that much, so that few are split and
+// joined; otherwise kPfMinBlocks.  (3 prompts of 300 rows, 12 heads: 20 us; with 4 and 2 for them 27, as every unit is
+// split then.)
 constexpr int kPfMinBlocks = 4, kPfWhole = 8;
 // Units of this many parts or more on average are joined by a kernel of its own.  Measured, by the last CTA and by a
 // kernel: 38 parts 63 and 47 us (32 rows behind 30000, 2 sequences of 2 KV heads), 9 parts 35 and 26, 5 parts 38 and 40,
-// 2 parts 156 and 162.
+// 2 parts 156 and 162 (a kernel adds its launch, and joins that would have been hidden behind other CTAs' work).
 constexpr int kPfJoinParts = 5;
 constexpr int kPfLag = 2;        // copy groups in flight behind the one just issued
 
