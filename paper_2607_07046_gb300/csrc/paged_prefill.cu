@@ -13,9 +13,9 @@
 // What bounds it: by operations the tensor cores (4 dh FLOPs a score), 2 x 2 x 520 cycles a block of both
 // tiles; the 2 x 128 x 128 exponentials take as long on the SM's special-function units.  In fact one tile's
 // chain, softmax (2200 cycles) and then P to V, S and its notice (2350), takes about 5000 cycles a block, of
-// which the two tiles hide half from each other.  Measured: 4096 rows, 32 heads, dh 128: 173 us, 790 TFLOP/s
-// (41% of what a matrix product reaches); 512 rows behind 16000, 8 KV heads of 4: 157 us, 870; 5 prompts of
-// 150 to 900 rows: 45 us, of which a CTA's start takes 7.  One tile a CTA with two threads a row
+// which the two tiles hide half from each other.  Measured: 4096 rows, 32 heads, dh 128: 170 us, 810 TFLOP/s
+// (42% of what a matrix product reaches); 512 rows behind 16000, 8 KV heads of 4: 156 us, 870; 5 prompts of
+// 150 to 900 rows: 42 us, of which a CTA's start takes 7.  One tile a CTA with two threads a row
 // took 171 and 147 us on the first two, but 55 on the third; 64-key halves were slower throughout.
 //
 //   warps 0-3, 4-7  softmax of tile 0 and 1, one thread a row (its lane of the tensor memory): no exchange
@@ -54,7 +54,7 @@ constexpr int kPfLaunchRegs = 168, kPfSoftmaxRegs = 208, kPfCopyRegs = 88;
 static_assert(256 * kPfSoftmaxRegs + 128 * kPfCopyRegs <= kPfThreads * kPfLaunchRegs,
               "the register split must fit in the registers the block is launched with");
 constexpr int kPfMaskRing = 8;   // validity words of the last blocks (the copies lead by fewer blocks)
-// The start and end of a unit cost as much as this many blocks.
+// The start and end of a unit cost as much as this many blocks (5 prompts: 46 us at 1, 42 at 2, 44 at 3).
 constexpr int kPfUnitCost = 2;
 // What a CTA takes at least: where the largest unit costs no more than kPfWhole, that much, so that few are split and
 // joined; otherwise kPfMinBlocks.  (3 prompts of 300 rows, 12 heads: 20 us; with 4 and 2 for them 27, as every unit is
@@ -64,6 +64,8 @@ constexpr int kPfMinBlocks = 4, kPfWhole = 8;
 // kernel: 38 parts 63 and 47 us (32 rows behind 30000, 2 sequences of 2 KV heads), 9 parts 35 and 26, 5 parts 38 and 40,
 // 2 parts 156 and 162 (a kernel adds its launch, and joins that would have been hidden behind other CTAs' work).
 constexpr int kPfJoinParts = 5;
+// Parts that the joining CTA reads at once; most units have two (with 4 at once: 45 us for 5 prompts instead of 42).
+constexpr int kPfJoinChunk = 2;
 constexpr int kPfLag = 2;        // copy groups in flight behind the one just issued
 
 template <int DH>
@@ -842,11 +844,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
 #pragma unroll
                             for (int e = 0; e < 32; ++e) o[e] = 0.f;
 #pragma unroll 1
-                            for (int p0 = first; p0 <= last; p0 += 4) {  // four parts' loads in flight
-                                float4 v[4][8];
-                                float f[4];
+                            for (int p0 = first; p0 <= last; p0 += kPfJoinChunk) {
+                                float4 v[kPfJoinChunk][8];
+                                float f[kPfJoinChunk];
 #pragma unroll
-                                for (int k = 0; k < 4; ++k) {
+                                for (int k = 0; k < kPfJoinChunk; ++k) {
                                     const float* src = pf_slot(a, min(p0 + k, last), first, x);
                                     const float2 ml = __ldcg(reinterpret_cast<const float2*>(src) + row);
                                     f[k] = p0 + k <= last && ml.y != 0.f ? fa_ex2(ml.x - ref) * inv : 0.f;
@@ -855,7 +857,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                                         v[k][u] = __ldcg(reinterpret_cast<const float4*>(src + 2 * kPfRows) + (8 * q + u) * kPfRows + row);
                                 }
 #pragma unroll
-                                for (int k = 0; k < 4; ++k)
+                                for (int k = 0; k < kPfJoinChunk; ++k)
                                     if (f[k] != 0.f)  // else nothing attended to there, and nothing stored
 #pragma unroll
                                         for (int u = 0; u < 8; ++u) {
