@@ -705,3 +705,28 @@ def test_prefill_repeats_bit_for_bit_wide_tables(vtlib, paged):
             outs.append(torch.empty_like(q))
             vt.vt_paged_prefill(paged, c.pool, c.batch(vt), q, outs[-1])
         assert all(torch.equal(outs[0], o) for o in outs[1:])
+
+
+def test_prefill_of_many_parts_in_a_graph(vtlib, paged):
+    """A captured call serves other lengths: parts of few long units, then no parts at all, then idle slots."""
+    vt = vtlib
+    c = Cache(vt, [9000, 5000], [60, 70], "f16", 2, 128, 64)
+    q = c.rows(4)
+    out = torch.empty_like(q)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        vt.vt_paged_prefill(paged, c.pool, c.batch(vt), q, out)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        batch = c.batch(vt)
+        with torch.cuda.graph(graph, stream=stream):
+            vt.vt_paged_prefill(paged, c.pool, batch, q, out)
+        for lens in ([9000, 5000], [40, 3], [-1, 5000], [8999, -1], [-1, -1], [9000, 5000]):
+            c.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+            c.lens_host = lens
+            out.fill_(7.0)
+            graph.replay()
+            stream.synchronize()
+            ref, tol = attention(c, q, 128 ** -0.5, 0)
+            assert ((out.double() - ref).abs() <= tol).all(), lens
+    assert vt.vt_paged_status(paged) == 0
