@@ -372,6 +372,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
     at.unit(a, tr);
     at.i = s_unit[3];
     if (lane == 0) *cursor = at;
+    fence_proxy_async_smem();  // tot was written and read as threads do; the copy engine writes Q and the ring over it
     tc::fence_before();
     __syncthreads();
     tc::fence_after();

@@ -1,0 +1,21 @@
+"""Orderings in the tiles' kernel of the paged prefill that no run shows (no GPU): read off its source.
+
+A missing one is a race whose outcome hardware decides, so the source itself is what can be checked: the fence
+or barrier stands between the two accesses that it orders."""
+from __future__ import annotations
+
+import re
+from pathlib import Path
+
+SOURCE = (Path(__file__).resolve().parents[1] / "paper_2607_07046_gb300" / "csrc" / "paged_prefill.cu").read_text()
+CODE = re.sub(r"//[^\n]*", "", SOURCE)
+KERNEL = CODE[CODE.index("k_paged_prefill(const __grid_constant__"):CODE.index("struct PfJoin")]
+
+
+def test_plain_stores_over_the_ring_are_fenced_before_tensor_copies():
+    """The blocks of each sequence lie in the memory of Q and the ring: written and read as threads do, then
+    written by the copy engine.  Every thread needs a proxy fence before the barrier that lets the copies begin."""
+    assert "reinterpret_cast<int64_t*>(smem)" in KERNEL and "uint8_t* Qs = smem" in KERNEL
+    between = KERNEL[KERNEL.rindex("tot["):KERNEL.index("const int w = warp - 8")]
+    fence = between.rindex("fence_proxy_async_smem()")
+    assert "__syncthreads()" in between[fence:]
