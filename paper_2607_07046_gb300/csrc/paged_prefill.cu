@@ -430,6 +430,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                 int64_t off[GROUPS];  // asynchronous copies: the lane's element in the first row of each group; -1: bad page
                 if (clean) {
                     if (w == 0 && lane < 4) valid[(blk % kPfMaskRing) * 4 + lane] = 0xffffffffu;
+                    __syncwarp();  // the words are stored before the elected lane arrives
                     flush();
                 } else {
                     if (w == 0)

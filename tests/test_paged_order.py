@@ -19,3 +19,11 @@ def test_plain_stores_over_the_ring_are_fenced_before_tensor_copies():
     between = KERNEL[KERNEL.rindex("tot["):KERNEL.index("const int w = warp - 8")]
     fence = between.rindex("fence_proxy_async_smem()")
     assert "__syncthreads()" in between[fence:]
+
+
+def test_a_clean_blocks_mask_is_stored_before_its_arrival():
+    """Lanes 0 to 3 store the validity words and one elected lane arrives: votes and shuffles order no memory."""
+    clean = KERNEL[KERNEL.index("= 0xffffffffu"):KERNEL.index("tma_load_4d")]
+    store, arrive = 0, clean.index("mbar_arrive_expect_tx(&full")
+    before_branch = clean[store:clean.index("else {")]
+    assert "__syncwarp()" in before_branch or "__syncwarp()" in clean[clean.index("if (clean)"):arrive]
