@@ -156,7 +156,9 @@ __device__ __forceinline__ bool pf_wait(uint64_t* bar, uint32_t parity) {
         if (__all_sync(0xffffffffu, fa_test(bar, parity))) return true;
     int ok = 1;
     if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity) ? 1 : 0;
-    return __shfl_sync(0xffffffffu, ok, 0) != 0;
+    ok = __shfl_sync(0xffffffffu, ok, 0);
+    __syncwarp();  // what the one lane acquired holds for all of them (a shuffle orders no memory)
+    return ok != 0;
 }
 // Two at once: their tests overlap.
 __device__ __forceinline__ bool pf_wait2(uint64_t* bar0, uint32_t parity0, uint64_t* bar1, uint32_t parity1) {

@@ -27,3 +27,10 @@ def test_a_clean_blocks_mask_is_stored_before_its_arrival():
     store, arrive = 0, clean.index("mbar_arrive_expect_tx(&full")
     before_branch = clean[store:clean.index("else {")]
     assert "__syncwarp()" in before_branch or "__syncwarp()" in clean[clean.index("if (clean)"):arrive]
+
+
+def test_a_bounded_wait_of_one_lane_is_passed_on_in_order():
+    """One lane acquires the phase; the others read what it announces only behind a barrier of the warp."""
+    body = CODE[CODE.index("bool pf_wait(uint64_t* bar"):]
+    body = body[:body.index("\n}\n")]
+    assert "__syncwarp()" in body[body.index("mbar_wait(bar, parity)"):]
