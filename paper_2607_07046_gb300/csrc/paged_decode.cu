@@ -269,21 +269,19 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
     ld_unit();
     bool more = ld_seek();
     const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * S * G::kStage);
-    int page = -1;  // lane r < 16: the page of row r of the next step to load (-1: not attended to)
+    int page = 0;         // lane r < 16: the table's entry for row r of the next step to load, whatever it holds;
+    bool needed = false;  // whether that row is attended to is known apart from it
     auto look_up = [&]() {
-        page = -1;
-        if (more && lane < kPdKeys) {
-            const int p = (ld.s.beg / kPdKeys + ld_i) * kPdKeys + lane;
-            if (p >= ld.s.beg && p < ld.s.end) page = c.tables[(int64_t)ld.b * c.per_seq + (p >> c.page_shift)];
-            else page = -2;
-        }
+        const int p = more ? (ld.s.beg / kPdKeys + ld_i) * kPdKeys + lane : -1;
+        needed = more && lane < kPdKeys && p >= ld.s.beg && p < ld.s.end;
+        if (needed) page = c.tables[(int64_t)ld.b * c.per_seq + (p >> c.page_shift)];
     };
     look_up();
     int st_load = 0;
     auto load_step = [&]() {
         if (more) {
-            const bool on = lane < kPdKeys && (unsigned)page < (unsigned)c.n_pages;
-            if (lane < kPdKeys && !on && page != -2) set_status(c.status, VT_DEV_BAD_PAGE);
+            const bool on = needed && (unsigned)page < (unsigned)c.n_pages;
+            if (needed && !on) set_status(c.status, VT_DEV_BAD_PAGE);
             const int p = (ld.s.beg / kPdKeys + ld_i) * kPdKeys + lane;
             const int64_t off = on ? page * c.page_stride + (ld.u / ld.s.tiles) * c.head_stride + (p & (c.page_size - 1)) * c.pos_stride
                                    : -1;
