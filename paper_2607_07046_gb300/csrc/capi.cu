@@ -2298,6 +2298,7 @@ vt_status paged_view(const vt_paged* g, const vt_paged_pool* p, const vt_paged_b
     c->tables = b->tables;
     c->per_seq = b->pages_per_seq;
     c->cap = b->pages_per_seq * p->page_size;
+    c->len_most = c->cap;
     c->lens = b->lens;
     c->starts = b->starts;
     c->n_seqs = b->n_seqs;
@@ -2334,6 +2335,7 @@ vt_status paged_attn(vt_paged* g, const vt_paged_pool* pool, const vt_paged_batc
     VT_TRY(paged_heads(pool, n_heads));
     if (!std::isfinite(scale) || scale < 0.f) return fail(VT_ERR_INVALID_ARG, "scale must be finite and >= 0");
     if (window < 0) return fail(VT_ERR_INVALID_ARG, "window %d is negative", window);
+    a->c.len_most = (int)std::min<int64_t>((int64_t)a->c.cap + window, ((int64_t)1 << 31) - (1 << 25));
     a->n_rows = n_rows;
     if (n_rows == 0 || batch->n_seqs == 0) return VT_OK;
     VT_TRY(paged_rows("q", q, q_ld, n_rows, n_heads, pool->d_head));

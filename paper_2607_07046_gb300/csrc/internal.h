@@ -291,6 +291,7 @@ struct PagedView {
     int n_pages, page_size, page_shift, n_kv_heads;
     const int32_t* tables;  // [n_seqs][per_seq]
     int per_seq, cap;       // cap: per_seq * page_size
+    int len_most;           // a length beyond it gives no other result than it (see paged_len)
     const int32_t* lens;
     const int32_t* starts;  // nullptr: row b is sequence b's
     int n_seqs;

@@ -52,8 +52,10 @@ struct Elem<__nv_bfloat16> {
     }
 };
 
-// Length of sequence b, clamped so that adding rows cannot overflow (capacity is at most 2^30).
-__device__ __forceinline__ int paged_len(const PagedView& c, int b) { return min(c.lens[b], c.cap); }
+// Length of sequence b, clamped so that adding rows cannot overflow.  A row's window ends at its true position, also past
+// the table, so lengths are true up to the one that leaves a window nothing of the table: the capacity (at most 2^30) plus
+// the window, and at most 2^31 - 2^25.
+__device__ __forceinline__ int paged_len(const PagedView& c, int b) { return min(c.lens[b], c.len_most); }
 
 // Element offset of the entry of position p of sequence b (K head h), or -1 when its page id is not
 // one of the pool's (flagged).  p is inside [0, cap).

@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
             for (int r = at.row0; r < end; ++r)
                 if (r % gridDim.x == blockIdx.x) pf_zero_row(a, r, a.n_heads * DH / 8, lane);
         } else {
-            if (blockIdx.x == 0 && lane == 0 && at.len + at.rows > c.cap) set_status(c.status, VT_DEV_KV_OVERFLOW);
+            if (blockIdx.x == 0 && lane == 0 && at.rows > 0 && at.len + at.rows > c.cap) set_status(c.status, VT_DEV_KV_OVERFLOW);
             for (int p0 = 0; p0 * 2 * tr < at.rows; p0 += 32) {
                 const int t0 = (p0 + lane) * 2 * tr;
                 int n = 0;

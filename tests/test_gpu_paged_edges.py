@@ -38,3 +38,32 @@ def test_a_page_id_of_any_bad_value_is_flagged(vtlib, paged, form):
     c.tables[0, 2] = want
     attend(vt, paged, c, form, q, 0.125, 0)
     assert vt.vt_paged_status(paged) == 0
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("window", [1, 16, 50])
+@pytest.mark.parametrize("past", [0, 5, 30, 1000, 2 ** 30])
+def test_window_of_a_length_past_the_table(vtlib, paged, form, window, past):
+    """Row i of a sequence whose length is `past` positions over its table attends to [p - window + 1, p] at its true
+    position p: to what of it the table has, and to nothing when it has none of it."""
+    vt = vtlib
+    rows, kv = {"decode": ([1, 1], 1), "few": ([40, 30], 1), "tiles": ([600, 30], 8)}[form]
+    c = Cache(vt, [704 - rows[0], 20], rows, "f16", kv, 64, 16)
+    cap = c.tables.shape[1] * 16
+    c.lens[0] = cap + past
+    q = c.rows(2 * kv)
+    out = attend(vt, paged, c, form, q, 0.125, window)
+    assert vt.vt_paged_status(paged, clear=True) == vt.VT_DEV_KV_OVERFLOW
+    for i in range(rows[0]):
+        seen = torch.arange(min(cap, max(0, cap + past + i - window + 1)), cap, device="cuda")
+        if len(seen) == 0:
+            assert not out[i:rows[0]].any(), i
+            break
+        page, off = c.tables[0].long()[seen // 16], seen % 16
+        k, v = (t[page, :, off].double().transpose(0, 1) for t in (c.k, c.v))
+        w = torch.softmax(q[i].double().reshape(kv, 2, 64) @ k.transpose(1, 2) / 8, -1)
+        o, a = (w @ v).reshape(2 * kv, 64), (w @ v.abs()).reshape(2 * kv, 64)
+        tol = U["f16"] * o.abs() + (U["f16"] + 2.0 ** -16) * a + TINY["f16"] * window * v.abs().max()
+        assert ((out[i].double() - o).abs() <= tol).all(), i
+    ref, tol = attention(c, q, 0.125, window)
+    assert ((out.double() - ref).abs() <= tol)[rows[0]:].all()
