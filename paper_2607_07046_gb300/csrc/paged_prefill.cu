@@ -19,8 +19,10 @@
 // took 171 and 147 us on the first two, but 55 on the third; 64-key halves were slower throughout.
 //
 //   warps 0-3, 4-7  softmax of tile 0 and 1, one thread a row (its lane of the tensor memory): no exchange
-//                   between threads.  m is a reference maximum; O and l are rescaled only when a block's
-//                   maximum exceeds it by more than 8 (log2), so P stays below 2^8.
+//                   between threads.  m is a reference: the maximum when it was set, less 7 (fp16) or 0 (bf16).
+//                   O and l are rescaled only when a block's maximum exceeds that by more than 8 (log2) more, so
+//                   the largest P is between 2^7 and 2^15 in fp16, whose smallest step is 2^-24 (a weight then
+//                   loses at most 2^-32 of the largest one), and between 1 and 2^8 in bf16.
 //   warps 8, 9      copies: Q, and K and V through the page table, by tensor copies of a page's rows; blocks that
 //                   hold positions outside the unit's range (whatever lies there must not reach V: they are
 //                   filled with zeros), bad pages or pages of fewer than 16 positions by 16-byte asynchronous
@@ -704,12 +706,14 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
                 const float bms = pm == -INFINITY ? pm : pm * sl2;
                 float alpha = 1.f;
                 bool resc = false;
-                if (bms > m_use + 8.f) {
+                constexpr float kPfUp = std::is_same<T, __half>::value ? 7.f : 0.f;
+                if (bms > m_use + (8.f + kPfUp)) {
+                    const float mn = bms - kPfUp;
                     if (m_use != -INFINITY) {
-                        alpha = fa_ex2(m_use - bms);
+                        alpha = fa_ex2(m_use - mn);
                         resc = true;
                     }
-                    m_use = bms;
+                    m_use = mn;
                 }
                 if (__any_sync(0xffffffffu, resc)) {  // O_x holds every earlier block (s_full)
 #pragma unroll

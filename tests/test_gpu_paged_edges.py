@@ -67,3 +67,33 @@ def test_window_of_a_length_past_the_table(vtlib, paged, form, window, past):
         assert ((out[i].double() - o).abs() <= tol).all(), i
     ref, tol = attention(c, q, 0.125, window)
     assert ((out.double() - ref).abs() <= tol)[rows[0]:].all()
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("bits", [20.3, 25.6, 27.1])
+def test_many_small_weights_add_up(vtlib, paged, form, dtype, bits):
+    """One key takes nearly all the weight and its value is 0; 40,000 others have 2^-bits of it each and a value of 1, so
+    that the output is their sum alone.  Weights may be rounded to the type, u each, and lose what lies below the type's
+    smallest step: fp16 weights that are scaled to 2^15 (decode, two terms) or to at least 2^7 (prefill) at the largest
+    lose at most 2^-40 and 2^-32 of it each.  Scores of up to 40 log2 units carry 2^-24 of that as fp32 values, two
+    roundings each, 2^-17 of a weight; at most 2504 products are added in a row, 2^-23 of their sum each, and 700 sums of
+    weights, 2^-24 each: less than 2^-11."""
+    n, seqs, each = 40000, 38, 130 if form == "tiles" else 1
+    c = Cache(vtlib, [n], [each], dtype, 8, 64, 64)
+    c.k.masked_fill_(c.live[:, None, :, None], 0.0)
+    c.v.masked_fill_(c.live[:, None, :, None], 1.0)
+    page, off = c.positions(0, n)
+    c.k[page[777], :, off[777], 0] = 1.0
+    c.v[page[777], :, off[777]] = 0.0
+    # as many sequences, on the same pages, as leave each CTA whole histories
+    c.tables, c.lens, c.n_rows = c.tables.repeat(seqs, 1), c.lens.repeat(seqs), seqs * each
+    c.starts = torch.arange(0, c.n_rows + 1, each, dtype=torch.int32, device="cuda")
+    q = torch.zeros(c.n_rows, 16, 64, dtype=TYPE[dtype], device="cuda")
+    q[:, :, 0] = 1.0
+    out = attend(vtlib, paged, c, form, q, bits * math.log(2.0), 0).double()
+    u, floor = U[dtype], 0.0 if dtype == "bf16" else 2.0 ** (-32 if form == "tiles" else -40)
+    m = (n + torch.arange(c.n_rows, device="cuda") % each).double()[:, None, None]
+    ref = m * 2.0 ** -bits / (1.0 + m * 2.0 ** -bits)
+    tol = (2 * u + 2.0 ** -11 + 2.0 ** -17) * ref + m * floor + (2.0 ** -25 if dtype == "f16" else 0.0)
+    assert ((out - ref).abs() <= tol).all(), float(((out - ref).abs() / ref).max())
