@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
     for (int b = tid * ch; b < min(c.n_seqs, (tid + 1) * ch); ++b) {
         PdSeq s;
         s.open<ROWS>(a, b, COLS);
-        if (blockIdx.x == 0 && (s.len + s.rows > c.cap || c.lens[b] > c.cap)) set_status(c.status, VT_DEV_KV_OVERFLOW);
+        if (blockIdx.x == 0 && s.rows > 0 && s.len >= 0 && s.len + s.rows > c.cap) set_status(c.status, VT_DEV_KV_OVERFLOW);
         idle |= s.steps == 0;
         largest = max(largest, s.steps);
         mine += s.cost();

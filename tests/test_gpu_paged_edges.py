@@ -97,3 +97,33 @@ def test_many_small_weights_add_up(vtlib, paged, form, dtype, bits):
     ref = m * 2.0 ** -bits / (1.0 + m * 2.0 ** -bits)
     tol = (2 * u + 2.0 ** -11 + 2.0 ** -17) * ref + m * floor + (2.0 ** -25 if dtype == "f16" else 0.0)
     assert ((out - ref).abs() <= tol).all(), float(((out - ref).abs() / ref).max())
+
+
+@pytest.mark.parametrize("window", [0, 16])
+@pytest.mark.parametrize("form", ["few", "tiles"])
+def test_a_slot_without_rows_overflows_nothing(vtlib, paged, form, window):
+    """A length past the table is reported where a new row is at or past it, and only there, by every call alike."""
+    vt = vtlib
+    c = Cache(vt, [30, 40], [0, 600 if form == "tiles" else 5], "f16", 8, 64, 16)
+    c.lens[0] = c.tables.shape[1] * 16 + 3
+    q = c.rows(16)
+    out = attend(vt, paged, c, form, q, 0.125, window)
+    assert vt.vt_paged_status(paged, clear=True) == 0
+    ref, tol = attention(c, q, 0.125, window)
+    assert ((out.double() - ref).abs() <= tol).all()
+    c.lens[0] = 30
+    c.lens[1] += c.tables.shape[1] * 16 - 600 - 40 + 1 if form == "tiles" else c.tables.shape[1] * 16 - 5 - 40 + 1
+    attend(vt, paged, c, form, q, 0.125, window)  # the last row is one position past the table
+    assert vt.vt_paged_status(paged, clear=True) == vt.VT_DEV_KV_OVERFLOW
+
+
+def test_an_idle_slot_overflows_nothing(vtlib, paged):
+    """An idle slot with more rows than the table has positions: zeros, and no status bit."""
+    vt = vtlib
+    c = Cache(vt, [-1, 30], [60, 5], "f16", 2, 64, 16)
+    assert c.tables.shape[1] * 16 < 59
+    q = c.rows(4)
+    out = attend(vt, paged, c, "few", q, 0.125, 0)
+    assert vt.vt_paged_status(paged, clear=True) == 0 and not out[:60].any()
+    ref, tol = attention(c, q, 0.125, 0)
+    assert ((out.double() - ref).abs() <= tol).all()
