@@ -18,10 +18,12 @@ from . import vt
 
 
 class PageTable:
-    """The host's side: `slots` sequences of at most `pages_per_seq` pages out of `n_pages`."""
+    """The host's side: `slots` sequences of at most `pages_per_seq` pages out of `n_pages`, and of at most `max_len`
+    positions (None: as many as the pages have)."""
 
-    def __init__(self, n_pages: int, page_size: int, slots: int, pages_per_seq: int):
+    def __init__(self, n_pages: int, page_size: int, slots: int, pages_per_seq: int, max_len: Optional[int] = None):
         self.page_size, self.pages_per_seq = page_size, pages_per_seq
+        self.max_len = pages_per_seq * page_size if max_len is None else max_len
         self.free: List[int] = list(range(n_pages - 1, -1, -1))
         self.pages: List[List[int]] = [[] for _ in range(slots)]
         self.lens: List[int] = [-1] * slots  # -1: an idle slot
@@ -42,6 +44,8 @@ class PageTable:
         """Pages for `rows` more positions; True when the slot got new ones.  Nothing changes on an error."""
         if self.lens[slot] < 0:
             raise ValueError(f"slot {slot} is idle")
+        if self.lens[slot] + rows > self.max_len:
+            raise RuntimeError(f"slot {slot} would hold {self.lens[slot] + rows} positions of at most {self.max_len}")
         want = -(-(self.lens[slot] + rows) // self.page_size)
         more = want - len(self.pages[slot])
         if want > self.pages_per_seq:
@@ -58,7 +62,7 @@ class PagedCache:
 
     def __init__(self, n_layers: int, n_kv_heads: int, d_head: int, page_size: int, n_pages: int, slots: int, max_len: int,
                  dtype=torch.float16, theta: float = 1e4):
-        self.table = PageTable(n_pages, page_size, slots, -(-max_len // page_size))
+        self.table = PageTable(n_pages, page_size, slots, -(-max_len // page_size), max_len)
         shape = (n_pages, n_kv_heads, page_size, d_head)
         self.pools = [vt.make_paged_pool(torch.zeros(shape, dtype=dtype, device="cuda"), torch.zeros(shape, dtype=dtype, device="cuda"))
                       for _ in range(n_layers)]
