@@ -84,14 +84,18 @@ class PagedCache:
 
     def step(self, rows: Dict[int, int], one_each: Optional[bool] = None):
         """(batch, first row of every slot) for these new rows.  one_each: one row for every slot, idle or not, as
-        vt_paged_decode takes them (row b belongs to slot b); by default where every sequence gets one row."""
+        vt_paged_decode takes them (row b belongs to slot b); by default where every sequence gets one row.  With it a
+        slot that is not in `rows` is idle for this step, and every count has to be 1."""
         if one_each is None:
             one_each = set(rows.values()) == {1} and len(rows) == sum(n >= 0 for n in self.table.lens)
+        elif one_each and any(n != 1 for n in rows.values()):
+            raise ValueError(f"one_each takes one row of each slot, got {rows}")
         for slot, n in rows.items():
             if self.table.reserve(slot, n):
                 pages = self.table.pages[slot]
                 self.tables[slot, :len(pages)] = torch.tensor(pages, dtype=torch.int32, device="cuda")
-        self.lens.copy_(torch.tensor(self.table.lens, dtype=torch.int32))
+        lens = [n if not one_each or slot in rows else -1 for slot, n in enumerate(self.table.lens)]
+        self.lens.copy_(torch.tensor(lens, dtype=torch.int32))
         starts = [0]
         for slot in range(len(self.table.lens)):
             starts.append(starts[-1] + (1 if one_each else rows.get(slot, 0)))

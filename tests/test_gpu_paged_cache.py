@@ -53,3 +53,40 @@ def test_every_position_that_a_step_accepts_is_stored(vtlib, make, max_len, page
     assert held(cache, slot) == [1.0] * (max_len - 1) + [2.0]
     with pytest.raises(RuntimeError):
         cache.step({slot: 1})
+
+
+def test_one_each_takes_one_row_of_each_slot(make):
+    cache = make(16, 40, 3, 100)
+    a, b = cache.admit(), cache.admit()
+    for rows in ({a: 3}, {a: 1, b: 2}, {a: 0}):
+        with pytest.raises(ValueError):
+            cache.step(rows, one_each=True)
+    assert cache.table.pages == [[], [], []] and len(cache.table.free) == 40
+
+
+def test_one_each_leaves_the_other_slots_alone(vtlib, make):
+    """A live slot that gets no row is idle for the step: nothing is stored for it, not even past its end."""
+    vt = vtlib
+    cache = make(16, 40, 3, 100)
+    a, b = cache.admit(), cache.admit()
+    batch, _ = cache.step({a: 16, b: 5})  # a's page is full
+    append(vt, cache, batch, 21, 1.0)
+    cache.advance({a: 16, b: 5})
+    before = cache.pools[0].tensors[1].clone()
+    batch, starts = cache.step({b: 1}, one_each=True)
+    assert batch.starts is None and starts == [0, 1, 2, 3]
+    q, status = append(vt, cache, batch, 3, 2.0)
+    assert status == 0 and q[b].any() and not q[a].any() and not q[2].any()
+    out = torch.full_like(q, 7.0)
+    vt.vt_paged_decode(cache.paged, cache.pools[0], batch, q, out)
+    assert vt.vt_paged_status(cache.paged) == 0
+    assert out[b].any() and not out[a].any() and not out[2].any()
+    cache.advance({b: 1})
+    assert held(cache, a) == [1.0] * 16 and held(cache, b) == [1.0] * 5 + [2.0]
+    v = cache.pools[0].tensors[1]
+    before[cache.table.pages[b][0], 0, 5] = 2.0
+    assert torch.equal(v, before)
+    batch, _ = cache.step({a: 1, b: 1})  # both take part again
+    _, status = append(vt, cache, batch, 3, 3.0)
+    cache.advance({a: 1, b: 1})
+    assert status == 0 and held(cache, a)[-1] == 3.0 and held(cache, b)[-1] == 3.0
