@@ -42,19 +42,29 @@ class PageTable:
 
     def reserve(self, slot: int, rows: int) -> bool:
         """Pages for `rows` more positions; True when the slot got new ones.  Nothing changes on an error."""
+        return bool(self.reserve_all({slot: rows}))
+
+    def reserve_all(self, rows: Dict[int, int]) -> List[int]:
+        """Pages for the new rows of several slots; those that got new ones.  Nothing changes on an error."""
+        more = {slot: self._missing(slot, n) for slot, n in rows.items()}
+        if sum(more.values()) > len(self.free):
+            raise RuntimeError(f"{sum(more.values())} pages are needed and {len(self.free)} are free")
+        for slot, n in more.items():
+            for _ in range(n):
+                self.pages[slot].append(self.free.pop())
+        return [slot for slot, n in more.items() if n > 0]
+
+    def _missing(self, slot: int, rows: int) -> int:
         if self.lens[slot] < 0:
             raise ValueError(f"slot {slot} is idle")
+        if rows < 0:
+            raise ValueError(f"{rows} rows for slot {slot}")
         if self.lens[slot] + rows > self.max_len:
             raise RuntimeError(f"slot {slot} would hold {self.lens[slot] + rows} positions of at most {self.max_len}")
         want = -(-(self.lens[slot] + rows) // self.page_size)
-        more = want - len(self.pages[slot])
         if want > self.pages_per_seq:
             raise RuntimeError(f"slot {slot} would need {want} pages of at most {self.pages_per_seq}")
-        if more > len(self.free):
-            raise RuntimeError(f"{more} pages are needed and {len(self.free)} are free")
-        for _ in range(max(0, more)):
-            self.pages[slot].append(self.free.pop())
-        return more > 0
+        return max(0, want - len(self.pages[slot]))
 
 
 class PagedCache:
@@ -90,10 +100,9 @@ class PagedCache:
             one_each = set(rows.values()) == {1} and len(rows) == sum(n >= 0 for n in self.table.lens)
         elif one_each and any(n != 1 for n in rows.values()):
             raise ValueError(f"one_each takes one row of each slot, got {rows}")
-        for slot, n in rows.items():
-            if self.table.reserve(slot, n):
-                pages = self.table.pages[slot]
-                self.tables[slot, :len(pages)] = torch.tensor(pages, dtype=torch.int32, device="cuda")
+        for slot in self.table.reserve_all(rows):
+            pages = self.table.pages[slot]
+            self.tables[slot, :len(pages)] = torch.tensor(pages, dtype=torch.int32, device="cuda")
         lens = [n if not one_each or slot in rows else -1 for slot, n in enumerate(self.table.lens)]
         self.lens.copy_(torch.tensor(lens, dtype=torch.int32))
         starts = [0]

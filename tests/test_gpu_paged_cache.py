@@ -90,3 +90,15 @@ def test_one_each_leaves_the_other_slots_alone(vtlib, make):
     _, status = append(vt, cache, batch, 3, 3.0)
     cache.advance({a: 1, b: 1})
     assert status == 0 and held(cache, a)[-1] == 3.0 and held(cache, b)[-1] == 3.0
+
+
+def test_a_step_that_is_refused_changes_nothing(make):
+    cache = make(8, 5, 3, 40)
+    a, b = cache.admit(), cache.admit()
+    cache.step({a: 9, b: 3})
+    cache.advance({a: 9, b: 3})
+    free, pages, tables = list(cache.table.free), [list(p) for p in cache.table.pages], cache.tables.clone()
+    for rows in ({a: 8, b: 14}, {a: 8, b: 60}, {a: 8, 2: 1}):
+        with pytest.raises((ValueError, RuntimeError)):
+            cache.step(rows)
+        assert (cache.table.free, cache.table.pages) == (free, pages) and torch.equal(cache.tables, tables)
