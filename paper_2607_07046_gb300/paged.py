@@ -91,6 +91,7 @@ class PagedCache:
     def release(self, slot: int) -> None:
         self.table.release(slot)
         self.lens[slot] = -1
+        self.tables[slot] = -1  # its pages are others' soon
 
     def step(self, rows: Dict[int, int], one_each: Optional[bool] = None):
         """(batch, first row of every slot) for these new rows.  one_each: one row for every slot, idle or not, as

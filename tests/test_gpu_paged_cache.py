@@ -102,3 +102,25 @@ def test_a_step_that_is_refused_changes_nothing(make):
         with pytest.raises((ValueError, RuntimeError)):
             cache.step(rows)
         assert (cache.table.free, cache.table.pages) == (free, pages) and torch.equal(cache.tables, tables)
+
+
+def test_a_released_slots_pages_leave_its_table(vtlib, make):
+    """Its next sequence has no entry for pages that others hold by now: a position that nothing was reserved for is
+    reported, not stored in their pages."""
+    vt = vtlib
+    cache = make(16, 6, 2, 100)
+    a = cache.admit()
+    cache.step({a: 80})
+    cache.advance({a: 80})
+    cache.release(a)
+    assert (cache.tables == -1).all()
+    a, b = cache.admit(), cache.admit()
+    batch, _ = cache.step({a: 16, b: 64})
+    append(vt, cache, batch, 80, 1.0)
+    cache.advance({a: 16, b: 64})
+    cache.lens[a] = 16  # a captured step that is replayed without a step of the cache
+    batch = vt.make_paged_batch(cache.tables, cache.lens)
+    cache.lens[b] = -1
+    _, status = append(vt, cache, batch, 2, 2.0)
+    assert status == vt.VT_DEV_BAD_PAGE
+    assert held(cache, a) == [1.0] * 16 and held(cache, b) == [1.0] * 64
