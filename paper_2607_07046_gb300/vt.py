@@ -709,7 +709,7 @@ def make_paged_batch(tables, lens, starts=None) -> vt_paged_batch:
         raise ValueError("tables, lens and starts need one device")
     b = vt_paged_batch(_ptr(tables, torch.int32), _ptr(lens, torch.int32), _ptr(starts, torch.int32), tables.shape[0],
                        tables.shape[1])
-    b.tensors = (tables, lens, starts)
+    b.tensors, b.device = (tables, lens, starts), tables.get_device()
     return b
 
 
@@ -740,6 +740,11 @@ def vt_rope_table(table, theta: float, stream=None) -> None:
                                _stream(stream)))
 
 
+def _same_device(pool, batch) -> None:
+    if batch.device != pool.device:
+        raise ValueError("the batch's tables lie on another device than the pool")
+
+
 def _rows(t, pool, heads: Optional[int] = None) -> Tuple[int, int]:
     """(data_ptr, elements between rows) of a CUDA tensor [rows, heads, head dim] of the pool's type and
     device whose rows are contiguous."""
@@ -761,8 +766,9 @@ def vt_paged_append(paged: int, pool: vt_paged_pool, batch: vt_paged_batch, q, k
     if k.shape[0] != n or v.shape[0] != n or q_out.shape[0] != n:
         raise ValueError("q, k, v and q_out need one number of rows")
     table = rope.shape
-    if len(table) != 3 or table[2] != 2 or 2 * table[1] != pool.d_head:
-        raise ValueError("expected rope [positions, head dim / 2, 2]")
+    if len(table) != 3 or table[2] != 2 or 2 * table[1] != pool.d_head or rope.get_device() != pool.device:
+        raise ValueError("expected rope [positions, head dim / 2, 2] on the pool's device")
+    _same_device(pool, batch)
     (qp, ql), (kp, kl), (vp, vl), (op, ol) = (_rows(q, pool), _rows(k, pool, pool.n_kv_heads),
                                              _rows(v, pool, pool.n_kv_heads), _rows(q_out, pool, heads))
     _check(lib().vt_paged_append(paged, pool, batch, n, heads, qp, ql, kp, kl, vp, vl, _ptr(rope, torch.float32),
@@ -776,6 +782,7 @@ def vt_paged_decode(paged: int, pool: vt_paged_pool, batch: vt_paged_batch, q, o
     heads = q.shape[1]
     if q.shape[0] != batch.n_seqs or out.shape[0] != batch.n_seqs:
         raise ValueError("one row of q and out per sequence")
+    _same_device(pool, batch)
     (qp, ql), (op, ol) = _rows(q, pool), _rows(out, pool, heads)
     _check(lib().vt_paged_decode(paged, pool, batch, heads, qp, ql, pool.d_head ** -0.5 if scale is None else scale,
                                  window, op, ol, _stream(stream)))
@@ -787,6 +794,7 @@ def vt_paged_prefill(paged: int, pool: vt_paged_pool, batch: vt_paged_batch, q, 
     n, heads = q.shape[0], q.shape[1]
     if out.shape[0] != n:
         raise ValueError("q and out need one number of rows")
+    _same_device(pool, batch)
     (qp, ql), (op, ol) = _rows(q, pool), _rows(out, pool, heads)
     _check(lib().vt_paged_prefill(paged, pool, batch, n, heads, qp, ql, pool.d_head ** -0.5 if scale is None else scale,
                                   window, op, ol, _stream(stream)))
