@@ -122,7 +122,7 @@ cudaError_t init_library() {
         if (g_init_err != cudaSuccess) return;
         g_init_err = init_paged_decode();
         if (g_init_err != cudaSuccess) return;
-        g_init_err = init_paged_prefill();
+        init_paged_prefill();  // (the calls that need it say when it cannot run)
     });
     return g_init_err;
 }
@@ -2418,6 +2418,7 @@ extern "C" vt_status vt_paged_prefill(vt_paged* g, const vt_paged_pool* pool, co
     constexpr int kFewColumns = 24, kFewSteps = 32;
     const bool few = (int64_t)n_rows * a.group <= (int64_t)kFewColumns * batch->n_seqs ||
                      paged_decode_line(a, 16) <= (int64_t)kFewSteps * 2 * g_num_sms;
+    if (const char* e = few ? nullptr : paged_tiles_error()) return fail(VT_ERR_CUDA, "%s", e);
     VT_CUDA((few ? launch_paged_decode : launch_paged_prefill)(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
     return ok();
 }

@@ -333,7 +333,8 @@ cudaError_t launch_paged_decode(const PagedAttnArgs& a, int dtype, int dh, cudaS
 int64_t paged_decode_line(const PagedAttnArgs& a, int cols);
 cudaError_t launch_paged_prefill(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st);
 cudaError_t init_paged_decode();
-cudaError_t init_paged_prefill();
+void init_paged_prefill();
+const char* paged_tiles_error();  // why launch_paged_prefill cannot run in this build; nullptr: it can
 
 // ------------------------------------------------------------------ static scratch
 // (static_scratch.cu) the decode step whose intermediates are in one file-scope __device__ array.

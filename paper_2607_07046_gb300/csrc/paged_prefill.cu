@@ -1015,7 +1015,7 @@ static cudaError_t init_one() {
     cudaFuncAttributes f;
     cudaError_t e = cudaFuncGetAttributes(&f, k_paged_prefill<T, DH, JOIN>);
     if (e != cudaSuccess) return e;
-    if (f.numRegs != kPfLaunchRegs) return cudaErrorInvalidConfiguration;  // the register split needs exactly these
+    if (f.numRegs != kPfLaunchRegs) return cudaErrorInvalidConfiguration;  // (see paged_tiles_error)
     return cudaFuncSetAttribute(k_paged_prefill<T, DH, JOIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PfGeom<DH>::kSmem);
 }
 template <class T, int DH>
@@ -1023,12 +1023,21 @@ static cudaError_t init_both() {
     const cudaError_t e = init_one<T, DH, false>();
     return e != cudaSuccess ? e : init_one<T, DH, true>();
 }
-cudaError_t init_paged_prefill() {
-    const cudaError_t e[4] = {init_both<__half, 64>(), init_both<__half, 128>(), init_both<__nv_bfloat16, 64>(),
-                              init_both<__nv_bfloat16, 128>()};
-    for (cudaError_t x : e)
-        if (x != cudaSuccess) return x;
-    return cudaSuccess;
+// The register split needs exactly the registers that it was planned with: a build that gives the kernel another number
+// fails the calls that need the kernel, and no others.
+static cudaError_t g_tiles_err = cudaErrorNotReady;
+void init_paged_prefill() {
+    g_tiles_err = cudaSuccess;
+    for (cudaError_t e : {init_both<__half, 64>(), init_both<__half, 128>(), init_both<__nv_bfloat16, 64>(),
+                          init_both<__nv_bfloat16, 128>()})
+        if (e != cudaSuccess) g_tiles_err = e;
+    if (g_tiles_err != cudaSuccess) cudaGetLastError();  // not the next call's
+}
+const char* paged_tiles_error() {
+    if (g_tiles_err == cudaSuccess) return nullptr;
+    return g_tiles_err == cudaErrorInvalidConfiguration
+               ? "the prefill kernel on tensor-core tiles was built with another register count than its split needs"
+               : cudaGetErrorString(g_tiles_err);
 }
 
 }  // namespace vt
