@@ -2204,6 +2204,7 @@ struct vt_paged {
     Allocator alloc;
     uint8_t* base = nullptr;     // status word, arrival counters, slots
     uint32_t* status = nullptr;
+    int* over = nullptr;         // see PagedAttnArgs
     int* arrived = nullptr;      // [kPagedMaxGrid]
     float* work = nullptr;       // [paged_work_floats()]
 };
@@ -2234,6 +2235,7 @@ extern "C" vt_status vt_paged_create(const vt_allocator* allocator, vt_stream st
         return fail(VT_ERR_ALLOC, "allocating the paged workspace failed");
     }
     g->status = reinterpret_cast<uint32_t*>(g->base);
+    g->over = reinterpret_cast<int*>(g->base + 128);
     g->arrived = reinterpret_cast<int*>(g->base + 256);
     g->work = reinterpret_cast<float*>(g->base + head);
     cudaError_t e = cudaMemsetAsync(g->base, 0, head, st);
@@ -2351,6 +2353,8 @@ vt_status paged_attn(vt_paged* g, const vt_paged_pool* pool, const vt_paged_batc
     a->window = window;
     a->out = static_cast<uint16_t*>(out);
     a->out_ld = n_rows > 1 ? out_ld : 0;
+    a->rows_most = std::numeric_limits<int>::max();
+    a->rows_over = 0;
     a->work = g->work;
     a->arrived = g->arrived;
     return VT_OK;
@@ -2415,10 +2419,22 @@ extern "C" vt_status vt_paged_prefill(vt_paged* g, const vt_paged_pool* pool, co
     // Or little work altogether, by the tables' width: that kernel starts sooner and spreads it over more SMs.  (8 KV heads
     // of 4 query heads, one sequence: 30 rows 6 and 12 us, 50 behind 1000 20 and 28, 77 behind 300 17 and 19; 30 behind
     // 5000, 70 steps a CTA, 35 and 26.)
-    constexpr int kFewColumns = 24, kFewSteps = 32;
-    const bool few = (int64_t)n_rows * a.group <= (int64_t)kFewColumns * batch->n_seqs ||
-                     paged_decode_line(a, 16) <= (int64_t)kFewSteps * 2 * g_num_sms;
-    if (const char* e = few ? nullptr : paged_tiles_error()) return fail(VT_ERR_CUDA, "%s", e);
-    VT_CUDA((few ? launch_paged_decode : launch_paged_prefill)(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
+    // The host knows the columns of the whole batch only, and slots may have none: a few on average may be a prompt in one
+    // slot, which the first kernel would stream K and V for a tile of 16 columns at a time.  So a batch of a few columns on
+    // average goes to both kernels, and each takes the sequences that suit it by their own rows.  (One launch and two: 380
+    // rows behind 4000 in one of 64 slots, group of 4, 238 and 66 us; 3000 rows in one of 128 slots, no group, 1245 and 138;
+    // 300 rows behind 4000 beside 63 tokens, 346 and 248.  Where the second finds nothing it costs 2 to 5 us: 32 sequences
+    // of 4 rows 56 and 59, 256 of one row 171 and 175.  With 64 columns altogether a prompt hides four tiles at most.)
+    constexpr int kFewColumns = 24, kFewSteps = 32, kFewAltogether = 64;
+    const int64_t columns = (int64_t)n_rows * a.group;
+    const bool few = columns <= (int64_t)kFewColumns * batch->n_seqs;
+    const bool all_few = (few && columns <= kFewAltogether) || paged_decode_line(a, 16) <= (int64_t)kFewSteps * 2 * g_num_sms;
+    if (const char* e = all_few ? nullptr : paged_tiles_error()) return fail(VT_ERR_CUDA, "%s", e);
+    if (few && !all_few) {
+        a.rows_most = a.rows_over = kFewColumns / a.group;
+        a.over = g->over;
+    }
+    if (few || all_few) VT_CUDA(launch_paged_decode(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
+    if (!all_few) VT_CUDA(launch_paged_prefill(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
     return ok();
 }

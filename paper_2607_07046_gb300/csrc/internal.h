@@ -318,6 +318,11 @@ struct PagedAttnArgs {
     int window;
     uint16_t* out;
     int64_t out_ld;
+    // Which sequences a launch takes, by their new rows: the kernel of single tokens those with rows_most at most, the
+    // tiles' kernel those with more than rows_over.  Where a batch goes to both, the first leaves in `over` whether there
+    // are any for the second (nullptr: it goes to one).
+    int rows_most, rows_over;
+    int* over;
     // workspace: slots for the parts of a unit that several CTAs share, and for the first CTA of each
     // such unit the number of parts that are there (zero between calls)
     float* work;

@@ -97,15 +97,19 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
 // A sequence's new rows, and the positions [beg, end) that they attend to (end 0: none).
 struct PdSeq {
     int row0, rows, len, beg, end, tiles, steps;
+    bool over;
     // tiles: units of a KV head, of `cols` columns
     template <bool ROWS>
     __device__ __forceinline__ void open(const PagedAttnArgs& a, int b, int cols) {
         len = paged_len(a.c, b);
         row0 = b;
         rows = 1;
+        over = false;
         if (ROWS) {
             row0 = paged_start(a.c, b, a.n_rows);
             rows = max(0, paged_start(a.c, b + 1, a.n_rows) - row0);
+            over = rows > a.rows_most;  // the next launch's
+            if (over) rows = 0;
         }
         end = len < 0 || rows == 0 ? 0 : min(len + rows, a.c.cap);
         beg = a.window > 0 ? max(0, len + 1 - a.window) : 0;
@@ -157,12 +161,13 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
     const int ch = (c.n_seqs + kPdThreads - 1) / kPdThreads;
     int64_t mine = 0;
     int largest = 0;
-    bool idle = false;
+    bool idle = false, over = false;
     for (int b = tid * ch; b < min(c.n_seqs, (tid + 1) * ch); ++b) {
         PdSeq s;
         s.open<ROWS>(a, b, COLS);
         if (blockIdx.x == 0 && s.rows > 0 && s.len >= 0 && s.len + s.rows > c.cap) set_status(c.status, VT_DEV_KV_OVERFLOW);
-        idle |= s.steps == 0;
+        idle |= s.steps == 0 && !s.over;
+        over |= s.over && s.len >= 0;
         largest = max(largest, s.steps);
         mine += s.cost();
     }
@@ -178,6 +183,10 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
         s_max[warp] = largest;
     }
     const bool any_idle = __syncthreads_or(idle);
+    if (ROWS && blockIdx.x == 0 && a.over) {
+        const bool any_over = __syncthreads_or(over);
+        if (tid == 0) *a.over = any_over;
+    }
     int64_t total = 0;
     for (int w = 0; w < kPdWarps; ++w) {
         if (w < warp) upto += s_sum[w];

@@ -92,6 +92,7 @@ struct PfCursor {
             len = paged_len(a.c, b);
             row0 = paged_start(a.c, b, a.n_rows);
             rows = len < 0 ? 0 : max(0, paged_start(a.c, b + 1, a.n_rows) - row0);
+            if (rows <= a.rows_over) rows = 0;  // another launch's
         }
     }
     // attended positions of tokens [t0, t1) of the sequence
@@ -251,6 +252,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
     pdl_wait();  // a preceding kernel may hold tensor memory
     pdl_launch_dependents();
     if (JOIN && tid == 0) P.split[blockIdx.x].parts = 0;
+    if (a.over && !__ldcg(a.over)) return;  // every sequence was the preceding launch's
     if (warp == kPfMma) {
         tc::tmem_alloc(tmem_slot, 512);
         tc::tmem_relinquish();

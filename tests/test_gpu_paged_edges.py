@@ -6,7 +6,7 @@ import math
 import pytest
 
 torch = pytest.importorskip("torch")
-from .test_gpu_paged import TINY, TYPE, U, Cache, attention, paged, widened  # noqa: E402,F401
+from .test_gpu_paged import TINY, TYPE, U, Cache, attention, check_attention, paged, widened  # noqa: E402,F401
 
 pytestmark = pytest.mark.gpu
 
@@ -127,3 +127,74 @@ def test_an_idle_slot_overflows_nothing(vtlib, paged):
     assert vt.vt_paged_status(paged, clear=True) == 0 and not out[:60].any()
     ref, tol = attention(c, q, 0.125, 0)
     assert ((out.double() - ref).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("window", [0, 200])
+@pytest.mark.parametrize("dtype,d_head,kv_heads,group", [("f16", 128, 2, 4), ("bf16", 64, 8, 1), ("f16", 64, 1, 30)])
+def test_a_prompt_among_tokens_and_empty_slots(vtlib, paged, dtype, d_head, kv_heads, group, window):
+    """Single tokens, a few drafted ones, prompts, idle slots (one of them with rows) and slots without rows in one
+    batch, by trimmed tables and by a server's."""
+    lens = [(i * 7919) % 3000 if i % 6 else -1 for i in range(150)]
+    rows = [(0, 1, 1, 0, 3, 0)[i % 6] for i in range(150)]
+    lens[40], rows[40] = 1500, 400
+    lens[41], rows[41] = 0, 130
+    lens[42], rows[42] = -1, 50
+    lens[149], rows[149] = 77, 24 // group + 1
+    c = Cache(vtlib, lens, rows, dtype, kv_heads, d_head, 16, "pos")
+    check_attention(vtlib, paged, c, "prefill", kv_heads * group, window)
+    check_attention(vtlib, paged, widened(c), "prefill", kv_heads * group, window)
+
+
+@pytest.mark.parametrize("heads,kv_heads,length,rows,slots", [(32, 8, 4000, 380, 64), (32, 32, 0, 3000, 128)])
+def test_empty_slots_cost_a_prompt_little(vtlib, paged, heads, kv_heads, length, rows, slots):
+    """A prompt takes about as long among slots without rows as by itself.  (The kernel of single tokens would take five
+    to eleven times as long; three times leaves room for another user of the machine.)"""
+    vt = vtlib
+    best = []
+    for n in (1, slots):
+        c = Cache(vt, [length] + [-1] * (n - 1), [rows] + [0] * (n - 1), "bf16", kv_heads, 128, 16)
+        q, batch = c.rows(heads), c.batch(vt)
+        out = torch.empty_like(q)
+        times = []
+        for _ in range(8):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            for _ in range(10):
+                vt.vt_paged_prefill(paged, c.pool, batch, q, out)
+            b.record()
+            b.synchronize()
+            times.append(a.elapsed_time(b))
+        best.append(min(times))
+    assert best[1] <= 3 * best[0], best
+
+
+def test_rows_that_move_between_slots_in_a_graph(vtlib, paged):
+    """A captured call serves other rows per slot: which kernel takes a slot goes by its rows at replay."""
+    vt = vtlib
+    n, total = 60, 300
+    c = Cache(vt, [2000 + i for i in range(n)], [5] * n, "f16", 2, 64, 64)
+    c.tables = torch.cat((c.tables, c.tables.roll(1, 0)[:, :8]), 1).contiguous()  # room for more rows in every slot
+    c.tables.clamp_(min=0)
+    c.k.nan_to_num_(0.25)
+    c.v.nan_to_num_(0.25)
+    q = torch.randn(total, 8, 64, generator=c.gen, device="cuda").half()
+    out, batch, stream = torch.empty_like(q), c.batch(vt), torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        vt.vt_paged_prefill(paged, c.pool, batch, q, out)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            vt.vt_paged_prefill(paged, c.pool, batch, q, out)
+        for kind in range(4):
+            rows = [[5] * n, [1] * (n - 1) + [total - n + 1], [0] * 10 + [total] + [0] * (n - 11), [7 * (i % 2) + 1 for i in range(n)]][kind]
+            starts = [0]
+            for r in rows:
+                starts.append(starts[-1] + r)
+            c.starts.copy_(torch.tensor(starts, dtype=torch.int32))
+            c.rows_host, c.starts_host = rows, starts
+            out.fill_(7.0)
+            graph.replay()
+            stream.synchronize()
+            ref, tol = attention(c, q, 0.125, 0)
+            assert ((out.double() - ref).abs() <= tol)[:starts[-1]].all(), kind
+    assert vt.vt_paged_status(paged) == 0
