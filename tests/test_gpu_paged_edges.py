@@ -198,3 +198,22 @@ def test_rows_that_move_between_slots_in_a_graph(vtlib, paged):
             ref, tol = attention(c, q, 0.125, 0)
             assert ((out.double() - ref).abs() <= tol)[:starts[-1]].all(), kind
     assert vt.vt_paged_status(paged) == 0
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("form,d_head,kv_heads,group,page", [
+    ("decode", 64, 2, 1, 16), ("decode", 128, 2, 4, 32), ("decode", 128, 1, 12, 16), ("decode", 64, 1, 40, 64),
+    ("few", 64, 2, 1, 16), ("few", 128, 2, 4, 32), ("few", 128, 1, 12, 16)])  # (a group of 40 is the tiles')
+def test_weights_of_single_tokens_carry_two_terms(vtlib, paged, form, dtype, d_head, kv_heads, group, page):
+    """The kernel of single tokens keeps a weight in two 16-bit terms: p - hi - lo is at most u^2 p, so beside the
+    output's own rounding, u |o|, only 2^-16 A (fp32 scores, exponentials and sums) and 2^-16 A (two bf16 terms) remain,
+    A = sum_j softmax_j |v_j|; fp16 outputs below 2^-14 are 2^-25 off at most.  (One term alone would be u A off.)"""
+    lens = [0, 1, 15, 16, 63, 200, 777, 3000, -1, 5000]
+    c = Cache(vtlib, lens, [1] * len(lens), dtype, kv_heads, d_head, page)
+    q = c.rows(kv_heads * group)
+    out = attend(vtlib, paged, c, form, q, d_head ** -0.5, 0).double()
+    ref, loose = attention(c, q, d_head ** -0.5, 0)
+    u = U[dtype]
+    a = (loose - u * ref.abs()) / (u + 2.0 ** -16)  # (with a little more in fp16: its bound for small weights)
+    tol = u * ref.abs() + (2.0 ** -15) * a + TINY[dtype]
+    assert ((out - ref).abs() <= tol).all(), float(((out - ref).abs() / tol.clamp(min=1e-30)).max())
