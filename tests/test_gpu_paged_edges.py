@@ -217,3 +217,60 @@ def test_weights_of_single_tokens_carry_two_terms(vtlib, paged, form, dtype, d_h
     a = (loose - u * ref.abs()) / (u + 2.0 ** -16)  # (with a little more in fp16: its bound for small weights)
     tol = u * ref.abs() + (2.0 ** -15) * a + TINY[dtype]
     assert ((out - ref).abs() <= tol).all(), float(((out - ref).abs() / tol.clamp(min=1e-30)).max())
+
+
+@pytest.mark.parametrize("form", ["decode", "few", "tiles"])
+def test_as_many_sequences_as_a_batch_takes(vtlib, paged, form):
+    """16384 sequences, short and idle ones; for the tiles' kernel some with rows enough for it."""
+    vt, n = vtlib, 16384
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    lens = (torch.arange(n, device="cuda") * 7919 % 40 - 3).int()  # below 0: idle
+    rows = torch.ones(n, dtype=torch.int32, device="cuda") if form != "tiles" else torch.arange(n, device="cuda").int() % 3 * 20
+    page, per = 16, 6
+    k, v = (torch.randn(500, 1, page, 64, generator=gen, device="cuda").half() for _ in range(2))
+    tables = torch.randint(500, (n, per), generator=gen, device="cuda").int()
+    starts = torch.cat((torch.zeros(1, dtype=torch.int32, device="cuda"), rows.cumsum(0).int()))
+    total = int(starts[-1])
+    q = torch.randn(total, 2, 64, generator=gen, device="cuda").half()
+    out, pool = torch.full_like(q, 7.0), vt.make_paged_pool(k, v)
+    batch = vt.make_paged_batch(tables, lens, None if form == "decode" else starts)
+    (vt.vt_paged_decode if form == "decode" else vt.vt_paged_prefill)(paged, pool, batch, q, out)
+    assert vt.vt_paged_status(paged) == 0
+    # every row padded to the table, in 64 bits, some thousands at a time
+    row = torch.arange(total, device="cuda")
+    seq = torch.searchsorted(starts.long(), row, right=True) - 1
+    at = lens.long()[seq] + row - starts.long()[seq]
+    pos = torch.arange(per * page, device="cuda")
+    u = U["f16"]
+    for part in torch.split(row, 8192):
+        b = seq[part]
+        sees = (pos <= at[part][:, None]) & (lens[b] >= 0)[:, None]
+        kk, vv = (t[tables[b].long()].squeeze(2).reshape(len(b), per * page, 64).double() for t in (k, v))
+        s = torch.einsum("rhd,rpd->rhp", q[part].double(), kk) / 8
+        w = torch.softmax(s.masked_fill(~sees[:, None], -math.inf), -1).nan_to_num(0.0)
+        o, a = w @ vv, w @ vv.abs()
+        far = (out[part].double() - o).abs()
+        assert (far <= u * o.abs() + (u + 2.0 ** -16) * a + 100 * 2.0 ** -25 * 6).all()
+
+
+def test_append_as_many_sequences_as_a_batch_takes(vtlib, paged):
+    vt, n = vtlib, 16384
+    lens = (torch.arange(n, device="cuda") * 7919 % 16 - 1).int()
+    rows = (torch.arange(n, device="cuda") % 2).int()
+    starts = torch.cat((torch.zeros(1, dtype=torch.int32, device="cuda"), rows.cumsum(0).int()))
+    total = int(starts[-1])
+    k, v = (torch.zeros(n, 1, 16, 64, dtype=torch.float16, device="cuda") for _ in range(2))
+    tables = torch.randperm(n, device="cuda").int()[:, None].contiguous()
+    x = torch.randn(total, 3, 64, device="cuda").half()
+    rope = torch.empty(16, 32, 2, device="cuda")
+    vt.vt_rope_table(rope, 1e4)
+    q_out = torch.full((total, 1, 64), 7.0, dtype=torch.float16, device="cuda")
+    vt.vt_paged_append(paged, vt.make_paged_pool(k, v), vt.make_paged_batch(tables, lens, starts), x[:, :1], x[:, 1:2],
+                       x[:, 2:], rope, q_out)
+    assert vt.vt_paged_status(paged) == 0
+    b = torch.arange(1, n, 2, device="cuda")
+    live = b[lens[b] >= 0]
+    want = torch.zeros_like(v)
+    want[tables[live, 0].long(), 0, lens[live].long()] = x[(live - 1) // 2, 2]
+    assert torch.equal(v, want)
+    assert not q_out[(lens[b] < 0)].any() and q_out[lens[b] >= 0].any(-1).all()
