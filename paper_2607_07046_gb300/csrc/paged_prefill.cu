@@ -63,8 +63,9 @@ constexpr int kPfUnitCost = 2;
 // split then.)
 constexpr int kPfMinBlocks = 4, kPfWhole = 8;
 // Units of this many parts or more on average are joined by a kernel of its own.  Measured, by the last CTA and by a
-// kernel: 38 parts 63 and 47 us (32 rows behind 30000, 2 sequences of 2 KV heads), 9 parts 35 and 26, 5 parts 38 and 40,
-// 2 parts 156 and 162 (a kernel adds its launch, and joins that would have been hidden behind other CTAs' work).
+// kernel: 38 parts 63 and 47 us (32 rows behind 30000, 2 sequences of 2 KV heads), 9 parts 37 and 29 (100 rows behind 3000,
+// 8 KV heads of 4), 7 parts 37 and 32, 6 parts 38 and 36, 5 parts 40 and 38 (150 rows behind 3000; 7, 8 and 10 KV heads of
+// 4), 2 parts 156 and 162 (a kernel adds its launch, and joins that would have been hidden behind other CTAs' work).
 constexpr int kPfJoinParts = 5;
 // Parts that the joining CTA reads at once; most units have two (with 4 at once: 45 us for 5 prompts instead of 42).
 constexpr int kPfJoinChunk = 2;
