@@ -2348,8 +2348,8 @@ vt_status paged_attn(vt_paged* g, const vt_paged_pool* pool, const vt_paged_batc
     a->q_ld = n_rows > 1 ? q_ld : 0;
     a->kpool = static_cast<const uint16_t*>(pool->k);
     a->vpool = static_cast<const uint16_t*>(pool->v);
-    // (not 0: a hidden score is -inf, and its product with the scale has to be -inf too)
-    a->scale_log2 = std::max(scale * 1.4426950408889634f, std::numeric_limits<float>::min());
+    // (neither 0 nor infinite: a hidden score is -inf, and its product with the scale has to be -inf too; that of 0 is 0)
+    a->scale_log2 = std::min(std::max(scale * 1.4426950408889634f, std::numeric_limits<float>::min()), std::numeric_limits<float>::max());
     a->window = window;
     a->out = static_cast<uint16_t*>(out);
     a->out_ld = n_rows > 1 ? out_ld : 0;

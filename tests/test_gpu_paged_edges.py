@@ -274,3 +274,17 @@ def test_append_as_many_sequences_as_a_batch_takes(vtlib, paged):
     want[tables[live, 0].long(), 0, lens[live].long()] = x[(live - 1) // 2, 2]
     assert torch.equal(v, want)
     assert not q_out[(lens[b] < 0)].any() and q_out[lens[b] >= 0].any(-1).all()
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("scale", [2.0 ** 127, 3.4e38, 1e-45, 1e-39])
+def test_the_largest_and_smallest_scales(vtlib, paged, form, scale):
+    """Scores of 0 weigh the same at every scale that the call takes; any scores do at the smallest."""
+    rows = [600, 3] if form == "tiles" else [1, 1]
+    c = Cache(vtlib, [50, 300], rows, "f16", 8, 64, 16)
+    q = c.rows(16)
+    if scale > 1:
+        q.zero_()
+    out = attend(vtlib, paged, c, form, q, scale, 0)
+    ref, tol = attention(c, q, 0.0, 0)
+    assert ((out.double() - ref).abs() <= tol).all()
