@@ -580,12 +580,13 @@ VT_API vt_status vt_prefill_tokens(const vt_partition* part, vt_kv* kv, const vo
  *
  * Nothing about the lengths or tables is known on the host, so all three calls can be captured into
  * a CUDA graph.  What only a kernel can see sets bits in the status word of the vt_paged
- * (vt_paged_status), and the offending entry is skipped: VT_DEV_KV_OVERFLOW for a position at or past
- * pages_per_seq * page_size (or past the rotation table), VT_DEV_BAD_PAGE for a page id outside
- * [0, n_pages) where a page is needed.  starts outside [0, n_rows] are clamped into it.  Entries of
- * a table past a sequence's last page, and pool entries that no sequence holds, are never used and
- * may hold anything.  The same call gives the same bits every time; the last bits of a row's attention
- * may change with the other sequences of the batch, whose lengths decide how its sums are cut.
+ * (vt_paged_status), and the offending entry is skipped: VT_DEV_KV_OVERFLOW for a new row at or past
+ * position pages_per_seq * page_size (vt_paged_append: or past the rotation table), which attends to what
+ * its window has of the table; VT_DEV_BAD_PAGE for a page id outside [0, n_pages) where a page is needed.
+ * starts outside [0, n_rows] are clamped into it.  Entries of a table past a sequence's last page, and
+ * pool entries that no sequence holds, are never used and may hold anything.  The same call gives the
+ * same bits every time; the last bits of a row's attention may change with the other sequences of the
+ * batch, whose lengths decide how its sums are cut.
  * Errors of all: VT_ERR_INVALID_ARG (null pointers, sizes out of range, a pointer that is not 16-byte
  * aligned, a stride that is not a multiple of 8 elements), VT_ERR_SHAPE (unsupported dtype, d_head,
  * page_size or heads), before anything is enqueued. */
@@ -648,7 +649,9 @@ VT_API vt_status vt_paged_append(vt_paged* paged, const vt_paged_pool* pool, con
  * (window 0: [0, p]):
  *   out[b][h] = sum_j softmax_j(scale * q[b][h] . k_j) v_j.
  * q, out [n_seqs][n_heads][d_head], rows q_ld / out_ld elements apart.  n_heads: a multiple of
- * n_kv_heads, at most 128 times it.  scale: finite, >= 0. */
+ * n_kv_heads, at most 128 times it.  scale: finite, >= 0.
+ * Weights meet v as two terms of the pool's dtype, so the output's one rounding is what counts.  An
+ * infinity in v at an attended position makes the outputs of its dimension infinite or NaN. */
 VT_API vt_status vt_paged_decode(vt_paged* paged, const vt_paged_pool* pool, const vt_paged_batch* batch,
                                  int32_t n_heads, const void* q, int64_t q_ld, float scale, int32_t window, void* out,
                                  int64_t out_ld, vt_stream stream);
@@ -656,6 +659,9 @@ VT_API vt_status vt_paged_decode(vt_paged* paged, const vt_paged_pool* pool, con
 /* vt_paged_prefill (Section 2.1, prefill phase): the same attention for any number of new rows per
  * sequence; row i of sequence b attends over [max(0, p - window + 1), p], p = lens[b] + i.  Rows
  * outside every sequence are left alone.
+ * A sequence of few rows goes as in vt_paged_decode; with more, its weights meet v rounded once to the
+ * pool's dtype (fp16: to no coarser steps than 2^-31 of the row's largest).  Which way a sequence goes may
+ * depend on the batch (its rows altogether, n_seqs, the tables' width).
  * Rows go through matrix products together, so a NaN or infinity in v at a position that one new row of
  * a sequence attends to may also reach other new rows of that sequence that do not (0 times it is NaN);
  * it reaches no other sequence. */
