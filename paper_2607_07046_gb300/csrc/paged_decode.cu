@@ -108,7 +108,7 @@ struct PdSeq {
         if (ROWS) {
             row0 = paged_start(a.c, b, a.n_rows);
             rows = max(0, paged_start(a.c, b + 1, a.n_rows) - row0);
-            over = rows > a.rows_most;  // the next launch's
+            over = rows > a.rows_most && len >= 0;  // the next launch's (idle slots' zeros are this one's)
             if (over) rows = 0;
         }
         end = len < 0 || rows == 0 ? 0 : min(len + rows, a.c.cap);
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
         s.open<ROWS>(a, b, COLS);
         if (blockIdx.x == 0 && s.rows > 0 && s.len >= 0 && s.len + s.rows > c.cap) set_status(c.status, VT_DEV_KV_OVERFLOW);
         idle |= s.steps == 0 && !s.over;
-        over |= s.over && s.len >= 0;
+        over |= s.over;
         largest = max(largest, s.steps);
         mine += s.cost();
     }

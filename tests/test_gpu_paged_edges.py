@@ -288,3 +288,14 @@ def test_the_largest_and_smallest_scales(vtlib, paged, form, scale):
     out = attend(vtlib, paged, c, form, q, scale, 0)
     ref, tol = attention(c, q, 0.0, 0)
     assert ((out.double() - ref).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("wide", [False, True])
+def test_an_idle_slot_of_many_rows_among_tokens(vtlib, paged, wide):
+    """Idle slots get zeros whichever kernels the batch goes to, also when no sequence has rows enough for the tiles'."""
+    n = 60
+    lens, rows = [1500 + 7 * i for i in range(n)], [1 + i % 2 for i in range(n)]
+    lens[3], rows[3] = -1, 194
+    lens[50], rows[50] = -1, 25
+    c = Cache(vtlib, lens, rows, "bf16", 8, 64, 128, "pos")
+    check_attention(vtlib, paged, widened(c) if wide else c, "prefill", 16)
