@@ -119,12 +119,23 @@ cudaError_t init_library() {
         g_init_err = init_token_kernels();
         if (g_init_err != cudaSuccess) return;
         g_init_err = init_quant_kernels();
-        if (g_init_err != cudaSuccess) return;
-        g_init_err = init_paged_decode();
-        if (g_init_err != cudaSuccess) return;
-        init_paged_prefill();  // (the calls that need it say when it cannot run)
     });
     return g_init_err;
+}
+
+// The paged kernels are set up by the first vt_paged_create: a process that has none does not load them.
+std::once_flag g_init_paged_once;
+cudaError_t g_init_paged_err = cudaSuccess;
+
+cudaError_t init_paged() {
+    std::call_once(g_init_paged_once, [] {
+        g_init_paged_err = init_library();
+        if (g_init_paged_err != cudaSuccess) return;
+        g_init_paged_err = init_paged_decode();
+        if (g_init_paged_err != cudaSuccess) return;
+        init_paged_prefill();  // (the calls that need it say when it cannot run)
+    });
+    return g_init_paged_err;
 }
 
 }  // namespace
@@ -2221,7 +2232,7 @@ extern "C" vt_status vt_paged_create(const vt_allocator* allocator, vt_stream st
     *out = nullptr;
     if (allocator && (!allocator->alloc || !allocator->free))
         return fail(VT_ERR_INVALID_ARG, "allocator callbacks must not be NULL");
-    VT_CUDA(init_library());
+    VT_CUDA(init_paged());
     cudaStream_t st = (cudaStream_t)stream;
     vt_paged* g = new vt_paged();
     if (allocator) {
