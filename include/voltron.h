@@ -669,6 +669,77 @@ VT_API vt_status vt_paged_prefill(vt_paged* paged, const vt_paged_pool* pool, co
                                   int32_t n_rows, int32_t n_heads, const void* q, int64_t q_ld, float scale,
                                   int32_t window, void* out, int64_t out_ld, vt_stream stream);
 
+/* ---- norms of queries and keys, other rotations, pools in 8 bits ----
+ * The paged calls for models whose heads are normalised or rotated otherwise, and for caches in half
+ * the memory.  What is said above of batches, rows, errors, status bits, idle slots, graphs and
+ * repeatability holds for them too. */
+typedef enum { VT_ROPE_HALVES = 0, VT_ROPE_NEIGHBOURS = 1 } vt_rope_pairs; /* (i, i + rotary_dim / 2); (2i, 2i + 1) */
+
+/* What a row's queries and keys go through before they are stored (Section 2.1, the projections'
+ * heads), in fp32 and head by head:
+ *   x = x / sqrt(mean(x^2) + eps) * gain     with a gain; NULL: x stays
+ *   (a, b) = (a cos - b sin, b cos + a sin)  for each pair i of the first rotary_dim dimensions, with
+ *                                            (cos, sin) = rope[position][i]; the others stay
+ * Values are left as they are: gains and rope are read by the kernels of each call. */
+typedef struct {
+    const void *q_gain, *k_gain; /* device [d_head] of the rows' dtype, 16-byte aligned, or NULL */
+    const float* rope;           /* device fp32 [rope_len][rotary_dim / 2][2]; not used with rotary_dim 0 */
+    int32_t rope_len;
+    int32_t rotary_dim;          /* a multiple of 16, at most d_head; 0: no rotation */
+    int32_t pairs;               /* vt_rope_pairs */
+    float eps;                   /* finite, >= 0 */
+} vt_qk_form;
+
+/* vt_paged_append_qk (Section 2.1, decode and prefill phases: K/V written to the cache): as
+ * vt_paged_append, with the rows' queries and keys through `form`.  VT_ERR_SHAPE for a rotary_dim
+ * that it does not take. */
+VT_API vt_status vt_paged_append_qk(vt_paged* paged, const vt_paged_pool* pool, const vt_paged_batch* batch,
+                                    int32_t n_rows, int32_t n_heads, const void* q, int64_t q_ld, const void* k,
+                                    int64_t k_ld, const void* v, int64_t v_ld, const vt_qk_form* form, void* q_out,
+                                    int64_t q_out_ld, vt_stream stream);
+
+/* A pool whose entries are codes of 8 bits with a scale for each 32 dimensions, a power of two: byte s
+ * stands for 2^(s - 127), and a value is code * 2^(s - 127).  Codes are e4m3 floats (largest 448) or
+ * whole numbers in two's complement (-127 .. 127).
+ * The append takes the least power of two with which the largest code is at least as large as every
+ * magnitude of the 32, so nothing saturates, and rounds to the nearest code, ties to even.  Powers
+ * stay where every value of an entry is one of the rows' type: in [-15, 7] (e4m3) and [-24, 9] (int8)
+ * for fp16, [-117, 7] and [-117, 119] for bf16; magnitudes past the largest (57344; 65024 or 127 2^119)
+ * become it.  32 dimensions with an infinity or a NaN are stored as NaN (s = 255, codes 0).  A pool
+ * that another program fills may hold any codes (e4m3's NaN codes read as +-480) and any scales in
+ * those ranges. */
+typedef enum { VT_MX_E4M3 = 0, VT_MX_INT8 = 1 } vt_mx_format;
+typedef struct {
+    void *k, *v;                 /* codes, a byte each; entry (page, head, position) as in vt_paged_pool */
+    void *k_scale, *v_scale;     /* scales: entry (page, head, position) has its d_head / 32 bytes at
+                                  * page * scale_page_stride + head * scale_head_stride + position * (d_head / 32) */
+    int32_t dtype;               /* vt_dtype of q, k, v and out */
+    int32_t format;              /* vt_mx_format */
+    int32_t n_pages;
+    int32_t page_size;           /* positions per page, a power of two in [8, 1024] */
+    int32_t n_kv_heads;
+    int32_t d_head;              /* 64 or 128 */
+    int64_t page_stride, head_stride, pos_stride;       /* bytes, multiples of 16 */
+    int64_t scale_page_stride, scale_head_stride;       /* bytes, multiples of 16 */
+} vt_paged_mx_pool;
+
+/* vt_paged_append_mx: as vt_paged_append_qk, into a pool in 8 bits.  v is stored as it is, queries stay
+ * in the rows' type; keys are rounded once, to their codes. */
+VT_API vt_status vt_paged_append_mx(vt_paged* paged, const vt_paged_mx_pool* pool, const vt_paged_batch* batch,
+                                    int32_t n_rows, int32_t n_heads, const void* q, int64_t q_ld, const void* k,
+                                    int64_t k_ld, const void* v, int64_t v_ld, const vt_qk_form* form, void* q_out,
+                                    int64_t q_out_ld, vt_stream stream);
+
+/* vt_paged_decode_mx, vt_paged_prefill_mx (Section 2.1, decode and prefill phases): as vt_paged_decode and
+ * vt_paged_prefill, over a pool in 8 bits.  K and V are the values that the entries stand for, exactly;
+ * nothing else is rounded than over a pool in 16 bits that holds these values. */
+VT_API vt_status vt_paged_decode_mx(vt_paged* paged, const vt_paged_mx_pool* pool, const vt_paged_batch* batch,
+                                    int32_t n_heads, const void* q, int64_t q_ld, float scale, int32_t window,
+                                    void* out, int64_t out_ld, vt_stream stream);
+VT_API vt_status vt_paged_prefill_mx(vt_paged* paged, const vt_paged_mx_pool* pool, const vt_paged_batch* batch,
+                                     int32_t n_rows, int32_t n_heads, const void* q, int64_t q_ld, float scale,
+                                     int32_t window, void* out, int64_t out_ld, vt_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -133,7 +133,12 @@ cudaError_t init_paged() {
         if (g_init_paged_err != cudaSuccess) return;
         g_init_paged_err = init_paged_decode();
         if (g_init_paged_err != cudaSuccess) return;
+        for (cudaError_t e : {init_paged_decode_e4m3(), init_paged_decode_int8()})
+            if (e != cudaSuccess) g_init_paged_err = e;
+        if (g_init_paged_err != cudaSuccess) return;
         init_paged_prefill();  // (the calls that need it say when it cannot run)
+        init_paged_prefill_e4m3();
+        init_paged_prefill_int8();
     });
     return g_init_paged_err;
 }
@@ -2371,6 +2376,34 @@ vt_status paged_attn(vt_paged* g, const vt_paged_pool* pool, const vt_paged_batc
     return VT_OK;
 }
 
+// Which kernels attend for several rows a sequence: that of single tokens, that of the tensor cores' tiles, or both.
+struct PagedWay {
+    bool tokens, tiles;
+};
+PagedWay paged_way(PagedAttnArgs* a, int n_seqs, int* over) {
+    // A few columns (rows times query heads of a group) per sequence: the kernel of single tokens, which streams K and V
+    // once for 16 of them; the tensor cores' tiles take 128.  (24 rows of 32 heads behind 300, 16 sequences: 48 us this
+    // way, 67 on the tiles; 32 rows of 20 heads behind 6000, 4 sequences: 81 and 72.)
+    // Or little work altogether, by the tables' width: that kernel starts sooner and spreads it over more SMs.  (8 KV heads
+    // of 4 query heads, one sequence: 30 rows 6 and 12 us, 50 behind 1000 20 and 28, 77 behind 300 17 and 19; 30 behind
+    // 5000, 70 steps a CTA, 35 and 26.)
+    // The host knows the columns of the whole batch only, and slots may have none: a few on average may be a prompt in one
+    // slot, which the first kernel would stream K and V for a tile of 16 columns at a time.  So a batch of a few columns on
+    // average goes to both kernels, and each takes the sequences that suit it by their own rows.  (One launch and two: 380
+    // rows behind 4000 in one of 64 slots, group of 4, 238 and 66 us; 3000 rows in one of 128 slots, no group, 1245 and 138;
+    // 300 rows behind 4000 beside 63 tokens, 346 and 248.  Where the second finds nothing it costs 2 to 5 us: 32 sequences
+    // of 4 rows 56 and 59, 256 of one row 171 and 175.  With 64 columns altogether a prompt hides four tiles at most.)
+    constexpr int kFewColumns = 24, kFewSteps = 32, kFewAltogether = 64;
+    const int64_t columns = (int64_t)a->n_rows * a->group;
+    const bool few = columns <= (int64_t)kFewColumns * n_seqs;
+    const bool all_few = (few && columns <= kFewAltogether) || paged_decode_line(*a, 16) <= (int64_t)kFewSteps * 2 * g_num_sms;
+    if (few && !all_few) {
+        a->rows_most = a->rows_over = kFewColumns / a->group;
+        a->over = over;
+    }
+    return {few || all_few, !all_few};
+}
+
 }  // namespace
 
 extern "C" vt_status vt_paged_append(vt_paged* g, const vt_paged_pool* pool, const vt_paged_batch* batch, int32_t n_rows,
@@ -2424,28 +2457,165 @@ extern "C" vt_status vt_paged_prefill(vt_paged* g, const vt_paged_pool* pool, co
     PagedAttnArgs a{};
     VT_TRY(paged_attn(g, pool, batch, n_rows, n_heads, q, q_ld, scale, window, out, out_ld, &a));
     if (a.n_rows == 0 || batch->n_seqs == 0) return ok();
-    // A few columns (rows times query heads of a group) per sequence: the kernel of single tokens, which streams K and V
-    // once for 16 of them; the tensor cores' tiles take 128.  (24 rows of 32 heads behind 300, 16 sequences: 48 us this
-    // way, 67 on the tiles; 32 rows of 20 heads behind 6000, 4 sequences: 81 and 72.)
-    // Or little work altogether, by the tables' width: that kernel starts sooner and spreads it over more SMs.  (8 KV heads
-    // of 4 query heads, one sequence: 30 rows 6 and 12 us, 50 behind 1000 20 and 28, 77 behind 300 17 and 19; 30 behind
-    // 5000, 70 steps a CTA, 35 and 26.)
-    // The host knows the columns of the whole batch only, and slots may have none: a few on average may be a prompt in one
-    // slot, which the first kernel would stream K and V for a tile of 16 columns at a time.  So a batch of a few columns on
-    // average goes to both kernels, and each takes the sequences that suit it by their own rows.  (One launch and two: 380
-    // rows behind 4000 in one of 64 slots, group of 4, 238 and 66 us; 3000 rows in one of 128 slots, no group, 1245 and 138;
-    // 300 rows behind 4000 beside 63 tokens, 346 and 248.  Where the second finds nothing it costs 2 to 5 us: 32 sequences
-    // of 4 rows 56 and 59, 256 of one row 171 and 175.  With 64 columns altogether a prompt hides four tiles at most.)
-    constexpr int kFewColumns = 24, kFewSteps = 32, kFewAltogether = 64;
-    const int64_t columns = (int64_t)n_rows * a.group;
-    const bool few = columns <= (int64_t)kFewColumns * batch->n_seqs;
-    const bool all_few = (few && columns <= kFewAltogether) || paged_decode_line(a, 16) <= (int64_t)kFewSteps * 2 * g_num_sms;
-    if (const char* e = all_few ? nullptr : paged_tiles_error()) return fail(VT_ERR_CUDA, "%s", e);
-    if (few && !all_few) {
-        a.rows_most = a.rows_over = kFewColumns / a.group;
-        a.over = g->over;
+    const PagedWay way = paged_way(&a, batch->n_seqs, g->over);
+    if (const char* e = way.tiles ? paged_tiles_error() : nullptr) return fail(VT_ERR_CUDA, "%s", e);
+    if (way.tokens) VT_CUDA(launch_paged_decode(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
+    if (way.tiles) VT_CUDA(launch_paged_prefill(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
+    return ok();
+}
+
+// ------------------------------------------------------------------ norms and other rotations; pools in 8 bits
+namespace {
+
+vt_status paged_qk_form(const vt_qk_form* f, int dh, PagedQkArgs* a) {
+    if (!f) return fail(VT_ERR_INVALID_ARG, "form must not be NULL");
+    if (f->rotary_dim < 0 || f->rotary_dim > dh || f->rotary_dim % 16)
+        return fail(VT_ERR_SHAPE, "rotary_dim %d must be a multiple of 16 in [0, d_head]", f->rotary_dim);
+    if (f->pairs != VT_ROPE_HALVES && f->pairs != VT_ROPE_NEIGHBOURS) return fail(VT_ERR_INVALID_ARG, "unknown pairs %d", f->pairs);
+    if (f->rotary_dim > 0) {
+        if (f->rope_len < 1) return fail(VT_ERR_INVALID_ARG, "rope_len must be >= 1");
+        if (!f->rope || !aligned16(f->rope)) return fail(VT_ERR_INVALID_ARG, "rope must be 16-byte aligned and not NULL");
     }
-    if (few || all_few) VT_CUDA(launch_paged_decode(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
-    if (!all_few) VT_CUDA(launch_paged_prefill(a, pool->dtype, pool->d_head, (cudaStream_t)stream));
+    if ((f->q_gain && !aligned16(f->q_gain)) || (f->k_gain && !aligned16(f->k_gain)))
+        return fail(VT_ERR_INVALID_ARG, "q_gain and k_gain must be 16-byte aligned");
+    if (!std::isfinite(f->eps) || f->eps < 0.f) return fail(VT_ERR_INVALID_ARG, "eps must be finite and >= 0");
+    a->q_gain = static_cast<const uint16_t*>(f->q_gain);
+    a->k_gain = static_cast<const uint16_t*>(f->k_gain);
+    a->eps = f->eps;
+    a->rope = reinterpret_cast<const float2*>(f->rope);
+    a->rope_len = f->rope_len;
+    a->rotary = f->rotary_dim;
+    a->neighbours = f->pairs == VT_ROPE_NEIGHBOURS;
+    return VT_OK;
+}
+
+// The rules of a pool in 8 bits; the pool with its codes as values, whose rules are the same otherwise.
+vt_status paged_mx_pool(const vt_paged_mx_pool* p, vt_paged_pool* as) {
+    if (!p) return fail(VT_ERR_INVALID_ARG, "paged, pool and batch must not be NULL");
+    if (p->format != VT_MX_E4M3 && p->format != VT_MX_INT8) return fail(VT_ERR_SHAPE, "unknown format %d", p->format);
+    if (p->d_head != 64 && p->d_head != 128) return fail(VT_ERR_SHAPE, "d_head must be 64 or 128 (got %d)", p->d_head);
+    if (p->page_size < 8 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)))
+        return fail(VT_ERR_SHAPE, "page_size must be a power of two in [8, 1024] (got %d)", p->page_size);
+    if (!p->k_scale || !p->v_scale || !aligned16(p->k_scale) || !aligned16(p->v_scale))
+        return fail(VT_ERR_INVALID_ARG, "the pool's k_scale and v_scale must be 16-byte aligned and not NULL");
+    const struct { int64_t stride; bool used; const char* what; } strides[3] = {
+        {p->page_stride, p->n_pages > 1, "page"}, {p->head_stride, p->n_kv_heads > 1, "head"}, {p->pos_stride, true, "pos"}};
+    for (const auto& s : strides)
+        if (s.used && s.stride % 16) return fail(VT_ERR_INVALID_ARG, "%s_stride %lld must be a multiple of 16", s.what, (long long)s.stride);
+    const int64_t least = (int64_t)p->page_size * (p->d_head / 32);
+    const struct { int64_t stride; bool used; const char* what; } scales[2] = {
+        {p->scale_page_stride, p->n_pages > 1, "page"}, {p->scale_head_stride, p->n_kv_heads > 1, "head"}};
+    for (const auto& s : scales)
+        if (s.used && (s.stride < least || s.stride % 16 || s.stride > ((int64_t)1 << 40)))
+            return fail(VT_ERR_INVALID_ARG, "scale_%s_stride %lld must be a multiple of 16, at least %lld and at most 2^40", s.what,
+                        (long long)s.stride, (long long)least);
+    *as = {p->k, p->v, p->dtype, p->n_pages, p->page_size, p->n_kv_heads, p->d_head, p->page_stride, p->head_stride, p->pos_stride};
+    return VT_OK;
+}
+
+vt_status paged_append_qk(vt_paged* g, const vt_paged_pool* pool, const vt_paged_batch* batch, int n_rows, int n_heads,
+                          const void* q, int64_t q_ld, const void* k, int64_t k_ld, const void* v, int64_t v_ld,
+                          const vt_qk_form* form, void* q_out, int64_t q_out_ld, PagedQkArgs* a) {
+    VT_TRY(paged_view(g, pool, batch, &a->c));
+    VT_TRY(paged_n_rows(batch, n_rows));
+    VT_TRY(paged_heads(pool, n_heads));
+    VT_TRY(paged_qk_form(form, pool->d_head, a));
+    if (n_rows == 0 || batch->n_seqs == 0) return VT_OK;
+    const int dh = pool->d_head, hk = pool->n_kv_heads;
+    VT_TRY(paged_rows("q", q, q_ld, n_rows, n_heads, dh));
+    VT_TRY(paged_rows("k", k, k_ld, n_rows, hk, dh));
+    VT_TRY(paged_rows("v", v, v_ld, n_rows, hk, dh));
+    VT_TRY(paged_rows("q_out", q_out, q_out_ld, n_rows, n_heads, dh));
+    a->n_rows = n_rows;
+    a->n_heads = n_heads;
+    a->q = static_cast<const uint16_t*>(q);
+    a->k = static_cast<const uint16_t*>(k);
+    a->v = static_cast<const uint16_t*>(v);
+    a->q_ld = n_rows > 1 ? q_ld : 0;
+    a->k_ld = n_rows > 1 ? k_ld : 0;
+    a->v_ld = n_rows > 1 ? v_ld : 0;
+    a->q_out = static_cast<uint16_t*>(q_out);
+    a->q_out_ld = n_rows > 1 ? q_out_ld : 0;
+    a->kpool = pool->k;
+    a->vpool = pool->v;
+    return VT_OK;
+}
+
+vt_status paged_attn_mx(vt_paged* g, const vt_paged_mx_pool* pool, const vt_paged_batch* batch, int n_rows, int n_heads,
+                        const void* q, int64_t q_ld, float scale, int window, void* out, int64_t out_ld, PagedAttnArgs* a) {
+    vt_paged_pool as;
+    VT_TRY(paged_mx_pool(pool, &as));
+    VT_TRY(paged_attn(g, &as, batch, n_rows, n_heads, q, q_ld, scale, window, out, out_ld, a));
+    a->kscale = static_cast<const uint8_t*>(pool->k_scale);
+    a->vscale = static_cast<const uint8_t*>(pool->v_scale);
+    a->scale_page = pool->n_pages > 1 ? pool->scale_page_stride : 0;
+    a->scale_head = pool->n_kv_heads > 1 ? pool->scale_head_stride : 0;
+    return VT_OK;
+}
+
+cudaError_t launch_decode_mx(const PagedAttnArgs& a, const vt_paged_mx_pool* pool, cudaStream_t st) {
+    return pool->format == VT_MX_E4M3 ? launch_paged_decode_e4m3(a, pool->dtype, pool->d_head, st)
+                                      : launch_paged_decode_int8(a, pool->dtype, pool->d_head, st);
+}
+
+}  // namespace
+
+extern "C" vt_status vt_paged_append_qk(vt_paged* g, const vt_paged_pool* pool, const vt_paged_batch* batch, int32_t n_rows,
+                                        int32_t n_heads, const void* q, int64_t q_ld, const void* k, int64_t k_ld,
+                                        const void* v, int64_t v_ld, const vt_qk_form* form, void* q_out, int64_t q_out_ld,
+                                        vt_stream stream) {
+    PagedQkArgs a{};
+    VT_TRY(paged_append_qk(g, pool, batch, n_rows, n_heads, q, q_ld, k, k_ld, v, v_ld, form, q_out, q_out_ld, &a));
+    if (a.n_rows == 0) return ok();
+    VT_CUDA(launch_paged_append_qk(a, pool->dtype, -1, pool->d_head, (cudaStream_t)stream));
+    return ok();
+}
+
+extern "C" vt_status vt_paged_append_mx(vt_paged* g, const vt_paged_mx_pool* pool, const vt_paged_batch* batch, int32_t n_rows,
+                                        int32_t n_heads, const void* q, int64_t q_ld, const void* k, int64_t k_ld,
+                                        const void* v, int64_t v_ld, const vt_qk_form* form, void* q_out, int64_t q_out_ld,
+                                        vt_stream stream) {
+    PagedQkArgs a{};
+    vt_paged_pool as;
+    VT_TRY(paged_mx_pool(pool, &as));
+    VT_TRY(paged_append_qk(g, &as, batch, n_rows, n_heads, q, q_ld, k, k_ld, v, v_ld, form, q_out, q_out_ld, &a));
+    if (a.n_rows == 0) return ok();
+    a.kscale = static_cast<uint8_t*>(pool->k_scale);
+    a.vscale = static_cast<uint8_t*>(pool->v_scale);
+    a.scale_page = pool->n_pages > 1 ? pool->scale_page_stride : 0;
+    a.scale_head = pool->n_kv_heads > 1 ? pool->scale_head_stride : 0;
+    // Where every code times its scale is a value of the rows' type: fp16's smallest step is 2^-24, its largest value 65504.
+    // bf16 has as many exponents as fp32; e4m3's largest is the one whose scale the kernels can multiply by (MxCodes::scale).
+    const bool half = pool->dtype == VT_F16, e4m3 = pool->format == VT_MX_E4M3;
+    a.e_lo = half ? (e4m3 ? -15 : -24) : -117;
+    a.e_hi = e4m3 ? 7 : half ? 9 : 119;
+    VT_CUDA(launch_paged_append_qk(a, pool->dtype, pool->format, pool->d_head, (cudaStream_t)stream));
+    return ok();
+}
+
+extern "C" vt_status vt_paged_decode_mx(vt_paged* g, const vt_paged_mx_pool* pool, const vt_paged_batch* batch, int32_t n_heads,
+                                        const void* q, int64_t q_ld, float scale, int32_t window, void* out, int64_t out_ld,
+                                        vt_stream stream) {
+    if (batch && batch->starts) return fail(VT_ERR_INVALID_ARG, "vt_paged_decode_mx takes one row per sequence: starts must be NULL");
+    PagedAttnArgs a{};
+    VT_TRY(paged_attn_mx(g, pool, batch, batch ? batch->n_seqs : 0, n_heads, q, q_ld, scale, window, out, out_ld, &a));
+    if (a.n_rows == 0) return ok();
+    VT_CUDA(launch_decode_mx(a, pool, (cudaStream_t)stream));
+    return ok();
+}
+
+extern "C" vt_status vt_paged_prefill_mx(vt_paged* g, const vt_paged_mx_pool* pool, const vt_paged_batch* batch, int32_t n_rows,
+                                         int32_t n_heads, const void* q, int64_t q_ld, float scale, int32_t window, void* out,
+                                         int64_t out_ld, vt_stream stream) {
+    PagedAttnArgs a{};
+    VT_TRY(paged_attn_mx(g, pool, batch, n_rows, n_heads, q, q_ld, scale, window, out, out_ld, &a));
+    if (a.n_rows == 0 || batch->n_seqs == 0) return ok();
+    const PagedWay way = paged_way(&a, batch->n_seqs, g->over);
+    const bool e4m3 = pool->format == VT_MX_E4M3;
+    if (const char* e = !way.tiles ? nullptr : e4m3 ? paged_tiles_error_e4m3() : paged_tiles_error_int8()) return fail(VT_ERR_CUDA, "%s", e);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (way.tokens) VT_CUDA(launch_decode_mx(a, pool, st));
+    if (way.tiles)
+        VT_CUDA(e4m3 ? launch_paged_prefill_e4m3(a, pool->dtype, pool->d_head, st) : launch_paged_prefill_int8(a, pool->dtype, pool->d_head, st));
     return ok();
 }

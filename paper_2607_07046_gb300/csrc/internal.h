@@ -308,12 +308,30 @@ struct PagedAppendArgs {
     int64_t q_out_ld;
     uint16_t *kpool, *vpool;
 };
+struct PagedQkArgs {
+    PagedView c;                // (8 bits: strides in bytes)
+    int n_rows, n_heads;
+    const uint16_t *q, *k, *v;  // rows q_ld, k_ld, v_ld elements apart
+    int64_t q_ld, k_ld, v_ld;
+    const uint16_t *q_gain, *k_gain;  // [dh], or nullptr: no norm
+    float eps;
+    const float2* rope;         // [rope_len][rotary / 2]
+    int rope_len, rotary, neighbours;
+    uint16_t* q_out;
+    int64_t q_out_ld;
+    void *kpool, *vpool;        // 16-bit values, or codes with scales
+    uint8_t *kscale, *vscale;
+    int64_t scale_page, scale_head;
+    int e_lo, e_hi;             // exponents that a scale may have
+};
 struct PagedAttnArgs {
     PagedView c;
     int n_rows, n_heads, group;
     const uint16_t* q;
     int64_t q_ld;
-    const uint16_t *kpool, *vpool;
+    const uint16_t *kpool, *vpool;  // 8 bits: codes, strides of the view in bytes, and their scales
+    const uint8_t *kscale, *vscale;
+    int64_t scale_page, scale_head;
     float scale_log2;           // scale * log2(e)
     int window;
     uint16_t* out;
@@ -334,12 +352,24 @@ constexpr int64_t kPagedPrefillSlot = 2 * 128 + 128 * 128;   // floats: (m, l) a
 constexpr int kPagedMaxSeqs = 16384;                         // sequences of a batch
 size_t paged_work_floats();
 cudaError_t launch_paged_append(const PagedAppendArgs& a, int dtype, int dh, cudaStream_t st);
+cudaError_t launch_paged_append_qk(const PagedQkArgs& a, int dtype, int format, int dh, cudaStream_t st);  // format -1: 16 bits
 cudaError_t launch_paged_decode(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st);
 int64_t paged_decode_line(const PagedAttnArgs& a, int cols);
 cudaError_t launch_paged_prefill(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st);
 cudaError_t init_paged_decode();
 void init_paged_prefill();
 const char* paged_tiles_error();  // why launch_paged_prefill cannot run in this build; nullptr: it can
+// the same over pools in 8 bits
+cudaError_t launch_paged_decode_e4m3(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st);
+cudaError_t launch_paged_decode_int8(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st);
+cudaError_t init_paged_decode_e4m3();
+cudaError_t init_paged_decode_int8();
+cudaError_t launch_paged_prefill_e4m3(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st);
+cudaError_t launch_paged_prefill_int8(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st);
+void init_paged_prefill_e4m3();
+void init_paged_prefill_int8();
+const char* paged_tiles_error_e4m3();
+const char* paged_tiles_error_int8();
 
 // ------------------------------------------------------------------ static scratch
 // (static_scratch.cu) the decode step whose intermediates are in one file-scope __device__ array.

@@ -1,0 +1,126 @@
+// Entries of a paged pool in 8 bits: a code for each dimension and a scale for each 32 of them, the power of two
+// 2^(s - 127) of its byte s.  Codes are e4m3 or whole numbers (two's complement).
+//
+// A code times its scale is a value of the rows' type (exactly: a code has 8 significant bits at most, and the
+// append keeps the scales where no step falls below the type's), so the products of attention are those of a pool
+// that holds these values in 16 bits, and neither scores nor weights carry scales.  Byte 255 marks a block that held
+// an infinity or NaN: its scale is infinite and its codes are zeros, whose product is NaN.  Any codes are finite here
+// (e4m3's two NaN codes read as 480), so scale 0 hides whatever lies in entries that nothing attends to.
+#pragma once
+
+#include <cuda_fp8.h>
+
+#include "paged.cuh"
+
+namespace vt {
+
+constexpr int kMxBlock = 32;  // dimensions that share a scale
+
+template <class T>
+__device__ __forceinline__ uint32_t mx_mul(uint32_t a, uint32_t b) {
+    if constexpr (std::is_same<T, __half>::value) {
+        const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+        return *reinterpret_cast<const uint32_t*>(&r);
+    } else {
+        const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+        return *reinterpret_cast<const uint32_t*>(&r);
+    }
+}
+
+// Codes of format F (VT_MX_*) as pairs of values of type T.  two<S>(w): the bytes S & 15 and S >> 4 of w, to be
+// multiplied by scale(): e4m3 codes are moved to their places in T's bits (no conversion: their value is then less by
+// the difference of the exponents' biases, which the scale makes up for, subnormal codes included); whole numbers
+// come from the sums 1024 + u (fp16, u the code + 128) and 128 + low 7 bits (bf16), both exact.
+template <class T, int F>
+struct MxCodes {
+    static constexpr bool kHalf = std::is_same<T, __half>::value, kFloat = F == VT_MX_E4M3;
+
+    template <int S>
+    static __device__ __forceinline__ uint32_t two(uint32_t w) {
+        constexpr uint32_t lo = S & 15, hi = S >> 4;
+        if constexpr (kFloat) {
+            const uint32_t x = __byte_perm(w, 0u, 4u | (lo << 4) | (4u << 8) | (hi << 12));  // codes in the upper bytes
+            const uint32_t y = (x >> (kHalf ? 1 : 4)) & (kHalf ? 0x3f803f80u : 0x07f007f0u);
+            return (x & 0x80008000u) | y;
+        } else if constexpr (kHalf) {
+            const uint32_t x = __byte_perm(w ^ 0x80808080u, 0x64646464u, lo | (4u << 4) | (hi << 8) | (4u << 12));
+            const uint32_t k = 0x64806480u;  // 1152
+            const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&k));
+            return *reinterpret_cast<const uint32_t*>(&r);
+        } else {
+            const uint32_t x = __byte_perm(w, 0u, lo | (4u << 4) | (hi << 8) | (4u << 12));
+            const uint32_t a = (x & 0x007f007fu) | 0x43004300u, b = (x & 0x00800080u) | 0x43004300u;  // less 128, or 256 for a sign
+            const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+            return *reinterpret_cast<const uint32_t*>(&r);
+        }
+    }
+    // Two scales of bytes s0 and s1; byte 0 gives 0.
+    static __device__ __forceinline__ uint32_t scale(uint32_t s0, uint32_t s1) {
+        const uint32_t p = kHalf ? Elem<T>::pack(__uint_as_float(s0 << 23), __uint_as_float(s1 << 23)) : (s0 << 7) | (s1 << 23);
+        return kFloat ? mx_mul<T>(p, kHalf ? 0x5c005c00u : 0x7b807b80u) : p;  // 2^8, 2^120
+    }
+    static __device__ __forceinline__ uint32_t mul(uint32_t a, uint32_t s) { return mx_mul<T>(a, s); }
+};
+
+// What a pool holds: 16-bit values of type T, or 8-bit codes of format F that stand for values of type T.
+template <class E>
+struct PoolPlain {
+    using T = E;
+    static constexpr bool kMx = false;
+    static constexpr int kBytes = 2;  // of a value
+};
+template <class E, int F>
+struct PoolMx {
+    using T = E;
+    using C = MxCodes<E, F>;
+    static constexpr bool kMx = true;
+    static constexpr int kBytes = 1;
+};
+
+__device__ __forceinline__ uint4 lds128_at(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts128_at(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t addr) {
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+// The scale of a block whose largest magnitude has the bits `most` (of a float): the least E with 2^E times the
+// largest code at least as large, kept in [lo, hi].
+template <int F>
+__device__ __forceinline__ int mx_exponent(uint32_t most, int lo, int hi) {
+    const int e = (int)(most >> 23) - 127;
+    const uint32_t part = most & 0x7fffffu;
+    const int E = F == VT_MX_E4M3 ? e - 8 + (part > 0x600000u) : e - 6 + (part > 0x7e0000u);  // 448 = 1.75 2^8, 127 = 1.984375 2^6
+    return max(lo, min(hi, E));
+}
+// Four codes of values already divided by the scale, ties to even; what is past the largest code becomes it.
+template <int F>
+__device__ __forceinline__ uint32_t mx_codes(float a, float b, float c, float d) {
+    if constexpr (F == VT_MX_E4M3) {
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+        return lo | (hi << 16);
+    } else {
+        auto code = [](float x) { return (uint32_t)__float2int_rn(fminf(fmaxf(x, -127.f), 127.f)) & 0xffu; };
+        return code(a) | (code(b) << 8) | (code(c) << 16) | (code(d) << 24);
+    }
+}
+
+}  // namespace vt

@@ -42,7 +42,7 @@
 #include <algorithm>
 #include <climits>
 
-#include "paged.cuh"
+#include "paged_mx.cuh"
 #include "tcgen05.cuh"
 
 namespace vt {
@@ -71,12 +71,16 @@ constexpr int kPfJoinParts = 5;
 constexpr int kPfJoinChunk = 2;
 constexpr int kPfLag = 2;        // copy groups in flight behind the one just issued
 
-template <int DH>
+constexpr int kPfRawLag = 2;     // 8 bits: blocks of K or V whose codes are on their way while one is converted
+
+template <class Src, int DH>
 struct PfGeom {
     static constexpr int kTile = kPfRows * DH * 2;         // bytes of a Q tile, of a K or V block
     static constexpr int kAtom = kPfRows * 128;            // its 64-column box
-    static constexpr int kSlots = DH == 128 ? 5 : 10;      // K and V blocks of the ring, in turn
-    static constexpr size_t kSmem = 1024 + (size_t)(2 + kSlots) * kTile + 512 + kPfThreads / 32 * 64;
+    static constexpr int kSlots = (DH == 128 ? 1 : 2) * (Src::kMx ? 3 : 5);  // K and V blocks of the ring, in turn
+    static constexpr int kRaw = Src::kMx ? kPfKeys * (DH + DH / kMxBlock) : 0;  // codes and scales of a block
+    static constexpr int kRaws = kPfRawLag + 1;
+    static constexpr size_t kSmem = 1024 + (size_t)(2 + kSlots) * kTile + kRaws * kRaw + 512 + kPfThreads / 32 * 64;
 };
 
 // The units in order: sequence, KV head, tile pair.
@@ -193,19 +197,193 @@ struct PfParams {
     CUtensorMap tk, tv;   // [pages][KV heads][positions][dh], boxes of a page's positions (128 at most) by 64 columns
 };
 
+// The copy warps over a pool of codes: codes and scales come by asynchronous copies of 16 bytes (a lane's own codes, its
+// warp's scales), kPfRawLag blocks of K or V ahead, and are converted to the type of Q into the ring, as the tensor copies of a
+// 16-bit pool would leave them there.  Positions outside the unit's range and bad pages get scale 0, whose product with
+// any code is 0.  A page holds 8 positions or more, so a group of 8 rows lies in one.  False: a wait ran out.
+struct PfShared {
+    uint8_t *Qs, *Rs, *raw;
+    uint32_t* valid;
+    uint64_t *full, *empty, *q_full, *q_empty;
+};
+template <class Src, int DH>
+__device__ __forceinline__ bool pf_convert(const PfParams& P, const PfShared& m, PfCursor at, int64_t left) {
+    using G = PfGeom<Src, DH>;
+    using C = typename Src::C;
+    constexpr int S = G::kSlots, HALVES = DH / 64, NB = DH / kMxBlock;
+    constexpr int CPR = DH / 16, RPI = 32 / CPR, PASSES = 8 / RPI, GROUPS = 16 / kPfCopyWarps;  // passes of a group, a warp's groups
+    constexpr int SCALES = GROUPS * 8 * NB / 16;  // 16-byte pieces of a warp's scales
+    const PagedAttnArgs& a = P.a;
+    const PagedView& c = a.c;
+    const int tid = threadIdx.x, lane = tid & 31, w = (tid >> 5) - 8, tr = kPfRows / a.group;
+    const int chunk = lane % CPR, sub = lane / CPR;
+    const uint32_t raw0 = smem_u32(m.raw) + (uint32_t)((w * 32 + lane) * 16);
+    const uint32_t scl0 = smem_u32(m.raw) + (uint32_t)(kPfKeys * DH + w * (SCALES * 16));
+
+    // ---- the copies' own place in the line: K or V of block ld_j of unit ld
+    PfCursor ld = at;
+    int64_t ld_left = left;
+    int ld_j = 0, ld_end = 0, ld_blk = 0, ld_raw = 0;
+    bool ld_v = false, more = true;
+    auto open = [&]() {
+        for (;;) {
+            more = ld_left > 0;
+            if (!more) return;
+            int n;
+            ld_j = ld.kb0 + ld.part(ld_left, n);
+            ld_end = ld_j + n;
+            ld_left -= ld.rest();
+            if (n > 0) return;
+            ld.next(a, tr);
+        }
+    };
+    open();
+    int page = 0;       // lane g < 16: the page of 8-row group g of block ld_j, and which of its rows are attended to
+    uint32_t rows = 0;
+    auto issue = [&]() -> uint32_t {  // the lane's chunks that hold something
+        uint32_t on = 0;
+        if (more) {
+            const int p0 = ld_j * kPfKeys;
+            if (!ld_v) {
+                const int g0 = p0 + 8 * (lane & 15);
+                page = 0;
+                rows = fa_range_bits(ld.kbeg - g0, ld.kend - g0) & 0xffu;
+                if (rows) page = c.tables[(int64_t)ld.b * c.per_seq + (g0 >> c.page_shift)];
+                if ((unsigned)page >= (unsigned)c.n_pages) {
+                    rows = 0;
+                    page = 0;
+                    if (w == 0) set_status(c.status, VT_DEV_BAD_PAGE);
+                }
+                if (w == 0 && lane < 16) reinterpret_cast<uint8_t*>(m.valid)[(ld_blk % kPfMaskRing) * 16 + lane] = (uint8_t)rows;
+            }
+            const uint8_t* pool = reinterpret_cast<const uint8_t*>(ld_v ? a.vpool : a.kpool) + ld.kvh * c.head_stride + chunk * 16;
+            const uint32_t dst = raw0 + (uint32_t)(ld_raw * G::kRaw);
+#pragma unroll
+            for (int i = 0; i < GROUPS; ++i) {
+                const int g = w + i * kPfCopyWarps;
+                const int pg = __shfl_sync(0xffffffffu, page, g);
+                const uint32_t bits = __shfl_sync(0xffffffffu, rows, g) >> sub;
+                const uint8_t* src = pool + pg * c.page_stride + (((p0 + 8 * g) & (c.page_size - 1)) + sub) * c.pos_stride;
+#pragma unroll
+                for (int k = 0; k < PASSES; ++k) {
+                    const bool one = (bits >> (k * RPI)) & 1u;
+                    on |= (one ? 1u : 0u) << (i * PASSES + k);
+                    pf_copy16(dst + (uint32_t)((i * PASSES + k) * (kPfCopyWarps * 512)), src + k * RPI * c.pos_stride, one);
+                }
+            }
+            {
+                const int g = w + lane % SCALES * GROUPS / SCALES * kPfCopyWarps;
+                const int pg = __shfl_sync(0xffffffffu, page, g);
+                const bool any = __shfl_sync(0xffffffffu, rows, g) != 0;
+                const uint8_t* src = (ld_v ? a.vscale : a.kscale) + pg * a.scale_page + ld.kvh * a.scale_head +
+                                     ((p0 + 8 * g) & (c.page_size - 1)) * NB + lane % (SCALES / GROUPS) * 16;
+                if (lane < SCALES) pf_copy16(scl0 + (uint32_t)(ld_raw * G::kRaw + lane * 16), src, any);
+            }
+            ld_raw = ld_raw + 1 == G::kRaws ? 0 : ld_raw + 1;
+            if (ld_v) {
+                ++ld_blk;
+                if (++ld_j == ld_end) {
+                    ld.next(a, tr);
+                    open();
+                }
+            }
+            ld_v = !ld_v;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        return on;
+    };
+    uint32_t ons[kPfRawLag];
+#pragma unroll
+    for (int i = 0; i < kPfRawLag; ++i) ons[i] = issue();
+
+    // ---- the conversions, in the same order
+    bool ok = true;
+    int slot = 0, round = 0, from = 0, nq = 0;
+    while (ok && left > 0) {
+        int n;
+        const int j0 = at.kb0 + at.part(left, n);
+        left -= at.rest();
+        for (int x = 0; ok && x < 2 * n; ++x) {
+            const uint32_t last = issue(), on = ons[0];
+#pragma unroll
+            for (int i = 0; i + 1 < kPfRawLag; ++i) ons[i] = ons[i + 1];
+            ons[kPfRawLag - 1] = last;
+            asm volatile("cp.async.wait_group %0;" ::"n"(kPfRawLag) : "memory");
+            __syncwarp();  // the scales are other lanes' copies
+            if (round > 0) ok = pf_wait(&m.empty[slot], (round - 1) & 1);
+            if (!ok) break;
+            const uint32_t dst = smem_u32(m.Rs + slot * G::kTile), src = raw0 + (uint32_t)(from * G::kRaw);
+            const uint32_t scl = scl0 + (uint32_t)(from * G::kRaw + sub * NB + (chunk >> 1));
+#pragma unroll
+            for (int i = 0; i < GROUPS; ++i)
+#pragma unroll
+                for (int k = 0; k < PASSES; ++k) {
+                    const uint4 w4 = lds128_at(src + (uint32_t)((i * PASSES + k) * (kPfCopyWarps * 512)));
+                    const uint32_t b = (on >> (i * PASSES + k)) & 1u ? lds8(scl + (uint32_t)((8 * i + k * RPI) * NB)) : 0u;
+                    const uint32_t f = C::scale(b, b), v[4] = {w4.x, w4.y, w4.z, w4.w};
+                    uint32_t y[8];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        y[2 * e] = C::mul(C::template two<0x10>(v[e]), f);
+                        y[2 * e + 1] = C::mul(C::template two<0x32>(v[e]), f);
+                    }
+                    const int r = 8 * (w + i * kPfCopyWarps) + k * RPI + sub;
+                    // chunks 2 chunk and 2 chunk + 1 of the row's 16-bit values; the second 64 columns' lanes begin with the
+                    // odd one, as both atoms' rows begin in the same bank
+                    const uint32_t row = dst + (uint32_t)((chunk >> 2) * (HALVES - 1) * G::kAtom + r * 128);
+                    const int odd = chunk >> 2, c2 = (2 * chunk) & 7;
+                    const uint32_t d0 = row + (uint32_t)(((c2 + odd) ^ (r & 7)) << 4), d1 = row + (uint32_t)(((c2 + 1 - odd) ^ (r & 7)) << 4);
+                    sts128_at(d0, odd ? y[4] : y[0], odd ? y[5] : y[1], odd ? y[6] : y[2], odd ? y[7] : y[3]);
+                    sts128_at(d1, odd ? y[0] : y[4], odd ? y[1] : y[5], odd ? y[2] : y[6], odd ? y[3] : y[7]);
+                }
+            fence_proxy_async_smem();  // written as threads do; the MMA reads as the copy engine does
+            __syncwarp();              // (and nobody's scales are overwritten before all lanes have read them)
+            if (lane == 0) mbar_arrive(&m.full[slot]);
+            from = from + 1 == G::kRaws ? 0 : from + 1;
+            if (++slot == S) slot = 0, ++round;
+            if (x == 0 && w == 0) {  // the unit's queries, once the last unit's products with its own are done
+                if (nq > 0) ok = pf_wait(m.q_empty, (nq - 1) & 1);
+                if (!ok) break;
+                ++nq;
+                const int tiles = (2 * at.pt + 1) * tr < at.rows ? 2 : 1;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(m.q_full, (uint32_t)(tiles * HALVES * tr * a.group * 128));
+                    for (int y = 0; y < tiles; ++y)
+                        for (int h = 0; h < HALVES; ++h)
+                            tc::tma_load_3d(m.Qs + y * G::kTile + h * G::kAtom, &P.tq, 64 * h, at.kvh * a.group,
+                                            at.row0 + (2 * at.pt + y) * tr, smem_u32(m.q_full));
+                }
+                __syncwarp();
+            }
+        }
+        at.next(a, tr);
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    // the CTA may not end while a commit that releases a slot, or a tensor copy, is on its way
+    const bool good = ok;
+    for (int s = 0; ok && s < S; ++s) {
+        const int fills = round + (s < slot ? 1 : 0);
+        if (fills > 0) ok = pf_wait(&m.empty[s], (fills - 1) & 1);
+    }
+    if (!ok && w == 0 && nq > 0) pf_wait(m.q_full, (nq - 1) & 1);
+    return good && ok;
+}
+
 // JOIN: the parts of units that several CTAs share are left to k_paged_join; otherwise the last of a unit's CTAs to finish
 // joins them.
-template <class T, int DH, bool JOIN>
+template <class Src, int DH, bool JOIN>
 __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_constant__ PfParams P) {
     const PagedAttnArgs& a = P.a;
+    using T = typename Src::T;
     using E = Elem<T>;
-    using G = PfGeom<DH>;
+    using G = PfGeom<Src, DH>;
     constexpr int S = G::kSlots;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* Qs = smem;                      // [2][kTile]
     uint8_t* Rs = Qs + 2 * G::kTile;         // [S][kTile]
-    uint32_t* valid = reinterpret_cast<uint32_t*>(Rs + S * G::kTile);  // [kPfMaskRing][4]
+    uint8_t* raw = Rs + S * G::kTile;        // [kRaws][kRaw]
+    uint32_t* valid = reinterpret_cast<uint32_t*>(raw + G::kRaws * G::kRaw);  // [kPfMaskRing][4]
     uint64_t* bars = reinterpret_cast<uint64_t*>(valid + kPfMaskRing * 4);
     uint64_t* full = bars;                   // [S]
     uint64_t* empty = full + S;              // [S]
@@ -388,7 +566,13 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
 
     if (warp >= 8)  // a whole warpgroup
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPfCopyRegs));
-    if (warp >= 8 && warp < kPfMma) {
+    if (Src::kMx && warp >= 8 && warp < kPfMma) {
+        if constexpr (Src::kMx)
+            if (!pf_convert<Src, DH>(P, {Qs, Rs, raw, valid, full, empty, q_full, q_empty}, *cursor, t1 - t0) && lane == 0) {
+                *s_err = 1;
+                set_status(c.status, VT_DEV_WAIT_TIMEOUT);
+            }
+    } else if (!Src::kMx && warp >= 8 && warp < kPfMma) {
         // ================================================================ copies
         const int w = warp - 8;
         bool ok = true;
@@ -971,11 +1155,13 @@ __global__ void __launch_bounds__(kPfJoinThreads) k_paged_join(const __grid_cons
 
 // Workspace of both attention kernels.
 static size_t part_floats() { return (size_t)(4 * g_num_sms * kPagedPrefillSlot); }
+#ifndef VT_POOL_CODES
 size_t paged_work_floats() {
     return std::max((size_t)(2 * kPagedMaxGrid * kPagedDecodeSlot), part_floats() + kPagedMaxGrid / 2 * sizeof(PfSplit) / sizeof(float));
 }
+#endif
 
-template <class T, int DH>
+template <class Src, int DH>
 static cudaError_t prefill_dh(const PagedAttnArgs& a, cudaStream_t st) {
     // the line at the longest lengths
     const int64_t pairs = (int64_t)a.n_rows / (2 * (kPfRows / a.group)) + a.c.n_seqs;
@@ -988,6 +1174,8 @@ static cudaError_t prefill_dh(const PagedAttnArgs& a, cudaStream_t st) {
     const bool join = pairs * a.c.n_kv_heads * kPfJoinParts <= grid && span / kPfKeys + 2 + kPfUnitCost > kPfWhole;
     P.split = reinterpret_cast<PfSplit*>(a.work + part_floats());
     const PagedView& c = a.c;
+    using T = typename Src::T;
+    constexpr size_t smem = PfGeom<Src, DH>::kSmem;
     const bool bf16 = !std::is_same<T, __half>::value;
     const uint64_t qd[3] = {DH, (uint64_t)a.n_heads, (uint64_t)a.n_rows};
     const uint64_t qs[2] = {DH * 2, (uint64_t)(a.q_ld ? a.q_ld : (int64_t)a.n_heads * DH) * 2};
@@ -995,52 +1183,59 @@ static cudaError_t prefill_dh(const PagedAttnArgs& a, cudaStream_t st) {
     if (!make_tensor_map(&P.tq, bf16, 3, a.q, qd, qs, qb)) return cudaErrorInvalidValue;
     // Boxes of fewer than 16 rows would cost more than the copies of 16 bytes (2 KB boxes: 1160 cycles a block of 32 KB,
     // 16 KB boxes 680, asynchronous copies 1210 to 1310, all of them measured with every SM copying from the L2).
-    if (c.page_size >= 16) {
+    if (!Src::kMx && c.page_size >= 16) {
         const uint64_t kd[4] = {DH, (uint64_t)c.page_size, (uint64_t)c.n_kv_heads, (uint64_t)c.n_pages};
         const uint64_t ks[3] = {(uint64_t)c.pos_stride * 2, (uint64_t)(c.head_stride ? c.head_stride : DH) * 2,
                                 (uint64_t)(c.page_stride ? c.page_stride : DH) * 2};
         const uint32_t kb[4] = {64, (uint32_t)std::min(c.page_size, kPfKeys), 1, 1};
         P.tma = make_tensor_map(&P.tk, bf16, 4, a.kpool, kd, ks, kb) && make_tensor_map(&P.tv, bf16, 4, a.vpool, kd, ks, kb);
     }
-    if (!join) return launch_paged_k(k_paged_prefill<T, DH, false>, (unsigned)grid, kPfThreads, PfGeom<DH>::kSmem, st, P);
-    const cudaError_t e = launch_paged_k(k_paged_prefill<T, DH, true>, (unsigned)grid, kPfThreads, PfGeom<DH>::kSmem, st, P);
+    if (!join) return launch_paged_k(k_paged_prefill<Src, DH, false>, (unsigned)grid, kPfThreads, smem, st, P);
+    const cudaError_t e = launch_paged_k(k_paged_prefill<Src, DH, true>, (unsigned)grid, kPfThreads, smem, st, P);
     if (e != cudaSuccess) return e;
     return launch_paged_k(k_paged_join<T, DH>, (unsigned)(2 * g_num_sms), kPfJoinThreads, 0, st, PfJoin{a, P.split, (int)grid});
 }
 
-cudaError_t launch_paged_prefill(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st) {
-    if (dtype == VT_F16) return dh == 128 ? prefill_dh<__half, 128>(a, st) : prefill_dh<__half, 64>(a, st);
-    return dh == 128 ? prefill_dh<__nv_bfloat16, 128>(a, st) : prefill_dh<__nv_bfloat16, 64>(a, st);
-}
-
-template <class T, int DH, bool JOIN>
+template <class Src, int DH, bool JOIN>
 static cudaError_t init_one() {
     cudaFuncAttributes f;
-    cudaError_t e = cudaFuncGetAttributes(&f, k_paged_prefill<T, DH, JOIN>);
+    cudaError_t e = cudaFuncGetAttributes(&f, k_paged_prefill<Src, DH, JOIN>);
     if (e != cudaSuccess) return e;
     if (f.numRegs != kPfLaunchRegs) return cudaErrorInvalidConfiguration;  // (see paged_tiles_error)
-    return cudaFuncSetAttribute(k_paged_prefill<T, DH, JOIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PfGeom<DH>::kSmem);
+    return cudaFuncSetAttribute(k_paged_prefill<Src, DH, JOIN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                (int)PfGeom<Src, DH>::kSmem);
 }
-template <class T, int DH>
+template <class Src, int DH>
 static cudaError_t init_both() {
-    const cudaError_t e = init_one<T, DH, false>();
-    return e != cudaSuccess ? e : init_one<T, DH, true>();
+    const cudaError_t e = init_one<Src, DH, false>();
+    return e != cudaSuccess ? e : init_one<Src, DH, true>();
 }
+
+// The library's entry points to the kernel over one kind of pool: POOL<T> is what it holds, SUFFIX its name.
 // The register split needs exactly the registers that it was planned with: a build that gives the kernel another number
 // fails the calls that need the kernel, and no others.
-static cudaError_t g_tiles_err = cudaErrorNotReady;
-void init_paged_prefill() {
-    g_tiles_err = cudaSuccess;
-    for (cudaError_t e : {init_both<__half, 64>(), init_both<__half, 128>(), init_both<__nv_bfloat16, 64>(),
-                          init_both<__nv_bfloat16, 128>()})
-        if (e != cudaSuccess) g_tiles_err = e;
-    if (g_tiles_err != cudaSuccess) cudaGetLastError();  // not the next call's
-}
-const char* paged_tiles_error() {
-    if (g_tiles_err == cudaSuccess) return nullptr;
-    return g_tiles_err == cudaErrorInvalidConfiguration
-               ? "the prefill kernel on tensor-core tiles was built with another register count than its split needs"
-               : cudaGetErrorString(g_tiles_err);
-}
+#define VT_PAGED_TILES(POOL, SUFFIX)                                                                                               \
+    cudaError_t launch_paged_prefill##SUFFIX(const PagedAttnArgs& a, int dtype, int dh, cudaStream_t st) {                         \
+        if (dtype == VT_F16) return dh == 128 ? prefill_dh<POOL<__half>, 128>(a, st) : prefill_dh<POOL<__half>, 64>(a, st);        \
+        return dh == 128 ? prefill_dh<POOL<__nv_bfloat16>, 128>(a, st) : prefill_dh<POOL<__nv_bfloat16>, 64>(a, st);               \
+    }                                                                                                                              \
+    static cudaError_t g_tiles_err = cudaErrorNotReady;                                                                            \
+    void init_paged_prefill##SUFFIX() {                                                                                            \
+        g_tiles_err = cudaSuccess;                                                                                                 \
+        for (cudaError_t e : {init_both<POOL<__half>, 64>(), init_both<POOL<__half>, 128>(), init_both<POOL<__nv_bfloat16>, 64>(), \
+                              init_both<POOL<__nv_bfloat16>, 128>()})                                                              \
+            if (e != cudaSuccess) g_tiles_err = e;                                                                                 \
+        if (g_tiles_err != cudaSuccess) cudaGetLastError(); /* not the next call's */                                              \
+    }                                                                                                                              \
+    const char* paged_tiles_error##SUFFIX() {                                                                                      \
+        if (g_tiles_err == cudaSuccess) return nullptr;                                                                            \
+        return g_tiles_err == cudaErrorInvalidConfiguration                                                                        \
+                   ? "the prefill kernel on tensor-core tiles was built with another register count than its split needs"          \
+                   : cudaGetErrorString(g_tiles_err);                                                                              \
+    }
+
+#ifndef VT_POOL_CODES  // (pools of codes: paged_prefill_e4m3.cu, paged_prefill_int8.cu, each a translation unit for itself)
+VT_PAGED_TILES(PoolPlain, )
+#endif
 
 }  // namespace vt

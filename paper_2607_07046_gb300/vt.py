@@ -36,6 +36,10 @@ VT_DEV_BAD_TOKEN = 4
 VT_DEV_BAD_PAGE = 8
 VT_F16 = 0
 VT_BF16 = 1
+VT_ROPE_HALVES = 0
+VT_ROPE_NEIGHBOURS = 1
+VT_MX_E4M3 = 0
+VT_MX_INT8 = 1
 VT_BLOCK_ATTN = 0
 VT_BLOCK_FFN = 1
 VT_PARTITION_PRUNE = 1
@@ -91,6 +95,18 @@ class vt_paged_pool(ctypes.Structure):
 
 class vt_paged_batch(ctypes.Structure):
     _fields_ = [("tables", _P), ("lens", _P), ("starts", _P), ("n_seqs", _I32), ("pages_per_seq", _I32)]
+
+
+class vt_qk_form(ctypes.Structure):
+    _fields_ = [("q_gain", _P), ("k_gain", _P), ("rope", _P), ("rope_len", _I32), ("rotary_dim", _I32),
+                ("pairs", _I32), ("eps", ctypes.c_float)]
+
+
+class vt_paged_mx_pool(ctypes.Structure):
+    _fields_ = [("k", _P), ("v", _P), ("k_scale", _P), ("v_scale", _P), ("dtype", _I32), ("format", _I32),
+                ("n_pages", _I32), ("page_size", _I32), ("n_kv_heads", _I32), ("d_head", _I32),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("pos_stride", ctypes.c_int64),
+                ("scale_page_stride", ctypes.c_int64), ("scale_head_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -184,6 +200,16 @@ def lib() -> ctypes.CDLL:
                                     _P, ctypes.c_int64, ctypes.c_float, _I32, _P, ctypes.c_int64, _P]),
             "vt_paged_prefill": (S, [_P, ctypes.POINTER(vt_paged_pool), ctypes.POINTER(vt_paged_batch), _I32, _I32,
                                      _P, ctypes.c_int64, ctypes.c_float, _I32, _P, ctypes.c_int64, _P]),
+            "vt_paged_append_qk": (S, [_P, ctypes.POINTER(vt_paged_pool), ctypes.POINTER(vt_paged_batch), _I32, _I32,
+                                       _P, ctypes.c_int64, _P, ctypes.c_int64, _P, ctypes.c_int64,
+                                       ctypes.POINTER(vt_qk_form), _P, ctypes.c_int64, _P]),
+            "vt_paged_append_mx": (S, [_P, ctypes.POINTER(vt_paged_mx_pool), ctypes.POINTER(vt_paged_batch), _I32,
+                                       _I32, _P, ctypes.c_int64, _P, ctypes.c_int64, _P, ctypes.c_int64,
+                                       ctypes.POINTER(vt_qk_form), _P, ctypes.c_int64, _P]),
+            "vt_paged_decode_mx": (S, [_P, ctypes.POINTER(vt_paged_mx_pool), ctypes.POINTER(vt_paged_batch), _I32,
+                                       _P, ctypes.c_int64, ctypes.c_float, _I32, _P, ctypes.c_int64, _P]),
+            "vt_paged_prefill_mx": (S, [_P, ctypes.POINTER(vt_paged_mx_pool), ctypes.POINTER(vt_paged_batch), _I32,
+                                        _I32, _P, ctypes.c_int64, ctypes.c_float, _I32, _P, ctypes.c_int64, _P]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -775,26 +801,125 @@ def vt_paged_append(paged: int, pool: vt_paged_pool, batch: vt_paged_batch, q, k
                                  table[0], op, ol, _stream(stream)))
 
 
-def vt_paged_decode(paged: int, pool: vt_paged_pool, batch: vt_paged_batch, q, out, scale: Optional[float] = None,
-                    window: int = 0, stream=None) -> None:
-    """Attention of one new row per sequence: q, out [sequences, heads, head dim]; scale: None for
-    1 / sqrt(head dim)."""
+def _decode(call: str, paged, pool, batch, q, out, scale, window, stream) -> None:
     heads = q.shape[1]
     if q.shape[0] != batch.n_seqs or out.shape[0] != batch.n_seqs:
         raise ValueError("one row of q and out per sequence")
     _same_device(pool, batch)
     (qp, ql), (op, ol) = _rows(q, pool), _rows(out, pool, heads)
-    _check(lib().vt_paged_decode(paged, pool, batch, heads, qp, ql, pool.d_head ** -0.5 if scale is None else scale,
-                                 window, op, ol, _stream(stream)))
+    _check(getattr(lib(), call)(paged, pool, batch, heads, qp, ql, pool.d_head ** -0.5 if scale is None else scale,
+                                window, op, ol, _stream(stream)))
 
 
-def vt_paged_prefill(paged: int, pool: vt_paged_pool, batch: vt_paged_batch, q, out, scale: Optional[float] = None,
-                     window: int = 0, stream=None) -> None:
-    """Causal attention of the new rows of every sequence: q, out [rows, heads, head dim]."""
+def _prefill(call: str, paged, pool, batch, q, out, scale, window, stream) -> None:
     n, heads = q.shape[0], q.shape[1]
     if out.shape[0] != n:
         raise ValueError("q and out need one number of rows")
     _same_device(pool, batch)
     (qp, ql), (op, ol) = _rows(q, pool), _rows(out, pool, heads)
-    _check(lib().vt_paged_prefill(paged, pool, batch, n, heads, qp, ql, pool.d_head ** -0.5 if scale is None else scale,
-                                  window, op, ol, _stream(stream)))
+    _check(getattr(lib(), call)(paged, pool, batch, n, heads, qp, ql, pool.d_head ** -0.5 if scale is None else scale,
+                                window, op, ol, _stream(stream)))
+
+
+def vt_paged_decode(paged: int, pool: vt_paged_pool, batch: vt_paged_batch, q, out, scale: Optional[float] = None,
+                    window: int = 0, stream=None) -> None:
+    """Attention of one new row per sequence: q, out [sequences, heads, head dim]; scale: None for
+    1 / sqrt(head dim)."""
+    _decode("vt_paged_decode", paged, pool, batch, q, out, scale, window, stream)
+
+
+def vt_paged_prefill(paged: int, pool: vt_paged_pool, batch: vt_paged_batch, q, out, scale: Optional[float] = None,
+                     window: int = 0, stream=None) -> None:
+    """Causal attention of the new rows of every sequence: q, out [rows, heads, head dim]."""
+    _prefill("vt_paged_prefill", paged, pool, batch, q, out, scale, window, stream)
+
+
+# ------------------------------------------------------------------ norms, other rotations, pools in 8 bits
+
+def make_paged_mx_pool(k, v, k_scale, v_scale, dtype) -> vt_paged_mx_pool:
+    """One layer's K and V in 8 bits: codes are CUDA tensors seen as [pages, KV heads, positions in a page, head
+    dim], of torch.float8_e4m3fn or torch.int8, with equal strides and a contiguous head dim; scales are
+    [pages, KV heads, positions in a page, head dim / 32], of torch.float8_e8m0fnu or torch.uint8, with equal
+    strides and contiguous positions.  dtype: torch.float16 or torch.bfloat16, that of q, k, v and the outputs.
+    The structure keeps the tensors alive."""
+    import torch
+    tensors = (k, v, k_scale, v_scale)
+    for t in tensors:
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 4:
+            raise ValueError("expected CUDA tensors [pages, KV heads, positions in a page, head dim or head dim / 32]")
+    if dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError(f"expected rows of float16 or bfloat16, got {dtype}")
+    if k.dtype not in (torch.float8_e4m3fn, torch.int8) or v.dtype != k.dtype:
+        raise TypeError(f"expected float8_e4m3fn or int8 codes of one type, got {k.dtype} and {v.dtype}")
+    if k_scale.dtype not in (torch.float8_e8m0fnu, torch.uint8) or v_scale.dtype != k_scale.dtype:
+        raise TypeError(f"expected float8_e8m0fnu or uint8 scales of one type, got {k_scale.dtype} and {v_scale.dtype}")
+    if k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1 or any(t.device != k.device for t in tensors):
+        raise ValueError("K and V need one shape, equal strides, one device and a contiguous head dim")
+    blocks = k.shape[3] // 32
+    if (tuple(k_scale.shape) != (*k.shape[:3], blocks) or k_scale.shape != v_scale.shape or k_scale.stride() != v_scale.stride()
+            or k_scale.stride(3) != 1 or k_scale.stride(2) != blocks):
+        raise ValueError("the scales need the codes' shape with head dim / 32, equal strides and contiguous positions")
+    p = vt_paged_mx_pool(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                         VT_F16 if dtype == torch.float16 else VT_BF16, VT_MX_E4M3 if k.dtype == torch.float8_e4m3fn else VT_MX_INT8,
+                         k.shape[0], k.shape[2], k.shape[1], k.shape[3], k.stride(0), k.stride(1), k.stride(2),
+                         k_scale.stride(0), k_scale.stride(1))
+    p.tensors, p.torch_dtype, p.device = tensors, dtype, k.get_device()
+    return p
+
+
+def make_qk_form(rope=None, neighbours: bool = False, q_gain=None, k_gain=None, eps: float = 1e-6) -> vt_qk_form:
+    """What rows go through before they are stored: rope float32 [positions, rotary dim / 2, 2] or None (no rotation),
+    whose pairs are dimensions i and i + rotary dim / 2 or, with `neighbours`, 2i and 2i + 1; q_gain and k_gain
+    [head dim] of the rows' type, or None (no norm).  The structure keeps the tensors alive."""
+    import torch
+    if rope is not None and (rope.dim() != 3 or rope.shape[2] != 2):
+        raise ValueError("expected rope [positions, rotary dim / 2, 2]")
+    gains = [g for g in (q_gain, k_gain) if g is not None]
+    if any(g.dim() != 1 or g.dtype not in (torch.float16, torch.bfloat16) for g in gains):
+        raise ValueError("expected gains [head dim] of float16 or bfloat16")
+    tensors = [t for t in (rope, *gains) if t is not None]
+    if any(t.get_device() != tensors[0].get_device() for t in tensors):
+        raise ValueError("rope and gains need one device")
+    f = vt_qk_form(*(None if g is None else _ptr(g, g.dtype) for g in (q_gain, k_gain)),
+                   None if rope is None else _ptr(rope, torch.float32), 0 if rope is None else rope.shape[0],
+                   0 if rope is None else 2 * rope.shape[1], VT_ROPE_NEIGHBOURS if neighbours else VT_ROPE_HALVES, float(eps))
+    f.tensors, f.gains, f.device = (rope, q_gain, k_gain), gains, tensors[0].get_device() if tensors else None
+    return f
+
+
+def _append_qk(call: str, paged, pool, batch, q, k, v, form, q_out, stream) -> None:
+    n, heads = q.shape[0], q.shape[1]
+    if k.shape[0] != n or v.shape[0] != n or q_out.shape[0] != n:
+        raise ValueError("q, k, v and q_out need one number of rows")
+    if form.device not in (None, pool.device):
+        raise ValueError("the form's tensors lie on another device than the pool")
+    if any(tuple(g.shape) != (pool.d_head,) or g.dtype is not pool.torch_dtype for g in form.gains):
+        raise ValueError(f"expected gains [{pool.d_head}] of {pool.torch_dtype}")
+    _same_device(pool, batch)
+    (qp, ql), (kp, kl), (vp, vl), (op, ol) = (_rows(q, pool), _rows(k, pool, pool.n_kv_heads),
+                                             _rows(v, pool, pool.n_kv_heads), _rows(q_out, pool, heads))
+    _check(getattr(lib(), call)(paged, pool, batch, n, heads, qp, ql, kp, kl, vp, vl, form, op, ol, _stream(stream)))
+
+
+def vt_paged_append_qk(paged: int, pool: vt_paged_pool, batch: vt_paged_batch, q, k, v, form: vt_qk_form, q_out,
+                       stream=None) -> None:
+    """As vt_paged_append, with queries and keys through `form` (make_qk_form)."""
+    _append_qk("vt_paged_append_qk", paged, pool, batch, q, k, v, form, q_out, stream)
+
+
+def vt_paged_append_mx(paged: int, pool: vt_paged_mx_pool, batch: vt_paged_batch, q, k, v, form: vt_qk_form, q_out,
+                       stream=None) -> None:
+    """vt_paged_append_qk into a pool in 8 bits."""
+    _append_qk("vt_paged_append_mx", paged, pool, batch, q, k, v, form, q_out, stream)
+
+
+def vt_paged_decode_mx(paged: int, pool: vt_paged_mx_pool, batch: vt_paged_batch, q, out, scale: Optional[float] = None,
+                       window: int = 0, stream=None) -> None:
+    """vt_paged_decode over a pool in 8 bits."""
+    _decode("vt_paged_decode_mx", paged, pool, batch, q, out, scale, window, stream)
+
+
+def vt_paged_prefill_mx(paged: int, pool: vt_paged_mx_pool, batch: vt_paged_batch, q, out, scale: Optional[float] = None,
+                        window: int = 0, stream=None) -> None:
+    """vt_paged_prefill over a pool in 8 bits."""
+    _prefill("vt_paged_prefill_mx", paged, pool, batch, q, out, scale, window, stream)
