@@ -87,11 +87,39 @@ __device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
                  : "r"(addr)
                  : "memory");
 }
-// Where 16-byte chunk x of row r of codes lies in its row of CPR chunks: 8 rows of one chunk, and the same chunks of
-// neighbouring rows, fall into different banks.
+// Where 16-byte chunk x of row r of codes lies in its row of CPR chunks: 8 rows of one chunk (ldmatrix), and 4 rows of one
+// pair of chunks (the 32 dimensions of a scale), fall into different banks.
 template <int CPR>
 __device__ __forceinline__ uint32_t pd_chunk(int r, int x) {
-    return (uint32_t)((x ^ (CPR == 8 ? r & 7 : (r >> 1) & 3)) << 4);
+    return (uint32_t)((x ^ ((CPR == 8 ? (r & 3) << 1 : r & 2) | ((r >> 2) & 1))) << 4);
+}
+// The scales of two neighbouring positions.
+template <int NB>
+__device__ __forceinline__ void pd_scales(uint32_t addr, float (&f)[2][NB]) {
+    uint2 w;
+    if (NB == 4)
+        w = lds64(addr);
+    else {
+        w.x = lds32(addr);
+        w.y = w.x >> 16;
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        f[0][b] = mx_scale(w.x, b);
+        f[1][b] = mx_scale(w.y, b);
+    }
+}
+// 1 / x of a power of two.
+__device__ __forceinline__ float pd_inverse(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }
+// 2^x; over codes without the steps that keep results below 2^-126, which are nothing beside weights up to 2^12 and more.
+template <class Src>
+__device__ __forceinline__ float pd_exp2(float x) {
+    if constexpr (Src::kMx) {
+        float y;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+        return y;
+    }
+    return exp2f(x);
 }
 template <class T>
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -158,6 +186,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
     using T = typename Src::T;
     using E = Elem<T>;
     using G = PdGeom<Src, DH>;
+    constexpr bool TWO = std::is_same<T, __half>::value;  // codes: weights in two terms
     constexpr int KEYS = G::kKeys, NB = DH / kMxBlock;
     constexpr int S = G::kStages, CPR = G::kRow / 16, RPI = 32 / CPR;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -303,6 +332,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
     };
     look_up();
     int st_load = 0;
+    const int64_t mine_at = (lane / CPR) * c.pos_stride + (lane % CPR) * 16;  // codes: a lane's piece of 8 rows
     auto load_step = [&]() {
         if (more) {
             const bool on = needed && (unsigned)page < (unsigned)c.n_pages;
@@ -327,13 +357,21 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
             } else {
                 const uint8_t *kp = reinterpret_cast<const uint8_t*>(a.kpool), *vp = reinterpret_cast<const uint8_t*>(a.vpool);
 #pragma unroll
-                for (int r0 = 0; r0 < KEYS; r0 += RPI) {
-                    const int r = r0 + lane / CPR;
-                    const int64_t o = __shfl_sync(0xffffffffu, off, r);
-                    const uint32_t d = dst + (uint32_t)(r * G::kRow + pd_chunk<CPR>(r, chunk));
-                    const int64_t src = (o < 0 ? 0 : o) + chunk * 16;
-                    cp_async16(d, kp + src, o >= 0);
-                    cp_async16(d + G::kSide, vp + src, o >= 0);
+                for (int h = 0; h < KEYS; h += 8) {  // a page holds 8 positions or more
+                    const uint32_t bits = mask >> h;
+                    const int pg = __shfl_sync(0xffffffffu, page, h + max(0, __ffs(bits & 0xffu) - 1));
+                    int64_t src = (bits & 0xffu) ? pg * c.page_stride + (ld.u / ld.s.tiles) * c.head_stride +
+                                                       (((ld.s.beg / KEYS + ld_i) * KEYS + h) & (c.page_size - 1)) * c.pos_stride + mine_at
+                                                 : 0;
+#pragma unroll
+                    for (int k = 0; k < 8; k += RPI) {
+                        const int r = h + k + lane / CPR;
+                        const uint32_t d = dst + (uint32_t)(r * G::kRow) + pd_chunk<CPR>(r, chunk);
+                        const bool full = (bits >> (k + lane / CPR)) & 1u;  // rows without a position are filled with zeros
+                        cp_async16(d, kp + src, full);
+                        cp_async16(d + G::kSide, vp + src, full);
+                        if (bits & 0xffu) src += RPI * c.pos_stride;
+                    }
                 }
                 // 16 bytes hold the scales of PER positions, which lie in one page
                 constexpr int PER = 16 / NB, CHUNKS = KEYS / PER;
@@ -373,17 +411,49 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
             return (at.s.row0 + row) * ld + (int64_t)(kvh * a.group + c0 + c - row * a.group) * DH;
         };
         uint32_t q[DH / 16][4];
+        float qs[NT];  // what a score is multiplied by
+#pragma unroll
+        for (int x = 0; x < NT; ++x) qs[x] = a.scale_log2;
+        float unit = 0x1p-100f;  // codes: o counts in this unit, the largest scale of V so far
         int last_key[NT];  // of this lane's columns, in the steps' keys
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             const bool on = x < NT && g + 8 * x < nc;
-            // codes: a lane takes DH / 4 bytes of a K row side by side, so product k is over the dimensions
-            // t DH / 4 + 4 k + 0 .. 3 of its four lanes
-            const uint16_t* src = a.q + (on ? col_at(g + 8 * x, a.q_ld) : 0) + (Src::kMx ? t * (DH / 4) : 2 * t);
+            if constexpr (!Src::kMx) {
+                const uint16_t* src = a.q + (on ? col_at(g + 8 * x, a.q_ld) : 0) + 2 * t;
 #pragma unroll
-            for (int k = 0; k < DH / 16; ++k) {
-                q[k][x] = on ? *reinterpret_cast<const uint32_t*>(src + k * (Src::kMx ? 4 : 16)) : 0u;
-                q[k][2 + x] = on ? *reinterpret_cast<const uint32_t*>(src + k * (Src::kMx ? 4 : 16) + (Src::kMx ? 2 : 8)) : 0u;
+                for (int k = 0; k < DH / 16; ++k) {
+                    q[k][x] = on ? *reinterpret_cast<const uint32_t*>(src + k * 16) : 0u;
+                    q[k][2 + x] = on ? *reinterpret_cast<const uint32_t*>(src + k * 16 + 8) : 0u;
+                }
+            } else {  // product k is over the dimensions 32 (k / 2) + 8 t + 4 (k % 2) + 0 .. 3 of its four lanes
+                const uint16_t* src = a.q + (on ? col_at(g + 8 * x, a.q_ld) : 0) + 8 * t;
+#pragma unroll
+                for (int k = 0; k < DH / 16; ++k) {
+                    const uint2 w = on ? *reinterpret_cast<const uint2*>(src + (k >> 1) * 32 + (k & 1) * 4) : make_uint2(0u, 0u);
+                    q[k][x] = w.x;
+                    q[k][2 + x] = w.y;
+                }
+                if constexpr (!std::is_same<T, __half>::value) {  // bf16 to fp16: the row's largest is brought to 2^10 .. 2^11
+                    uint32_t most = 0u;
+#pragma unroll
+                    for (int k = 0; k < DH / 16; ++k) {
+                        most = max(most, max(q[k][x] & 0x7fffu, (q[k][x] >> 16) & 0x7fffu));
+                        most = max(most, max(q[k][2 + x] & 0x7fffu, (q[k][2 + x] >> 16) & 0x7fffu));
+                    }
+                    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+                    most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+                    const int up = 10 - max((int)(most >> 7) - 127, -116);
+                    const float f = __uint_as_float((uint32_t)(127 + up) << 23);
+#pragma unroll
+                    for (int k = 0; k < DH / 16; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; e += 2) {
+                            const float2 v = E::unpack(q[k][e + x]);
+                            q[k][e + x] = Elem<__half>::pack(v.x * f, v.y * f);
+                        }
+                    if (x < NT) qs[x] = a.scale_log2 * __uint_as_float((uint32_t)(127 - up) << 23);
+                }
             }
             if (x < NT) last_key[x] = ROWS ? at.s.len + (c0 + g + 8 * x) / a.group : 0;
         }
@@ -415,23 +485,44 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
                     mma16816<T>(s[1], q[k], kb[2], kb[3]);
                 }
             } else {
-                using C = typename Src::C;
+                using C = typename Src::H;
+                float f[NS][2][NB];
 #pragma unroll
-                for (int n = 0; n < NS; ++n) {  // keys 8 n + g
+                for (int n = 0; n < NS; ++n) pd_scales<NB>(vs + G::kSide + (uint32_t)((8 * n + 2 * t) * NB), f[n]);
+#pragma unroll
+                for (int n = 0; n < NS; ++n) {  // keys 8 n + g; a scale's 32 dimensions into a sum of their own
                     const int r = 8 * n + g;
-                    const uint32_t b = lds8(vs + G::kSide + (uint32_t)(r * NB + t * NB / 4)), f = C::scale(b, b);
 #pragma unroll
-                    for (int k = 0; k < DH / 16; k += 4) {
-                        const uint4 w4 = lds128_at(ks + (uint32_t)(r * G::kRow + pd_chunk<CPR>(r, t * (DH / 64) + k / 4)));
-                        const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+                    for (int b = 0; b < NB; ++b) {
+                        const uint2 w = lds64(ks + (uint32_t)(r * G::kRow + ((t & 1) << 3)) + pd_chunk<CPR>(r, 2 * b + (t >> 1)));
+                        float sum[4] = {};
+                        mma16816<__half>(sum, q[2 * b], C::lo(w.x), C::hi(w.x));
+                        mma16816<__half>(sum, q[2 * b + 1], C::lo(w.y), C::hi(w.y));
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            mma16816<T>(s[n], q[k + e], C::mul(C::template two<0x10>(w[e]), f), C::mul(C::template two<0x32>(w[e]), f));
+                        for (int e = 0; e < 2 * NT; ++e) s[n][e] = fmaf(sum[e], f[n][e & 1][b], s[n][e]);
                     }
                 }
+                // an infinite scale marks a NaN, whatever its codes are
+                float far = 0.f;
+#pragma unroll
+                for (int n = 0; n < NS; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2 * NT; ++e) far += fabsf(s[n][e]);
+                if (__any_sync(0xffffffffu, !(far < INFINITY)))
+#pragma unroll
+                    for (int n = 0; n < NS; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2 * NT; ++e)
+#pragma unroll
+                            for (int b = 0; b < NB; ++b)
+                                if (f[n][e & 1][b] == INFINITY) s[n][e] = __int_as_float(0x7fc00000);
             }
-            uint32_t hi[NT][NS], lo[NT][NS];
-            float al[NT];
+            // Weights.  m is a reference: the maximum less kUp where P is fp16, so that P goes up to 2^15 (it has no steps below
+            // 2^-24); over codes it moves only when P would pass that, down to 2^12.  l, o and every later join agree on it.
+            constexpr bool HALF_P = Src::kMx || std::is_same<T, __half>::value;
+            constexpr float kUp = !HALF_P ? 0.f : Src::kMx ? 12.f : 15.f, kSlack = Src::kMx ? 3.f : 0.f;
+            uint32_t hi[NT][NS], lo[NT][NS];  // of 16-bit values' weights
+            float al[NT], pw[Src::kMx ? NT : 1][2 * NS];
             bool moved = false;
 #pragma unroll
             for (int x = 0; x < NT; ++x) {
@@ -441,29 +532,30 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
                     const int key = 8 * (e >> 1) + 2 * t + (e & 1);
                     bool on = (mask >> key) & 1u;
                     if (ROWS) on = on && p0 + key <= last_key[x] && (a.window == 0 || p0 + key > last_key[x] - a.window);
-                    v[e] = on ? s[e >> 1][2 * x + (e & 1)] * a.scale_log2 : -INFINITY;
+                    v[e] = on ? s[e >> 1][2 * x + (e & 1)] * qs[x] : -INFINITY;
                     mx = fmaxf(mx, v[e]);
                 }
                 mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
                 mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                // m is the maximum less kPdUp, so that P goes up to 2^kPdUp; l, o and every later join agree on it
-                constexpr float kPdUp = std::is_same<T, __half>::value ? 15.f : 0.f;
-                const float mn = fmaxf(m[x], mx - kPdUp), ref = mn == -INFINITY ? 0.f : mn;
-                al[x] = exp2f(m[x] - ref);
+                const float mn = Src::kMx && !(mx > m[x] + (kUp + kSlack)) ? m[x] : fmaxf(m[x], mx - kUp);
+                const float ref = mn == -INFINITY ? 0.f : mn;
+                al[x] = pd_exp2<Src>(m[x] - ref);
                 moved |= mn != m[x];
                 m[x] = mn;
-                float p[2 * NS];
+                float(&p)[2 * NS] = pw[Src::kMx ? x : 0];
 #pragma unroll
-                for (int e = 0; e < 2 * NS; ++e) p[e] = exp2f(v[e] - ref);
+                for (int e = 0; e < 2 * NS; ++e) p[e] = pd_exp2<Src>(v[e] - ref);
                 float sum = (p[0] + p[1]) + (p[2] + p[3]);
 #pragma unroll
                 for (int e = 4; e < 2 * NS; e += 4) sum += (p[e] + p[e + 1]) + (p[e + 2] + p[e + 3]);
                 l[x] = l[x] * al[x] + sum;
+                if constexpr (!Src::kMx) {
 #pragma unroll
-                for (int e = 0; e < NS; ++e) {
-                    hi[x][e] = E::pack(p[2 * e], p[2 * e + 1]);
-                    const float2 f = E::unpack(hi[x][e]);
-                    lo[x][e] = E::pack(p[2 * e] - f.x, p[2 * e + 1] - f.y);
+                    for (int e = 0; e < NS; ++e) {
+                        hi[x][e] = E::pack(p[2 * e], p[2 * e + 1]);
+                        const float2 f = E::unpack(hi[x][e]);
+                        lo[x][e] = E::pack(p[2 * e] - f.x, p[2 * e + 1] - f.y);
+                    }
                 }
             }
             if (__any_sync(0xffffffffu, moved)) {
@@ -493,46 +585,97 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
                 }
             } else {
                 // Two codes of a row go through ldmatrix.trans as one element: a lane gets dimensions 2 g and 2 g + 1 of
-                // positions 2 t and 2 t + 1.  Row g of A is made of the first, row g + 8 of the second.
-                using C = typename Src::C;
+                // positions 2 t and 2 t + 1.  Row g of A is made of the first, row g + 8 of the second.  The scales go to the
+                // weights, which for 32 dimensions at a time are then those of the codes.
+                using C = typename Src::H;
+                using H = Elem<__half>;
                 const int mr = (lane & 7) + (lane & 8), mc = lane >> 4;  // ldmatrix: row, chunk of a pair
+                float f[NS][2][NB], most = 0.f;
 #pragma unroll
-                for (int n = 0; n < KEYS / 16; ++n) {
-                    const uint32_t vsc = vs + G::kSide + G::kScales + (uint32_t)((16 * n + 2 * t) * NB);
-                    uint32_t e[2][2][NB];  // scales: half of the 16 positions, position of the pair, block
+                for (int n = 0; n < NS; ++n) {
+                    pd_scales<NB>(vs + G::kSide + G::kScales + (uint32_t)((8 * n + 2 * t) * NB), f[n]);
+                    if (mask != (KEYS == 32 ? 0xffffffffu : (1u << (KEYS & 31)) - 1u))  // what nothing attends to may be anything
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+                        for (int j = 0; j < 2; ++j)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const uint32_t w = NB == 4 ? lds32(vsc + (8 * h + j) * NB) : lds16(vsc + (8 * h + j) * NB);
-                            const bool on = (mask >> (16 * n + 8 * h + 2 * t + j)) & 1u;  // scales that nothing attends to may be anything
+                            for (int b = 0; b < NB; ++b)
+                                if (!((mask >> (8 * n + 2 * t + j)) & 1u)) f[n][j][b] = 0.f;
 #pragma unroll
-                            for (int i = 0; i < NB; ++i) e[h][j][i] = on ? (w >> (8 * i)) & 0xffu : 0u;
-                        }
+                    for (int b = 0; b < NB; ++b) most = fmaxf(most, fmaxf(f[n][0][b], f[n][1][b]));
+                }
+                if (__any_sync(0xffffffffu, most > unit)) {
+                    most = 0.f;
 #pragma unroll
-                    for (int i = 0; i < NB; ++i) {
-                        const uint32_t f0 = C::scale(e[0][0][i], e[0][1][i]), f1 = C::scale(e[1][0][i], e[1][1][i]);
+                    for (int n = 0; n < NS; ++n)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+#pragma unroll
+                            for (int b = 0; b < NB; ++b) {  // (an infinite scale marks a NaN: it sets no unit)
+                                if (f[n][j][b] == INFINITY) f[n][j][b] = __int_as_float(0x7fc00000);
+                                most = fmaxf(most, f[n][j][b]);
+                            }
+                    const float next = fmaxf(unit, __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most))));
+                    const float r = unit * pd_inverse(next);
+                    unit = next;
+#pragma unroll
+                    for (int x = 0; x < NT; ++x)
+#pragma unroll
+                        for (int i = 0; i < DH / 16; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[i][x][e] *= r;
+                }
+                const float inv = pd_inverse(unit);
+#pragma unroll
+                for (int x = 0; x < NT; ++x)
+#pragma unroll
+                    for (int e = 0; e < 2 * NS; ++e) pw[x][e] *= inv;
+#pragma unroll
+                for (int n = 0; n < KEYS / 16; ++n)
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        uint32_t hi[NT][2], lo[NT][2];
+#pragma unroll
+                        for (int x = 0; x < NT; ++x)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const float w0 = pw[x][4 * n + 2 * e] * f[2 * n + e][0][b], w1 = pw[x][4 * n + 2 * e + 1] * f[2 * n + e][1][b];
+                                hi[x][e] = H::pack(w0, w1);
+                                if constexpr (TWO) {
+                                    const float2 h = H::unpack(hi[x][e]);
+                                    lo[x][e] = H::pack(w0 - h.x, w1 - h.y);
+                                }
+                            }
                         const int r = 16 * n + mr;
                         uint32_t w[4];
-                        ldsm4_t(vs + (uint32_t)(r * G::kRow + pd_chunk<CPR>(r, 2 * i + mc)), w);
+                        ldsm4_t(vs + (uint32_t)(r * G::kRow) + pd_chunk<CPR>(r, 2 * b + mc), w);
 #pragma unroll
                         for (int y = 0; y < 2; ++y) {
-                            const uint32_t vt[4] = {C::mul(C::template two<0x20>(w[2 * y]), f0), C::mul(C::template two<0x31>(w[2 * y]), f0),
-                                                    C::mul(C::template two<0x20>(w[2 * y + 1]), f1),
-                                                    C::mul(C::template two<0x31>(w[2 * y + 1]), f1)};
+                            uint32_t vt[4];
+                            C::split(w[2 * y], vt[0], vt[1]);
+                            C::split(w[2 * y + 1], vt[2], vt[3]);
 #pragma unroll
                             for (int x = 0; x < NT; ++x) {
-                                mma16816<T>(o[2 * i + y][x], vt, hi[x][2 * n], hi[x][2 * n + 1]);
-                                mma16816<T>(o[2 * i + y][x], vt, lo[x][2 * n], lo[x][2 * n + 1]);
+                                mma16816<__half>(o[2 * b + y][x], vt, hi[x][0], hi[x][1]);
+                                if constexpr (TWO) mma16816<__half>(o[2 * b + y][x], vt, lo[x][0], lo[x][1]);
                             }
                         }
                     }
-                }
             }
             __syncwarp();
             st = st + 1 == S ? 0 : st + 1;
         }
         skip = k0 - n;
+        if constexpr (Src::kMx) {  // in the values' units, of weights up to 1
+            unit *= 0x1p-15f;
+#pragma unroll
+            for (int x = 0; x < NT; ++x) {
+                l[x] *= 0x1p-15f;
+#pragma unroll
+                for (int i = 0; i < DH / 16; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[i][x][e] *= unit;
+            }
+        }
 
         if (solo) {  // ---- the unit's end: one warp's (m, l, o)
             float* ws = so + warp * 8 * DH;

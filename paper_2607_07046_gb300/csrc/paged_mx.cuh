@@ -2,10 +2,8 @@
 // 2^(s - 127) of its byte s.  Codes are e4m3 or whole numbers (two's complement).
 //
 // A code times its scale is a value of the rows' type (exactly: a code has 8 significant bits at most, and the
-// append keeps the scales where no step falls below the type's), so the products of attention are those of a pool
-// that holds these values in 16 bits, and neither scores nor weights carry scales.  Byte 255 marks a block that held
-// an infinity or NaN: its scale is infinite and its codes are zeros, whose product is NaN.  Any codes are finite here
-// (e4m3's two NaN codes read as 480), so scale 0 hides whatever lies in entries that nothing attends to.
+// append keeps the scales where no step falls below the type's).  Byte 255 is NaN.  Scale 0 (which no entry has) hides
+// whatever finite codes lie in entries that nothing attends to.
 #pragma once
 
 #include <cuda_fp8.h>
@@ -54,13 +52,46 @@ struct MxCodes {
             return *reinterpret_cast<const uint32_t*>(&r);
         }
     }
-    // Two scales of bytes s0 and s1; byte 0 gives 0.
-    static __device__ __forceinline__ uint32_t scale(uint32_t s0, uint32_t s1) {
-        const uint32_t p = kHalf ? Elem<T>::pack(__uint_as_float(s0 << 23), __uint_as_float(s1 << 23)) : (s0 << 7) | (s1 << 23);
+    // The scale of byte s, twice; byte 0 gives 0, 255 NaN.
+    static __device__ __forceinline__ uint32_t scale(uint32_t s) {
+        if (s == 255u) return 0x7fff7fffu;
+        const uint32_t p = kHalf ? Elem<T>::pack(__uint_as_float(s << 23), __uint_as_float(s << 23)) : s * 0x00800080u;
         return kFloat ? mx_mul<T>(p, kHalf ? 0x5c005c00u : 0x7b807b80u) : p;  // 2^8, 2^120
     }
     static __device__ __forceinline__ uint32_t mul(uint32_t a, uint32_t s) { return mx_mul<T>(a, s); }
 };
+
+// Codes as pairs of fp16, without their scale: the lower and upper two of w, or its bytes 0, 2 and 1, 3.
+template <int F>
+struct MxHalf {
+    static __device__ __forceinline__ uint32_t convert(uint16_t two) {
+        uint32_t r;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(two));
+        return r;
+    }
+    static __device__ __forceinline__ uint32_t lo(uint32_t w) {
+        if constexpr (F == VT_MX_E4M3) return convert((uint16_t)w);
+        return MxCodes<__half, F>::template two<0x10>(w);
+    }
+    static __device__ __forceinline__ uint32_t hi(uint32_t w) {
+        if constexpr (F == VT_MX_E4M3) return convert((uint16_t)(w >> 16));
+        return MxCodes<__half, F>::template two<0x32>(w);
+    }
+    static __device__ __forceinline__ void split(uint32_t w, uint32_t& even, uint32_t& odd) {
+        if constexpr (F == VT_MX_E4M3) {
+            const uint32_t x = __byte_perm(w, 0u, 0x3120);
+            even = lo(x);
+            odd = hi(x);
+        } else {
+            even = MxCodes<__half, F>::template two<0x20>(w);
+            odd = MxCodes<__half, F>::template two<0x31>(w);
+        }
+    }
+};
+// Scale b of a word of scales.
+__device__ __forceinline__ float mx_scale(uint32_t w, int b) {
+    return __uint_as_float((b == 3 ? w >> 1 : w << (23 - 8 * b)) & 0x7f800000u);
+}
 
 // What a pool holds: 16-bit values of type T, or 8-bit codes of format F that stand for values of type T.
 template <class E>
@@ -73,6 +104,7 @@ template <class E, int F>
 struct PoolMx {
     using T = E;
     using C = MxCodes<E, F>;
+    using H = MxHalf<F>;
     static constexpr bool kMx = true;
     static constexpr int kBytes = 1;
 };
@@ -84,6 +116,11 @@ __device__ __forceinline__ uint4 lds128_at(uint32_t addr) {
 }
 __device__ __forceinline__ void sts128_at(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint2 lds64(uint32_t addr) {
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+    return v;
 }
 __device__ __forceinline__ uint32_t lds32(uint32_t addr) {
     uint32_t v;

@@ -320,7 +320,7 @@ __device__ __forceinline__ bool pf_convert(const PfParams& P, const PfShared& m,
                 for (int k = 0; k < PASSES; ++k) {
                     const uint4 w4 = lds128_at(src + (uint32_t)((i * PASSES + k) * (kPfCopyWarps * 512)));
                     const uint32_t b = (on >> (i * PASSES + k)) & 1u ? lds8(scl + (uint32_t)((8 * i + k * RPI) * NB)) : 0u;
-                    const uint32_t f = C::scale(b, b), v[4] = {w4.x, w4.y, w4.z, w4.w};
+                    const uint32_t f = C::scale(b), v[4] = {w4.x, w4.y, w4.z, w4.w};
                     uint32_t y[8];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {

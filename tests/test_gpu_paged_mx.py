@@ -7,7 +7,11 @@ tiles' kernel takes the whole batch, its operands are those that it has over a 1
 are its outputs' bits.  Two terms come on top: an fp16 output below 2^-14 is rounded to steps of 2^-24, half of one being
 2^-25 whatever its size; and a weight below 2^-126 of the row's largest is 0 in 32 bits (2^-126 is their
 smallest normal number), which shows where the large ones meet values of exactly 0, as codes are often: (positions)
-2^-126 max|v|."""
+2^-126 max|v|.
+The kernel of few rows takes weights to fp16 (with the scale of their values, over the largest scale), the largest between 2^12 and
+2^15: the type's steps of 2^-24 below its normal numbers leave each off by 2^-25, which is 2^-37 of the row's largest weight, times
+the largest scale and code, which is less than twice the largest value (the scale is the least power of two that holds it):
+(positions) 2^-36 max|v|, which takes the place of the term before."""
 from __future__ import annotations
 
 import math
@@ -42,7 +46,7 @@ def check(vt, g, c, call, heads, window=0, scale=None, q=None, same_bits=False):
     scale = c.d_head ** -0.5 if scale is None else scale
     attend(vt, g, c, call, q, out, scale, window)
     ref, tol = attention(c, q, scale, window)
-    tol = tol + 2.0 ** -126 * c.k.shape[0] * c.page * c.v.masked_fill(c.v.isnan(), 0.0).double().abs().max()
+    tol = tol + 2.0 ** -36 * c.k.shape[0] * c.page * c.v.masked_fill(c.v.isnan(), 0.0).double().abs().max()
     tol = tol + TINY[c.dtype]
     far = (out.double() - ref).abs()
     assert torch.isfinite(out).all()
