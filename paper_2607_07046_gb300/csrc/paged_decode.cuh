@@ -35,12 +35,12 @@
 #include <algorithm>
 
 #include "paged_mx.cuh"
+#include "tcgen05.cuh"
 
 namespace vt {
 
 constexpr int kPdWarps = 4, kPdThreads = kPdWarps * 32;
 constexpr int kPdRing = 96 * 1024;           // bytes of the four warps' rings, at most
-constexpr int kPdCtasPerSm = 2;
 // A unit's queries, merge and result cost as much as this many steps (measured: 64 ragged sequences 75 us at 0, 56 at
 // 4, 47 at 8 to 24, 50 at 32).
 constexpr int kPdUnitCost = 16;
@@ -55,20 +55,25 @@ constexpr int kPdMinSteps = 16, kPdWhole = 28;
 // 24 sequences of 201 to 251, 32 heads, 24 and 22.  At 32 steps 300 sequences of 21 to 501 positions lost (51 to 63).
 constexpr int kPdSoloSteps = 16, kPdSoloUnits = 2;
 
-template <class Src, int DH>
+template <class Src, int DH, int NT>
 struct PdGeom {
-    static constexpr int kKeys = 16;                                              // positions of a step
-    static constexpr int kRow = DH * Src::kBytes;                                 // bytes of a K or V row
-    static constexpr int kSide = kKeys * kRow;                               // of a step's K
-    static constexpr int kScales = Src::kMx ? kKeys * (DH / kMxBlock) : 0;   // of its scales
-    static constexpr int kStage = 2 * (kSide + kScales);                          // K rows, V rows, K scales, V scales
-    static constexpr int kStages = kPdRing / (kPdWarps * kStage);                 // 16 bits: 3 (dh 128) or 6 (dh 64); 8 bits: 5 or 11
+    static constexpr int kCtas = Src::kMx && NT == 1 ? 3 : 2;                    // an SM
+    static constexpr int kKeys = 16;                                             // positions of a step
+    static constexpr int kRow = DH * Src::kBytes;                                // bytes of a K or V row
+    static constexpr int kSide = kKeys * kRow;                                   // of a step's K
+    static constexpr int kScales = Src::kMx ? kKeys * (DH / kMxBlock) : 0;       // of its scales
+    static constexpr int kStage = 2 * (kSide + kScales);                         // K rows, V rows, K scales, V scales
+    static constexpr int kStages = (kCtas == 3 ? kPdRing / 2 : kPdRing) / (kPdWarps * kStage) + (kCtas == 3 && DH == 128 ? 1 : 0);
     static constexpr int kRing = kPdWarps * kStages * kStage;
-    static constexpr size_t kSmem = kRing + (size_t)kPdWarps * 8 * DH * 4;
+    static constexpr int kFloats = 2 * kKeys * (DH / kMxBlock) * (Src::kMx ? 1 : 0);  // of a warp: a step's scales
+    static constexpr size_t kSmem = kRing + (size_t)kPdWarps * (8 * DH + kFloats) * 4;
 };
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool full) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(full ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -93,21 +98,20 @@ template <int CPR>
 __device__ __forceinline__ uint32_t pd_chunk(int r, int x) {
     return (uint32_t)((x ^ ((CPR == 8 ? (r & 3) << 1 : r & 2) | ((r >> 2) & 1))) << 4);
 }
-// The scales of two neighbouring positions.
-template <int NB>
-__device__ __forceinline__ void pd_scales(uint32_t addr, float (&f)[2][NB]) {
-    uint2 w;
-    if (NB == 4)
-        w = lds64(addr);
-    else {
-        w.x = lds32(addr);
-        w.y = w.x >> 16;
-    }
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        f[0][b] = mx_scale(w.x, b);
-        f[1][b] = mx_scale(w.y, b);
-    }
+__device__ __forceinline__ void sts32(uint32_t addr, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
+// Two floats in a register pair, one or two such pairs.
+__device__ __forceinline__ uint64_t lds1x64(uint32_t addr) {
+    uint64_t v;
+    asm volatile("ld.shared.b64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void lds2x64(uint32_t addr, uint64_t (&v)[2]) {
+    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(v[0]), "=l"(v[1]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
 }
 // 1 / x of a power of two.
 __device__ __forceinline__ float pd_inverse(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }
@@ -131,6 +135,13 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
         asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
             : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// The product alone, of fp16.
+__device__ __forceinline__ void mma16816_new(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 // A sequence's new rows, and the positions [beg, end) that they attend to (end 0: none), in steps of KEYS.
@@ -182,10 +193,10 @@ struct PdCursor {
 };
 
 template <class Src, int DH, int NT, bool ROWS>
-__global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const __grid_constant__ PagedAttnArgs a) {
+__global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_paged_decode(const __grid_constant__ PagedAttnArgs a) {
     using T = typename Src::T;
     using E = Elem<T>;
-    using G = PdGeom<Src, DH>;
+    using G = PdGeom<Src, DH, NT>;
     constexpr bool TWO = std::is_same<T, __half>::value;  // codes: weights in two terms
     constexpr int KEYS = G::kKeys, NB = DH / kMxBlock;
     constexpr int S = G::kStages, CPR = G::kRow / 16, RPI = 32 / CPR;
@@ -302,10 +313,12 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
     PdCursor<ROWS, COLS, KEYS> ld = at;               // of this warp's copies: the unit of its next step
     int64_t ld_now = t0;                        // where that unit's part begins in the line
     int ld_i, ld_n, ld_skip = solo ? 0 : warp;  // next step of the unit, steps of it here, steps until this warp's next
+    int ld_head = 0;                            // codes: its KV head
     auto ld_unit = [&]() {                      // the steps [first, n) of the unit that lie in this part
         const int first = max(0, ld.i - kPdUnitCost);
         ld_n = (int)min((int64_t)ld.s.steps, t1 - ld_now + ld.i - kPdUnitCost);
         ld_i = first;
+        if constexpr (Src::kMx) ld_head = ld.u / ld.s.tiles;
     };
     // moves to this warp's next step; false: none
     auto ld_seek = [&]() -> bool {
@@ -332,19 +345,24 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
     };
     look_up();
     int st_load = 0;
-    const int64_t mine_at = (lane / CPR) * c.pos_stride + (lane % CPR) * 16;  // codes: a lane's piece of 8 rows
+    // codes: a lane's 16 bytes of the first rows (RPI of them a copy), and of the scales, which hold those of PER positions
+    constexpr int PER = Src::kMx ? 16 / NB : 1, CHUNKS = KEYS / PER;
+    const int64_t mine_at = (lane / CPR) * c.pos_stride + (lane % CPR) * 16, hop = RPI * c.pos_stride;
+    const uint8_t *k_at = reinterpret_cast<const uint8_t*>(a.kpool) + mine_at, *v_at = reinterpret_cast<const uint8_t*>(a.vpool) + mine_at;
+    const uint8_t* s_at = (lane % (2 * CHUNKS) < CHUNKS ? a.kscale : a.vscale) + (lane % CHUNKS) * 16;
+    const uint32_t mine_to = (uint32_t)((lane / CPR) * G::kRow) + pd_chunk<CPR>(lane / CPR, lane % CPR);
     auto load_step = [&]() {
         if (more) {
             const bool on = needed && (unsigned)page < (unsigned)c.n_pages;
             if (needed && !on) set_status(c.status, VT_DEV_BAD_PAGE);
-            const int p = (ld.s.beg / KEYS + ld_i) * KEYS + lane;
-            const int64_t off = on ? page * c.page_stride + (ld.u / ld.s.tiles) * c.head_stride + (p & (c.page_size - 1)) * c.pos_stride
-                                   : -1;
             const uint32_t mask = __ballot_sync(0xffffffffu, on);
             if (lane == 0) s_mask[warp][st_load] = mask;
             const uint32_t dst = ring + (uint32_t)(st_load * G::kStage);
             const int chunk = lane % CPR;
             if constexpr (!Src::kMx) {
+                const int p = (ld.s.beg / KEYS + ld_i) * KEYS + lane;
+                const int64_t off = on ? page * c.page_stride + (ld.u / ld.s.tiles) * c.head_stride + (p & (c.page_size - 1)) * c.pos_stride
+                                       : -1;
 #pragma unroll
                 for (int r0 = 0; r0 < KEYS; r0 += RPI) {
                     const int r = r0 + lane / CPR;
@@ -355,31 +373,42 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
                     cp_async16(d + KEYS * G::kRow, a.vpool + src, o >= 0);
                 }
             } else {
-                const uint8_t *kp = reinterpret_cast<const uint8_t*>(a.kpool), *vp = reinterpret_cast<const uint8_t*>(a.vpool);
+                const int first = (ld.s.beg / KEYS + ld_i) * KEYS, in_page = first & (c.page_size - 1);
+                if (mask == 0xffffu && c.page_size >= KEYS) {  // all of one page
+                    const int pg = __shfl_sync(0xffffffffu, page, 0);
+                    const int64_t at = pg * c.page_stride + ld_head * c.head_stride + in_page * c.pos_stride;
+                    const uint8_t *ksrc = k_at + at, *vsrc = v_at + at;
 #pragma unroll
-                for (int h = 0; h < KEYS; h += 8) {  // a page holds 8 positions or more
-                    const uint32_t bits = mask >> h;
-                    const int pg = __shfl_sync(0xffffffffu, page, h + max(0, __ffs(bits & 0xffu) - 1));
-                    int64_t src = (bits & 0xffu) ? pg * c.page_stride + (ld.u / ld.s.tiles) * c.head_stride +
-                                                       (((ld.s.beg / KEYS + ld_i) * KEYS + h) & (c.page_size - 1)) * c.pos_stride + mine_at
-                                                 : 0;
-#pragma unroll
-                    for (int k = 0; k < 8; k += RPI) {
-                        const int r = h + k + lane / CPR;
-                        const uint32_t d = dst + (uint32_t)(r * G::kRow) + pd_chunk<CPR>(r, chunk);
-                        const bool full = (bits >> (k + lane / CPR)) & 1u;  // rows without a position are filled with zeros
-                        cp_async16(d, kp + src, full);
-                        cp_async16(d + G::kSide, vp + src, full);
-                        if (bits & 0xffu) src += RPI * c.pos_stride;
+                    for (int r = 0; r < KEYS; r += RPI) {
+                        const uint32_t d = dst + (uint32_t)(r * G::kRow) + (mine_to ^ (CPR == 8 && (r & 4) ? 16u : 0u));
+                        cp_async16(d, ksrc);
+                        cp_async16(d + G::kSide, vsrc);
+                        ksrc += hop;
+                        vsrc += hop;
                     }
+                    if (lane < 2 * CHUNKS)
+                        cp_async16(dst + (uint32_t)(2 * G::kSide + lane * 16),
+                                   s_at + (pg * a.scale_page + ld_head * a.scale_head + in_page * NB));
+                } else {
+#pragma unroll
+                    for (int h = 0; h < KEYS; h += 8) {  // a page holds 8 positions or more
+                        const uint32_t bits = (mask >> h) & 0xffu;
+                        const int pg = __shfl_sync(0xffffffffu, page, h + max(0, __ffs(bits) - 1));
+                        int64_t at = bits ? pg * c.page_stride + ld_head * c.head_stride + ((first + h) & (c.page_size - 1)) * c.pos_stride : 0;
+#pragma unroll
+                        for (int k = 0; k < 8; k += RPI) {
+                            const uint32_t d = dst + (uint32_t)((h + k) * G::kRow) + (mine_to ^ (CPR == 8 && (k & 4) ? 16u : 0u));
+                            const bool full = (bits >> (k + lane / CPR)) & 1u;  // rows without a position are filled with zeros
+                            cp_async16(d, full ? k_at + at : k_at - mine_at, full);
+                            cp_async16(d + G::kSide, full ? v_at + at : v_at - mine_at, full);
+                            at += hop;
+                        }
+                    }
+                    const int x = lane % CHUNKS * PER, some = __ffs((mask >> x) & ((1u << PER) - 1u));
+                    const int pg = __shfl_sync(0xffffffffu, page, x + max(0, some - 1));
+                    const int64_t at = some ? pg * a.scale_page + ld_head * a.scale_head + ((first + x) & (c.page_size - 1)) * NB - lane % CHUNKS * 16 : 0;
+                    if (lane < 2 * CHUNKS) cp_async16(dst + (uint32_t)(2 * G::kSide + lane * 16), s_at + at, some > 0);
                 }
-                // 16 bytes hold the scales of PER positions, which lie in one page
-                constexpr int PER = 16 / NB, CHUNKS = KEYS / PER;
-                const int x = lane % CHUNKS, first = __ffs((mask >> (x * PER)) & ((1u << PER) - 1u));
-                const int64_t so = __shfl_sync(0xffffffffu, on ? page * a.scale_page + (ld.u / ld.s.tiles) * a.scale_head +
-                                                                    (p & (c.page_size - 1)) / PER * 16 : 0, x * PER + max(0, first - 1));
-                if (lane < 2 * CHUNKS)
-                    cp_async16(dst + (uint32_t)(2 * G::kSide + lane * 16), (lane < CHUNKS ? a.kscale : a.vscale) + so, first > 0);
             }
             ld_skip = stride;
             more = ld_seek();
@@ -394,6 +423,7 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
     // ---- the steps, unit by unit
     int st = 0, skip = solo ? 0 : warp;  // skip: steps until this warp's next
     float* so = reinterpret_cast<float*>(smem + G::kRing);
+    const uint32_t fs = smem_u32(smem) + (uint32_t)(G::kRing + kPdWarps * 8 * DH * 4 + warp * G::kFloats * 4);  // codes: a step's scales
     auto dim_of = [&](int i, int e) { return 16 * i + (Src::kMx ? 2 * g + (e >> 1) : g + 8 * (e >> 1)); };  // of o[i][.][e]
     for (int64_t now = t0; now < t1;) {
         // steps [i0, i0 + n) of the unit are in this part
@@ -485,38 +515,76 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
                     mma16816<T>(s[1], q[k], kb[2], kb[3]);
                 }
             } else {
-                using C = typename Src::H;
-                float f[NS][2][NB];
+                // The step's scales as floats, [K, V][pair of positions][block][position], each worked out by one lane; those of V
+                // over the unit.
+                constexpr int WORDS = 2 * KEYS * NB / 4;  // of 4 bytes
+                {
+                    const bool of_v = lane % WORDS >= WORDS / 2;
+                    uint32_t w = lds32(vs + G::kSide + (uint32_t)(lane % WORDS * 4));
+                    if (of_v && mask != 0xffffu) {  // what nothing attends to may be anything
+                        const uint32_t bits = mask >> (lane % (WORDS / 2) * (4 / NB));
+                        if (NB == 4)
+                            w = bits & 1u ? w : 0u;
+                        else
+                            w &= (bits & 1u ? 0xffffu : 0u) | (bits & 2u ? 0xffff0000u : 0u);
+                    }
+                    float f[4] = {mx_scale(w, 0), mx_scale(w, 1), mx_scale(w, 2), mx_scale(w, 3)};
+                    float most = fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3]));
+                    if (__any_sync(0xffffffffu, of_v ? most > unit : most == INFINITY)) {  // (an infinite scale is NaN's: it sets no unit)
+                        most = 0.f;
 #pragma unroll
-                for (int n = 0; n < NS; ++n) pd_scales<NB>(vs + G::kSide + (uint32_t)((8 * n + 2 * t) * NB), f[n]);
+                        for (int e = 0; e < 4; ++e) {
+                            if (f[e] == INFINITY) f[e] = __int_as_float(0x7fc00000);
+                            most = fmaxf(most, f[e]);
+                        }
+                        const float next = fmaxf(unit, __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(of_v ? most : 0.f))));
+                        const float r = unit * pd_inverse(next);
+                        unit = next;
+#pragma unroll
+                        for (int x = 0; x < NT; ++x)
+#pragma unroll
+                            for (int i = 0; i < DH / 16; ++i)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) o[i][x][e] *= r;
+                    }
+                    const float inv = of_v ? pd_inverse(unit) : 1.f;
+                    const uint32_t to = fs + (uint32_t)(of_v ? KEYS * NB * 4 : 0);
+                    const int i = lane % (WORDS / 2);
+                    if (NB == 4) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sts32(to + (uint32_t)((i >> 1) * 32 + e * 8 + (i & 1) * 4), f[e] * inv);
+                    } else {
+                        sts128_at(to + (uint32_t)(i * 16), __float_as_uint(f[0] * inv), __float_as_uint(f[2] * inv),
+                                  __float_as_uint(f[1] * inv), __float_as_uint(f[3] * inv));
+                    }
+                    __syncwarp();
+                }
+                using C = typename Src::H;
 #pragma unroll
                 for (int n = 0; n < NS; ++n) {  // keys 8 n + g; a scale's 32 dimensions into a sum of their own
                     const int r = 8 * n + g;
+                    uint64_t sum2[NT] = {};
 #pragma unroll
-                    for (int b = 0; b < NB; ++b) {
-                        const uint2 w = lds64(ks + (uint32_t)(r * G::kRow + ((t & 1) << 3)) + pd_chunk<CPR>(r, 2 * b + (t >> 1)));
-                        float sum[4] = {};
-                        mma16816<__half>(sum, q[2 * b], C::lo(w.x), C::hi(w.x));
-                        mma16816<__half>(sum, q[2 * b + 1], C::lo(w.y), C::hi(w.y));
+                    for (int b = 0; b < NB; b += 2) {
+                        uint64_t f2[2];
+                        lds2x64(fs + (uint32_t)((4 * n + t) * NB * 8 + b * 8), f2);
 #pragma unroll
-                        for (int e = 0; e < 2 * NT; ++e) s[n][e] = fmaf(sum[e], f[n][e & 1][b], s[n][e]);
+                        for (int e = 0; e < 2; ++e) {
+                            const uint2 w = lds64(ks + (uint32_t)(r * G::kRow + ((t & 1) << 3)) + pd_chunk<CPR>(r, 2 * (b + e) + (t >> 1)));
+                            float part[4];
+                            mma16816_new(part, q[2 * (b + e)], C::lo(w.x), C::hi(w.x));
+                            mma16816<__half>(part, q[2 * (b + e) + 1], C::lo(w.y), C::hi(w.y));
+#pragma unroll
+                            for (int x = 0; x < NT; ++x) sum2[x] = f2_fma(f2_pack(part[2 * x], part[2 * x + 1]), f2[e], sum2[x]);
+                        }
                     }
+#pragma unroll
+                    for (int x = 0; x < NT; ++x) f2_unpack(sum2[x], s[n][2 * x], s[n][2 * x + 1]);
                 }
-                // an infinite scale marks a NaN, whatever its codes are
-                float far = 0.f;
-#pragma unroll
-                for (int n = 0; n < NS; ++n)
-#pragma unroll
-                    for (int e = 0; e < 2 * NT; ++e) far += fabsf(s[n][e]);
-                if (__any_sync(0xffffffffu, !(far < INFINITY)))
-#pragma unroll
-                    for (int n = 0; n < NS; ++n)
-#pragma unroll
-                        for (int e = 0; e < 2 * NT; ++e)
-#pragma unroll
-                            for (int b = 0; b < NB; ++b)
-                                if (f[n][e & 1][b] == INFINITY) s[n][e] = __int_as_float(0x7fc00000);
             }
+            // whether some column does not attend to all of the step
+            const bool partial = !Src::kMx || mask != 0xffffu ||
+                                 (ROWS && (p0 + KEYS - 1 > at.s.len || (a.window > 0 && p0 <= at.s.len + at.s.rows - 1 - a.window)));
             // Weights.  m is a reference: the maximum less kUp where P is fp16, so that P goes up to 2^15 (it has no steps below
             // 2^-24); over codes it moves only when P would pass that, down to 2^12.  l, o and every later join agree on it.
             constexpr bool HALF_P = Src::kMx || std::is_same<T, __half>::value;
@@ -529,10 +597,13 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
                 float v[2 * NS], mx = -INFINITY;
 #pragma unroll
                 for (int e = 0; e < 2 * NS; ++e) {  // keys 2t, 2t + 1, 2t + 8, 2t + 9, ... of column g + 8x
-                    const int key = 8 * (e >> 1) + 2 * t + (e & 1);
-                    bool on = (mask >> key) & 1u;
-                    if (ROWS) on = on && p0 + key <= last_key[x] && (a.window == 0 || p0 + key > last_key[x] - a.window);
-                    v[e] = on ? s[e >> 1][2 * x + (e & 1)] * qs[x] : -INFINITY;
+                    v[e] = s[e >> 1][2 * x + (e & 1)] * qs[x];
+                    if (partial) {
+                        const int key = 8 * (e >> 1) + 2 * t + (e & 1);
+                        bool on = (mask >> key) & 1u;
+                        if (ROWS) on = on && p0 + key <= last_key[x] && (a.window == 0 || p0 + key > last_key[x] - a.window);
+                        v[e] = on ? v[e] : -INFINITY;
+                    }
                     mx = fmaxf(mx, v[e]);
                 }
                 mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
@@ -590,55 +661,20 @@ __global__ void __launch_bounds__(kPdThreads, kPdCtasPerSm) k_paged_decode(const
                 using C = typename Src::H;
                 using H = Elem<__half>;
                 const int mr = (lane & 7) + (lane & 8), mc = lane >> 4;  // ldmatrix: row, chunk of a pair
-                float f[NS][2][NB], most = 0.f;
-#pragma unroll
-                for (int n = 0; n < NS; ++n) {
-                    pd_scales<NB>(vs + G::kSide + G::kScales + (uint32_t)((8 * n + 2 * t) * NB), f[n]);
-                    if (mask != (KEYS == 32 ? 0xffffffffu : (1u << (KEYS & 31)) - 1u))  // what nothing attends to may be anything
-#pragma unroll
-                        for (int j = 0; j < 2; ++j)
-#pragma unroll
-                            for (int b = 0; b < NB; ++b)
-                                if (!((mask >> (8 * n + 2 * t + j)) & 1u)) f[n][j][b] = 0.f;
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) most = fmaxf(most, fmaxf(f[n][0][b], f[n][1][b]));
-                }
-                if (__any_sync(0xffffffffu, most > unit)) {
-                    most = 0.f;
-#pragma unroll
-                    for (int n = 0; n < NS; ++n)
-#pragma unroll
-                        for (int j = 0; j < 2; ++j)
-#pragma unroll
-                            for (int b = 0; b < NB; ++b) {  // (an infinite scale marks a NaN: it sets no unit)
-                                if (f[n][j][b] == INFINITY) f[n][j][b] = __int_as_float(0x7fc00000);
-                                most = fmaxf(most, f[n][j][b]);
-                            }
-                    const float next = fmaxf(unit, __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most))));
-                    const float r = unit * pd_inverse(next);
-                    unit = next;
-#pragma unroll
-                    for (int x = 0; x < NT; ++x)
-#pragma unroll
-                        for (int i = 0; i < DH / 16; ++i)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o[i][x][e] *= r;
-                }
-                const float inv = pd_inverse(unit);
-#pragma unroll
-                for (int x = 0; x < NT; ++x)
-#pragma unroll
-                    for (int e = 0; e < 2 * NS; ++e) pw[x][e] *= inv;
 #pragma unroll
                 for (int n = 0; n < KEYS / 16; ++n)
 #pragma unroll
                     for (int b = 0; b < NB; ++b) {
+                        uint64_t f2[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) f2[e] = lds1x64(fs + (uint32_t)(KEYS * NB * 4 + (8 * n + 4 * e + t) * NB * 8 + b * 8));
                         uint32_t hi[NT][2], lo[NT][2];
 #pragma unroll
                         for (int x = 0; x < NT; ++x)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                const float w0 = pw[x][4 * n + 2 * e] * f[2 * n + e][0][b], w1 = pw[x][4 * n + 2 * e + 1] * f[2 * n + e][1][b];
+                                float w0, w1;
+                                f2_unpack(f2_mul(f2_pack(pw[x][4 * n + 2 * e], pw[x][4 * n + 2 * e + 1]), f2[e]), w0, w1);
                                 hi[x][e] = H::pack(w0, w1);
                                 if constexpr (TWO) {
                                     const float2 h = H::unpack(hi[x][e]);
@@ -822,9 +858,9 @@ inline int64_t paged_decode_line_of(const PagedAttnArgs& a, int cols, int keys) 
 
 template <class Src, int DH, int NT, bool ROWS>
 static cudaError_t decode_nt(const PagedAttnArgs& a, cudaStream_t st) {
-    const int64_t most = paged_decode_line_of(a, 8 * NT, PdGeom<Src, DH>::kKeys);
-    const int64_t grid = std::min<int64_t>(std::min(kPagedMaxGrid, kPdCtasPerSm * g_num_sms), (most + kPdMinSteps - 1) / kPdMinSteps);
-    return launch_paged_k(k_paged_decode<Src, DH, NT, ROWS>, (unsigned)grid, kPdThreads, PdGeom<Src, DH>::kSmem, st, a);
+    const int64_t most = paged_decode_line_of(a, 8 * NT, PdGeom<Src, DH, NT>::kKeys);
+    const int64_t grid = std::min<int64_t>(std::min(kPagedMaxGrid, PdGeom<Src, DH, NT>::kCtas * g_num_sms), (most + kPdMinSteps - 1) / kPdMinSteps);
+    return launch_paged_k(k_paged_decode<Src, DH, NT, ROWS>, (unsigned)grid, kPdThreads, PdGeom<Src, DH, NT>::kSmem, st, a);
 }
 template <class Src, bool ROWS>
 static cudaError_t decode_dh(const PagedAttnArgs& a, int dh, cudaStream_t st) {
@@ -841,10 +877,10 @@ static cudaError_t decode_src(const PagedAttnArgs& a, int dh, cudaStream_t st) {
 template <class Src, int DH, int NT>
 static cudaError_t init_one() {
     const cudaError_t e = cudaFuncSetAttribute(k_paged_decode<Src, DH, NT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               (int)PdGeom<Src, DH>::kSmem);
+                                               (int)PdGeom<Src, DH, NT>::kSmem);
     return e != cudaSuccess ? e
                             : cudaFuncSetAttribute(k_paged_decode<Src, DH, NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   (int)PdGeom<Src, DH>::kSmem);
+                                                   (int)PdGeom<Src, DH, NT>::kSmem);
 }
 template <class Src>
 static cudaError_t init_src() {
