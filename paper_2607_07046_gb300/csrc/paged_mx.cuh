@@ -14,80 +14,86 @@ namespace vt {
 
 constexpr int kMxBlock = 32;  // dimensions that share a scale
 
-template <class T>
-__device__ __forceinline__ uint32_t mx_mul(uint32_t a, uint32_t b) {
-    if constexpr (std::is_same<T, __half>::value) {
-        const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
-        return *reinterpret_cast<const uint32_t*>(&r);
-    } else {
-        const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
-        return *reinterpret_cast<const uint32_t*>(&r);
-    }
-}
-
-// Codes of format F (VT_MX_*) as pairs of values of type T.  two<S>(w): the bytes S & 15 and S >> 4 of w, to be
-// multiplied by scale(): e4m3 codes are moved to their places in T's bits (no conversion: their value is then less by
-// the difference of the exponents' biases, which the scale makes up for, subnormal codes included); whole numbers
-// come from the sums 1024 + u (fp16, u the code + 128) and 128 + low 7 bits (bf16), both exact.
+// Codes of format F as pairs of values of type T, without their scale: the lower and upper two of w, or its bytes 0, 2 and
+// 1, 3; and the scale of byte s as a pair to multiply them by (byte 0 gives 0, 255 NaN).
 template <class T, int F>
-struct MxCodes {
-    static constexpr bool kHalf = std::is_same<T, __half>::value, kFloat = F == VT_MX_E4M3;
+struct MxCodes;
 
-    template <int S>
-    static __device__ __forceinline__ uint32_t two(uint32_t w) {
-        constexpr uint32_t lo = S & 15, hi = S >> 4;
-        if constexpr (kFloat) {
-            const uint32_t x = __byte_perm(w, 0u, 4u | (lo << 4) | (4u << 8) | (hi << 12));  // codes in the upper bytes
-            const uint32_t y = (x >> (kHalf ? 1 : 4)) & (kHalf ? 0x3f803f80u : 0x07f007f0u);
-            return (x & 0x80008000u) | y;
-        } else if constexpr (kHalf) {
-            const uint32_t x = __byte_perm(w ^ 0x80808080u, 0x64646464u, lo | (4u << 4) | (hi << 8) | (4u << 12));
-            const uint32_t k = 0x64806480u;  // 1152
-            const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&k));
-            return *reinterpret_cast<const uint32_t*>(&r);
-        } else {
-            const uint32_t x = __byte_perm(w, 0u, lo | (4u << 4) | (hi << 8) | (4u << 12));
-            const uint32_t a = (x & 0x007f007fu) | 0x43004300u, b = (x & 0x00800080u) | 0x43004300u;  // less 128, or 256 for a sign
-            const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
-            return *reinterpret_cast<const uint32_t*>(&r);
-        }
-    }
-    // The scale of byte s, twice; byte 0 gives 0, 255 NaN.
-    static __device__ __forceinline__ uint32_t scale(uint32_t s) {
-        if (s == 255u) return 0x7fff7fffu;
-        const uint32_t p = kHalf ? Elem<T>::pack(__uint_as_float(s << 23), __uint_as_float(s << 23)) : s * 0x00800080u;
-        return kFloat ? mx_mul<T>(p, kHalf ? 0x5c005c00u : 0x7b807b80u) : p;  // 2^8, 2^120
-    }
-    static __device__ __forceinline__ uint32_t mul(uint32_t a, uint32_t s) { return mx_mul<T>(a, s); }
-};
-
-// Codes as pairs of fp16, without their scale: the lower and upper two of w, or its bytes 0, 2 and 1, 3.
+// e4m3: one conversion for two codes.  int8: 1024 + u, u the code + 128, is a sum of bits, less 1152.
 template <int F>
-struct MxHalf {
+struct MxCodes<__half, F> {
+    static constexpr bool kFloat = F == VT_MX_E4M3;
     static __device__ __forceinline__ uint32_t convert(uint16_t two) {
         uint32_t r;
         asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(two));
         return r;
     }
+    template <int S>  // bytes S & 15 and S >> 4
+    static __device__ __forceinline__ uint32_t whole(uint32_t w) {
+        const uint32_t x = __byte_perm(w ^ 0x80808080u, 0x64646464u, (S & 15) | (4u << 4) | ((S >> 4) << 8) | (4u << 12));
+        const uint32_t k = 0x64806480u;  // 1152
+        const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&k));
+        return *reinterpret_cast<const uint32_t*>(&r);
+    }
     static __device__ __forceinline__ uint32_t lo(uint32_t w) {
-        if constexpr (F == VT_MX_E4M3) return convert((uint16_t)w);
-        return MxCodes<__half, F>::template two<0x10>(w);
+        if constexpr (kFloat) return convert((uint16_t)w);
+        return whole<0x10>(w);
     }
     static __device__ __forceinline__ uint32_t hi(uint32_t w) {
-        if constexpr (F == VT_MX_E4M3) return convert((uint16_t)(w >> 16));
-        return MxCodes<__half, F>::template two<0x32>(w);
+        if constexpr (kFloat) return convert((uint16_t)(w >> 16));
+        return whole<0x32>(w);
     }
     static __device__ __forceinline__ void split(uint32_t w, uint32_t& even, uint32_t& odd) {
-        if constexpr (F == VT_MX_E4M3) {
+        if constexpr (kFloat) {
             const uint32_t x = __byte_perm(w, 0u, 0x3120);
             even = lo(x);
             odd = hi(x);
         } else {
-            even = MxCodes<__half, F>::template two<0x20>(w);
-            odd = MxCodes<__half, F>::template two<0x31>(w);
+            even = whole<0x20>(w);
+            odd = whole<0x31>(w);
         }
     }
+    static __device__ __forceinline__ uint32_t scale(uint32_t s) {
+        const float f = __uint_as_float(s << 23);
+        return s == 255u ? 0x7fff7fffu : Elem<__half>::pack(f, f);
+    }
+    static __device__ __forceinline__ uint32_t mul(uint32_t a, uint32_t b) {
+        const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+        return *reinterpret_cast<const uint32_t*>(&r);
+    }
 };
+
+// e4m3: the bits move to their places (no conversion: the value is then less by 2^120, the difference of the exponents'
+// biases, which the scale makes up for; subnormal codes become subnormal numbers).  int8: 128 + the low 7 bits is a sum of
+// bits, less 128, or 256 for a negative code.
+template <int F>
+struct MxCodes<__nv_bfloat16, F> {
+    static constexpr bool kFloat = F == VT_MX_E4M3;
+    template <int S>
+    static __device__ __forceinline__ uint32_t two(uint32_t w) {
+        if constexpr (kFloat) {
+            const uint32_t x = __byte_perm(w, 0u, 4u | ((S & 15) << 4) | (4u << 8) | ((S >> 4) << 12));  // codes in the upper bytes
+            const uint32_t y = (x >> 4) & 0x07f007f0u;
+            return (x & 0x80008000u) | y;
+        } else {
+            const uint32_t x = __byte_perm(w, 0u, (S & 15) | (4u << 4) | ((S >> 4) << 8) | (4u << 12));
+            const uint32_t a = (x & 0x007f007fu) | 0x43004300u, b = (x & 0x00800080u) | 0x43004300u;
+            const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+            return *reinterpret_cast<const uint32_t*>(&r);
+        }
+    }
+    static __device__ __forceinline__ uint32_t lo(uint32_t w) { return two<0x10>(w); }
+    static __device__ __forceinline__ uint32_t hi(uint32_t w) { return two<0x32>(w); }
+    static __device__ __forceinline__ uint32_t scale(uint32_t s) {
+        const uint32_t p = s * 0x00800080u;
+        return s == 255u ? 0x7fff7fffu : kFloat ? mul(p, 0x7b807b80u) : p;  // 2^120
+    }
+    static __device__ __forceinline__ uint32_t mul(uint32_t a, uint32_t b) {
+        const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+        return *reinterpret_cast<const uint32_t*>(&r);
+    }
+};
+
 // Scale b of a word of scales.
 __device__ __forceinline__ float mx_scale(uint32_t w, int b) {
     return __uint_as_float((b == 3 ? w >> 1 : w << (23 - 8 * b)) & 0x7f800000u);
@@ -104,7 +110,7 @@ template <class E, int F>
 struct PoolMx {
     using T = E;
     using C = MxCodes<E, F>;
-    using H = MxHalf<F>;
+    using H = MxCodes<__half, F>;
     static constexpr bool kMx = true;
     static constexpr int kBytes = 1;
 };

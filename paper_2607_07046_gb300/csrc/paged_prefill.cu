@@ -48,13 +48,6 @@
 namespace vt {
 
 constexpr int kPfRows = 128, kPfKeys = 128;  // rows of a tile, keys of a block
-constexpr int kPfThreads = 384;
-constexpr int kPfCopyWarps = 2, kPfMma = 8 + kPfCopyWarps;  // then one MMA warp a tile
-// registers a thread: at launch 65536 / 384, rounded down to 8; then 2 x 128 threads of softmax and 128 of
-// copies and MMAs
-constexpr int kPfLaunchRegs = 168, kPfSoftmaxRegs = 208, kPfCopyRegs = 88;
-static_assert(256 * kPfSoftmaxRegs + 128 * kPfCopyRegs <= kPfThreads * kPfLaunchRegs,
-              "the register split must fit in the registers the block is launched with");
 constexpr int kPfMaskRing = 8;   // validity words of the last blocks (the copies lead by fewer blocks)
 // The start and end of a unit cost as much as this many blocks (5 prompts: 46 us at 1, 42 at 2, 44 at 3).
 constexpr int kPfUnitCost = 2;
@@ -71,16 +64,25 @@ constexpr int kPfJoinParts = 5;
 constexpr int kPfJoinChunk = 2;
 constexpr int kPfLag = 2;        // copy groups in flight behind the one just issued
 
-constexpr int kPfRawLag = 2;     // 8 bits: blocks of K or V whose codes are on their way while one is converted
 
 template <class Src, int DH>
 struct PfGeom {
+    // Warps: 8 of softmax, those of the copies, then one MMA warp a tile.  Codes: four warps convert them, so that each of the
+    // SM's four schedulers has one (a warp's conversions of a block take it about 1000 instructions).
+    static constexpr int kCopyWarps = Src::kMx ? 4 : 2, kMma = 8 + kCopyWarps;
+    static constexpr int kThreads = Src::kMx ? 512 : 384;
+    // Registers a thread: at launch 65536 / threads, rounded down to 8; then 2 x 128 threads of softmax, and 128 of copies and
+    // MMAs, or 128 of each.
+    static constexpr int kLaunchRegs = Src::kMx ? 128 : 168, kSoftmaxRegs = Src::kMx ? 184 : 208, kCopyRegs = Src::kMx ? 64 : 88;
+    static constexpr int kMmaRegs = Src::kMx ? 80 : 88;
+    static_assert(256 * kSoftmaxRegs + 128 * kCopyRegs + (kThreads - 384) * kMmaRegs <= kThreads * kLaunchRegs,
+                  "the register split must fit in the registers the block is launched with");
     static constexpr int kTile = kPfRows * DH * 2;         // bytes of a Q tile, of a K or V block
     static constexpr int kAtom = kPfRows * 128;            // its 64-column box
     static constexpr int kSlots = (DH == 128 ? 1 : 2) * (Src::kMx ? 3 : 5);  // K and V blocks of the ring, in turn
     static constexpr int kRaw = Src::kMx ? kPfKeys * (DH + DH / kMxBlock) : 0;  // codes and scales of a block
-    static constexpr int kRaws = kPfRawLag + 1;
-    static constexpr size_t kSmem = 1024 + (size_t)(2 + kSlots) * kTile + kRaws * kRaw + 512 + kPfThreads / 32 * 64;
+    static constexpr int kRaws = 3;                        // of them on their way
+    static constexpr size_t kSmem = 1024 + (size_t)(2 + kSlots) * kTile + kRaws * kRaw + 512 + (Src::kMx ? 128 : 0) + kThreads / 32 * 64;
 };
 
 // The units in order: sequence, KV head, tile pair.
@@ -197,187 +199,227 @@ struct PfParams {
     CUtensorMap tk, tv;   // [pages][KV heads][positions][dh], boxes of a page's positions (128 at most) by 64 columns
 };
 
-// The copy warps over a pool of codes: codes and scales come by asynchronous copies of 16 bytes (a lane's own codes, its
-// warp's scales), kPfRawLag blocks of K or V ahead, and are converted to the type of Q into the ring, as the tensor copies of a
-// 16-bit pool would leave them there.  Positions outside the unit's range and bad pages get scale 0, whose product with
-// any code is 0.  A page holds 8 positions or more, so a group of 8 rows lies in one.  False: a wait ran out.
-struct PfShared {
-    uint8_t *Qs, *Rs, *raw;
-    uint32_t* valid;
-    uint64_t *full, *empty, *q_full, *q_empty;
+// Over a pool of codes, three roles take the place of the copy warps:
+//   copies        (one warp) codes and scales of a block of K or V as they are, by asynchronous copies of 16 bytes, into
+//                 one of kRaws buffers
+//   conversions   (four warps) from there to the type of Q, into the ring, as the tensor copies of a 16-bit pool would leave
+//                 them there.  They know nothing of units: they follow the buffers until one says that it is the last
+//   queries       (one warp)
+// Positions outside the unit's range and bad pages get scale 0, whose product with any code (they are filled with zeros) is
+// 0.  A page holds 8 positions or more, so a group of 8 rows lies in one.
+struct PfRaw {
+    uint8_t* data;         // [kRaws][kRaw]: codes [128][dh] (the halves of odd rows of 128 bytes swapped), scales [128][dh / 32]
+    uint64_t *full, *empty;
+    uint32_t* rows;        // [kRaws][4] which rows hold something
+    int* last;             // [kRaws] nothing follows, and nothing is there
 };
+template <int CPR>
+__device__ __forceinline__ uint32_t pf_raw_chunk(int row, int chunk) {
+    return (uint32_t)((row * CPR + (CPR == 8 ? chunk ^ ((row & 1) << 2) : chunk)) * 16);
+}
+
 template <class Src, int DH>
-__device__ __forceinline__ bool pf_convert(const PfParams& P, const PfShared& m, PfCursor at, int64_t left) {
+__device__ __forceinline__ bool pf_copy_codes(const PagedAttnArgs& a, const PfRaw& m, uint32_t* valid, PfCursor at, int64_t left) {
     using G = PfGeom<Src, DH>;
-    using C = typename Src::C;
-    constexpr int S = G::kSlots, HALVES = DH / 64, NB = DH / kMxBlock;
-    constexpr int CPR = DH / 16, RPI = 32 / CPR, PASSES = 8 / RPI, GROUPS = 16 / kPfCopyWarps;  // passes of a group, a warp's groups
-    constexpr int SCALES = GROUPS * 8 * NB / 16;  // 16-byte pieces of a warp's scales
-    const PagedAttnArgs& a = P.a;
+    constexpr int NB = DH / kMxBlock, CPR = DH / 16, RPI = 32 / CPR, PIECES = kPfKeys * NB / 16;  // 16-byte pieces of the scales
     const PagedView& c = a.c;
-    const int tid = threadIdx.x, lane = tid & 31, w = (tid >> 5) - 8, tr = kPfRows / a.group;
-    const int chunk = lane % CPR, sub = lane / CPR;
-    const uint32_t raw0 = smem_u32(m.raw) + (uint32_t)((w * 32 + lane) * 16);
-    const uint32_t scl0 = smem_u32(m.raw) + (uint32_t)(kPfKeys * DH + w * (SCALES * 16));
-
-    // ---- the copies' own place in the line: K or V of block ld_j of unit ld
-    PfCursor ld = at;
-    int64_t ld_left = left;
-    int ld_j = 0, ld_end = 0, ld_blk = 0, ld_raw = 0;
-    bool ld_v = false, more = true;
-    auto open = [&]() {
-        for (;;) {
-            more = ld_left > 0;
-            if (!more) return;
-            int n;
-            ld_j = ld.kb0 + ld.part(ld_left, n);
-            ld_end = ld_j + n;
-            ld_left -= ld.rest();
-            if (n > 0) return;
-            ld.next(a, tr);
-        }
-    };
-    open();
-    int page = 0;       // lane g < 16: the page of 8-row group g of block ld_j, and which of its rows are attended to
-    uint32_t rows = 0;
-    auto issue = [&]() -> uint32_t {  // the lane's chunks that hold something
-        uint32_t on = 0;
-        if (more) {
-            const int p0 = ld_j * kPfKeys;
-            if (!ld_v) {
-                const int g0 = p0 + 8 * (lane & 15);
-                page = 0;
-                rows = fa_range_bits(ld.kbeg - g0, ld.kend - g0) & 0xffu;
-                if (rows) page = c.tables[(int64_t)ld.b * c.per_seq + (g0 >> c.page_shift)];
-                if ((unsigned)page >= (unsigned)c.n_pages) {
-                    rows = 0;
-                    page = 0;
-                    if (w == 0) set_status(c.status, VT_DEV_BAD_PAGE);
-                }
-                if (w == 0 && lane < 16) reinterpret_cast<uint8_t*>(m.valid)[(ld_blk % kPfMaskRing) * 16 + lane] = (uint8_t)rows;
-            }
-            const uint8_t* pool = reinterpret_cast<const uint8_t*>(ld_v ? a.vpool : a.kpool) + ld.kvh * c.head_stride + chunk * 16;
-            const uint32_t dst = raw0 + (uint32_t)(ld_raw * G::kRaw);
-#pragma unroll
-            for (int i = 0; i < GROUPS; ++i) {
-                const int g = w + i * kPfCopyWarps;
-                const int pg = __shfl_sync(0xffffffffu, page, g);
-                const uint32_t bits = __shfl_sync(0xffffffffu, rows, g) >> sub;
-                const uint8_t* src = pool + pg * c.page_stride + (((p0 + 8 * g) & (c.page_size - 1)) + sub) * c.pos_stride;
-#pragma unroll
-                for (int k = 0; k < PASSES; ++k) {
-                    const bool one = (bits >> (k * RPI)) & 1u;
-                    on |= (one ? 1u : 0u) << (i * PASSES + k);
-                    pf_copy16(dst + (uint32_t)((i * PASSES + k) * (kPfCopyWarps * 512)), src + k * RPI * c.pos_stride, one);
-                }
-            }
-            {
-                const int g = w + lane % SCALES * GROUPS / SCALES * kPfCopyWarps;
-                const int pg = __shfl_sync(0xffffffffu, page, g);
-                const bool any = __shfl_sync(0xffffffffu, rows, g) != 0;
-                const uint8_t* src = (ld_v ? a.vscale : a.kscale) + pg * a.scale_page + ld.kvh * a.scale_head +
-                                     ((p0 + 8 * g) & (c.page_size - 1)) * NB + lane % (SCALES / GROUPS) * 16;
-                if (lane < SCALES) pf_copy16(scl0 + (uint32_t)(ld_raw * G::kRaw + lane * 16), src, any);
-            }
-            ld_raw = ld_raw + 1 == G::kRaws ? 0 : ld_raw + 1;
-            if (ld_v) {
-                ++ld_blk;
-                if (++ld_j == ld_end) {
-                    ld.next(a, tr);
-                    open();
-                }
-            }
-            ld_v = !ld_v;
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        return on;
-    };
-    uint32_t ons[kPfRawLag];
-#pragma unroll
-    for (int i = 0; i < kPfRawLag; ++i) ons[i] = issue();
-
-    // ---- the conversions, in the same order
+    const int lane = threadIdx.x & 31, tr = kPfRows / a.group, chunk = lane % CPR, sub = lane / CPR;
+    const int64_t mine = sub * c.pos_stride + chunk * 16, hop = RPI * c.pos_stride;
+    const uint32_t to = smem_u32(m.data) + pf_raw_chunk<CPR>(sub, chunk);  // (sub, sub + RPI: the same parity)
+    int buf = 0, round = 0, blk = 0;
     bool ok = true;
-    int slot = 0, round = 0, from = 0, nq = 0;
+    // lane g < 16: the page of 8-row group g of block j (-1: not needed), requested a block ahead
+    auto request = [&](int j) {
+        const int p = j * kPfKeys + 8 * (lane & 15);
+        return p + 8 > at.kbeg && p < at.kend ? c.tables[(int64_t)at.b * c.per_seq + (p >> c.page_shift)] : 0;
+    };
     while (ok && left > 0) {
         int n;
         const int j0 = at.kb0 + at.part(left, n);
         left -= at.rest();
-        for (int x = 0; ok && x < 2 * n; ++x) {
-            const uint32_t last = issue(), on = ons[0];
-#pragma unroll
-            for (int i = 0; i + 1 < kPfRawLag; ++i) ons[i] = ons[i + 1];
-            ons[kPfRawLag - 1] = last;
-            asm volatile("cp.async.wait_group %0;" ::"n"(kPfRawLag) : "memory");
-            __syncwarp();  // the scales are other lanes' copies
-            if (round > 0) ok = pf_wait(&m.empty[slot], (round - 1) & 1);
-            if (!ok) break;
-            const uint32_t dst = smem_u32(m.Rs + slot * G::kTile), src = raw0 + (uint32_t)(from * G::kRaw);
-            const uint32_t scl = scl0 + (uint32_t)(from * G::kRaw + sub * NB + (chunk >> 1));
-#pragma unroll
-            for (int i = 0; i < GROUPS; ++i)
-#pragma unroll
-                for (int k = 0; k < PASSES; ++k) {
-                    const uint4 w4 = lds128_at(src + (uint32_t)((i * PASSES + k) * (kPfCopyWarps * 512)));
-                    const uint32_t b = (on >> (i * PASSES + k)) & 1u ? lds8(scl + (uint32_t)((8 * i + k * RPI) * NB)) : 0u;
-                    const uint32_t f = C::scale(b), v[4] = {w4.x, w4.y, w4.z, w4.w};
-                    uint32_t y[8];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        y[2 * e] = C::mul(C::template two<0x10>(v[e]), f);
-                        y[2 * e + 1] = C::mul(C::template two<0x32>(v[e]), f);
-                    }
-                    const int r = 8 * (w + i * kPfCopyWarps) + k * RPI + sub;
-                    // chunks 2 chunk and 2 chunk + 1 of the row's 16-bit values; the second 64 columns' lanes begin with the
-                    // odd one, as both atoms' rows begin in the same bank
-                    const uint32_t row = dst + (uint32_t)((chunk >> 2) * (HALVES - 1) * G::kAtom + r * 128);
-                    const int odd = chunk >> 2, c2 = (2 * chunk) & 7;
-                    const uint32_t d0 = row + (uint32_t)(((c2 + odd) ^ (r & 7)) << 4), d1 = row + (uint32_t)(((c2 + 1 - odd) ^ (r & 7)) << 4);
-                    sts128_at(d0, odd ? y[4] : y[0], odd ? y[5] : y[1], odd ? y[6] : y[2], odd ? y[7] : y[3]);
-                    sts128_at(d1, odd ? y[0] : y[4], odd ? y[1] : y[5], odd ? y[2] : y[6], odd ? y[3] : y[7]);
-                }
-            fence_proxy_async_smem();  // written as threads do; the MMA reads as the copy engine does
-            __syncwarp();              // (and nobody's scales are overwritten before all lanes have read them)
-            if (lane == 0) mbar_arrive(&m.full[slot]);
-            from = from + 1 == G::kRaws ? 0 : from + 1;
-            if (++slot == S) slot = 0, ++round;
-            if (x == 0 && w == 0) {  // the unit's queries, once the last unit's products with its own are done
-                if (nq > 0) ok = pf_wait(m.q_empty, (nq - 1) & 1);
+        int next = n > 0 ? request(j0) : 0;
+        for (int j = j0; ok && j < j0 + n; ++j, ++blk) {
+            int page = next;
+            if (j + 1 < j0 + n) next = request(j + 1);
+            const int p0 = j * kPfKeys, g0 = p0 + 8 * (lane & 15);
+            uint32_t rows = fa_range_bits(at.kbeg - g0, at.kend - g0) & 0xffu;
+            if (rows && (unsigned)page >= (unsigned)c.n_pages) {
+                rows = 0;
+                set_status(c.status, VT_DEV_BAD_PAGE);
+            }
+            if (!rows) page = 0;
+            const bool whole = __all_sync(0xffffffffu, rows == 0xffu);
+            if (lane < 16) reinterpret_cast<uint8_t*>(valid)[(blk % kPfMaskRing) * 16 + lane] = (uint8_t)rows;
+#pragma unroll 1
+            for (int kv = 0; kv < 2; ++kv) {
+                if (round > 0) ok = pf_wait(&m.empty[buf], (round - 1) & 1);
                 if (!ok) break;
-                ++nq;
-                const int tiles = (2 * at.pt + 1) * tr < at.rows ? 2 : 1;
-                if (elect_one()) {
-                    mbar_arrive_expect_tx(m.q_full, (uint32_t)(tiles * HALVES * tr * a.group * 128));
-                    for (int y = 0; y < tiles; ++y)
-                        for (int h = 0; h < HALVES; ++h)
-                            tc::tma_load_3d(m.Qs + y * G::kTile + h * G::kAtom, &P.tq, 64 * h, at.kvh * a.group,
-                                            at.row0 + (2 * at.pt + y) * tr, smem_u32(m.q_full));
+                if (lane < 16) reinterpret_cast<uint8_t*>(m.rows)[buf * 16 + lane] = (uint8_t)rows;
+                if (lane == 0) m.last[buf] = 0;
+                const uint8_t* pool = reinterpret_cast<const uint8_t*>(kv ? a.vpool : a.kpool) + at.kvh * c.head_stride + mine;
+                const uint32_t dst = to + (uint32_t)(buf * G::kRaw);
+                auto group = [&](int g) {
+                    return pool + __shfl_sync(0xffffffffu, page, g) * c.page_stride + ((p0 + 8 * g) & (c.page_size - 1)) * c.pos_stride;
+                };
+                if (whole)
+#pragma unroll 4
+                    for (int g = 0; g < 16; ++g) {
+                        const uint8_t* src = group(g);
+#pragma unroll
+                        for (int k = 0; k < 8; k += RPI, src += hop) pf_copy16(dst + (uint32_t)((8 * g + k) * DH), src, true);
+                    }
+                else
+#pragma unroll 1
+                    for (int g = 0; g < 16; ++g) {
+                        const uint8_t* src = group(g);
+                        const uint32_t bits = __shfl_sync(0xffffffffu, rows, g) >> sub;
+#pragma unroll
+                        for (int k = 0; k < 8; k += RPI, src += hop) pf_copy16(dst + (uint32_t)((8 * g + k) * DH), src, (bits >> k) & 1u);
+                    }
+                {
+                    const int x = lane % PIECES, g = x * 16 / PIECES, pg = __shfl_sync(0xffffffffu, page, g);
+                    const bool any = __shfl_sync(0xffffffffu, rows, g) != 0;
+                    const uint8_t* src = (kv ? a.vscale : a.kscale) + pg * a.scale_page + at.kvh * a.scale_head +
+                                         ((p0 + x * (16 / NB)) & (c.page_size - 1)) * NB;
+                    if (lane < PIECES) pf_copy16(smem_u32(m.data) + (uint32_t)(buf * G::kRaw + kPfKeys * DH + lane * 16), src, any);
                 }
                 __syncwarp();
+                if (lane == 0) mbar_arrive(&m.full[buf]);  // for what was stored
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(&m.full[buf])) : "memory");
+                if (++buf == G::kRaws) buf = 0, ++round;
             }
         }
         at.next(a, tr);
     }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
-    // the CTA may not end while a commit that releases a slot, or a tensor copy, is on its way
-    const bool good = ok;
+    if (ok && round > 0) ok = pf_wait(&m.empty[buf], (round - 1) & 1);
+    if (ok) {
+        if (lane == 0) m.last[buf] = 1;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&m.full[buf]);
+        mbar_arrive(&m.full[buf]);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    return ok;
+}
+
+struct PfRing {
+    uint8_t* data;  // [kSlots][kTile]
+    uint64_t *full, *empty;
+};
+template <class Src, int DH>
+__device__ __forceinline__ bool pf_convert(const PfRaw& m, const PfRing& ring, int w, volatile int* err) {
+    using G = PfGeom<Src, DH>;
+    using C = typename Src::C;
+    constexpr int S = G::kSlots, NB = DH / kMxBlock, CPR = DH / 16, RPI = 32 / CPR, CHUNKS = 128 / (RPI * G::kCopyWarps);
+    const int lane = threadIdx.x & 31;
+    // A pass of the four warps covers 4 RPI rows.  8 lanes have 4 chunks of two rows: their loads and stores fall into
+    // different banks
+    const int chunk = CPR == 8 ? (lane & 3) | ((lane >> 1) & 4) : lane & 3;
+    const int row0 = w * RPI + (CPR == 8 ? ((lane >> 2) & 1) | ((lane >> 3) & 2) : lane >> 2);
+    const uint32_t from = smem_u32(m.data) + pf_raw_chunk<CPR>(row0, chunk), scl = smem_u32(m.data) + (uint32_t)(kPfKeys * DH + row0 * NB + (chunk >> 1));
+    // chunks 2 chunk and 2 chunk + 1 of the row's 16-bit values (the steps of a pass are multiples of 8 rows or of 4)
+    const uint32_t to = smem_u32(ring.data) + (uint32_t)((chunk >> 2) * G::kAtom + row0 * 128);
+    const int c2 = (2 * chunk) & 7;
+    int buf = 0, bufs = 0, slot = 0, round = 0;
+    bool ok = true;
+    for (;;) {
+        ok = pf_wait(&m.full[buf], bufs & 1);
+        if (!ok || m.last[buf]) break;
+        if (round > 0) ok = pf_wait(&ring.empty[slot], (round - 1) & 1);
+        if (!ok || *err) break;
+        const uint32_t dst = to + (uint32_t)(slot * G::kTile), src = from + (uint32_t)(buf * G::kRaw), sc = scl + (uint32_t)(buf * G::kRaw);
+        const uint4 have = *reinterpret_cast<const uint4*>(m.rows + 4 * buf);
+        const bool whole = (have.x & have.y & have.z & have.w) == 0xffffffffu;
+        constexpr int BATCH = 4;  // chunks whose loads are in flight together
+#pragma unroll
+        for (int x0 = 0; x0 < CHUNKS; x0 += BATCH) {
+            uint4 w4[BATCH];
+            uint32_t f[BATCH];
+#pragma unroll
+            for (int y = 0; y < BATCH; ++y) {
+                const int r = (x0 + y) * RPI * G::kCopyWarps;
+                w4[y] = lds128_at(src + (uint32_t)(r * DH));
+                f[y] = lds8(sc + (uint32_t)(r * NB));
+            }
+            if (!whole)
+#pragma unroll
+                for (int y = 0; y < BATCH; ++y) {
+                    const int r = row0 + (x0 + y) * RPI * G::kCopyWarps;
+                    if (!((m.rows[4 * buf + (r >> 5)] >> (r & 31)) & 1u)) f[y] = 0u;
+                }
+#pragma unroll
+            for (int y = 0; y < BATCH; ++y) {
+                const uint32_t v[4] = {w4[y].x, w4[y].y, w4[y].z, w4[y].w}, k = C::scale(f[y]);
+                uint32_t z[8];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    z[2 * e] = C::mul(C::lo(v[e]), k);
+                    z[2 * e + 1] = C::mul(C::hi(v[e]), k);
+                }
+                const int r = (x0 + y) * RPI * G::kCopyWarps;
+                const uint32_t at = dst + (uint32_t)(r * 128) + (uint32_t)((c2 ^ (row0 & 7)) << 4);
+                sts128_at(at, z[0], z[1], z[2], z[3]);
+                sts128_at(at ^ 16u, z[4], z[5], z[6], z[7]);
+            }
+        }
+        fence_proxy_async_smem();  // written as threads do; the MMA reads as the copy engine does
+        __syncwarp();
+        if (lane == 0) {
+            mbar_arrive(&m.empty[buf]);
+            mbar_arrive(&ring.full[slot]);
+        }
+        if (++buf == G::kRaws) buf = 0, ++bufs;
+        if (++slot == S) slot = 0, ++round;
+    }
+    // the CTA may not end while a commit that releases a slot is on its way
     for (int s = 0; ok && s < S; ++s) {
         const int fills = round + (s < slot ? 1 : 0);
-        if (fills > 0) ok = pf_wait(&m.empty[s], (fills - 1) & 1);
+        if (fills > 0) ok = pf_wait(&ring.empty[s], (fills - 1) & 1);
     }
-    if (!ok && w == 0 && nq > 0) pf_wait(m.q_full, (nq - 1) & 1);
-    return good && ok;
+    return ok;
+}
+
+// Each unit's queries, once the last unit's products with its own are done.
+template <class Src, int DH>
+__device__ __forceinline__ bool pf_load_queries(const PfParams& P, uint8_t* Qs, uint64_t* q_full, uint64_t* q_empty, PfCursor at, int64_t left) {
+    using G = PfGeom<Src, DH>;
+    const PagedAttnArgs& a = P.a;
+    const int tr = kPfRows / a.group;
+    int nq = 0;
+    bool ok = true;
+    while (left > 0) {
+        int n;
+        at.part(left, n);
+        left -= at.rest();
+        if (n > 0) {
+            if (nq > 0) ok = pf_wait(q_empty, (nq - 1) & 1);
+            if (!ok) break;
+            ++nq;
+            const int tiles = (2 * at.pt + 1) * tr < at.rows ? 2 : 1;
+            if (elect_one()) {
+                mbar_arrive_expect_tx(q_full, (uint32_t)(tiles * (DH / 64) * tr * a.group * 128));
+                for (int y = 0; y < tiles; ++y)
+                    for (int h = 0; h < DH / 64; ++h)
+                        tc::tma_load_3d(Qs + y * G::kTile + h * G::kAtom, &P.tq, 64 * h, at.kvh * a.group, at.row0 + (2 * at.pt + y) * tr,
+                                        smem_u32(q_full));
+            }
+            __syncwarp();
+        }
+        at.next(a, tr);
+    }
+    if (nq > 0 && !pf_wait(q_full, (nq - 1) & 1)) ok = false;  // no tensor copy may be in flight when the CTA ends
+    return ok;
 }
 
 // JOIN: the parts of units that several CTAs share are left to k_paged_join; otherwise the last of a unit's CTAs to finish
 // joins them.
 template <class Src, int DH, bool JOIN>
-__global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_constant__ PfParams P) {
+__global__ void __launch_bounds__(PfGeom<Src, DH>::kThreads, 1) k_paged_prefill(const __grid_constant__ PfParams P) {
     const PagedAttnArgs& a = P.a;
     using T = typename Src::T;
     using E = Elem<T>;
     using G = PfGeom<Src, DH>;
-    constexpr int S = G::kSlots;
+    constexpr int S = G::kSlots, kPfCopyWarps = G::kCopyWarps, kPfMma = G::kMma, kPfThreads = G::kThreads;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* Qs = smem;                      // [2][kTile]
@@ -385,6 +427,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
     uint8_t* raw = Rs + S * G::kTile;        // [kRaws][kRaw]
     uint32_t* valid = reinterpret_cast<uint32_t*>(raw + G::kRaws * G::kRaw);  // [kPfMaskRing][4]
     uint64_t* bars = reinterpret_cast<uint64_t*>(valid + kPfMaskRing * 4);
+    // codes: the raw buffers' own barriers and words
+    const PfRaw rw = {raw, bars, bars + G::kRaws, reinterpret_cast<uint32_t*>(bars + 2 * G::kRaws),
+                      reinterpret_cast<int*>(bars + 4 * G::kRaws)};
+    if (Src::kMx) bars += 4 * G::kRaws + 2;
     uint64_t* full = bars;                   // [S]
     uint64_t* empty = full + S;              // [S]
     uint64_t* q_full = empty + S;
@@ -422,6 +468,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
             mbar_init(&o_full[x], 1);
             mbar_init(&o_free[x], 4);
         }
+        if (Src::kMx)
+            for (int s = 0; s < G::kRaws; ++s) {
+                mbar_init(&rw.full[s], 33);  // the copying lanes, and one for what they stored
+                mbar_init(&rw.empty[s], G::kCopyWarps);
+            }
         mbar_init(&done[0], 1);
         mbar_init(&done[1], 1);
         *s_err = 0;
@@ -564,14 +615,24 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
     const uint32_t tmem = *tmem_slot;  // S_0, S_1 (128 columns each, P over them), O_0, O_1
     constexpr uint32_t kOCol = 2 * kPfKeys;
 
-    if (warp >= 8)  // a whole warpgroup
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPfCopyRegs));
+    if (warp >= 8 && warp < 12)  // a whole warpgroup
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(G::kCopyRegs));
+    if (G::kThreads > 384 && warp >= 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(G::kMmaRegs));
     if (Src::kMx && warp >= 8 && warp < kPfMma) {
         if constexpr (Src::kMx)
-            if (!pf_convert<Src, DH>(P, {Qs, Rs, raw, valid, full, empty, q_full, q_empty}, *cursor, t1 - t0) && lane == 0) {
+            if (!pf_convert<Src, DH>(rw, {Rs, full, empty}, warp - 8, s_err) && lane == 0) {
                 *s_err = 1;
                 set_status(c.status, VT_DEV_WAIT_TIMEOUT);
             }
+    } else if (Src::kMx && warp >= kPfMma + 2) {
+        if constexpr (Src::kMx) {
+            const bool ok = warp == kPfMma + 2 ? pf_copy_codes<Src, DH>(a, rw, valid, *cursor, t1 - t0)
+                                               : pf_load_queries<Src, DH>(P, Qs, q_full, q_empty, *cursor, t1 - t0);
+            if (!ok && lane == 0) {
+                *s_err = 1;
+                set_status(c.status, VT_DEV_WAIT_TIMEOUT);
+            }
+        }
     } else if (!Src::kMx && warp >= 8 && warp < kPfMma) {
         // ================================================================ copies
         const int w = warp - 8;
@@ -736,7 +797,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
             }
             if (w == 0 && nq > 0) pf_wait(q_full, (nq - 1) & 1);
         }
-    } else if (warp >= kPfMma) {
+    } else if (warp >= kPfMma && warp < kPfMma + 2) {
         // ================================================================ MMAs of tile x
         constexpr uint32_t kType = std::is_same<T, __half>::value ? 0u : tc::kIdescBf16;
         constexpr uint32_t idesc_s = tc::idesc_f16(kPfRows, kPfKeys) | kType, idesc_o = tc::idesc_f16_bmn(kPfRows, DH) | kType;
@@ -831,9 +892,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) k_paged_prefill(const __grid_co
         if (elect_one()) tc::mma_commit(&done[x]);
         __syncwarp();
         if (!pf_wait(&done[x], 0) && lane == 0) set_status(c.status, VT_DEV_WAIT_TIMEOUT);
-    } else {
+    } else if (warp < 8) {
         // ================================================================ softmax of tile x
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPfSoftmaxRegs));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(G::kSoftmaxRegs));
         const int x = warp >> 2, row = tid & 127;
         const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at_col = tmem + lane_off + (uint32_t)(x * kPfKeys), o_at_col = tmem + lane_off + kOCol + (uint32_t)(x * DH);
@@ -1190,8 +1251,8 @@ static cudaError_t prefill_dh(const PagedAttnArgs& a, cudaStream_t st) {
         const uint32_t kb[4] = {64, (uint32_t)std::min(c.page_size, kPfKeys), 1, 1};
         P.tma = make_tensor_map(&P.tk, bf16, 4, a.kpool, kd, ks, kb) && make_tensor_map(&P.tv, bf16, 4, a.vpool, kd, ks, kb);
     }
-    if (!join) return launch_paged_k(k_paged_prefill<Src, DH, false>, (unsigned)grid, kPfThreads, smem, st, P);
-    const cudaError_t e = launch_paged_k(k_paged_prefill<Src, DH, true>, (unsigned)grid, kPfThreads, smem, st, P);
+    if (!join) return launch_paged_k(k_paged_prefill<Src, DH, false>, (unsigned)grid, PfGeom<Src, DH>::kThreads, smem, st, P);
+    const cudaError_t e = launch_paged_k(k_paged_prefill<Src, DH, true>, (unsigned)grid, PfGeom<Src, DH>::kThreads, smem, st, P);
     if (e != cudaSuccess) return e;
     return launch_paged_k(k_paged_join<T, DH>, (unsigned)(2 * g_num_sms), kPfJoinThreads, 0, st, PfJoin{a, P.split, (int)grid});
 }
@@ -1201,7 +1262,7 @@ static cudaError_t init_one() {
     cudaFuncAttributes f;
     cudaError_t e = cudaFuncGetAttributes(&f, k_paged_prefill<Src, DH, JOIN>);
     if (e != cudaSuccess) return e;
-    if (f.numRegs != kPfLaunchRegs) return cudaErrorInvalidConfiguration;  // (see paged_tiles_error)
+    if (f.numRegs != PfGeom<Src, DH>::kLaunchRegs) return cudaErrorInvalidConfiguration;  // (see paged_tiles_error)
     return cudaFuncSetAttribute(k_paged_prefill<Src, DH, JOIN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 (int)PfGeom<Src, DH>::kSmem);
 }
