@@ -73,8 +73,8 @@ struct PfGeom {
     static constexpr int kThreads = Src::kMx ? 512 : 384;
     // Registers a thread: at launch 65536 / threads, rounded down to 8; then 2 x 128 threads of softmax, and 128 of copies and
     // MMAs, or 128 of each.
-    static constexpr int kLaunchRegs = Src::kMx ? 128 : 168, kSoftmaxRegs = Src::kMx ? 184 : 208, kCopyRegs = Src::kMx ? 64 : 88;
-    static constexpr int kMmaRegs = Src::kMx ? 80 : 88;
+    static constexpr int kLaunchRegs = Src::kMx ? 128 : 168, kSoftmaxRegs = Src::kMx ? 168 : 208, kCopyRegs = Src::kMx ? 72 : 88;
+    static constexpr int kMmaRegs = Src::kMx ? 104 : 88;
     static_assert(256 * kSoftmaxRegs + 128 * kCopyRegs + (kThreads - 384) * kMmaRegs <= kThreads * kLaunchRegs,
                   "the register split must fit in the registers the block is launched with");
     static constexpr int kTile = kPfRows * DH * 2;         // bytes of a Q tile, of a K or V block
@@ -200,35 +200,37 @@ struct PfParams {
 };
 
 // Over a pool of codes, three roles take the place of the copy warps:
-//   copies        (one warp) codes and scales of a block of K or V as they are, by asynchronous copies of 16 bytes, into
-//                 one of kRaws buffers
+//   copies        (one warp) codes and scales of a block of K or V as they are, into one of kRaws buffers: by tensor copies of
+//                 a page's rows, or by asynchronous copies of 16 bytes where a block is not whole or pages are small
 //   conversions   (four warps) from there to the type of Q, into the ring, as the tensor copies of a 16-bit pool would leave
 //                 them there.  They know nothing of units: they follow the buffers until one says that it is the last
 //   queries       (one warp)
 // Positions outside the unit's range and bad pages get scale 0, whose product with any code (they are filled with zeros) is
 // 0.  A page holds 8 positions or more, so a group of 8 rows lies in one.
 struct PfRaw {
-    uint8_t* data;         // [kRaws][kRaw]: codes [128][dh] (the halves of odd rows of 128 bytes swapped), scales [128][dh / 32]
+    uint8_t* data;         // [kRaws] codes [128][dh] with the swizzle of dh bytes, then [kRaws] scales [128][dh / 32]
     uint64_t *full, *empty;
     uint32_t* rows;        // [kRaws][4] which rows hold something
     int* last;             // [kRaws] nothing follows, and nothing is there
 };
-template <int CPR>
-__device__ __forceinline__ uint32_t pf_raw_chunk(int row, int chunk) {
-    return (uint32_t)((row * CPR + (CPR == 8 ? chunk ^ ((row & 1) << 2) : chunk)) * 16);
+template <int DH>
+__device__ __forceinline__ uint32_t pf_raw_at(int row, int chunk) {
+    const uint32_t at = (uint32_t)(row * DH + chunk * 16);
+    return at ^ ((at >> 3) & (DH == 128 ? 0x70u : 0x30u));
 }
 
 template <class Src, int DH>
-__device__ __forceinline__ bool pf_copy_codes(const PagedAttnArgs& a, const PfRaw& m, uint32_t* valid, PfCursor at, int64_t left) {
+__device__ __forceinline__ bool pf_copy_codes(const PfParams& P, const PfRaw& m, uint32_t* valid, PfCursor at, int64_t left) {
     using G = PfGeom<Src, DH>;
     constexpr int NB = DH / kMxBlock, CPR = DH / 16, RPI = 32 / CPR, PIECES = kPfKeys * NB / 16;  // 16-byte pieces of the scales
+    const PagedAttnArgs& a = P.a;
     const PagedView& c = a.c;
     const int lane = threadIdx.x & 31, tr = kPfRows / a.group, chunk = lane % CPR, sub = lane / CPR;
-    const int64_t mine = sub * c.pos_stride + chunk * 16, hop = RPI * c.pos_stride;
-    const uint32_t to = smem_u32(m.data) + pf_raw_chunk<CPR>(sub, chunk);  // (sub, sub + RPI: the same parity)
+    const int box_rows = min(c.page_size, kPfKeys);
+    const uint32_t codes = smem_u32(m.data), scales = codes + G::kRaws * kPfKeys * DH;
     int buf = 0, round = 0, blk = 0;
     bool ok = true;
-    // lane g < 16: the page of 8-row group g of block j (-1: not needed), requested a block ahead
+    // lane g < 16: the page of 8-row group g of block j, requested a block ahead
     auto request = [&](int j) {
         const int p = j * kPfKeys + 8 * (lane & 15);
         return p + 8 > at.kbeg && p < at.kend ? c.tables[(int64_t)at.b * c.per_seq + (p >> c.page_shift)] : 0;
@@ -248,7 +250,7 @@ __device__ __forceinline__ bool pf_copy_codes(const PagedAttnArgs& a, const PfRa
                 set_status(c.status, VT_DEV_BAD_PAGE);
             }
             if (!rows) page = 0;
-            const bool whole = __all_sync(0xffffffffu, rows == 0xffu);
+            const bool whole = P.tma && __all_sync(0xffffffffu, rows == 0xffu);
             if (lane < 16) reinterpret_cast<uint8_t*>(valid)[(blk % kPfMaskRing) * 16 + lane] = (uint8_t)rows;
 #pragma unroll 1
             for (int kv = 0; kv < 2; ++kv) {
@@ -256,36 +258,39 @@ __device__ __forceinline__ bool pf_copy_codes(const PagedAttnArgs& a, const PfRa
                 if (!ok) break;
                 if (lane < 16) reinterpret_cast<uint8_t*>(m.rows)[buf * 16 + lane] = (uint8_t)rows;
                 if (lane == 0) m.last[buf] = 0;
-                const uint8_t* pool = reinterpret_cast<const uint8_t*>(kv ? a.vpool : a.kpool) + at.kvh * c.head_stride + mine;
-                const uint32_t dst = to + (uint32_t)(buf * G::kRaw);
-                auto group = [&](int g) {
-                    return pool + __shfl_sync(0xffffffffu, page, g) * c.page_stride + ((p0 + 8 * g) & (c.page_size - 1)) * c.pos_stride;
-                };
-                if (whole)
-#pragma unroll 4
-                    for (int g = 0; g < 16; ++g) {
-                        const uint8_t* src = group(g);
-#pragma unroll
-                        for (int k = 0; k < 8; k += RPI, src += hop) pf_copy16(dst + (uint32_t)((8 * g + k) * DH), src, true);
+                const uint32_t dst = codes + (uint32_t)(buf * kPfKeys * DH), sdst = scales + (uint32_t)(buf * kPfKeys * NB);
+                const uint8_t* scale = (kv ? a.vscale : a.kscale) + at.kvh * a.scale_head;
+                __syncwarp();  // what the lanes stored, before any of them arrives
+                if (whole) {
+                    if (elect_one()) mbar_arrive_expect_tx(&m.full[buf], (uint32_t)(kPfKeys * (DH + NB)));
+                    for (int r = 0; r < kPfKeys; r += box_rows) {
+                        const int pg = __shfl_sync(0xffffffffu, page, r >> 3), first = (p0 + r) & (c.page_size - 1);
+                        if (elect_one()) {
+                            tc::tma_load_4d(dst + (uint32_t)(r * DH), kv ? &P.tv : &P.tk, 0, first, at.kvh, pg, &m.full[buf]);
+                            bulk_g2s(m.data + (sdst - codes) + r * NB, scale + pg * a.scale_page + first * NB, (uint32_t)(box_rows * NB),
+                                     &m.full[buf]);
+                        }
+                        __syncwarp();
                     }
-                else
-#pragma unroll 1
+                    mbar_arrive(&m.full[buf]);
+                } else {
+                    const uint8_t* pool = reinterpret_cast<const uint8_t*>(kv ? a.vpool : a.kpool) + at.kvh * c.head_stride + chunk * 16;
+#pragma unroll 2
                     for (int g = 0; g < 16; ++g) {
-                        const uint8_t* src = group(g);
+                        const uint8_t* src = pool + __shfl_sync(0xffffffffu, page, g) * c.page_stride +
+                                             (((p0 + 8 * g) & (c.page_size - 1)) + sub) * c.pos_stride;
                         const uint32_t bits = __shfl_sync(0xffffffffu, rows, g) >> sub;
 #pragma unroll
-                        for (int k = 0; k < 8; k += RPI, src += hop) pf_copy16(dst + (uint32_t)((8 * g + k) * DH), src, (bits >> k) & 1u);
+                        for (int k = 0; k < 8; k += RPI, src += RPI * c.pos_stride)
+                            pf_copy16(dst + pf_raw_at<DH>(8 * g + k + sub, chunk), src, (bits >> k) & 1u);
                     }
-                {
                     const int x = lane % PIECES, g = x * 16 / PIECES, pg = __shfl_sync(0xffffffffu, page, g);
                     const bool any = __shfl_sync(0xffffffffu, rows, g) != 0;
-                    const uint8_t* src = (kv ? a.vscale : a.kscale) + pg * a.scale_page + at.kvh * a.scale_head +
-                                         ((p0 + x * (16 / NB)) & (c.page_size - 1)) * NB;
-                    if (lane < PIECES) pf_copy16(smem_u32(m.data) + (uint32_t)(buf * G::kRaw + kPfKeys * DH + lane * 16), src, any);
+                    if (lane < PIECES)
+                        pf_copy16(sdst + (uint32_t)(lane * 16), scale + pg * a.scale_page + ((p0 + x * (16 / NB)) & (c.page_size - 1)) * NB, any);
+                    if (lane == 0) mbar_arrive(&m.full[buf]);
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(&m.full[buf])) : "memory");
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&m.full[buf]);  // for what was stored
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(&m.full[buf])) : "memory");
                 if (++buf == G::kRaws) buf = 0, ++round;
             }
         }
@@ -299,6 +304,11 @@ __device__ __forceinline__ bool pf_copy_codes(const PagedAttnArgs& a, const PfRa
         mbar_arrive(&m.full[buf]);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+    if (!ok)  // no tensor copy may still be in flight when the CTA ends
+        for (int b = 0; b < G::kRaws; ++b) {
+            const int fills = round + (b < buf ? 1 : 0);
+            if (fills > 0) pf_wait(&m.full[b], (fills - 1) & 1);
+        }
     return ok;
 }
 
@@ -312,12 +322,13 @@ __device__ __forceinline__ bool pf_convert(const PfRaw& m, const PfRing& ring, i
     using C = typename Src::C;
     constexpr int S = G::kSlots, NB = DH / kMxBlock, CPR = DH / 16, RPI = 32 / CPR, CHUNKS = 128 / (RPI * G::kCopyWarps);
     const int lane = threadIdx.x & 31;
-    // A pass of the four warps covers 4 RPI rows.  8 lanes have 4 chunks of two rows: their loads and stores fall into
-    // different banks
+    // A pass of the four warps covers 4 RPI rows.  8 lanes have 4 chunks of two rows whose numbers differ in bits 0 and 2
+    // (dh 64: bit 0): then their loads and their stores fall into different banks
     const int chunk = CPR == 8 ? (lane & 3) | ((lane >> 1) & 4) : lane & 3;
-    const int row0 = w * RPI + (CPR == 8 ? ((lane >> 2) & 1) | ((lane >> 3) & 2) : lane >> 2);
-    const uint32_t from = smem_u32(m.data) + pf_raw_chunk<CPR>(row0, chunk), scl = smem_u32(m.data) + (uint32_t)(kPfKeys * DH + row0 * NB + (chunk >> 1));
-    // chunks 2 chunk and 2 chunk + 1 of the row's 16-bit values (the steps of a pass are multiples of 8 rows or of 4)
+    const int row0 = CPR == 8 ? 8 * (w >> 1) + ((2 * (w & 1) + (lane >> 4)) ^ (lane & 4 ? 5 : 0)) : 8 * w + (lane >> 2);
+    const uint32_t from = smem_u32(m.data) + pf_raw_at<DH>(row0, chunk);
+    const uint32_t scl = smem_u32(m.data) + (uint32_t)(G::kRaws * kPfKeys * DH + row0 * NB + (chunk >> 1));
+    // chunks 2 chunk and 2 chunk + 1 of the row's 16-bit values (a pass is 16 or 32 rows further)
     const uint32_t to = smem_u32(ring.data) + (uint32_t)((chunk >> 2) * G::kAtom + row0 * 128);
     const int c2 = (2 * chunk) & 7;
     int buf = 0, bufs = 0, slot = 0, round = 0;
@@ -327,11 +338,11 @@ __device__ __forceinline__ bool pf_convert(const PfRaw& m, const PfRing& ring, i
         if (!ok || m.last[buf]) break;
         if (round > 0) ok = pf_wait(&ring.empty[slot], (round - 1) & 1);
         if (!ok || *err) break;
-        const uint32_t dst = to + (uint32_t)(slot * G::kTile), src = from + (uint32_t)(buf * G::kRaw), sc = scl + (uint32_t)(buf * G::kRaw);
+        const uint32_t dst = to + (uint32_t)(slot * G::kTile), src = from + (uint32_t)(buf * kPfKeys * DH), sc = scl + (uint32_t)(buf * kPfKeys * NB);
         const uint4 have = *reinterpret_cast<const uint4*>(m.rows + 4 * buf);
         const bool whole = (have.x & have.y & have.z & have.w) == 0xffffffffu;
-        constexpr int BATCH = 4;  // chunks whose loads are in flight together
-#pragma unroll
+        constexpr int BATCH = 2;  // chunks whose loads are in flight together
+#pragma unroll 1
         for (int x0 = 0; x0 < CHUNKS; x0 += BATCH) {
             uint4 w4[BATCH];
             uint32_t f[BATCH];
@@ -626,7 +637,7 @@ __global__ void __launch_bounds__(PfGeom<Src, DH>::kThreads, 1) k_paged_prefill(
             }
     } else if (Src::kMx && warp >= kPfMma + 2) {
         if constexpr (Src::kMx) {
-            const bool ok = warp == kPfMma + 2 ? pf_copy_codes<Src, DH>(a, rw, valid, *cursor, t1 - t0)
+            const bool ok = warp == kPfMma + 2 ? pf_copy_codes<Src, DH>(P, rw, valid, *cursor, t1 - t0)
                                                : pf_load_queries<Src, DH>(P, Qs, q_full, q_empty, *cursor, t1 - t0);
             if (!ok && lane == 0) {
                 *s_err = 1;
@@ -928,9 +939,12 @@ __global__ void __launch_bounds__(PfGeom<Src, DH>::kThreads, 1) k_paged_prefill(
                 ++ns;
                 if (!ok) continue;
                 tc::fence_after();
-                uint32_t sv[4][32];
+                // S by 32 keys.  Codes: the block's threads have fewer registers, so of the maximum's pass only the first 64 keys stay,
+                // and the others are read again while the weights of these are worked out.
+                constexpr int KEPT = Src::kMx ? 3 : 4;
+                uint32_t sv[KEPT][32];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) tc::tmem_ld32(s_at_col + 32 * q, sv[q]);
+                for (int q = 0; q < KEPT; ++q) tc::tmem_ld32(s_at_col + 32 * q, sv[q]);
                 const uint32_t* vw = valid + ((blk + j - j0) % kPfMaskRing) * 4;
                 const int kp0 = j * kPfKeys, cb = first_key - kp0, ce = qp + 1 - kp0;
                 uint32_t mw[4];
@@ -938,18 +952,25 @@ __global__ void __launch_bounds__(PfGeom<Src, DH>::kThreads, 1) k_paged_prefill(
                 for (int q = 0; q < 4; ++q) mw[q] = fa_range_bits(cb - 32 * q, ce - 32 * q) & vw[q];
                 const bool plain = __all_sync(0xffffffffu, (mw[0] & mw[1] & mw[2] & mw[3]) == 0xffffffffu);
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    tc::tmem_ld_wait_on(sv[q]);
+                auto arrived = [&](uint32_t(&v)[32], int q) {  // keys 32 q ..
+                    tc::tmem_ld_wait_on(v);
                     if (!plain)
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
-                            if (!((mw[q] >> e) & 1u)) sv[q][e] = 0xff800000u;  // -inf
-                }
+                            if (!((mw[q] >> e) & 1u)) v[e] = 0xff800000u;  // -inf
+                };
+#pragma unroll
+                for (int q = 0; q < KEPT; ++q) arrived(sv[q], q);
 #pragma unroll
                 for (int e = 0; e < 32; e += 2)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) mx[q] = fa_max3(mx[q], __uint_as_float(sv[q][e]), __uint_as_float(sv[q][e + 1]));
+                    for (int q = 0; q < KEPT; ++q) mx[q] = fa_max3(mx[q], __uint_as_float(sv[q][e]), __uint_as_float(sv[q][e + 1]));
+                if constexpr (Src::kMx) {
+                    tc::tmem_ld32(s_at_col + 96, sv[2]);
+                    arrived(sv[2], 3);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) mx[3] = fa_max3(mx[3], __uint_as_float(sv[2][e]), __uint_as_float(sv[2][e + 1]));
+                }
                 const float pm = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                 const float bms = pm == -INFINITY ? pm : pm * sl2;
                 float alpha = 1.f;
@@ -981,12 +1002,19 @@ __global__ void __launch_bounds__(PfGeom<Src, DH>::kThreads, 1) k_paged_prefill(
                 const float nm = m_use == -INFINITY ? 0.f : -m_use;
                 const uint64_t sl2x2 = f2_pack(sl2, sl2), nmx2 = f2_pack(nm, nm);
                 uint64_t ls[2] = {0ull, 0ull};
+                if constexpr (Src::kMx) tc::tmem_ld32(s_at_col + 64, sv[2]);
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
+                    if constexpr (Src::kMx)
+                        if (q == 1) {
+                            tc::tmem_ld32(s_at_col + 96, sv[1]);
+                            arrived(sv[2], 2);
+                            arrived(sv[1], 3);
+                        }
                     uint32_t w[32];
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
-                        const uint32_t* s2 = &sv[2 * q + (e >> 4)][2 * (e & 15)];
+                        const uint32_t* s2 = &sv[Src::kMx && q == 1 ? 2 - (e >> 4) : 2 * q + (e >> 4)][2 * (e & 15)];
                         float p0, p1;
                         f2_unpack(f2_fma(f2_pack(__uint_as_float(s2[0]), __uint_as_float(s2[1])), sl2x2, nmx2), p0, p1);
                         p0 = fa_ex2(p0);
@@ -1244,12 +1272,14 @@ static cudaError_t prefill_dh(const PagedAttnArgs& a, cudaStream_t st) {
     if (!make_tensor_map(&P.tq, bf16, 3, a.q, qd, qs, qb)) return cudaErrorInvalidValue;
     // Boxes of fewer than 16 rows would cost more than the copies of 16 bytes (2 KB boxes: 1160 cycles a block of 32 KB,
     // 16 KB boxes 680, asynchronous copies 1210 to 1310, all of them measured with every SM copying from the L2).
-    if (!Src::kMx && c.page_size >= 16) {
-        const uint64_t kd[4] = {DH, (uint64_t)c.page_size, (uint64_t)c.n_kv_heads, (uint64_t)c.n_pages};
-        const uint64_t ks[3] = {(uint64_t)c.pos_stride * 2, (uint64_t)(c.head_stride ? c.head_stride : DH) * 2,
-                                (uint64_t)(c.page_stride ? c.page_stride : DH) * 2};
-        const uint32_t kb[4] = {64, (uint32_t)std::min(c.page_size, kPfKeys), 1, 1};
-        P.tma = make_tensor_map(&P.tk, bf16, 4, a.kpool, kd, ks, kb) && make_tensor_map(&P.tv, bf16, 4, a.vpool, kd, ks, kb);
+    if (c.page_size >= 16) {  // (codes: two of them as an element of 16 bits, strides in bytes)
+        constexpr uint64_t W = Src::kMx ? DH / 2 : DH, B = Src::kBytes;
+        const uint64_t kd[4] = {W, (uint64_t)c.page_size, (uint64_t)c.n_kv_heads, (uint64_t)c.n_pages};
+        const uint64_t ks[3] = {(uint64_t)c.pos_stride * B, (uint64_t)(c.head_stride ? c.head_stride : DH) * B,
+                                (uint64_t)(c.page_stride ? c.page_stride : DH) * B};
+        const uint32_t kb[4] = {(uint32_t)std::min<uint64_t>(W, 64), (uint32_t)std::min(c.page_size, kPfKeys), 1, 1};
+        constexpr int span = W * 2 < 128 ? 64 : 128;
+        P.tma = make_tensor_map(&P.tk, bf16, 4, a.kpool, kd, ks, kb, span) && make_tensor_map(&P.tv, bf16, 4, a.vpool, kd, ks, kb, span);
     }
     if (!join) return launch_paged_k(k_paged_prefill<Src, DH, false>, (unsigned)grid, PfGeom<Src, DH>::kThreads, smem, st, P);
     const cudaError_t e = launch_paged_k(k_paged_prefill<Src, DH, true>, (unsigned)grid, PfGeom<Src, DH>::kThreads, smem, st, P);

@@ -1275,7 +1275,7 @@ static bool make_map_k2(CUtensorMap* map, const void* base, int64_t inner, int64
 }
 
 bool make_tensor_map(CUtensorMap* map, bool bf16, int rank, const void* base, const uint64_t* dims, const uint64_t* strides,
-                     const uint32_t* box) {
+                     const uint32_t* box, int swizzle) {
     cuuint64_t d[5], s[4];
     cuuint32_t b[5], one[5];
     for (int i = 0; i < rank; ++i) {
@@ -1285,7 +1285,8 @@ bool make_tensor_map(CUtensorMap* map, bool bf16, int rank, const void* base, co
         if (i + 1 < rank) s[i] = strides[i];
     }
     return g_encode && g_encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank,
-                                const_cast<void*>(base), d, s, b, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                const_cast<void*>(base), d, s, b, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                swizzle == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

@@ -9,10 +9,10 @@
 
 namespace vt {
 
-// (prefill.cu) Map of a 16-bit tensor for tiled copies with the 128-byte swizzle; strides (bytes) of the
-// dimensions after the first.  False when the driver refuses it.
+// (prefill.cu) Map of a 16-bit tensor for tiled copies with the 128-byte swizzle (or, for boxes of 64 bytes, that of 64);
+// strides (bytes) of the dimensions after the first.  False when the driver refuses it.
 bool make_tensor_map(CUtensorMap* map, bool bf16, int rank, const void* base, const uint64_t* dims, const uint64_t* strides,
-                     const uint32_t* box);
+                     const uint32_t* box, int swizzle = 128);
 
 namespace tc {
 
