@@ -323,6 +323,7 @@ struct PagedQkArgs {
     uint8_t *kscale, *vscale;
     int64_t scale_page, scale_head;
     int e_lo, e_hi;             // exponents that a scale may have
+    int batches;                // (set by the launch)
 };
 struct PagedAttnArgs {
     PagedView c;

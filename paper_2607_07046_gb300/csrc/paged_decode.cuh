@@ -108,11 +108,6 @@ __device__ __forceinline__ uint64_t lds1x64(uint32_t addr) {
 __device__ __forceinline__ void lds2x64(uint32_t addr, uint64_t (&v)[2]) {
     asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(v[0]), "=l"(v[1]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 // 1 / x of a power of two.
 __device__ __forceinline__ float pd_inverse(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }
 // 2^x; over codes without the steps that keep results below 2^-126, which are nothing beside weights up to 2^12 and more.

@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 
 #include "paged_mx.cuh"
+#include "tcgen05.cuh"
 
 namespace vt {
 
@@ -12,36 +13,42 @@ namespace vt {
 //                                                   or the neighbours (2i, 2i + 1)
 // and rounded once: to the rows' type, or (F) to codes with the scale of their 32 dimensions.
 //
-// dh / 8 lanes hold a head, 8 dimensions each (one 16-byte load): the sum of squares takes a few shuffles, the other
-// half of a pair comes from one other lane (neighbours lie in the lane), and four lanes share a scale.  A pass of a
-// warp covers 32 / (dh / 8) heads of one row.
+// dh / 16 lanes hold a head, two chunks of 8 dimensions each (two 16-byte loads): for pairs of halves those that are paired,
+// so that no value goes from lane to lane but the sum of squares, and the unrotated ones side by side; for neighbours, and
+// for values, 16 dimensions side by side.  A pass of a warp covers 32 / (dh / 16) heads of one row.  A warp has queries or
+// keys and values only: the gains times the rotation's cosines and sines, four numbers a pair, are worked out once and serve
+// all its passes.
 constexpr int kQkWarps = 8;
 
-template <class T, int DH, int F, int PASSES>
-__global__ void __launch_bounds__(kQkWarps * 32) k_paged_append_qk(const __grid_constant__ PagedQkArgs a) {
-    constexpr int LPH = DH / 8, HPW = 32 / LPH, NB = DH / kMxBlock;
-    constexpr bool MX = F >= 0;
-    constexpr int FF = MX ? F : 0;
+// One row's queries, or its keys and values, from head `at` (of this lane) on: `batches` times PASSES passes.
+template <class T, int DH, int F, bool NEIGH, int PASSES, bool OF_Q>
+__device__ __forceinline__ void qk_heads(const PagedQkArgs& a, int row, int at, int batches) {
+    constexpr int LPH = DH / 16, HPW = 32 / LPH, NB = DH / kMxBlock;
+    constexpr bool MX = F >= 0 && !OF_Q;
     using E = Elem<T>;
-    pdl_wait();
-    pdl_launch_dependents();
     const PagedView& c = a.c;
-    const int lane = threadIdx.x & 31, sub = lane % LPH;
-    const int H = a.n_heads, K = c.n_kv_heads, heads = H + 2 * K;
-    const int per_row = (heads + HPW * PASSES - 1) / (HPW * PASSES);  // warps of a row
-    const int64_t gw = (int64_t)blockIdx.x * kQkWarps + (threadIdx.x >> 5);
-    const int row = (int)(gw / per_row), h0 = (int)(gw - (int64_t)row * per_row) * HPW * PASSES + lane / LPH;
-    if (row >= a.n_rows) return;
-    // the data does not depend on the position: its loads go out first
-    uint4 x[PASSES];
+    const int lane = threadIdx.x & 31, s = lane % LPH, K = c.n_kv_heads, heads = OF_Q ? a.n_heads : 2 * K;
+    const int part = a.rotary / 16;  // lanes of a head that rotate
+    const bool turns = s < part, split = !NEIGH && turns;
+    const int side = split ? s : 2 * s, other = split ? s + part : 2 * s + 1;  // the lane's chunks of queries and keys
+    const uint16_t *q = a.q + row * a.q_ld + (int64_t)at * DH, *k = a.k + row * a.k_ld, *v = a.v + row * a.v_ld;
+    uint4 x[PASSES][2];
+    auto load = [&](int h0) {
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-        const int h = h0 + i * HPW;
-        const uint16_t* src = h < H       ? a.q + row * a.q_ld + (int64_t)h * DH
-                              : h < H + K ? a.k + row * a.k_ld + (int64_t)(h - H) * DH
-                                          : a.v + row * a.v_ld + (int64_t)(h - H - K) * DH;
-        x[i] = h < heads ? *reinterpret_cast<const uint4*>(src + sub * 8) : make_uint4(0u, 0u, 0u, 0u);
-    }
+        for (int i = 0; i < PASSES; ++i) {
+            const int h = h0 + i * HPW;
+            const bool is_v = !OF_Q && h >= K;
+            const uint16_t* src = OF_Q ? q + i * HPW * DH : is_v ? v + (h - K) * DH : k + h * DH;
+            if (h < heads) {
+                x[i][0] = *reinterpret_cast<const uint4*>(src + (is_v ? 2 * s : side) * 8);
+                x[i][1] = *reinterpret_cast<const uint4*>(src + (is_v ? 2 * s + 1 : other) * 8);
+            } else {
+                x[i][0] = x[i][1] = make_uint4(0u, 0u, 0u, 0u);
+            }
+        }
+        q += PASSES * HPW * DH;
+    };
+    load(at);  // the data does not depend on the position: its loads go out first
     const int b = paged_seq_of_row(c, row, lane);
     if (b < 0) return;
     const int len = paged_len(c, b), pos = len + (row - paged_start(c, b, a.n_rows));
@@ -50,146 +57,202 @@ __global__ void __launch_bounds__(kQkWarps * 32) k_paged_append_qk(const __grid_
         fits = false;
         if (lane == 0) set_status(c.status, VT_DEV_KV_OVERFLOW);
     }
-    // this lane's part of the rotation.  Halves: lanes 0 .. part - 1 have a, the next `part` b; neighbours: each has 4 pairs
-    const int part = a.rotary / 16;
-    const bool turns = sub < 2 * part, second = turns && !a.neighbours && sub >= part;
-    const int other = a.neighbours || !turns ? lane : second ? lane - part : lane + part;
-    float2 cs[8];
-    int page = -1;
-    if (fits) {
-        if (turns) {
-            const float4* t = reinterpret_cast<const float4*>(a.rope + (int64_t)pos * (a.rotary / 2) +
-                                                              (a.neighbours ? sub * 4 : (second ? sub - part : sub) * 8));
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < 2 || !a.neighbours) {
-                    const float4 f = t[e];
-                    cs[2 * e] = make_float2(f.x, f.y);
-                    cs[2 * e + 1] = make_float2(f.z, f.w);
-                }
-        }
-        page = c.tables[(int64_t)b * c.per_seq + (pos >> c.page_shift)];
-        if ((unsigned)page >= (unsigned)c.n_pages) {
-            page = -1;
-            if (lane == 0) set_status(c.status, VT_DEV_BAD_PAGE);
-        }
+    if (!fits) {
+        if (OF_Q)
+            for (int h = at; h < min(heads, at + batches * PASSES * HPW); h += HPW) {
+                uint4* dst = reinterpret_cast<uint4*>(a.q_out + row * a.q_out_ld + (int64_t)h * DH);
+                dst[2 * s] = dst[2 * s + 1] = make_uint4(0u, 0u, 0u, 0u);
+            }
+        return;
     }
-    const int in_page = pos & (c.page_size - 1);
-#pragma unroll
-    for (int i = 0; i < PASSES; ++i) {  // (every lane takes part in the shuffles)
-        const int h = h0 + i * HPW;
-        const uint32_t u[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-        float y[8];
+    uint16_t* out_at = a.q_out + row * a.q_out_ld + (int64_t)at * DH;
+    int64_t entry = 0, scale = 0;
+    if (!OF_Q) {
+        const int page = c.tables[(int64_t)b * c.per_seq + (pos >> c.page_shift)], in_page = pos & (c.page_size - 1);
+        if ((unsigned)page >= (unsigned)c.n_pages) {
+            if (lane == 0) set_status(c.status, VT_DEV_BAD_PAGE);
+            return;
+        }
+        entry = page * c.page_stride + in_page * c.pos_stride;
+        scale = page * a.scale_page + in_page * NB;
+    }
+    auto unpack = [](const uint4& u, float* y) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float2 p = E::unpack(u[e]);
+            const float2 p = E::unpack(w[e]);
             y[2 * e] = p.x;
             y[2 * e + 1] = p.y;
         }
-        const bool formed = h < H + K;
-        const uint16_t* gain = h < H ? a.q_gain : formed ? a.k_gain : nullptr;
-        if (__any_sync(0xffffffffu, gain != nullptr)) {
-            float ss = 0.f;
+    };
+    // pair e of the lane is values first(e) and second(e) of its 16; two pairs go through an instruction
+    auto first = [](int e) { return NEIGH ? 2 * e : e; };
+    auto second = [](int e) { return NEIGH ? 2 * e + 1 : 8 + e; };
+    // a' = a ca - b sb, b' = b cb + a sa, with the gains; msb = -sb
+    uint64_t ca[4], sa[4], cb[4], msb[4];
+    {
+        const uint16_t* gain = OF_Q ? a.q_gain : a.k_gain;
+        float g[16];
+        if (gain) {
+            unpack(*reinterpret_cast<const uint4*>(gain + side * 8), g);
+            unpack(*reinterpret_cast<const uint4*>(gain + other * 8), g + 8);
+        } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ss += y[e] * y[e];
+            for (int e = 0; e < 16; ++e) g[e] = 1.f;
+        }
+        const float4* t = reinterpret_cast<const float4*>(a.rope + (int64_t)pos * (a.rotary / 2) + s * 8);
 #pragma unroll
-            for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-            if (gain) {
-                const float inv = rsqrtf(ss * (1.f / DH) + a.eps);
-                const uint4 g = *reinterpret_cast<const uint4*>(gain + sub * 8);
-                const uint32_t gu[4] = {g.x, g.y, g.z, g.w};
+        for (int e = 0; e < 8; e += 2) {
+            const float4 f = turns ? t[e / 2] : make_float4(1.f, 0.f, 1.f, 0.f);
+            ca[e / 2] = f2_pack(g[first(e)] * f.x, g[first(e + 1)] * f.z), sa[e / 2] = f2_pack(g[first(e)] * f.y, g[first(e + 1)] * f.w);
+            cb[e / 2] = f2_pack(g[second(e)] * f.x, g[second(e + 1)] * f.z);
+            msb[e / 2] = f2_pack(-g[second(e)] * f.y, -g[second(e + 1)] * f.w);
+        }
+    }
+    const bool norm = OF_Q ? a.q_gain != nullptr : a.k_gain != nullptr;
+    for (int h0 = at;;) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 f = E::unpack(gu[e]);
-                    y[2 * e] *= inv * f.x;
-                    y[2 * e + 1] *= inv * f.y;
+        for (int i = 0; i < PASSES; ++i) {  // (every lane takes part in the shuffles)
+            const int h = h0 + i * HPW;
+            const bool formed = OF_Q || h < K, here = h < heads;
+            const int c0 = formed ? side : 2 * s, c1 = formed ? other : 2 * s + 1;
+            float y[16];
+            unpack(x[i][0], y);
+            unpack(x[i][1], y + 8);
+            float inv = 1.f;
+            if (norm) {
+                uint64_t sum = f2_mul(f2_pack(y[0], y[1]), f2_pack(y[0], y[1]));
+#pragma unroll
+                for (int e = 2; e < 16; e += 2) sum = f2_fma(f2_pack(y[e], y[e + 1]), f2_pack(y[e], y[e + 1]), sum);
+                float ss, s1;
+                f2_unpack(sum, ss, s1);
+                ss += s1;
+#pragma unroll
+                for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+                inv = rsqrtf(fmaf(ss, 1.f / DH, a.eps));
+            }
+            if (formed) {
+                const uint64_t inv2 = f2_pack(inv, inv);
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const uint64_t p = f2_mul(f2_pack(y[first(e)], y[first(e + 1)]), inv2), r = f2_mul(f2_pack(y[second(e)], y[second(e + 1)]), inv2);
+                    uint64_t pp = f2_mul(p, ca[e / 2]), rr = f2_mul(r, cb[e / 2]);
+                    if (turns) pp = f2_fma(r, msb[e / 2], pp), rr = f2_fma(p, sa[e / 2], rr);
+                    f2_unpack(pp, y[first(e)], y[first(e + 1)]);
+                    f2_unpack(rr, y[second(e)], y[second(e + 1)]);
                 }
             }
-        }
-        if (part > 0 && __any_sync(0xffffffffu, formed)) {
-            if (a.neighbours) {
-                if (formed && turns && fits)
+            if constexpr (!MX) {
+                uint4 out[2];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float p = y[2 * e], r = y[2 * e + 1];
-                        y[2 * e] = p * cs[e].x - r * cs[e].y;
-                        y[2 * e + 1] = r * cs[e].x + p * cs[e].y;
-                    }
+                for (int j = 0; j < 2; ++j)
+                    out[j] = make_uint4(E::pack(y[8 * j], y[8 * j + 1]), E::pack(y[8 * j + 2], y[8 * j + 3]), E::pack(y[8 * j + 4], y[8 * j + 5]),
+                                        E::pack(y[8 * j + 6], y[8 * j + 7]));
+                if (!formed) out[0] = x[i][0], out[1] = x[i][1];  // (a value goes as it came: a NaN keeps its bits)
+                if (here) {
+                    uint16_t* dst = OF_Q ? out_at + i * HPW * DH
+                                         : static_cast<uint16_t*>(formed ? a.kpool : a.vpool) + entry + (formed ? h : h - K) * c.head_stride;
+                    *reinterpret_cast<uint4*>(dst + c0 * 8) = out[0];
+                    *reinterpret_cast<uint4*>(dst + c1 * 8) = out[1];
+                }
             } else {
-                float w[8];
+                // largest magnitudes of the chunks, then of their 32 dimensions; as whole numbers, in which NaN is above infinity
+                uint32_t m[2] = {0u, 0u};
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = __shfl_sync(0xffffffffu, y[e], other);
-                if (formed && turns && fits)
+                for (int e = 0; e < 16; ++e) m[e / 8] = max(m[e / 8], __float_as_uint(y[e]) & 0x7fffffffu);
+                if (NEIGH || part % 4 == 0) {
+                    const bool whole = NEIGH || !turns || !formed;  // side by side: a scale's chunks are two lanes', else one of four lanes'
+                    if (whole) m[0] = m[1] = max(m[0], m[1]);
+                    m[0] = max(m[0], __shfl_xor_sync(0xffffffffu, m[0], 1));
+                    m[1] = max(m[1], __shfl_xor_sync(0xffffffffu, m[1], 1));
+                    const uint32_t n0 = __shfl_xor_sync(0xffffffffu, m[0], 2), n1 = __shfl_xor_sync(0xffffffffu, m[1], 2);
+                    if (!whole) m[0] = max(m[0], n0), m[1] = max(m[1], n1);
+                } else {
+                    uint32_t most[NB];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = y[e] * cs[e].x + (second ? w[e] : -w[e]) * cs[e].y;
-            }
-        }
-        const bool q_row = h < H, is_k = formed && !q_row, stored = !q_row && h < heads && page >= 0;
-        const int kvh = is_k ? h - H : h - H - K;
-        uint32_t out[4];
+                    for (int n = 0; n < NB; ++n) {
+                        most[n] = max((c0 >> 2) == n ? m[0] : 0u, (c1 >> 2) == n ? m[1] : 0u);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) out[e] = fits ? E::pack(y[2 * e], y[2 * e + 1]) : 0u;
-        if (q_row) {
-            *reinterpret_cast<uint4*>(a.q_out + row * a.q_out_ld + (int64_t)h * DH + sub * 8) =
-                make_uint4(out[0], out[1], out[2], out[3]);
-        } else if (!MX && stored) {
-            uint16_t* dst = static_cast<uint16_t*>(is_k ? a.kpool : a.vpool) + page * c.page_stride + kvh * c.head_stride +
-                            in_page * c.pos_stride;
-            // (a value goes as it came: a NaN keeps its bits)
-            *reinterpret_cast<uint4*>(dst + sub * 8) = is_k ? make_uint4(out[0], out[1], out[2], out[3]) : x[i];
-        }
-        if constexpr (MX)
-            if (__any_sync(0xffffffffu, stored)) {
-            uint32_t most = 0u;  // compared as whole numbers, in which NaN is above infinity
+                        for (int o = LPH / 2; o > 0; o >>= 1) most[n] = max(most[n], __shfl_xor_sync(0xffffffffu, most[n], o));
+                    }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(y[e]) & 0x7fffffffu);
-            most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-            most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-            const bool finite = most < 0x7f800000u;
-            const int p2 = mx_exponent<FF>(most, a.e_lo, a.e_hi);
-            const float inv = finite ? __uint_as_float((uint32_t)(127 - p2) << 23) : 0.f;
-            uint32_t lo = 0u, hi = 0u;
-            if (finite) {
-                lo = mx_codes<FF>(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
-                hi = mx_codes<FF>(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv);
-            }
-            // the head's scales in one word
-            uint32_t s = (finite ? (uint32_t)(p2 + 127) : 255u) << (8 * (sub >> 2));
-            s |= __shfl_xor_sync(0xffffffffu, s, 4);
-            if (NB == 4) s |= __shfl_xor_sync(0xffffffffu, s, 8);
-            if (stored) {
-                uint8_t* dst = static_cast<uint8_t*>(is_k ? a.kpool : a.vpool) + page * c.page_stride + kvh * c.head_stride +
-                               in_page * c.pos_stride;
-                *reinterpret_cast<uint2*>(dst + sub * 8) = make_uint2(lo, hi);
-                uint8_t* sd = (is_k ? a.kscale : a.vscale) + page * a.scale_page + kvh * a.scale_head + in_page * NB;
-                if (sub == 0) {
-                    if (NB == 4)
-                        *reinterpret_cast<uint32_t*>(sd) = s;
-                    else
-                        *reinterpret_cast<uint16_t*>(sd) = (uint16_t)s;
+                    for (int n = 0; n < NB; ++n) {
+                        if ((c0 >> 2) == n) m[0] = most[n];
+                        if ((c1 >> 2) == n) m[1] = most[n];
+                    }
+                }
+                if (here) {
+                    const int kvh = formed ? h : h - K;
+                    uint8_t* dst = static_cast<uint8_t*>(formed ? a.kpool : a.vpool) + entry + kvh * c.head_stride;
+                    uint8_t* sd = (formed ? a.kscale : a.vscale) + scale + kvh * a.scale_head;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const bool finite = m[j] < 0x7f800000u;
+                        const int p2 = mx_exponent<F>(m[j], a.e_lo, a.e_hi), ch = j == 0 ? c0 : c1;
+                        const float by = __uint_as_float((uint32_t)(127 - p2) << 23);
+                        uint2 code = make_uint2(0u, 0u);
+                        if (finite) {
+                            const float* z = y + 8 * j;
+                            code.x = mx_codes<F>(z[0] * by, z[1] * by, z[2] * by, z[3] * by);
+                            code.y = mx_codes<F>(z[4] * by, z[5] * by, z[6] * by, z[7] * by);
+                        }
+                        *reinterpret_cast<uint2*>(dst + ch * 8) = code;
+                        if ((ch & 3) == 0) sd[ch >> 2] = finite ? (uint8_t)(p2 + 127) : (uint8_t)255;
+                    }
                 }
             }
         }
+        if (--batches == 0) return;
+        h0 += PASSES * HPW;
+        out_at += PASSES * HPW * DH;
+        load(h0);
     }
 }
 
-// Few rows: a warp a pass, so that all loads are in flight at once.  Many: several passes a warp share the rotation
-// and the search for the sequence.
-constexpr int kQkPasses = 3, kQkManyRows = 512;
+// A row's warps: its queries', then its keys' and values', of `batches` times PASSES passes each at most.
+template <class T, int DH, int F, bool NEIGH, int PASSES>
+__global__ void __launch_bounds__(kQkWarps * 32, 2) k_paged_append_qk(const __grid_constant__ PagedQkArgs a) {
+    constexpr int HPW = 32 / (DH / 16), HPB = HPW * PASSES;  // heads of a batch
+    pdl_wait();
+    pdl_launch_dependents();
+    const int lane = threadIdx.x & 31;
+    const int q_warps = (a.n_heads + HPB * a.batches - 1) / (HPB * a.batches), kv_warps = (2 * a.c.n_kv_heads + HPB * a.batches - 1) / (HPB * a.batches);
+    const int64_t gw = (int64_t)blockIdx.x * kQkWarps + (threadIdx.x >> 5);
+    const int row = (int)paged_div(gw, q_warps + kv_warps);
+    if (row >= a.n_rows) return;
+    const int w = (int)(gw - (int64_t)row * (q_warps + kv_warps)), sub = lane / (DH / 16);
+    if (w < q_warps) {
+        const int from = w * HPB * a.batches;
+        qk_heads<T, DH, F, NEIGH, PASSES, true>(a, row, from + sub, min(a.batches, (a.n_heads - from + HPB - 1) / HPB));
+    } else {
+        const int from = (w - q_warps) * HPB * a.batches;
+        qk_heads<T, DH, F, NEIGH, PASSES, false>(a, row, from + sub, min(a.batches, (2 * a.c.n_kv_heads - from + HPB - 1) / HPB));
+    }
+}
 
-template <class T, int DH, int F, int PASSES>
-static cudaError_t qk_passes(const PagedQkArgs& a, cudaStream_t st) {
-    constexpr int HPW = 32 / (DH / 8);
-    const int heads = a.n_heads + 2 * a.c.n_kv_heads;
-    const int64_t warps = (int64_t)a.n_rows * ((heads + HPW * PASSES - 1) / (HPW * PASSES));
-    return launch_paged_k(k_paged_append_qk<T, DH, F, PASSES>, (unsigned)((warps + kQkWarps - 1) / kQkWarps), kQkWarps * 32, 0,
+// Few rows: a warp a pass, so that all loads are in flight at once.  Many: several passes a warp share the rotation,
+// the gains and the search for the sequence.  (7 prompts of 300 to 2500 rows, 32 query and 8 KV heads of 128, 16 bits: 4 passes twice
+// 36.8 us, 4 once 40, 2 four times 38 to 41, 1 eight times 40; 3 CTAs an SM instead of 2 cost registers and 1 to 3 us, as did
+// loading the next passes ahead.)
+constexpr int kQkPasses = 4, kQkBatches = 2, kQkManyRows = 512;
+
+template <class T, int DH, int F, bool NEIGH, int PASSES>
+static cudaError_t qk_passes(PagedQkArgs a, cudaStream_t st) {
+    constexpr int HPB = 32 / (DH / 16) * PASSES;
+    a.batches = PASSES == 1 ? 1 : kQkBatches;
+    const int64_t warps = (int64_t)a.n_rows * ((a.n_heads + HPB * a.batches - 1) / (HPB * a.batches) + (2 * a.c.n_kv_heads + HPB * a.batches - 1) / (HPB * a.batches));
+    return launch_paged_k(k_paged_append_qk<T, DH, F, NEIGH, PASSES>, (unsigned)((warps + kQkWarps - 1) / kQkWarps), kQkWarps * 32, 0,
                           st, a);
+}
+template <class T, int DH, int F>
+static cudaError_t qk_pairs(const PagedQkArgs& a, cudaStream_t st) {
+    const bool many = a.n_rows >= kQkManyRows;
+    if (a.neighbours) return many ? qk_passes<T, DH, F, true, kQkPasses>(a, st) : qk_passes<T, DH, F, true, 1>(a, st);
+    return many ? qk_passes<T, DH, F, false, kQkPasses>(a, st) : qk_passes<T, DH, F, false, 1>(a, st);
 }
 template <class T, int F>
 static cudaError_t qk_dh(const PagedQkArgs& a, int dh, cudaStream_t st) {
-    const bool many = a.n_rows >= kQkManyRows;
-    if (dh == 128) return many ? qk_passes<T, 128, F, kQkPasses>(a, st) : qk_passes<T, 128, F, 1>(a, st);
-    return many ? qk_passes<T, 64, F, kQkPasses>(a, st) : qk_passes<T, 64, F, 1>(a, st);
+    return dh == 128 ? qk_pairs<T, 128, F>(a, st) : qk_pairs<T, 64, F>(a, st);
 }
 template <class T>
 static cudaError_t qk_format(const PagedQkArgs& a, int format, int dh, cudaStream_t st) {
