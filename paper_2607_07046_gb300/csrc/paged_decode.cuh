@@ -9,7 +9,7 @@
 // HBM.  The work of a unit (a sequence's KV head and up to 8 NT of its columns) is cut into steps of 16
 // positions; the steps of all units form one line, and CTA c takes its c-th equal part, whatever the
 // sequences' lengths are.  They are known on the device only, so that a captured launch serves any
-// lengths.  A unit counts kPdUnitCost steps more than it has, as its queries and its result take that time.
+// lengths.  A unit counts kUnitCost steps more than it has, as its queries and its result take that time.
 // Inside a CTA step i goes to warp i % 4 (short units: whole units to a warp), each with its own ring of
 // asynchronous 16-byte copies (K and V rows gathered through the page table), so no barrier stands in the
 // stream; 128 KB or more a SM are in flight.  A unit that several CTAs share is joined by the last of them
@@ -41,32 +41,36 @@ namespace vt {
 
 constexpr int kPdWarps = 4, kPdThreads = kPdWarps * 32;
 constexpr int kPdRing = 96 * 1024;           // bytes of the four warps' rings, at most
-// A unit's queries, merge and result cost as much as this many steps (measured: 64 ragged sequences 75 us at 0, 56 at
-// 4, 47 at 8 to 24, 50 at 32).
-constexpr int kPdUnitCost = 16;
-// What a CTA takes at least: where the largest unit costs no more than kPdWhole (12 steps), that much, so that few are
-// split and joined (8 heads of 128 positions: 5.4 us, split 6.7; at 48, units of 20 to 30 steps lost up to 2 us);
-// otherwise kPdMinSteps.
-constexpr int kPdMinSteps = 16, kPdWhole = 28;
-
-// Where the largest unit has no more steps than kPdSoloSteps and there are kPdSoloUnits or more such units for every CTA,
-// each warp has units of its own: merging four warps would cost more than the steps.  Measured, merged and alone: 168
-// sequences of 1 to 3 positions, 32 heads, 38 and 15 us; 1024 sequences of 61 to 65 positions, 8 KV heads, 87 and 56;
-// 24 sequences of 201 to 251, 32 heads, 24 and 22.  At 32 steps 300 sequences of 21 to 501 positions lost (51 to 63).
-constexpr int kPdSoloSteps = 16, kPdSoloUnits = 2;
+constexpr int kPdSoloUnits = 2;              // (see kSoloSteps)
+// Codes: parts that are joined by several threads an item (131,000 positions, 38 parts a head, 57.7 us by one, 54.9 by several;
+// 64 ragged sequences, 2 to 3 parts, 38.3 and 39.8: the longer code comes from far away).
+constexpr int kPdManyParts = 8;
 
 template <class Src, int DH, int NT>
 struct PdGeom {
-    static constexpr int kCtas = Src::kMx && NT == 1 ? 3 : 2;                    // an SM
-    static constexpr int kKeys = 16;                                             // positions of a step
+    static constexpr bool kMx = Src::kMx;
+    static constexpr int kCtas = 2;                                                // an SM
+    static constexpr int kKeys = kMx ? 32 : 16;                                  // positions of a step
     static constexpr int kRow = DH * Src::kBytes;                                // bytes of a K or V row
     static constexpr int kSide = kKeys * kRow;                                   // of a step's K
-    static constexpr int kScales = Src::kMx ? kKeys * (DH / kMxBlock) : 0;       // of its scales
+    static constexpr int kScales = kMx ? kKeys * (DH / kMxBlock) : 0;            // of its scales
     static constexpr int kStage = 2 * (kSide + kScales);                         // K rows, V rows, K scales, V scales
-    static constexpr int kStages = (kCtas == 3 ? kPdRing / 2 : kPdRing) / (kPdWarps * kStage) + (kCtas == 3 && DH == 128 ? 1 : 0);
+    static constexpr int kStages = kMx ? (DH == 128 ? 3 : 6) : kPdRing / (kPdWarps * kStage);
     static constexpr int kRing = kPdWarps * kStages * kStage;
-    static constexpr int kFloats = 2 * kKeys * (DH / kMxBlock) * (Src::kMx ? 1 : 0);  // of a warp: a step's scales
-    static constexpr size_t kSmem = kRing + (size_t)kPdWarps * (8 * DH + kFloats) * 4;
+    static constexpr int kFloats = kMx ? 2 * kKeys * (DH / kMxBlock) : 8 * DH;   // of a warp: a step's scales; results to be merged
+    static constexpr size_t kSmem = kRing + (size_t)kPdWarps * kFloats * 4;
+    // A unit's queries, merge and result cost as much as this many steps (measured, 16 bits: 64 ragged sequences 75 us at 0,
+    // 56 at 4, 47 at 8 to 24, 50 at 32).
+    static constexpr int kUnitCost = 256 / kKeys;
+    // What a CTA takes at least: where the largest unit costs no more than kWhole (16 bits: 12 steps), that much, so that few
+    // are split and joined (8 heads of 128 positions: 5.4 us, split 6.7; at 48, units of 20 to 30 steps lost up to 2 us);
+    // otherwise kMinSteps.
+    static constexpr int kMinSteps = 256 / kKeys, kWhole = 448 / kKeys;
+    // Where the largest unit has no more steps than kSoloSteps and there are kPdSoloUnits or more such units for every CTA,
+    // each warp has units of its own: merging four warps would cost more than the steps.  Measured (16 bits), merged and alone:
+    // 168 sequences of 1 to 3 positions, 32 heads, 38 and 15 us; 1024 sequences of 61 to 65 positions, 8 KV heads, 87 and 56;
+    // 24 sequences of 201 to 251, 32 heads, 24 and 22.  At 32 steps 300 sequences of 21 to 501 positions lost (51 to 63).
+    static constexpr int kSoloSteps = 256 / kKeys;
 };
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool full) {
@@ -139,9 +143,10 @@ __device__ __forceinline__ void mma16816_new(float (&d)[4], const uint32_t (&a)[
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 
-// A sequence's new rows, and the positions [beg, end) that they attend to (end 0: none), in steps of KEYS.
-template <int KEYS>
+// A sequence's new rows, and the positions [beg, end) that they attend to (end 0: none), in steps of kKeys.
+template <class G>
 struct PdSeq {
+    static constexpr int KEYS = G::kKeys;
     int row0, rows, len, beg, end, tiles, steps;
     bool over;
     // tiles: units of a KV head, of `cols` columns
@@ -164,14 +169,14 @@ struct PdSeq {
         tiles = (rows * a.group + cols - 1) / cols;
     }
     // its share of the line, for one KV head
-    __device__ __forceinline__ int64_t cost() const { return steps > 0 ? (int64_t)tiles * (steps + kPdUnitCost) : 0; }
+    __device__ __forceinline__ int64_t cost() const { return steps > 0 ? (int64_t)tiles * (steps + G::kUnitCost) : 0; }
 };
 
-// Where a walk over the steps of the units stands: unit u of sequence b (KV head u / tiles), step i - kPdUnitCost.
-template <bool ROWS, int COLS, int KEYS>
+// Where a walk over the steps of the units stands: unit u of sequence b (KV head u / tiles), step i - kUnitCost.
+template <bool ROWS, int COLS, class G>
 struct PdCursor {
     int b, u, i;
-    PdSeq<KEYS> s;
+    PdSeq<G> s;
     __device__ __forceinline__ void open(const PagedAttnArgs& a, int seq) {
         b = seq;
         s.steps = 0;
@@ -193,6 +198,7 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
     using E = Elem<T>;
     using G = PdGeom<Src, DH, NT>;
     constexpr bool TWO = std::is_same<T, __half>::value;  // codes: weights in two terms
+    constexpr uint32_t FULL = G::kKeys == 32 ? 0xffffffffu : 0xffffu;
     constexpr int KEYS = G::kKeys, NB = DH / kMxBlock;
     constexpr int S = G::kStages, CPR = G::kRow / 16, RPI = 32 / CPR;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -200,6 +206,7 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
     __shared__ int s_seq[kPdWarps + 1], s_last, s_max[kPdWarps];
     __shared__ float s_ml[2][kPdWarps][8 * NT];
     __shared__ uint32_t s_mask[kPdWarps][S];
+    __shared__ int s_free[kPdWarps];
     const PagedView& c = a.c;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     constexpr int COLS = 8 * NT;
@@ -212,7 +219,7 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
     int largest = 0;
     bool idle = false, over = false;
     for (int b = tid * ch; b < min(c.n_seqs, (tid + 1) * ch); ++b) {
-        PdSeq<KEYS> s;
+        PdSeq<G> s;
         s.template open<ROWS>(a, b, COLS);
         if (blockIdx.x == 0 && s.rows > 0 && s.len >= 0 && s.len + s.rows > c.cap) set_status(c.status, VT_DEV_KV_OVERFLOW);
         idle |= s.steps == 0 && !s.over;
@@ -244,7 +251,7 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
     }
     if (any_idle)  // rows that attend to nothing get zeros
         for (int b = blockIdx.x; b < c.n_seqs; b += gridDim.x) {
-            PdSeq<KEYS> s;
+            PdSeq<G> s;
             s.template open<ROWS>(a, b, COLS);
             if (s.steps == 0)
                 for (int r = s.row0; r < s.row0 + s.rows; ++r)
@@ -252,9 +259,9 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
                         reinterpret_cast<uint4*>(a.out + r * a.out_ld)[e] = make_uint4(0u, 0u, 0u, 0u);
         }
     const int64_t line = total * c.n_kv_heads;
-    const bool solo = largest <= kPdSoloSteps && line >= (int64_t)kPdSoloUnits * gridDim.x * (largest + kPdUnitCost);
+    const bool solo = largest <= G::kSoloSteps && line >= (int64_t)kPdSoloUnits * gridDim.x * (largest + G::kUnitCost);
     const int64_t per = max(paged_div(line + gridDim.x - 1, gridDim.x),
-                            (int64_t)(largest + kPdUnitCost <= kPdWhole ? largest + kPdUnitCost : kPdMinSteps));
+                            (int64_t)(largest + G::kUnitCost <= G::kWhole ? largest + G::kUnitCost : G::kMinSteps));
     int64_t t0 = blockIdx.x * per, t1 = min(line, t0 + per);
     if (t0 >= t1) return;
     // the sequences that hold t0 and, for warps with units of their own, the beginnings of their parts and the last one's end
@@ -265,7 +272,7 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
             int64_t before = upto - mine;
             int b = tid * ch;
             for (;; ++b) {
-                PdSeq<KEYS> s;
+                PdSeq<G> s;
                 s.template open<ROWS>(a, b, COLS);
                 if (head < before + s.cost()) break;
                 before += s.cost();
@@ -279,20 +286,20 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
     // ---- the copies.  Step k of the CTA's part (unit costs left out) is warp k % 4's, or each warp has its own part, from
     // the first unit that begins in it to the first that begins in the next.
     const int stride = solo ? 1 : kPdWarps;
-    PdCursor<ROWS, COLS, KEYS> at;  // of the whole CTA, or of the warp
+    PdCursor<ROWS, COLS, G> at;  // of the whole CTA, or of the warp
     if (solo) {
         auto unit_start = [&](int64_t pos, int k) {  // of the first unit that begins at pos or after it
             if (pos >= line) return line;
-            PdSeq<KEYS> s;
+            PdSeq<G> s;
             s.template open<ROWS>(a, s_seq[k], COLS);
-            const int64_t r = pos - s_before[k] * c.n_kv_heads, cost = s.steps + kPdUnitCost;
+            const int64_t r = pos - s_before[k] * c.n_kv_heads, cost = s.steps + G::kUnitCost;
             return pos + (cost - 1 - (r + cost - 1 - paged_div(r + cost - 1, cost) * cost));
         };
         const int64_t w0 = unit_start(min(t1, t0 + warp * per_warp), warp);
         const int64_t w1 = unit_start(min(t1, t0 + (warp + 1) * per_warp), warp + 1);
         if (w0 >= w1) return;  // (no barrier of the whole CTA follows)
         at.open(a, s_seq[warp]);
-        const int64_t r = w0 - s_before[warp] * c.n_kv_heads, cost = at.s.steps + kPdUnitCost;
+        const int64_t r = w0 - s_before[warp] * c.n_kv_heads, cost = at.s.steps + G::kUnitCost;
         at.u = (int)paged_div(r, cost) - 1;  // the unit before it, unless it is the sequence's first
         at.i = 0;
         if (at.u < 0) at.u = 0;
@@ -302,24 +309,27 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
     } else {
         at.open(a, s_seq[0]);
         const int64_t r = t0 - s_before[0] * c.n_kv_heads;
-        at.u = (int)paged_div(r, at.s.steps + kPdUnitCost);
-        at.i = (int)(r - (int64_t)at.u * (at.s.steps + kPdUnitCost));
+        at.u = (int)paged_div(r, at.s.steps + G::kUnitCost);
+        at.i = (int)(r - (int64_t)at.u * (at.s.steps + G::kUnitCost));
     }
-    PdCursor<ROWS, COLS, KEYS> ld = at;               // of this warp's copies: the unit of its next step
+    PdCursor<ROWS, COLS, G> ld = at;               // of this warp's copies: the unit of its next step
     int64_t ld_now = t0;                        // where that unit's part begins in the line
     int ld_i, ld_n, ld_skip = solo ? 0 : warp;  // next step of the unit, steps of it here, steps until this warp's next
-    int ld_head = 0;                            // codes: its KV head
+    int64_t ld_hoff = 0, ld_soff = 0;           // codes: its KV head's offsets
     auto ld_unit = [&]() {                      // the steps [first, n) of the unit that lie in this part
-        const int first = max(0, ld.i - kPdUnitCost);
-        ld_n = (int)min((int64_t)ld.s.steps, t1 - ld_now + ld.i - kPdUnitCost);
+        const int first = max(0, ld.i - G::kUnitCost);
+        ld_n = (int)min((int64_t)ld.s.steps, t1 - ld_now + ld.i - G::kUnitCost);
         ld_i = first;
-        if constexpr (Src::kMx) ld_head = ld.u / ld.s.tiles;
+        if constexpr (Src::kMx) {
+            ld_hoff = (ld.u / ld.s.tiles) * c.head_stride;
+            ld_soff = (ld.u / ld.s.tiles) * a.scale_head;
+        }
     };
     // moves to this warp's next step; false: none
     auto ld_seek = [&]() -> bool {
         while (ld_i + ld_skip >= ld_n) {
             if (ld_n > ld_i) ld_skip -= ld_n - ld_i;
-            ld_now += ld.s.steps + kPdUnitCost - ld.i;
+            ld_now += ld.s.steps + G::kUnitCost - ld.i;
             if (ld_now >= t1) return false;
             ld.next(a);
             ld_unit();
@@ -344,7 +354,7 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
     constexpr int PER = Src::kMx ? 16 / NB : 1, CHUNKS = KEYS / PER;
     const int64_t mine_at = (lane / CPR) * c.pos_stride + (lane % CPR) * 16, hop = RPI * c.pos_stride;
     const uint8_t *k_at = reinterpret_cast<const uint8_t*>(a.kpool) + mine_at, *v_at = reinterpret_cast<const uint8_t*>(a.vpool) + mine_at;
-    const uint8_t* s_at = (lane % (2 * CHUNKS) < CHUNKS ? a.kscale : a.vscale) + (lane % CHUNKS) * 16;
+    const uint8_t* s_at = lane % (2 * CHUNKS) < CHUNKS ? a.kscale : a.vscale;
     const uint32_t mine_to = (uint32_t)((lane / CPR) * G::kRow) + pd_chunk<CPR>(lane / CPR, lane % CPR);
     auto load_step = [&]() {
         if (more) {
@@ -368,28 +378,38 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
                     cp_async16(d + KEYS * G::kRow, a.vpool + src, o >= 0);
                 }
             } else {
-                const int first = (ld.s.beg / KEYS + ld_i) * KEYS, in_page = first & (c.page_size - 1);
-                if (mask == 0xffffu && c.page_size >= KEYS) {  // all of one page
-                    const int pg = __shfl_sync(0xffffffffu, page, 0);
-                    const int64_t at = pg * c.page_stride + ld_head * c.head_stride + in_page * c.pos_stride;
-                    const uint8_t *ksrc = k_at + at, *vsrc = v_at + at;
+                const int first = (ld.s.beg / KEYS + ld_i) * KEYS;
+                if (mask == FULL && c.page_size >= 16) {  // 16 rows of one page
+                    int pg = 0;
+                    int64_t at = 0;
 #pragma unroll
-                    for (int r = 0; r < KEYS; r += RPI) {
-                        const uint32_t d = dst + (uint32_t)(r * G::kRow) + (mine_to ^ (CPR == 8 && (r & 4) ? 16u : 0u));
-                        cp_async16(d, ksrc);
-                        cp_async16(d + G::kSide, vsrc);
-                        ksrc += hop;
-                        vsrc += hop;
+                    for (int h = 0; h < KEYS; h += 16) {
+                        if (h == 0 || c.page_size == 16) {
+                            pg = __shfl_sync(0xffffffffu, page, h);
+                            at = pg * c.page_stride + ld_hoff + ((first + h) & (c.page_size - 1)) * c.pos_stride;
+                        }
+                        const uint8_t *ksrc = k_at + at, *vsrc = v_at + at;
+#pragma unroll
+                        for (int r = h; r < h + 16; r += RPI) {
+                            const uint32_t d = dst + (uint32_t)(r * G::kRow) + (mine_to ^ (CPR == 8 && (r & 4) ? 16u : 0u));
+                            cp_async16(d, ksrc);
+                            cp_async16(d + G::kSide, vsrc);
+                            ksrc += hop;
+                            vsrc += hop;
+                        }
+                        at += 16 * c.pos_stride;
                     }
+                    const int x = lane % CHUNKS * PER;  // the first position of this lane's scales
+                    if (c.page_size == 16) pg = __shfl_sync(0xffffffffu, page, x);
                     if (lane < 2 * CHUNKS)
                         cp_async16(dst + (uint32_t)(2 * G::kSide + lane * 16),
-                                   s_at + (pg * a.scale_page + ld_head * a.scale_head + in_page * NB));
+                                   s_at + (pg * a.scale_page + ld_soff + ((first + x) & (c.page_size - 1)) * NB));
                 } else {
-#pragma unroll
+#pragma unroll 1
                     for (int h = 0; h < KEYS; h += 8) {  // a page holds 8 positions or more
                         const uint32_t bits = (mask >> h) & 0xffu;
                         const int pg = __shfl_sync(0xffffffffu, page, h + max(0, __ffs(bits) - 1));
-                        int64_t at = bits ? pg * c.page_stride + ld_head * c.head_stride + ((first + h) & (c.page_size - 1)) * c.pos_stride : 0;
+                        int64_t at = bits ? pg * c.page_stride + ld_hoff + ((first + h) & (c.page_size - 1)) * c.pos_stride : 0;
 #pragma unroll
                         for (int k = 0; k < 8; k += RPI) {
                             const uint32_t d = dst + (uint32_t)((h + k) * G::kRow) + (mine_to ^ (CPR == 8 && (k & 4) ? 16u : 0u));
@@ -401,7 +421,7 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
                     }
                     const int x = lane % CHUNKS * PER, some = __ffs((mask >> x) & ((1u << PER) - 1u));
                     const int pg = __shfl_sync(0xffffffffu, page, x + max(0, some - 1));
-                    const int64_t at = some ? pg * a.scale_page + ld_head * a.scale_head + ((first + x) & (c.page_size - 1)) * NB - lane % CHUNKS * 16 : 0;
+                    const int64_t at = some ? pg * a.scale_page + ld_soff + ((first + x) & (c.page_size - 1)) * NB : 0;
                     if (lane < 2 * CHUNKS) cp_async16(dst + (uint32_t)(2 * G::kSide + lane * 16), s_at + at, some > 0);
                 }
             }
@@ -417,14 +437,17 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
 
     // ---- the steps, unit by unit
     int st = 0, skip = solo ? 0 : warp;  // skip: steps until this warp's next
-    float* so = reinterpret_cast<float*>(smem + G::kRing);
-    const uint32_t fs = smem_u32(smem) + (uint32_t)(G::kRing + kPdWarps * 8 * DH * 4 + warp * G::kFloats * 4);  // codes: a step's scales
+    // where warp w leaves its results to be merged.  Codes: in the stage that it fills next
+    auto merge_at = [&](int w) {
+        return reinterpret_cast<float*>(smem + (Src::kMx ? (w * S + s_free[w]) * G::kStage : G::kRing + w * 8 * DH * 4));
+    };
+    const uint32_t fs = smem_u32(smem) + (uint32_t)(G::kRing + warp * G::kFloats * 4);  // codes: a step's scales
     auto dim_of = [&](int i, int e) { return 16 * i + (Src::kMx ? 2 * g + (e >> 1) : g + 8 * (e >> 1)); };  // of o[i][.][e]
     for (int64_t now = t0; now < t1;) {
         // steps [i0, i0 + n) of the unit are in this part
-        const int i0 = max(0, at.i - kPdUnitCost), n = (int)min((int64_t)at.s.steps, t1 - now + at.i - kPdUnitCost) - i0;
-        const int64_t u0 = now - at.i + kPdUnitCost;  // where its steps begin in the line
-        now += at.s.steps + kPdUnitCost - at.i;
+        const int i0 = max(0, at.i - G::kUnitCost), n = (int)min((int64_t)at.s.steps, t1 - now + at.i - G::kUnitCost) - i0;
+        const int64_t u0 = now - at.i + G::kUnitCost;  // where its steps begin in the line
+        now += at.s.steps + G::kUnitCost - at.i;
         if (n <= 0) {
             at.next(a);
             continue;
@@ -512,48 +535,61 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
             } else {
                 // The step's scales as floats, [K, V][pair of positions][block][position], each worked out by one lane; those of V
                 // over the unit.
-                constexpr int WORDS = 2 * KEYS * NB / 4;  // of 4 bytes
-                {
-                    const bool of_v = lane % WORDS >= WORDS / 2;
-                    uint32_t w = lds32(vs + G::kSide + (uint32_t)(lane % WORDS * 4));
-                    if (of_v && mask != 0xffffu) {  // what nothing attends to may be anything
-                        const uint32_t bits = mask >> (lane % (WORDS / 2) * (4 / NB));
+                constexpr int WORDS = 2 * KEYS * NB / 4, PASSES = (WORDS + 31) / 32;  // of 4 bytes; half of them K's
+                float f[PASSES][4];
+                bool odd = false;
+#pragma unroll
+                for (int j = 0; j < PASSES; ++j) {
+                    const int i = (32 * j + lane) % WORDS;
+                    const bool of_v = i >= WORDS / 2;
+                    uint32_t w = lds32(vs + G::kSide + (uint32_t)(i * 4));
+                    if (of_v && mask != FULL) {  // what nothing attends to may be anything
+                        const uint32_t bits = mask >> (i % (WORDS / 2) * (4 / NB));
                         if (NB == 4)
                             w = bits & 1u ? w : 0u;
                         else
                             w &= (bits & 1u ? 0xffffu : 0u) | (bits & 2u ? 0xffff0000u : 0u);
                     }
-                    float f[4] = {mx_scale(w, 0), mx_scale(w, 1), mx_scale(w, 2), mx_scale(w, 3)};
-                    float most = fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3]));
-                    if (__any_sync(0xffffffffu, of_v ? most > unit : most == INFINITY)) {  // (an infinite scale is NaN's: it sets no unit)
-                        most = 0.f;
+                    float most = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) most = fmaxf(most, f[j][e] = mx_scale(w, e));
+                    odd |= of_v ? most > unit : most == INFINITY;
+                }
+                if (__any_sync(0xffffffffu, odd)) {  // (an infinite scale is NaN's: it sets no unit)
+                    float most = 0.f;
+#pragma unroll
+                    for (int j = 0; j < PASSES; ++j)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            if (f[e] == INFINITY) f[e] = __int_as_float(0x7fc00000);
-                            most = fmaxf(most, f[e]);
+                            if (f[j][e] == INFINITY) f[j][e] = __int_as_float(0x7fc00000);
+                            if ((32 * j + lane) % WORDS >= WORDS / 2) most = fmaxf(most, f[j][e]);
                         }
-                        const float next = fmaxf(unit, __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(of_v ? most : 0.f))));
-                        const float r = unit * pd_inverse(next);
-                        unit = next;
+                    const float next = fmaxf(unit, __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most))));
+                    const float r = unit * pd_inverse(next);
+                    unit = next;
 #pragma unroll
-                        for (int x = 0; x < NT; ++x)
+                    for (int x = 0; x < NT; ++x)
 #pragma unroll
-                            for (int i = 0; i < DH / 16; ++i)
+                        for (int i = 0; i < DH / 16; ++i)
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) o[i][x][e] *= r;
-                    }
-                    const float inv = of_v ? pd_inverse(unit) : 1.f;
+                            for (int e = 0; e < 4; ++e) o[i][x][e] *= r;
+                }
+                const float by = pd_inverse(unit);
+#pragma unroll
+                for (int j = 0; j < PASSES; ++j) {
+                    const int i = (32 * j + lane) % WORDS, at = i % (WORDS / 2);
+                    const bool of_v = i >= WORDS / 2;
+                    const float inv = of_v ? by : 1.f;
                     const uint32_t to = fs + (uint32_t)(of_v ? KEYS * NB * 4 : 0);
-                    const int i = lane % (WORDS / 2);
                     if (NB == 4) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) sts32(to + (uint32_t)((i >> 1) * 32 + e * 8 + (i & 1) * 4), f[e] * inv);
+                        for (int e = 0; e < 4; ++e) sts32(to + (uint32_t)((at >> 1) * 32 + e * 8 + (at & 1) * 4), f[j][e] * inv);
                     } else {
-                        sts128_at(to + (uint32_t)(i * 16), __float_as_uint(f[0] * inv), __float_as_uint(f[2] * inv),
-                                  __float_as_uint(f[1] * inv), __float_as_uint(f[3] * inv));
+                        sts128_at(to + (uint32_t)(at * 16), __float_as_uint(f[j][0] * inv), __float_as_uint(f[j][2] * inv),
+                                  __float_as_uint(f[j][1] * inv), __float_as_uint(f[j][3] * inv));
                     }
-                    __syncwarp();
                 }
+                __syncwarp();
                 using C = typename Src::H;
 #pragma unroll
                 for (int n = 0; n < NS; ++n) {  // keys 8 n + g; a scale's 32 dimensions into a sum of their own
@@ -578,7 +614,7 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
                 }
             }
             // whether some column does not attend to all of the step
-            const bool partial = !Src::kMx || mask != 0xffffu ||
+            const bool partial = !Src::kMx || mask != FULL ||
                                  (ROWS && (p0 + KEYS - 1 > at.s.len || (a.window > 0 && p0 <= at.s.len + at.s.rows - 1 - a.window)));
             // Weights.  m is a reference: the maximum less kUp where P is fp16, so that P goes up to 2^15 (it has no steps below
             // 2^-24); over codes it moves only when P would pass that, down to 2^12.  l, o and every later join agree on it.
@@ -709,7 +745,9 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
         }
 
         if (solo) {  // ---- the unit's end: one warp's (m, l, o)
-            float* ws = so + warp * 8 * DH;
+            if (Src::kMx && lane == 0) s_free[warp] = st_load;
+            __syncwarp();
+            float* ws = merge_at(warp);
 #pragma unroll
             for (int x = 0; x < NT; ++x) {
                 l[x] += __shfl_xor_sync(0xffffffffu, l[x], 1);
@@ -748,7 +786,9 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
                 s_ml[1][warp][8 * x + g] = l[x];
             }
         }
+        if (Src::kMx && lane == 0) s_free[warp] = st_load;
         __syncthreads();
+        float* mine_so = merge_at(warp);
         const int slot = (int)(2 * blockIdx.x + (first == blockIdx.x ? 1 : 0));
         float* part = a.work + (int64_t)slot * kPagedDecodeSlot;
 #pragma unroll
@@ -767,7 +807,7 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int h = 2 * t + (e & 1), d = dim_of(i, e) ^ (8 * t);
-                    so[(warp * 8 + h) * DH + d] = o[i][x][e] * f[e & 1];
+                    mine_so[h * DH + d] = o[i][x][e] * f[e & 1];
                 }
             __syncthreads();
             for (int e = tid; e < 8 * DH / 8; e += kPdThreads) {  // 8 dims of a head
@@ -780,7 +820,7 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
 #pragma unroll
                 for (int w = 0; w < kPdWarps; ++w) {
                     ll += s_ml[1][w][8 * x + h] * exp2f(s_ml[0][w][8 * x + h] - ref);
-                    const float4* v = reinterpret_cast<const float4*>(so + (w * 8 + h) * DH + ds);
+                    const float4* v = reinterpret_cast<const float4*>(merge_at(w) + h * DH + ds);
                     const float4 v0 = v[0], v1 = v[1];
                     sum[0] += v0.x, sum[1] += v0.y, sum[2] += v0.z, sum[3] += v0.w;
                     sum[4] += v1.x, sum[5] += v1.y, sum[6] += v1.z, sum[7] += v1.w;
@@ -811,7 +851,67 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
                 if (s_last) a.arrived[first] = 0;  // ready for the next call
             }
             __syncthreads();
-            if (s_last) {
+            if (Src::kMx && s_last && last - first >= kPdManyParts) {
+                // Several threads an item (8 dims of a column), each with every so many-th part, and eight of them on their way at
+                // once.  One warp a scheduler is left here: what counts is the instructions of a thread.
+                __threadfence();
+                constexpr int UP = 8;
+                const int items = nc * (DH / 8), tpi = items <= 16 ? 8 : items <= 32 ? 4 : items <= 64 ? 2 : 1, parts = (int)(last - first) + 1;
+                const float* base = a.work + 2 * first * kPagedDecodeSlot;  // of part p: 2 p slots further (the first: one)
+#pragma unroll 1
+                for (int e0 = 0; e0 < items; e0 += kPdThreads / tpi) {
+                    const int e = e0 + tid / tpi, sub = tid % tpi, h = min(e, items - 1) / (DH / 8), d = (e % (DH / 8)) * 8;
+                    float sum[8] = {}, mm = -INFINITY, ll = 0.f;
+#pragma unroll 1
+                    for (int p0 = sub; p0 < parts; p0 += UP * tpi) {
+                        float pm[UP], pl[UP];
+                        float4 v[UP][2];
+                        float mn = mm;
+#pragma unroll
+                        for (int k = 0; k < UP; ++k) {
+                            const int p = min(p0 + k * tpi, parts - 1);
+                            const float* src = base + (p == 0 ? 1 : 2 * p) * (int)kPagedDecodeSlot;
+                            pm[k] = __ldcg(src + h);
+                            pl[k] = __ldcg(src + 8 * NT + h);
+                            v[k][0] = __ldcg(reinterpret_cast<const float4*>(src + 16 * NT + h * DH + d));
+                            v[k][1] = __ldcg(reinterpret_cast<const float4*>(src + 16 * NT + h * DH + d) + 1);
+                        }
+#pragma unroll
+                        for (int k = 0; k < UP; ++k) {
+                            if (p0 + k * tpi >= parts) pm[k] = -INFINITY, pl[k] = 0.f;
+                            mn = fmaxf(mn, pm[k]);
+                        }
+                        const float ref = mn == -INFINITY ? 0.f : mn, fa = pd_exp2<Src>(mm - ref);
+                        mm = mn;
+                        ll *= fa;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) sum[i] *= fa;
+#pragma unroll
+                        for (int k = 0; k < UP; ++k) {
+                            const float fb = pd_exp2<Src>(pm[k] - ref);
+                            ll = fmaf(pl[k], fb, ll);
+                            sum[0] = fmaf(v[k][0].x, fb, sum[0]), sum[1] = fmaf(v[k][0].y, fb, sum[1]);
+                            sum[2] = fmaf(v[k][0].z, fb, sum[2]), sum[3] = fmaf(v[k][0].w, fb, sum[3]);
+                            sum[4] = fmaf(v[k][1].x, fb, sum[4]), sum[5] = fmaf(v[k][1].y, fb, sum[5]);
+                            sum[6] = fmaf(v[k][1].z, fb, sum[6]), sum[7] = fmaf(v[k][1].w, fb, sum[7]);
+                        }
+                    }
+#pragma unroll 1
+                    for (int o = 1; o < tpi; o <<= 1) {  // the item's threads, side by side
+                        const float om = __shfl_xor_sync(0xffffffffu, mm, o), mn = fmaxf(mm, om), ref = mn == -INFINITY ? 0.f : mn;
+                        const float fa = pd_exp2<Src>(mm - ref), fb = pd_exp2<Src>(om - ref);
+                        mm = mn;
+                        ll = ll * fa + __shfl_xor_sync(0xffffffffu, ll, o) * fb;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) sum[i] = sum[i] * fa + __shfl_xor_sync(0xffffffffu, sum[i], o) * fb;
+                    }
+                    const float inv = ll == 0.f ? 0.f : 1.f / ll;
+                    if (sub == 0 && e < items)
+                        *reinterpret_cast<uint4*>(a.out + col_at(h, a.out_ld) + d) =
+                            make_uint4(E::pack(sum[0] * inv, sum[1] * inv), E::pack(sum[2] * inv, sum[3] * inv),
+                                       E::pack(sum[4] * inv, sum[5] * inv), E::pack(sum[6] * inv, sum[7] * inv));
+                }
+            } else if (s_last) {
                 __threadfence();
                 for (int e = tid; e < nc * (DH / 8); e += kPdThreads) {
                     const int h = e / (DH / 8), d = (e % (DH / 8)) * 8;
@@ -838,24 +938,26 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
                 }
             }
         }
-        __syncthreads();  // so and s_ml are free for the next unit
+        __syncthreads();  // results and s_ml are free for the next unit
         at.next(a);
     }
     cp_async_wait<0>();
 }
 
-// Length of the line at the longest lengths, with units of `cols` columns and steps of `keys` positions.
-inline int64_t paged_decode_line_of(const PagedAttnArgs& a, int cols, int keys) {
+// Length of the line at the longest lengths, with units of `cols` columns.
+template <class G>
+int64_t paged_decode_line_of(const PagedAttnArgs& a, int cols) {
     const int64_t tiles = (int64_t)a.n_rows * a.group / cols + a.c.n_seqs;
     const int64_t span = a.window > 0 ? std::min<int64_t>((int64_t)a.window + a.n_rows, a.c.cap) : a.c.cap;
-    return tiles * a.c.n_kv_heads * (span / keys + 2 + kPdUnitCost);
+    return tiles * a.c.n_kv_heads * (span / G::kKeys + 2 + G::kUnitCost);
 }
 
 template <class Src, int DH, int NT, bool ROWS>
 static cudaError_t decode_nt(const PagedAttnArgs& a, cudaStream_t st) {
-    const int64_t most = paged_decode_line_of(a, 8 * NT, PdGeom<Src, DH, NT>::kKeys);
-    const int64_t grid = std::min<int64_t>(std::min(kPagedMaxGrid, PdGeom<Src, DH, NT>::kCtas * g_num_sms), (most + kPdMinSteps - 1) / kPdMinSteps);
-    return launch_paged_k(k_paged_decode<Src, DH, NT, ROWS>, (unsigned)grid, kPdThreads, PdGeom<Src, DH, NT>::kSmem, st, a);
+    using G = PdGeom<Src, DH, NT>;
+    const int64_t most = paged_decode_line_of<G>(a, 8 * NT);
+    const int64_t grid = std::min<int64_t>(std::min(kPagedMaxGrid, G::kCtas * g_num_sms), (most + G::kMinSteps - 1) / G::kMinSteps);
+    return launch_paged_k(k_paged_decode<Src, DH, NT, ROWS>, (unsigned)grid, kPdThreads, G::kSmem, st, a);
 }
 template <class Src, bool ROWS>
 static cudaError_t decode_dh(const PagedAttnArgs& a, int dh, cudaStream_t st) {
