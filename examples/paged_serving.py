@@ -1,11 +1,14 @@
 """Several users of one small model: prompts come in together and one at a time, tokens are decoded for all of
 them at once, a sequence that ends gives its pages to the next.
 
-The attention of every step runs through the paged cache (vt_paged_append, then vt_paged_prefill or
-vt_paged_decode); the projections around it are torch products.  Every sequence's hidden states are checked
-against the same model run for that sequence alone, without a cache, in 64 bits.
+The attention of every step runs through the paged cache (PagedCache.append, then PagedCache.attend); the
+projections around it are torch products.  Every sequence's hidden states are checked against the same model run
+for that sequence alone, without a cache, in 64 bits.
 
-    python examples/paged_serving.py
+    python examples/paged_serving.py [e4m3 | int8]
+
+With a code the cache holds 8-bit codes, and the model's queries and keys are normalised for each head and rotated
+by neighbours in the first half of their dimensions.
 """
 from __future__ import annotations
 
@@ -24,9 +27,13 @@ EPS, THETA = 1e-5, 1e4
 
 
 def weights(seed=0):
+    """Of each layer; the gains of queries and keys, and half of a head rotated, are for models that have them."""
     g = torch.Generator(device="cuda").manual_seed(seed)
     shapes = {"qkv": ((HEADS + 2 * KV_HEADS) * DH, D), "o": (D, HEADS * DH), "gate": (F, D), "up": (F, D), "down": (D, F)}
-    return [{n: (torch.randn(s, generator=g, device="cuda") / math.sqrt(s[1])).half() for n, s in shapes.items()} for _ in range(LAYERS)]
+    layers = [{n: (torch.randn(s, generator=g, device="cuda") / math.sqrt(s[1])).half() for n, s in shapes.items()} for _ in range(LAYERS)]
+    for w in layers:
+        w["q_gain"], w["k_gain"] = ((1 + 0.1 * torch.randn(DH, generator=g, device="cuda")).half() for _ in range(2))
+    return layers
 
 
 def norm(x):
@@ -42,19 +49,23 @@ def forward(layers, x, attend):
     return x
 
 
-def alone(layers, x):
+def alone(layers, x, norms=False):
     """One sequence by itself, in 64 bits."""
-    n = x.shape[0]
-    ang = torch.arange(n, device="cuda").double()[:, None] * THETA ** (-2.0 * torch.arange(DH // 2, device="cuda").double() / DH)
+    n, rotary = x.shape[0], DH // 2 if norms else DH
+    ang = torch.arange(n, device="cuda").double()[:, None] * THETA ** (-2.0 * torch.arange(rotary // 2, device="cuda").double() / rotary)
+    c, s = ang.cos()[:, None], ang.sin()[:, None]
 
-    def turn(y):
-        a, b = y[..., :DH // 2], y[..., DH // 2:]
-        c, s = ang.cos()[:, None], ang.sin()[:, None]
-        return torch.cat((a * c - b * s, b * c + a * s), -1)
+    def turn(y, gain):
+        if not norms:
+            a, b = y[..., :DH // 2], y[..., DH // 2:]
+            return torch.cat((a * c - b * s, b * c + a * s), -1)
+        y = norm(y) * gain.double()
+        a, b = y[..., 0:rotary:2], y[..., 1:rotary:2]
+        return torch.cat((torch.stack((a * c - b * s, b * c + a * s), -1).flatten(-2), y[..., rotary:]), -1)
 
-    def attend(_, qkv):
-        y = qkv.reshape(n, -1, DH)
-        q, k, v = turn(y[:, :HEADS]), turn(y[:, HEADS:HEADS + KV_HEADS]), y[:, HEADS + KV_HEADS:]
+    def attend(l, qkv):
+        y, w = qkv.reshape(n, -1, DH), layers[l]
+        q, k, v = turn(y[:, :HEADS], w["q_gain"]), turn(y[:, HEADS:HEADS + KV_HEADS], w["k_gain"]), y[:, HEADS + KV_HEADS:]
         k, v = (t.repeat_interleave(HEADS // KV_HEADS, 1).transpose(0, 1) for t in (k, v))
         s = q.transpose(0, 1) @ k.transpose(1, 2) / math.sqrt(DH)
         hide = torch.ones(n, n, dtype=torch.bool, device="cuda").triu(1)
@@ -64,15 +75,16 @@ def alone(layers, x):
 
 
 class Server:
-    def __init__(self, layers, slots=4, pages=40, page_size=16, max_len=400):
+    def __init__(self, layers, slots=4, pages=40, page_size=16, max_len=400, code=None):
         self.layers = layers
-        self.cache = PagedCache(LAYERS, KV_HEADS, DH, page_size, pages, slots, max_len, theta=THETA)
+        self.cache = PagedCache(LAYERS, KV_HEADS, DH, page_size, pages, slots, max_len, theta=THETA, code=code,
+                                rotary_dim=DH if code is None else DH // 2)
+        self.forms = [None if code is None else vt.make_qk_form(self.cache.rope, True, w["q_gain"], w["k_gain"], EPS) for w in layers]
 
     def step(self, new):
         """new: {slot: rows of inputs}; the hidden states of those rows."""
         c, rows = self.cache, {slot: x.shape[0] for slot, x in new.items()}
         batch, starts = c.step(rows)
-        one_each = batch.starts is None
         x = torch.zeros(starts[-1], D, dtype=torch.float16, device="cuda")
         for slot, part in new.items():
             x[starts[slot]:starts[slot] + part.shape[0]] = part
@@ -80,8 +92,8 @@ class Server:
 
         def attend(l, qkv):
             y = qkv.reshape(starts[-1], HEADS + 2 * KV_HEADS, DH)
-            vt.vt_paged_append(c.paged, c.pools[l], batch, y[:, :HEADS], y[:, HEADS:HEADS + KV_HEADS], y[:, HEADS + KV_HEADS:], c.rope, q_rot)
-            (vt.vt_paged_decode if one_each else vt.vt_paged_prefill)(c.paged, c.pools[l], batch, q_rot, out)
+            c.append(l, batch, y[:, :HEADS], y[:, HEADS:HEADS + KV_HEADS], y[:, HEADS + KV_HEADS:], q_rot, self.forms[l])
+            c.attend(l, batch, q_rot, out)
             return out.reshape(starts[-1], HEADS * DH)
 
         y = forward(self.layers, x, attend)
@@ -89,11 +101,11 @@ class Server:
         return {slot: y[starts[slot]:starts[slot] + n] for slot, n in rows.items()}
 
 
-def serve():
-    """The largest relative error of any sequence's hidden states against the sequence alone."""
+def serve(code=None):
+    """The largest relative error of any sequence's hidden states against the sequence alone, and how many there were."""
     layers = weights()
     g = torch.Generator(device="cuda").manual_seed(1)
-    server = Server(layers)
+    server = Server(layers, code=code)
     inputs, outputs, finished = {}, {}, []
 
     def feed(new):
@@ -132,11 +144,11 @@ def serve():
     assert status == 0, f"status {status}"
     worst = 0.0
     for x, y in finished:
-        ref = alone(layers, x)
+        ref = alone(layers, x, norms=code is not None)
         worst = max(worst, float((y.double() - ref).norm() / ref.norm()))
     return worst, len(finished)
 
 
 if __name__ == "__main__":
-    err, n = serve()
+    err, n = serve(*sys.argv[1:2])
     print(f"{n} sequences served; largest relative error of a sequence's hidden states against 64 bits: {err:.2e}")

@@ -5,8 +5,11 @@ The pools hold one layer's K and V each; tables and lengths are the same for eve
 
     rows = {slot: new rows, ...}
     batch, starts = cache.step(rows)               # pages for the new rows; slots without rows take no part
-    for layer: vt_paged_append(cache.paged, cache.pools[layer], batch, ...), then vt_paged_decode or _prefill
+    for layer: cache.append(layer, batch, q, k, v, q_out), then cache.attend(layer, batch, q_out, out)
     cache.advance(rows)                            # the new rows are held now
+
+append and attend make the calls that suit the cache (vt_paged_append, _append_qk, _append_mx; vt_paged_decode,
+_prefill, _decode_mx, _prefill_mx); a program may make them itself.
 """
 from __future__ import annotations
 
@@ -68,22 +71,66 @@ class PageTable:
 
 
 class PagedCache:
-    """`n_layers` pools [pages, KV heads, positions in a page, head dim] and one PageTable."""
+    """`n_layers` pools [pages, KV heads, positions in a page, head dim] and one PageTable.
+
+    code: None for values of `dtype`, or "e4m3" or "int8" for 8-bit codes with a scale for each 32 dimensions (pages of 8
+    positions or more), about half the memory.  rotary_dim: the first dimensions of a head that are rotated (None: all)."""
 
     def __init__(self, n_layers: int, n_kv_heads: int, d_head: int, page_size: int, n_pages: int, slots: int, max_len: int,
-                 dtype=torch.float16, theta: float = 1e4):
+                 dtype=torch.float16, theta: float = 1e4, code: Optional[str] = None, rotary_dim: Optional[int] = None):
+        if code not in (None, "e4m3", "int8"):
+            raise ValueError(f"code {code!r}: expected None, 'e4m3' or 'int8'")
+        if code is not None and page_size < 8:
+            raise ValueError(f"codes need pages of 8 positions or more, got {page_size}")
+        if rotary_dim is not None and (rotary_dim % 16 or not 0 <= rotary_dim <= d_head):
+            raise ValueError(f"rotary_dim {rotary_dim}: expected a multiple of 16 in [0, {d_head}]")
+        self.code = code
         self.table = PageTable(n_pages, page_size, slots, -(-max_len // page_size), max_len)
         shape = (n_pages, n_kv_heads, page_size, d_head)
-        self.pools = [vt.make_paged_pool(torch.zeros(shape, dtype=dtype, device="cuda"), torch.zeros(shape, dtype=dtype, device="cuda"))
-                      for _ in range(n_layers)]
+        self.pools = [self._pool(shape, dtype) for _ in range(n_layers)]
         self.tables = torch.full((slots, self.table.pages_per_seq), -1, dtype=torch.int32, device="cuda")
         self.lens = torch.full((slots,), -1, dtype=torch.int32, device="cuda")
         self.starts = torch.zeros(slots + 1, dtype=torch.int32, device="cuda")
-        self.rope = torch.empty(max_len, d_head // 2, 2, device="cuda")
-        vt.vt_rope_table(self.rope, theta)
+        rotary_dim = d_head if rotary_dim is None else rotary_dim
+        self.rope = torch.empty(max_len, rotary_dim // 2, 2, device="cuda") if rotary_dim else None
+        if rotary_dim in (64, 128):
+            vt.vt_rope_table(self.rope, theta)
+        elif rotary_dim:
+            at = torch.arange(max_len, device="cuda", dtype=torch.float64)[:, None] * theta ** (
+                torch.arange(rotary_dim // 2, device="cuda", dtype=torch.float64) * (-2.0 / rotary_dim))
+            self.rope.copy_(torch.stack((at.cos(), at.sin()), -1))
+        # vt_paged_append's own: all of a head, pairs of halves, no norms, values of `dtype`
+        self._form = None if code is None and rotary_dim == d_head else vt.make_qk_form(self.rope)
         self.paged = vt.vt_paged_create()
         self._each = vt.make_paged_batch(self.tables, self.lens)
         self._ragged = vt.make_paged_batch(self.tables, self.lens, self.starts)
+
+    def _pool(self, shape, dtype):
+        if self.code is None:
+            return vt.make_paged_pool(torch.zeros(shape, dtype=dtype, device="cuda"), torch.zeros(shape, dtype=dtype, device="cuda"))
+        kind = torch.float8_e4m3fn if self.code == "e4m3" else torch.int8
+        k, v = (torch.zeros(shape, dtype=torch.uint8, device="cuda").view(kind) for _ in range(2))
+        k_scale, v_scale = (torch.zeros(*shape[:3], shape[3] // 32, dtype=torch.uint8, device="cuda") for _ in range(2))
+        return vt.make_paged_mx_pool(k, v, k_scale, v_scale, dtype)
+
+    def append(self, layer: int, batch, q, k, v, q_out, form=None, stream=None) -> None:
+        """The new rows' queries rotated into q_out, keys rotated and values stored.  form: vt.make_qk_form(cache.rope, ...) for
+        norms of queries and keys or pairs of neighbours."""
+        form = self._form if form is None else form
+        if self.code is not None:
+            vt.vt_paged_append_mx(self.paged, self.pools[layer], batch, q, k, v, form, q_out, stream)
+        elif form is not None:
+            vt.vt_paged_append_qk(self.paged, self.pools[layer], batch, q, k, v, form, q_out, stream)
+        else:
+            vt.vt_paged_append(self.paged, self.pools[layer], batch, q, k, v, self.rope, q_out, stream)
+
+    def attend(self, layer: int, batch, q, out, scale: Optional[float] = None, window: int = 0, stream=None) -> None:
+        """Attention of the step's rows, which append has stored."""
+        if batch.starts is None:
+            call = vt.vt_paged_decode if self.code is None else vt.vt_paged_decode_mx
+        else:
+            call = vt.vt_paged_prefill if self.code is None else vt.vt_paged_prefill_mx
+        call(self.paged, self.pools[layer], batch, q, out, scale, window, stream)
 
     def admit(self) -> int:
         return self.table.admit()
