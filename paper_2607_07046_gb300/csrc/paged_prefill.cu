@@ -73,8 +73,8 @@ struct PfGeom {
     static constexpr int kThreads = Src::kMx ? 512 : 384;
     // Registers a thread: at launch 65536 / threads, rounded down to 8; then 2 x 128 threads of softmax, and 128 of copies and
     // MMAs, or 128 of each.
-    static constexpr int kLaunchRegs = Src::kMx ? 128 : 168, kSoftmaxRegs = Src::kMx ? 168 : 208, kCopyRegs = Src::kMx ? 72 : 88;
-    static constexpr int kMmaRegs = Src::kMx ? 104 : 88;
+    static constexpr int kLaunchRegs = Src::kMx ? 128 : 168, kSoftmaxRegs = Src::kMx ? 176 : 208, kCopyRegs = Src::kMx ? 72 : 88;
+    static constexpr int kMmaRegs = Src::kMx ? 88 : 88;
     static_assert(256 * kSoftmaxRegs + 128 * kCopyRegs + (kThreads - 384) * kMmaRegs <= kThreads * kLaunchRegs,
                   "the register split must fit in the registers the block is launched with");
     static constexpr int kTile = kPfRows * DH * 2;         // bytes of a Q tile, of a K or V block
@@ -341,7 +341,9 @@ __device__ __forceinline__ bool pf_convert(const PfRaw& m, const PfRing& ring, i
         const uint32_t dst = to + (uint32_t)(slot * G::kTile), src = from + (uint32_t)(buf * kPfKeys * DH), sc = scl + (uint32_t)(buf * kPfKeys * NB);
         const uint4 have = *reinterpret_cast<const uint4*>(m.rows + 4 * buf);
         const bool whole = (have.x & have.y & have.z & have.w) == 0xffffffffu;
-        constexpr int BATCH = 2;  // chunks whose loads are in flight together
+        // Chunks whose loads are in flight together.  The loop stays one: unrolled, the code of all roles did not fit in the
+        // instruction cache (4096 rows of int8 codes: 310 us, 215 as it is).
+        constexpr int BATCH = 2;
 #pragma unroll 1
         for (int x0 = 0; x0 < CHUNKS; x0 += BATCH) {
             uint4 w4[BATCH];
@@ -943,18 +945,36 @@ __global__ void __launch_bounds__(PfGeom<Src, DH>::kThreads, 1) k_paged_prefill(
                 // and the others are read again while the weights of these are worked out.
                 constexpr int KEPT = Src::kMx ? 3 : 4;
                 uint32_t sv[KEPT][32];
+                if constexpr (!Src::kMx)
 #pragma unroll
-                for (int q = 0; q < KEPT; ++q) tc::tmem_ld32(s_at_col + 32 * q, sv[q]);
+                    for (int q = 0; q < KEPT; ++q) tc::tmem_ld32(s_at_col + 32 * q, sv[q]);
                 const uint32_t* vw = valid + ((blk + j - j0) % kPfMaskRing) * 4;
                 const int kp0 = j * kPfKeys, cb = first_key - kp0, ce = qp + 1 - kp0;
                 uint32_t mw[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) mw[q] = fa_range_bits(cb - 32 * q, ce - 32 * q) & vw[q];
                 const bool plain = __all_sync(0xffffffffu, (mw[0] & mw[1] & mw[2] & mw[3]) == 0xffffffffu);
+                if constexpr (Src::kMx) {
+                    if (!plain) {  // hidden scores become -inf where they lie (a loop: less code, see pf_convert)
+#pragma unroll 1
+                        for (int q = 0; q < 4; ++q) {
+                            const uint32_t on = fa_range_bits(cb - 32 * q, ce - 32 * q) & vw[q];
+                            tc::tmem_ld32(s_at_col + 32 * q, sv[0]);
+                            tc::tmem_ld_wait_on(sv[0]);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!((on >> e) & 1u)) sv[0][e] = 0xff800000u;
+                            tc::tmem_st32(s_at_col + 32 * q, sv[0]);
+                        }
+                        tc::tmem_st_wait();
+                    }
+#pragma unroll
+                    for (int q = 0; q < KEPT; ++q) tc::tmem_ld32(s_at_col + 32 * q, sv[q]);
+                }
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 auto arrived = [&](uint32_t(&v)[32], int q) {  // keys 32 q ..
                     tc::tmem_ld_wait_on(v);
-                    if (!plain)
+                    if (!Src::kMx && !plain)
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
                             if (!((mw[q] >> e) & 1u)) v[e] = 0xff800000u;  // -inf
@@ -985,7 +1005,7 @@ __global__ void __launch_bounds__(PfGeom<Src, DH>::kThreads, 1) k_paged_prefill(
                     m_use = mn;
                 }
                 if (__any_sync(0xffffffffu, resc)) {  // O_x holds every earlier block (s_full)
-#pragma unroll
+#pragma unroll(Src::kMx ? 1 : DH / 32)
                     for (int q = 0; q < DH / 32; ++q) {
                         uint32_t o[32];
                         tc::tmem_ld32(o_at_col + 32 * q, o);
@@ -1047,7 +1067,30 @@ __global__ void __launch_bounds__(PfGeom<Src, DH>::kThreads, 1) k_paged_prefill(
                 set_status(c.status, VT_DEV_WAIT_TIMEOUT);
             }
             uint16_t* dst = a.out + (at.row0 + tok) * a.out_ld + (int64_t)(at.kvh * a.group + row % a.group) * DH;
-            if (whole) {
+            if (Src::kMx && whole) {  // by 32 columns: less code (see pf_convert)
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                uint4* to = reinterpret_cast<uint4*>(dst);
+#pragma unroll 1
+                for (uint32_t q = 0; q < DH; q += 32, to += 4) {
+                    uint32_t o[32];
+                    if (any && ok) {
+                        tc::tmem_ld32(o_at_col + q, o);
+                        tc::tmem_ld_wait_on(o);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = 0u;
+                    }
+                    if (live && ok)
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                w[e] = E::pack(__uint_as_float(o[8 * u + 2 * e]) * inv, __uint_as_float(o[8 * u + 2 * e + 1]) * inv);
+                            to[u] = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                }
+            } else if (whole) {
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 uint32_t o[DH / 32][32];
                 if (any && ok) {
