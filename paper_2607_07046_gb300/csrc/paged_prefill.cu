@@ -941,10 +941,16 @@ __global__ void __launch_bounds__(PfGeom<Src, DH>::kThreads, 1) k_paged_prefill(
                 ++ns;
                 if (!ok) continue;
                 tc::fence_after();
-                // S by 32 keys.  Codes: the block's threads have fewer registers, so of the maximum's pass only the first 64 keys stay,
-                // and the others are read again while the weights of these are worked out.
-                constexpr int KEPT = Src::kMx ? 3 : 4;
+                // S by 32 keys.  Codes: the block's threads have fewer registers and more code, so S is read in halves, once for
+                // the maximum and once for the weights, both in loops.
+                constexpr int KEPT = Src::kMx ? 2 : 4;
                 uint32_t sv[KEPT][32];
+                auto half_of_s = [&](int q) {
+                    tc::tmem_ld32(s_at_col + 64 * q, sv[0]);
+                    tc::tmem_ld32(s_at_col + 64 * q + 32, sv[1]);
+                    tc::tmem_ld_wait_on(sv[0]);
+                    tc::tmem_ld_wait_on(sv[1]);
+                };
                 if constexpr (!Src::kMx)
 #pragma unroll
                     for (int q = 0; q < KEPT; ++q) tc::tmem_ld32(s_at_col + 32 * q, sv[q]);
@@ -968,28 +974,32 @@ __global__ void __launch_bounds__(PfGeom<Src, DH>::kThreads, 1) k_paged_prefill(
                         }
                         tc::tmem_st_wait();
                     }
-#pragma unroll
-                    for (int q = 0; q < KEPT; ++q) tc::tmem_ld32(s_at_col + 32 * q, sv[q]);
                 }
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 auto arrived = [&](uint32_t(&v)[32], int q) {  // keys 32 q ..
                     tc::tmem_ld_wait_on(v);
-                    if (!Src::kMx && !plain)
+                    if (!plain)
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
                             if (!((mw[q] >> e) & 1u)) v[e] = 0xff800000u;  // -inf
                 };
+                if constexpr (!Src::kMx) {
 #pragma unroll
-                for (int q = 0; q < KEPT; ++q) arrived(sv[q], q);
+                    for (int q = 0; q < KEPT; ++q) arrived(sv[q], q);
 #pragma unroll
-                for (int e = 0; e < 32; e += 2)
+                    for (int e = 0; e < 32; e += 2)
 #pragma unroll
-                    for (int q = 0; q < KEPT; ++q) mx[q] = fa_max3(mx[q], __uint_as_float(sv[q][e]), __uint_as_float(sv[q][e + 1]));
-                if constexpr (Src::kMx) {
-                    tc::tmem_ld32(s_at_col + 96, sv[2]);
-                    arrived(sv[2], 3);
+                        for (int q = 0; q < KEPT; ++q) mx[q] = fa_max3(mx[q], __uint_as_float(sv[q][e]), __uint_as_float(sv[q][e + 1]));
+                } else {
+#pragma unroll 1
+                    for (int q = 0; q < 2; ++q) {
+                        half_of_s(q);
 #pragma unroll
-                    for (int e = 0; e < 32; e += 2) mx[3] = fa_max3(mx[3], __uint_as_float(sv[2][e]), __uint_as_float(sv[2][e + 1]));
+                        for (int e = 0; e < 32; e += 4)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                mx[k] = fa_max3(mx[k], __uint_as_float(sv[k & 1][e + (k & 2)]), __uint_as_float(sv[k & 1][e + (k & 2) + 1]));
+                    }
                 }
                 const float pm = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                 const float bms = pm == -INFINITY ? pm : pm * sl2;
@@ -1022,19 +1032,13 @@ __global__ void __launch_bounds__(PfGeom<Src, DH>::kThreads, 1) k_paged_prefill(
                 const float nm = m_use == -INFINITY ? 0.f : -m_use;
                 const uint64_t sl2x2 = f2_pack(sl2, sl2), nmx2 = f2_pack(nm, nm);
                 uint64_t ls[2] = {0ull, 0ull};
-                if constexpr (Src::kMx) tc::tmem_ld32(s_at_col + 64, sv[2]);
-#pragma unroll
+#pragma unroll(Src::kMx ? 1 : 2)
                 for (int q = 0; q < 2; ++q) {
-                    if constexpr (Src::kMx)
-                        if (q == 1) {
-                            tc::tmem_ld32(s_at_col + 96, sv[1]);
-                            arrived(sv[2], 2);
-                            arrived(sv[1], 3);
-                        }
+                    if constexpr (Src::kMx) half_of_s(q);
                     uint32_t w[32];
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
-                        const uint32_t* s2 = &sv[Src::kMx && q == 1 ? 2 - (e >> 4) : 2 * q + (e >> 4)][2 * (e & 15)];
+                        const uint32_t* s2 = &sv[Src::kMx ? e >> 4 : 2 * q + (e >> 4)][2 * (e & 15)];
                         float p0, p1;
                         f2_unpack(f2_fma(f2_pack(__uint_as_float(s2[0]), __uint_as_float(s2[1])), sl2x2, nmx2), p0, p1);
                         p0 = fa_ex2(p0);
@@ -1121,7 +1125,19 @@ __global__ void __launch_bounds__(PfGeom<Src, DH>::kThreads, 1) k_paged_prefill(
                 const int first = (int)paged_div(u0, per), last = (int)paged_div(u0 + at.n - 1, per);
                 float* part = pf_slot(a, (int)blockIdx.x, first, x);
                 reinterpret_cast<float2*>(part)[row] = ok ? make_float2(m_use, l) : make_float2(-INFINITY, 0.f);
-                if (any && ok) {
+                if (Src::kMx && any && ok) {
+#pragma unroll 1
+                    for (int q = 0; q < DH / 32; ++q) {
+                        uint32_t o[32];
+                        tc::tmem_ld32(o_at_col + 32 * q, o);
+                        tc::tmem_ld_wait_on(o);
+                        if (live)
+#pragma unroll
+                            for (int u = 0; u < 8; ++u)
+                                reinterpret_cast<uint4*>(part + 2 * kPfRows)[(8 * q + u) * kPfRows + row] =
+                                    make_uint4(o[4 * u], o[4 * u + 1], o[4 * u + 2], o[4 * u + 3]);
+                    }
+                } else if (any && ok) {
                     uint32_t o[DH / 32][32];
 #pragma unroll
                     for (int q = 0; q < DH / 32; ++q) tc::tmem_ld32(o_at_col + 32 * q, o[q]);
