@@ -18,6 +18,11 @@ namespace vt {
 // for values, 16 dimensions side by side.  A pass of a warp covers 32 / (dh / 16) heads of one row.  A warp has queries or
 // keys and values only: the gains times the rotation's cosines and sines, four numbers a pair, are worked out once and serve
 // all its passes.
+//
+// What bounds it: for prompts bytes (as for the plain append), and behind them the registers: 16 warps an SM have 64 KB of
+// loads on their way.  7 prompts of 300 to 2500 rows, 32 query and 8 KV heads of 128, with norms and full rotation: 36.2 us, 5120
+// GB/s (16 bits) and 36.9 us (e4m3); without either 32.  With a lane for 8 dimensions and the pairs' other halves by
+// shuffles it took 50 and 53.  For single tokens the chain starts, lengths, table, rotation.
 constexpr int kQkWarps = 8;
 
 // One row's queries, or its keys and values, from head `at` (of this lane) on: `batches` times PASSES passes.

@@ -875,15 +875,17 @@ def make_qk_form(rope=None, neighbours: bool = False, q_gain=None, k_gain=None, 
     if rope is not None and (rope.dim() != 3 or rope.shape[2] != 2):
         raise ValueError("expected rope [positions, rotary dim / 2, 2]")
     gains = [g for g in (q_gain, k_gain) if g is not None]
-    if any(g.dim() != 1 or g.dtype not in (torch.float16, torch.bfloat16) for g in gains):
-        raise ValueError("expected gains [head dim] of float16 or bfloat16")
+    if any(len(g.shape) != 1 or g.shape != gains[0].shape or g.dtype is not gains[0].dtype for g in gains) or (
+            gains and gains[0].dtype not in (torch.float16, torch.bfloat16)):
+        raise ValueError("expected gains [head dim] of one type, float16 or bfloat16")
     tensors = [t for t in (rope, *gains) if t is not None]
     if any(t.get_device() != tensors[0].get_device() for t in tensors):
         raise ValueError("rope and gains need one device")
     f = vt_qk_form(*(None if g is None else _ptr(g, g.dtype) for g in (q_gain, k_gain)),
                    None if rope is None else _ptr(rope, torch.float32), 0 if rope is None else rope.shape[0],
                    0 if rope is None else 2 * rope.shape[1], VT_ROPE_NEIGHBOURS if neighbours else VT_ROPE_HALVES, float(eps))
-    f.tensors, f.gains, f.device = (rope, q_gain, k_gain), gains, tensors[0].get_device() if tensors else None
+    f.tensors, f.device = (rope, q_gain, k_gain), tensors[0].get_device() if tensors else None
+    f.gains = (gains[0].shape[0], gains[0].dtype) if gains else None
     return f
 
 
@@ -891,9 +893,9 @@ def _append_qk(call: str, paged, pool, batch, q, k, v, form, q_out, stream) -> N
     n, heads = q.shape[0], q.shape[1]
     if k.shape[0] != n or v.shape[0] != n or q_out.shape[0] != n:
         raise ValueError("q, k, v and q_out need one number of rows")
-    if form.device not in (None, pool.device):
+    if form.device is not None and form.device != pool.device:
         raise ValueError("the form's tensors lie on another device than the pool")
-    if any(tuple(g.shape) != (pool.d_head,) or g.dtype is not pool.torch_dtype for g in form.gains):
+    if form.gains is not None and form.gains != (pool.d_head, pool.torch_dtype):
         raise ValueError(f"expected gains [{pool.d_head}] of {pool.torch_dtype}")
     _same_device(pool, batch)
     (qp, ql), (kp, kl), (vp, vl), (op, ol) = (_rows(q, pool), _rows(k, pool, pool.n_kv_heads),

@@ -347,3 +347,141 @@ def test_two_workspaces_on_two_streams(vtlib):
     for g in gs:
         assert vt.vt_paged_status(g) == 0
         vt.vt_paged_destroy(g)
+
+
+def spread(vt, c, pos=16, head=48, page=112, scale_head=16, scale_page=64):
+    """The cache's pool again, its entries, heads and pages further apart; what lies between is 0x7f and 255."""
+    out = []
+    n, K, P, d = c.codes[0].shape
+    for t in c.codes:
+        ps, hs = d + pos, P * (d + pos) + head
+        base = torch.full((n * (K * hs + page),), 0x7f, dtype=torch.uint8, device="cuda")
+        s = base.as_strided((n, K, P, d), (K * hs + page, hs, ps, 1))
+        s.copy_(t.view(torch.uint8))
+        out.append(s.view(t.dtype))
+    for t in c.scales:
+        nb = t.shape[3]
+        hs = P * nb + scale_head
+        base = torch.full((n * (K * hs + scale_page),), 255, dtype=torch.uint8, device="cuda")
+        s = base.as_strided(t.shape, (K * hs + scale_page, hs, nb, 1))
+        s.copy_(t)
+        out.append(s)
+    return vt.make_paged_mx_pool(*out, TYPE[c.dtype])
+
+
+@pytest.mark.parametrize("dtype,code", KINDS)
+@pytest.mark.parametrize("d_head,page", [(128, 16), (64, 64), (128, 8), (64, 256)])
+def test_pools_with_gaps(vtlib, paged, dtype, code, d_head, page):
+    vt = vtlib
+    for call, lens, rows, heads in (("decode", LENS, [1] * len(LENS), 6), ("prefill", [2000, 0, 700], [300, 513, 40], 48)):
+        c = MxCache(vt, lens, rows, code, dtype, 3 if call == "decode" else 12, d_head, page)
+        q = c.rows(heads)
+        want, out = torch.empty_like(q), torch.empty_like(q)
+        attend(vt, paged, c, call, q, want)
+        c.pool = spread(vt, c)
+        attend(vt, paged, c, call, q, out)
+        assert torch.equal(out.view(torch.int16), want.view(torch.int16))
+        ref, tol = attention(c, q, d_head ** -0.5, 0)
+        tol = tol + TINY[dtype] + 2.0 ** -36 * c.k.shape[0] * page * c.v.masked_fill(c.v.isnan(), 0.0).double().abs().max()
+        assert ((out.double() - ref).abs() <= tol).all()
+        assert vt.vt_paged_status(paged) == 0
+
+
+def test_tiles_with_offsets_past_32_bits(vtlib, paged):
+    """Pages far apart, and enough rows for the tiles' kernel: the same bits as from pages side by side."""
+    vt, stride = vtlib, 2 ** 27 + 16
+    c = MxCache(vt, [70, 3], [300, 40], "e4m3", "f16", 1, 128, 16, spare=0)
+    n = c.k.shape[0]
+    assert (n - 1) * stride > 2 ** 31
+    far = []
+    for t, entry in zip(c.codes + c.scales, (128, 128, 4, 4)):
+        base = torch.full(((n - 1) * stride + 16 * 128,), 127, dtype=torch.uint8, device="cuda")
+        s = base.as_strided((n, 1, 16, entry), (stride, 16 * entry, entry, 1))
+        s.copy_(t.view(torch.uint8))
+        far.append(s)
+    q = c.rows(16)
+    want, out = torch.empty_like(q), torch.empty_like(q)
+    attend(vt, paged, c, "prefill", q, want)
+    plain = torch.empty_like(q)
+    vt.vt_paged_prefill(paged, c.plain, c.batch(vt), q, plain)
+    assert torch.equal(want.view(torch.int16), plain.view(torch.int16))  # the tiles' kernel took it
+    c.pool = vt.make_paged_mx_pool(far[0].view(torch.float8_e4m3fn), far[1].view(torch.float8_e4m3fn), far[2], far[3], torch.float16)
+    attend(vt, paged, c, "prefill", q, out)
+    assert torch.equal(out.view(torch.int16), want.view(torch.int16))
+
+
+@pytest.mark.parametrize("d_head", [64, 128])
+def test_as_many_sequences_as_a_batch_takes(vtlib, paged, d_head):
+    """16384 slots of one position and more, most of them idle or without rows: one batch through all three calls."""
+    vt, n = vtlib, 16384
+    lens = [(i * 37) % 20 if i % 61 == 0 else -1 for i in range(n)]
+    for rows in ([1] * n, [3 if i % 61 == 0 else 0 for i in range(n)]):
+        c = MxCache(vt, lens, rows, "int8", "bf16", 1, d_head, 8)
+        q = c.rows(2)
+        out = torch.full_like(q, 7.0)
+        one = rows[1] == 1
+        attend(vt, paged, c, "decode" if one else "prefill", q, out)
+        live = [b for b in range(n) if lens[b] >= 0]
+        for b in live[::20] + live[-1:]:
+            s0, r, p = c.starts_host[b], rows[b], lens[b]
+            page, off = c.positions(b, p + r)
+            k, v = (t[page, 0, off].double() for t in (c.k, c.v))
+            hide = torch.arange(p + r, device="cuda") > torch.arange(p, p + r, device="cuda")[:, None]
+            for h in range(2):
+                w = torch.softmax((q[s0:s0 + r, h].double() @ k.T * d_head ** -0.5).masked_fill(hide, -math.inf), -1)
+                o, a = w @ v, w @ v.abs()
+                assert ((out[s0:s0 + r, h].double() - o).abs() <= U["bf16"] * o.abs() + (U["bf16"] + 2.0 ** -16) * a + 2.0 ** -30).all()
+        idle = torch.tensor([c.starts_host[b] for b in range(n) if lens[b] < 0 and rows[b]][::50], dtype=torch.long, device="cuda")
+        assert not out[idle].any() and vt.vt_paged_status(paged) == 0
+
+
+@pytest.mark.parametrize("code", ["e4m3", "int8"])
+def test_captured_prefill_at_other_lengths(vtlib, paged, code):
+    """One capture of append and prefill, replayed with other lengths, tables and row starts than it was captured with."""
+    vt, H, K, d = vtlib, 8, 2, 128
+    caches = [MxCache(vt, lens, rows, code, "bf16", K, d, 16, seed=i) for i, (lens, rows) in enumerate((
+        ([200, 0, 33], [100, 300, 7]), ([0, 900, -1], [7, 250, 150]), ([31, 64, 500], [1, 405, 1])))]
+    most = max(c.codes[0].shape[0] for c in caches)
+    per = max(c.tables.shape[1] for c in caches)
+    codes = [torch.zeros(most, K, 16, d, dtype=torch.uint8, device="cuda").view(mx.CODES[code]) for _ in range(2)]
+    scales = [torch.full((most, K, 16, d // 32), 255, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    pool = vt.make_paged_mx_pool(*codes, *scales, torch.bfloat16)
+    tables = torch.full((3, per), -1, dtype=torch.int32, device="cuda")
+    lens, starts = torch.full((3,), -1, dtype=torch.int32, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    x = torch.zeros(407, H + 2 * K, d, dtype=torch.bfloat16, device="cuda")
+    q, out = torch.zeros_like(x[:, :H]), torch.zeros_like(x[:, :H])
+    form = vt.make_qk_form(table(per * 16, 128))
+    batch = vt.make_paged_batch(tables, lens, starts)
+
+    def calls():
+        vt.vt_paged_append_mx(paged, pool, batch, x[:, :H], x[:, H:H + K], x[:, H + K:], form, q)
+        vt.vt_paged_prefill_mx(paged, pool, batch, q, out)
+
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        calls()
+    for c in caches:
+        with torch.cuda.stream(side):
+            n = c.codes[0].shape[0]
+            for dst, src in zip(codes + scales, c.codes + c.scales):
+                dst.view(torch.uint8)[:n] = src.view(torch.uint8)
+            tables.fill_(-1)
+            tables[:, :c.tables.shape[1]] = c.tables
+            lens.copy_(c.lens)
+            starts.copy_(c.starts)
+            x.normal_(generator=c.gen)
+            out.fill_(7.0)
+            graph.replay()
+        side.synchronize()
+        got, gq, pools = out.clone(), q.clone(), [t.clone() for t in codes + scales]
+        calls()  # the same, not captured
+        torch.cuda.synchronize()
+        assert torch.equal(got, out) and torch.equal(gq, q)
+        assert all(torch.equal(s.view(torch.uint8), t.view(torch.uint8)) for s, t in zip(pools, codes + scales))
+        for i, t in enumerate((c.k, c.v)):
+            t.copy_(mx.decode(codes[i][:n], scales[i][:n]).masked_fill(~c.live[:, None, :, None], float("nan")))
+        ref, tol = attention(c, q[:c.n_rows], d ** -0.5, 0)
+        assert ((out[:c.n_rows].double() - ref).abs() <= tol + 2.0 ** -30).all() and (out[c.n_rows:] == 7.0).all()
+        assert vt.vt_paged_status(paged) == 0
