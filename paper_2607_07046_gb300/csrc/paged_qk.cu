@@ -16,18 +16,19 @@ namespace vt {
 // dh / 16 lanes hold a head, two chunks of 8 dimensions each (two 16-byte loads): for pairs of halves those that are paired,
 // so that no value goes from lane to lane but the sum of squares, and the unrotated ones side by side; for neighbours, and
 // for values, 16 dimensions side by side.  A pass of a warp covers 32 / (dh / 16) heads of one row.  A warp has queries or
-// keys and values only: the gains times the rotation's cosines and sines, four numbers a pair, are worked out once and serve
-// all its passes.
+// keys and values only: the gains times the rotation's cosines and sines, four numbers a pair, are worked out once, lie in
+// shared memory and serve all its passes.
 //
-// What bounds it: for prompts bytes (as for the plain append), and behind them the registers: 16 warps an SM have 64 KB of
-// loads on their way.  7 prompts of 300 to 2500 rows, 32 query and 8 KV heads of 128, with norms and full rotation: 36.2 us, 5120
-// GB/s (16 bits) and 36.9 us (e4m3); without either 32.  With a lane for 8 dimensions and the pairs' other halves by
-// shuffles it took 50 and 53.  For single tokens the chain starts, lengths, table, rotation.
-constexpr int kQkWarps = 8;
+// What bounds it: for prompts bytes (as for the plain append), and behind them the registers, which leave 24 warps an SM.  7
+// prompts of 300 to 2500 rows, 32 query and 8 KV heads of 128, with norms and full rotation: 35.3 us, 5250 GB/s (16 bits) and
+// 35.3 us (e4m3); without either 32.  With a lane for 8 dimensions and the pairs' other halves by shuffles it took 50 and 53,
+// with the four numbers in registers and 16 warps 36.8 and 37.1.  For single tokens the chain starts, lengths, table,
+// rotation.
+constexpr int kQkWarps = 8, kQkCtas = 3;
 
 // One row's queries, or its keys and values, from head `at` (of this lane) on: `batches` times PASSES passes.
 template <class T, int DH, int F, bool NEIGH, int PASSES, bool OF_Q>
-__device__ __forceinline__ void qk_heads(const PagedQkArgs& a, int row, int at, int batches) {
+__device__ __forceinline__ void qk_heads(const PagedQkArgs& a, ulonglong2 (*coef)[DH / 16], int row, int at, int batches) {
     constexpr int LPH = DH / 16, HPW = 32 / LPH, NB = DH / kMxBlock;
     constexpr bool MX = F >= 0 && !OF_Q;
     using E = Elem<T>;
@@ -93,9 +94,8 @@ __device__ __forceinline__ void qk_heads(const PagedQkArgs& a, int row, int at, 
     // pair e of the lane is values first(e) and second(e) of its 16; two pairs go through an instruction
     auto first = [](int e) { return NEIGH ? 2 * e : e; };
     auto second = [](int e) { return NEIGH ? 2 * e + 1 : 8 + e; };
-    // a' = a ca - b sb, b' = b cb + a sa, with the gains; msb = -sb
-    uint64_t ca[4], sa[4], cb[4], msb[4];
-    {
+    // a' = a ca - b sb, b' = b cb + a sa, with the gains: (ca, -sb) and (cb, sa) of two pairs, which the heads of the warp share
+    if (lane < LPH) {
         const uint16_t* gain = OF_Q ? a.q_gain : a.k_gain;
         float g[16];
         if (gain) {
@@ -109,11 +109,11 @@ __device__ __forceinline__ void qk_heads(const PagedQkArgs& a, int row, int at, 
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
             const float4 f = turns ? t[e / 2] : make_float4(1.f, 0.f, 1.f, 0.f);
-            ca[e / 2] = f2_pack(g[first(e)] * f.x, g[first(e + 1)] * f.z), sa[e / 2] = f2_pack(g[first(e)] * f.y, g[first(e + 1)] * f.w);
-            cb[e / 2] = f2_pack(g[second(e)] * f.x, g[second(e + 1)] * f.z);
-            msb[e / 2] = f2_pack(-g[second(e)] * f.y, -g[second(e + 1)] * f.w);
+            coef[e][s] = {f2_pack(g[first(e)] * f.x, g[first(e + 1)] * f.z), f2_pack(-g[second(e)] * f.y, -g[second(e + 1)] * f.w)};
+            coef[e + 1][s] = {f2_pack(g[second(e)] * f.x, g[second(e + 1)] * f.z), f2_pack(g[first(e)] * f.y, g[first(e + 1)] * f.w)};
         }
     }
+    __syncwarp();
     const bool norm = OF_Q ? a.q_gain != nullptr : a.k_gain != nullptr;
     for (int h0 = at;;) {
 #pragma unroll
@@ -141,8 +141,9 @@ __device__ __forceinline__ void qk_heads(const PagedQkArgs& a, int row, int at, 
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
                     const uint64_t p = f2_mul(f2_pack(y[first(e)], y[first(e + 1)]), inv2), r = f2_mul(f2_pack(y[second(e)], y[second(e + 1)]), inv2);
-                    uint64_t pp = f2_mul(p, ca[e / 2]), rr = f2_mul(r, cb[e / 2]);
-                    if (turns) pp = f2_fma(r, msb[e / 2], pp), rr = f2_fma(p, sa[e / 2], rr);
+                    const ulonglong2 of_a = coef[e][s], of_b = coef[e + 1][s];
+                    uint64_t pp = f2_mul(p, of_a.x), rr = f2_mul(r, of_b.x);
+                    if (turns) pp = f2_fma(r, of_a.y, pp), rr = f2_fma(p, of_b.y, rr);
                     f2_unpack(pp, y[first(e)], y[first(e + 1)]);
                     f2_unpack(rr, y[second(e)], y[second(e + 1)]);
                 }
@@ -216,8 +217,9 @@ __device__ __forceinline__ void qk_heads(const PagedQkArgs& a, int row, int at, 
 
 // A row's warps: its queries', then its keys' and values', of `batches` times PASSES passes each at most.
 template <class T, int DH, int F, bool NEIGH, int PASSES>
-__global__ void __launch_bounds__(kQkWarps * 32, 2) k_paged_append_qk(const __grid_constant__ PagedQkArgs a) {
+__global__ void __launch_bounds__(kQkWarps * 32, kQkCtas) k_paged_append_qk(const __grid_constant__ PagedQkArgs a) {
     constexpr int HPW = 32 / (DH / 16), HPB = HPW * PASSES;  // heads of a batch
+    __shared__ ulonglong2 coef[kQkWarps][8][DH / 16];
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31;
@@ -228,17 +230,17 @@ __global__ void __launch_bounds__(kQkWarps * 32, 2) k_paged_append_qk(const __gr
     const int w = (int)(gw - (int64_t)row * (q_warps + kv_warps)), sub = lane / (DH / 16);
     if (w < q_warps) {
         const int from = w * HPB * a.batches;
-        qk_heads<T, DH, F, NEIGH, PASSES, true>(a, row, from + sub, min(a.batches, (a.n_heads - from + HPB - 1) / HPB));
+        qk_heads<T, DH, F, NEIGH, PASSES, true>(a, coef[threadIdx.x >> 5], row, from + sub, min(a.batches, (a.n_heads - from + HPB - 1) / HPB));
     } else {
         const int from = (w - q_warps) * HPB * a.batches;
-        qk_heads<T, DH, F, NEIGH, PASSES, false>(a, row, from + sub, min(a.batches, (2 * a.c.n_kv_heads - from + HPB - 1) / HPB));
+        qk_heads<T, DH, F, NEIGH, PASSES, false>(a, coef[threadIdx.x >> 5], row, from + sub, min(a.batches, (2 * a.c.n_kv_heads - from + HPB - 1) / HPB));
     }
 }
 
 // Few rows: a warp a pass, so that all loads are in flight at once.  Many: several passes a warp share the rotation,
-// the gains and the search for the sequence.  (7 prompts of 300 to 2500 rows, 32 query and 8 KV heads of 128, 16 bits: 4 passes twice
-// 36.8 us, 4 once 40, 2 four times 38 to 41, 1 eight times 40; 3 CTAs an SM instead of 2 cost registers and 1 to 3 us, as did
-// loading the next passes ahead.)
+// the gains and the search for the sequence.  (The prompts above, 16 bits and e4m3: 4 passes twice
+// 35.3 and 35.3 us, 4 once 35.4 and 39.2, 3 three times 37.1 and 37.3; 2 passes and 4 CTAs an SM 34.1 and 36.4 twice, 37.6 and 36.5
+// four times; 2 CTAs 38.)
 constexpr int kQkPasses = 4, kQkBatches = 2, kQkManyRows = 512;
 
 template <class T, int DH, int F, bool NEIGH, int PASSES>
