@@ -511,7 +511,8 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
                             const float2 v = E::unpack(q[k][e + x]);
                             q[k][e + x] = Elem<__half>::pack(v.x * f, v.y * f);
                         }
-                    if (x < NT) qs[x] = a.scale_log2 * __uint_as_float((uint32_t)(127 - up) << 23);
+                    // (not infinite: its product with a score of 0 is 0)
+                    if (x < NT) qs[x] = fminf(a.scale_log2 * __uint_as_float((uint32_t)(127 - up) << 23), 3.4028235e38f);
                 }
             }
             if (x < NT) last_key[x] = ROWS ? at.s.len + (c0 + g + 8 * x) / a.group : 0;

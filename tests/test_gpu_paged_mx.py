@@ -485,3 +485,20 @@ def test_captured_prefill_at_other_lengths(vtlib, paged, code):
         ref, tol = attention(c, q[:c.n_rows], d ** -0.5, 0)
         assert ((out[:c.n_rows].double() - ref).abs() <= tol + 2.0 ** -30).all() and (out[c.n_rows:] == 7.0).all()
         assert vt.vt_paged_status(paged) == 0
+
+
+@pytest.mark.parametrize("call", ["decode", "prefill"])
+@pytest.mark.parametrize("dtype,code", KINDS)
+def test_largest_scale_and_scores_of_zero(vtlib, paged, call, dtype, code):
+    """Keys of zeros, and large queries: every score is 0 whatever the scale, and the output the mean of the values."""
+    vt = vtlib
+    c = MxCache(vt, [40, 3], [1, 1] if call == "decode" else [5, 90], code, dtype, 1, 64, 16)
+    live = c.live[:, None, :, None]
+    c.codes[0].view(torch.uint8).masked_fill_(live, 0)
+    c.k.masked_fill_(live, 0.0)
+    q = c.rows(4).mul_(2.0 ** 13 if dtype == "f16" else 2.0 ** 40)
+    for scale in (0.0, 1.0, 3.4028234663852886e38):
+        out = torch.empty_like(q)
+        attend(vt, paged, c, call, q, out, scale)
+        ref, tol = attention(c, torch.zeros_like(q), 1.0, 0)
+        assert ((out.double() - ref).abs() <= tol + TINY[dtype]).all()
