@@ -134,18 +134,20 @@ __device__ __forceinline__ void qk_heads(const PagedQkArgs& a, ulonglong2 (*coef
                 ss += s1;
 #pragma unroll
                 for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-                inv = rsqrtf(fmaf(ss, 1.f / DH, a.eps));
+                const float ms = fmaf(ss, 1.f / DH, a.eps), r = rsqrtf(ms);
+                // one step of Newton's method: what the root is off by, all of the head's values are, next to borders of codes too
+                inv = ms < INFINITY ? fmaf(0.5f * r, fmaf(-ms * r, r, 1.f), r) : r;
             }
             if (formed) {
                 const uint64_t inv2 = f2_pack(inv, inv);
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const uint64_t p = f2_mul(f2_pack(y[first(e)], y[first(e + 1)]), inv2), r = f2_mul(f2_pack(y[second(e)], y[second(e + 1)]), inv2);
+                for (int e = 0; e < 8; e += 2) {  // (the root's inverse last: of products of a 16-bit value fewer are rounded)
+                    const uint64_t p = f2_pack(y[first(e)], y[first(e + 1)]), r = f2_pack(y[second(e)], y[second(e + 1)]);
                     const ulonglong2 of_a = coef[e][s], of_b = coef[e + 1][s];
                     uint64_t pp = f2_mul(p, of_a.x), rr = f2_mul(r, of_b.x);
                     if (turns) pp = f2_fma(r, of_a.y, pp), rr = f2_fma(p, of_b.y, rr);
-                    f2_unpack(pp, y[first(e)], y[first(e + 1)]);
-                    f2_unpack(rr, y[second(e)], y[second(e + 1)]);
+                    f2_unpack(f2_mul(pp, inv2), y[first(e)], y[first(e + 1)]);
+                    f2_unpack(f2_mul(rr, inv2), y[second(e)], y[second(e + 1)]);
                 }
             }
             if constexpr (!MX) {
