@@ -716,12 +716,14 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
                         for (int x = 0; x < NT; ++x)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
+                                const uint64_t w = f2_mul(f2_pack(pw[x][4 * n + 2 * e], pw[x][4 * n + 2 * e + 1]), f2[e]);
                                 float w0, w1;
-                                f2_unpack(f2_mul(f2_pack(pw[x][4 * n + 2 * e], pw[x][4 * n + 2 * e + 1]), f2[e]), w0, w1);
+                                f2_unpack(w, w0, w1);
                                 hi[x][e] = H::pack(w0, w1);
                                 if constexpr (TWO) {
                                     const float2 h = H::unpack(hi[x][e]);
-                                    lo[x][e] = H::pack(w0 - h.x, w1 - h.y);
+                                    f2_unpack(f2_fma(f2_pack(h.x, h.y), f2_pack(-1.f, -1.f), w), w0, w1);
+                                    lo[x][e] = H::pack(w0, w1);
                                 }
                             }
                         const int r = 16 * n + mr;
