@@ -734,9 +734,8 @@ VT_API vt_status vt_paged_append_mx(vt_paged* paged, const vt_paged_mx_pool* poo
 /* vt_paged_decode_mx, vt_paged_prefill_mx (Section 2.1, decode and prefill phases): as vt_paged_decode and
  * vt_paged_prefill, over a pool in 8 bits.  K and V are the values that the entries stand for, exactly.
  * Weights of single tokens, and of a sequence's few rows, meet the codes in fp16 with the scale of their
- * value (fp16 rows: as two terms; bf16 rows: one, half an fp16 step), and lose at most 2^-37 of the
- * row's largest weight times twice the largest value that it attends to; with more rows they are rounded
- * to the rows' type as over a pool in 16 bits. */
+ * value, as two terms (22 bits), and lose at most 2^-37 of the row's largest weight times twice the largest
+ * value that it attends to; with more rows they are rounded to the rows' type as over a pool in 16 bits. */
 VT_API vt_status vt_paged_decode_mx(vt_paged* paged, const vt_paged_mx_pool* pool, const vt_paged_batch* batch,
                                     int32_t n_heads, const void* q, int64_t q_ld, float scale, int32_t window,
                                     void* out, int64_t out_ld, vt_stream stream);

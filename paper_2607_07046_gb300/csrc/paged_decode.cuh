@@ -28,9 +28,9 @@
 //   S = sum_b scale_K[key][b] (Q_b . codes_b)     a sum for each 32 dimensions b, multiplied and added in fp32
 //   O_b += (P scale_V[.][b] / unit) . codes_b     weights for each b; unit: the largest scale of V so far, by which O
 //                                                 is rescaled when it grows
-// bf16 queries become fp16 times a power of two of their row.  The weights have two terms for fp16 rows and one for bf16
-// rows, whose own step is eight times an fp16 step.  m moves only when P would pass 2^15, down to 2^12, so that a weight loses
-// at most 2^-37 of the largest one, times the largest value.  What it costs beside the 16-bit pool's kernel are the
+// bf16 queries become fp16 times a power of two of their row.  Weights have two terms, 22 bits (one, for bf16 rows, left outputs
+// 9e-4 of their size off beside their own rounding, two 7e-5, for 1 us of 55 on the long history below).  m moves only when P would
+// pass 2^15, down to 2^12, so that a weight loses at most 2^-37 of the largest one, times the largest value.  What it costs beside the 16-bit pool's kernel are the
 // conversions: 350 instructions a 16 positions and warp, which fit beside the copies at the memory's rate.
 //
 // Measured: one history of 131,000 positions, 8 KV heads of 4, dh 128: 92 us, 5830 GB/s (86% of a copy's rate: the
@@ -208,7 +208,6 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
     using T = typename Src::T;
     using E = Elem<T>;
     using G = PdGeom<Src, DH, NT>;
-    constexpr bool TWO = std::is_same<T, __half>::value;  // codes: weights in two terms
     constexpr uint32_t FULL = G::kKeys == 32 ? 0xffffffffu : 0xffffu;
     constexpr int KEYS = G::kKeys, NB = DH / kMxBlock;
     constexpr int S = G::kStages, CPR = G::kRow / 16, RPI = 32 / CPR;
@@ -720,11 +719,9 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
                                 float w0, w1;
                                 f2_unpack(w, w0, w1);
                                 hi[x][e] = H::pack(w0, w1);
-                                if constexpr (TWO) {
-                                    const float2 h = H::unpack(hi[x][e]);
-                                    f2_unpack(f2_fma(f2_pack(h.x, h.y), f2_pack(-1.f, -1.f), w), w0, w1);
-                                    lo[x][e] = H::pack(w0, w1);
-                                }
+                                const float2 h = H::unpack(hi[x][e]);
+                                f2_unpack(f2_fma(f2_pack(h.x, h.y), f2_pack(-1.f, -1.f), w), w0, w1);
+                                lo[x][e] = H::pack(w0, w1);
                             }
                         const int r = 16 * n + mr;
                         uint32_t w[4];
@@ -737,7 +734,7 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
 #pragma unroll
                             for (int x = 0; x < NT; ++x) {
                                 mma16816<__half>(o[2 * b + y][x], vt, hi[x][0], hi[x][1]);
-                                if constexpr (TWO) mma16816<__half>(o[2 * b + y][x], vt, lo[x][0], lo[x][1]);
+                                mma16816<__half>(o[2 * b + y][x], vt, lo[x][0], lo[x][1]);
                             }
                         }
                     }
