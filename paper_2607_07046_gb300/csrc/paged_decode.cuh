@@ -26,12 +26,15 @@
 // Over a pool of codes (paged_mx.cuh) a step has 32 positions, about as many bytes, and both products are of fp16, whatever
 // the rows' type: a code is an fp16 number, and the scales of 32 dimensions stay outside,
 //   S = sum_b scale_K[key][b] (Q_b . codes_b)     a sum for each 32 dimensions b, multiplied and added in fp32
-//   O_b += (P scale_V[.][b] / unit) . codes_b     weights for each b; unit: the largest scale of V so far, by which O
-//                                                 is rescaled when it grows
+//   O_b += (P scale_V[.][b] / unit) . codes_b     weights for each b; unit: the largest scale of V that the column has
+//                                                 attended to, by which O is rescaled when it grows
+// Columns of one row share the unit.  Of several rows each has its own: what a column does not attend to, such as the new rows
+// behind its own, may be any powers above the rest and would leave its weights no bits.
 // bf16 queries become fp16 times a power of two of their row.  Weights have two terms, 22 bits (one, for bf16 rows, left outputs
 // 9e-4 of their size off beside their own rounding, two 7e-5, for 1 us of 55 on the long history below).  m moves only when P would
-// pass 2^15, down to 2^12, so that a weight loses at most 2^-37 of the largest one, times the largest value.  What it costs beside the 16-bit pool's kernel are the
-// conversions: 350 instructions a 16 positions and warp, which fit beside the copies at the memory's rate.
+// pass 2^15, down to 2^12, so that a weight loses at most 2^-37 of the largest one, times the largest value.  What it costs beside
+// the 16-bit pool's kernel are the conversions: 350 instructions a 16 positions and warp, which fit beside the copies at the
+// memory's rate.
 //
 // Measured: one history of 131,000 positions, 8 KV heads of 4, dh 128: 92 us, 5830 GB/s (86% of a copy's rate: the
 // start, the last steps and the join of 38 parts a head are the rest); 64 sequences of up to 8191, some idle: 47 us, 5310
@@ -41,6 +44,7 @@
 #pragma once
 
 #include <cuda_runtime.h>
+#include <limits.h>
 #include <math.h>
 
 #include <algorithm>
@@ -56,6 +60,10 @@ constexpr int kPdSoloUnits = 2;              // (see kSoloSteps)
 // Codes: parts that are joined by several threads an item (131,000 positions, 38 parts a head, 57.7 us by one, 54.9 by several;
 // 64 ragged sequences, 2 to 3 parts, 38.3 and 39.8: the longer code comes from far away).
 constexpr int kPdManyParts = 8;
+// Codes: units begin at kPdLeastScale.  Where columns have their own, V's scales are kept times 2^kPdShift and weights over the
+// unit times 2^-kPdShift, so that neither a weight of 2^15 over the least unit nor a scale of 2^119 passes the largest fp32 number.
+constexpr float kPdLeastScale = 0x1p-100f;
+constexpr int kPdShift = 6;
 
 template <class Src, int DH, int NT>
 struct PdGeom {
@@ -123,8 +131,9 @@ __device__ __forceinline__ uint64_t lds1x64(uint32_t addr) {
 __device__ __forceinline__ void lds2x64(uint32_t addr, uint64_t (&v)[2]) {
     asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(v[0]), "=l"(v[1]) : "r"(addr) : "memory");
 }
-// 1 / x of a power of two.
+// 1 / x of a power of two; 2^e.
 __device__ __forceinline__ float pd_inverse(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }
+__device__ __forceinline__ constexpr float pd_power(int e) { return e < 0 ? 1.f / (float)(1 << -e) : (float)(1 << e); }
 // 2^x; over codes without the steps that keep results below 2^-126, which are nothing beside weights up to 2^12 and more.
 template <class Src>
 __device__ __forceinline__ float pd_exp2(float x) {
@@ -472,7 +481,11 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
         float qs[NT];  // what a score is multiplied by
 #pragma unroll
         for (int x = 0; x < NT; ++x) qs[x] = a.scale_log2;
-        float unit = 0x1p-100f;  // codes: o counts in this unit, the largest scale of V so far
+        // codes: a column of o counts in the largest scale of V that it has attended to (single tokens: one for all columns);
+        // least: of the warp's columns
+        float unit[NT], least = kPdLeastScale;
+#pragma unroll
+        for (int x = 0; x < NT; ++x) unit[x] = kPdLeastScale;
         int last_key[NT];  // of this lane's columns, in the steps' keys
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -535,6 +548,7 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
             const int lr = ((lane >> 4) << 3) + (lane & 7), lc = (lane >> 3) & 1;  // ldmatrix: row, chunk of a pair
             constexpr int NS = KEYS / 8;
             float s[NS][4] = {};
+            float v_most = 0.f, grown = 1.f;  // codes: the step's largest scale of V, where some column's unit is less
             if constexpr (!Src::kMx) {
 #pragma unroll
                 for (int k = 0; k < DH / 16; ++k) {
@@ -545,7 +559,7 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
                 }
             } else {
                 // The step's scales as floats, [K, V][pair of positions][block][position], each worked out by one lane; those of V
-                // over the unit.
+                // over the unit or, where columns have units of their own, times 2^kPdShift.
                 constexpr int WORDS = 2 * KEYS * NB / 4, PASSES = (WORDS + 31) / 32;  // of 4 bytes; half of them K's
                 float f[PASSES][4];
                 bool odd = false;
@@ -564,7 +578,7 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
                     float most = 0.f;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) most = fmaxf(most, f[j][e] = mx_scale(w, e));
-                    odd |= of_v ? most > unit : most == INFINITY;
+                    odd |= of_v ? most > least : most == INFINITY;
                 }
                 if (__any_sync(0xffffffffu, odd)) {  // (an infinite scale is NaN's: it sets no unit)
                     float most = 0.f;
@@ -575,29 +589,24 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
                             if (f[j][e] == INFINITY) f[j][e] = __int_as_float(0x7fc00000);
                             if ((32 * j + lane) % WORDS >= WORDS / 2) most = fmaxf(most, f[j][e]);
                         }
-                    const float next = fmaxf(unit, __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most))));
-                    const float r = unit * pd_inverse(next);
-                    unit = next;
-#pragma unroll
-                    for (int x = 0; x < NT; ++x)
-#pragma unroll
-                        for (int i = 0; i < DH / 16; ++i)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o[i][x][e] *= r;
+                    v_most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
+                    if (!ROWS && v_most > least) {
+                        grown = least * pd_inverse(v_most);
+                        unit[0] = least = v_most;
+                    }
                 }
-                const float by = pd_inverse(unit);
 #pragma unroll
                 for (int j = 0; j < PASSES; ++j) {
                     const int i = (32 * j + lane) % WORDS, at = i % (WORDS / 2);
                     const bool of_v = i >= WORDS / 2;
-                    const float inv = of_v ? by : 1.f;
+                    const float by = !of_v ? 1.f : ROWS ? pd_power(kPdShift) : pd_inverse(unit[0]);
                     const uint32_t to = fs + (uint32_t)(of_v ? KEYS * NB * 4 : 0);
                     if (NB == 4) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) sts32(to + (uint32_t)((at >> 1) * 32 + e * 8 + (at & 1) * 4), f[j][e] * inv);
+                        for (int e = 0; e < 4; ++e) sts32(to + (uint32_t)((at >> 1) * 32 + e * 8 + (at & 1) * 4), f[j][e] * by);
                     } else {
-                        sts128_at(to + (uint32_t)(at * 16), __float_as_uint(f[j][0] * inv), __float_as_uint(f[j][2] * inv),
-                                  __float_as_uint(f[j][1] * inv), __float_as_uint(f[j][3] * inv));
+                        sts128_at(to + (uint32_t)(at * 16), __float_as_uint(f[j][0] * by), __float_as_uint(f[j][2] * by),
+                                  __float_as_uint(f[j][1] * by), __float_as_uint(f[j][3] * by));
                     }
                 }
                 __syncwarp();
@@ -669,6 +678,49 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
                         const float2 f = E::unpack(hi[x][e]);
                         lo[x][e] = E::pack(p[2 * e] - f.x, p[2 * e + 1] - f.y);
                     }
+                }
+            }
+            if constexpr (Src::kMx && !ROWS) {
+#pragma unroll
+                for (int x = 0; x < NT; ++x) al[x] *= grown;
+                moved |= grown != 1.f;
+            }
+            if constexpr (Src::kMx && ROWS) {
+                if (v_most > least) {
+#pragma unroll
+                    for (int x = 0; x < NT; ++x) {
+                        float most = v_most;
+                        if (partial) {  // of the positions that this lane's column attends to (weights of the others are 0)
+                            most = 0.f;
+#pragma unroll
+                            for (int e = 0; e < NS; ++e)
+#pragma unroll
+                                for (int b = 0; b < NB; ++b) {
+                                    float f0, f1;
+                                    f2_unpack(lds1x64(fs + (uint32_t)(KEYS * NB * 4 + (4 * e + t) * NB * 8 + b * 8)), f0, f1);
+                                    const int key = p0 + 8 * e + 2 * t, first = a.window == 0 ? INT_MIN : last_key[x] - a.window;
+                                    if (key <= last_key[x] && key > first) most = fmaxf(most, f0);
+                                    if (key + 1 <= last_key[x] && key + 1 > first) most = fmaxf(most, f1);
+                                }
+                            most *= pd_power(-kPdShift);
+                            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+                            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+                        }
+                        most = fmaxf(most, unit[x]);
+                        al[x] *= unit[x] * pd_inverse(most);
+                        moved |= most != unit[x];
+                        unit[x] = most;
+                    }
+                    least = unit[0];
+#pragma unroll
+                    for (int x = 1; x < NT; ++x) least = fminf(least, unit[x]);
+                    least = __uint_as_float(__reduce_min_sync(0xffffffffu, __float_as_uint(least)));
+                }
+#pragma unroll
+                for (int x = 0; x < NT; ++x) {
+                    const float by = pd_inverse(unit[x]) * pd_power(-kPdShift);
+#pragma unroll
+                    for (int e = 0; e < 2 * NS; ++e) pw[x][e] *= by;
                 }
             }
             if (__any_sync(0xffffffffu, moved)) {
@@ -744,14 +796,16 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
         }
         skip = k0 - n;
         if constexpr (Src::kMx) {  // in the values' units, of weights up to 1
-            unit *= 0x1p-15f;
 #pragma unroll
             for (int x = 0; x < NT; ++x) {
                 l[x] *= 0x1p-15f;
+                const float own = (ROWS ? unit[x] : unit[0]) * 0x1p-15f;
+                const float u[2] = {ROWS ? __shfl_sync(0xffffffffu, own, 8 * t) : own,
+                                    ROWS ? __shfl_sync(0xffffffffu, own, 8 * t + 4) : own};  // of o's columns
 #pragma unroll
                 for (int i = 0; i < DH / 16; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[i][x][e] *= unit;
+                    for (int e = 0; e < 4; ++e) o[i][x][e] *= u[e & 1];
             }
         }
 

@@ -13,11 +13,29 @@ import math
 import pytest
 
 torch = pytest.importorskip("torch")
+from tests import mx_reference as mx  # noqa: E402
 from tests.test_gpu_paged import TINY, TYPE, U  # noqa: E402
 from tests.test_gpu_paged_mx import KINDS, attend, paged  # noqa: E402,F401
 from tests.test_gpu_paged_qk import MxCache  # noqa: E402
 
 pytestmark = pytest.mark.gpu
+
+
+def set_values(c, side, x):
+    """The live entries of one side (0: K, 1: V) anew, from values [pages, KV heads, positions, head dim]."""
+    live = c.live[:, None, :, None]
+    codes, scales = mx.encode(x.double().masked_fill(~live, 0.0), c.code, c.dtype)
+    values = mx.decode(codes, scales)
+    codes = (codes if c.code == "int8" else codes.float()).to(mx.CODES[c.code]).view(torch.uint8)
+    c.codes[side].view(torch.uint8).copy_(torch.where(live, codes, c.codes[side].view(torch.uint8)))
+    c.scales[side].copy_(torch.where(live, scales, c.scales[side]))
+    (c.k, c.v)[side].copy_(values.masked_fill(~live, float("nan")))
+
+
+def entry(c, b, j):
+    """Index of position j of sequence b in a side of the pool, all KV heads."""
+    page, off = c.positions(b, j + 1)
+    return page[j], slice(None), off[j]
 
 
 def bounded(c, q, scale, window):
@@ -56,6 +74,31 @@ def check(vt, g, c, call, q, window=0, scale=None):
     return out
 
 
+@pytest.mark.parametrize("window", [0, 3])
+@pytest.mark.parametrize("d_head,group,held", [(64, 1, 41), (128, 1, 61), (128, 3, 41), (64, 5, 0), (128, 4, 3000)])
+@pytest.mark.parametrize("dtype,code", KINDS)
+def test_a_row_is_not_disturbed_by_values_that_it_does_not_attend_to(vtlib, paged, dtype, code, d_head, group, held, window):
+    """The values of the last of four new rows, and with a window those of a position that the first row alone attends to, far
+    above the others: rows that attend to neither have the bits that they have without."""
+    vt = vtlib
+    up = 2.0 ** (60 if (dtype, code) == ("bf16", "int8") else 12)
+    low = 2.0 ** (-44 if (dtype, code) == ("bf16", "e4m3") else -4 if dtype == "f16" else 0)
+    c = MxCache(vt, [held, 9], [4, 1], code, dtype, 2, d_head, 16, spare=0)
+    live = c.live[:, None, :, None]
+    v = c.v.double().masked_fill(~live, 0.0) * low
+    set_values(c, 1, v)
+    q = c.rows(2 * group)
+    plain = check(vt, paged, c, "prefill", q, window)
+    v[entry(c, 0, held + 3)] *= up / low
+    first = held - 2
+    if window and first >= 0:
+        v[entry(c, 0, first)] *= up / low
+    set_values(c, 1, v)
+    out = check(vt, paged, c, "prefill", q, window)
+    quiet = slice(1 if window else 0, 3)
+    assert torch.equal(out[quiet].view(torch.int16), plain[quiet].view(torch.int16))
+
+
 @pytest.mark.parametrize("d_head,kv_heads,group,page", [(64, 2, 1, 16), (128, 2, 4, 32), (128, 1, 12, 16), (64, 1, 16, 64)])
 @pytest.mark.parametrize("call", ["decode", "prefill"])
 @pytest.mark.parametrize("dtype,code", KINDS)
@@ -63,6 +106,28 @@ def test_weights_carry_two_terms(vtlib, paged, dtype, code, call, d_head, kv_hea
     lens = [0, 1, 15, 16, 63, 200, 777, 3000, -1, 5000]
     c = MxCache(vtlib, lens, [1] * len(lens), code, dtype, kv_heads, d_head, page)
     check(vtlib, paged, c, call, c.rows(kv_heads * group))
+
+
+@pytest.mark.parametrize("call,rows", [("decode", [1] * 5), ("prefill", [3, 1, 4, 2, 6])])
+@pytest.mark.parametrize("d_head,group", [(64, 1), (128, 4), (128, 12)])
+@pytest.mark.parametrize("dtype,code", KINDS)
+def test_values_of_many_magnitudes(vtlib, paged, dtype, code, d_head, group, call, rows):
+    """Each position's values have a magnitude of their own, over as many powers of two as the type and the code have: in any order,
+    and growing all along."""
+    lo, hi = {("f16", "e4m3"): (-10, 12), ("bf16", "e4m3"): (-60, 12), ("f16", "int8"): (-14, 12), ("bf16", "int8"): (-60, 60)}[dtype, code]
+    c = MxCache(vtlib, [0, 37, 700, -1, 4000], rows, code, dtype, 2, d_head, 16)
+    live = c.live[:, None, :, None]
+    std = c.v.double().masked_fill(~live, 0.0)
+    q = c.rows(2 * group)
+    set_values(c, 1, std * torch.exp2(torch.randint(lo, hi, c.live.shape, generator=c.gen, device="cuda").double())[:, None, :, None])
+    check(vtlib, paged, c, call, q)
+    grown = std.clone()
+    for b, (p, r) in enumerate(zip(c.lens_host, c.rows_host)):
+        if p >= 0:
+            page, off = c.positions(b, p + r)
+            grown[page, :, off] *= torch.exp2(torch.linspace(lo, hi, p + r, dtype=torch.float64, device="cuda").floor())[:, None, None]
+    set_values(c, 1, grown)
+    check(vtlib, paged, c, call, q)
 
 
 @pytest.mark.parametrize("d_head,heads", [(64, 4), (128, 4), (128, 12)])
