@@ -60,9 +60,9 @@ constexpr int kPdSoloUnits = 2;              // (see kSoloSteps)
 // Codes: parts that are joined by several threads an item (131,000 positions, 38 parts a head, 57.7 us by one, 54.9 by several;
 // 64 ragged sequences, 2 to 3 parts, 38.3 and 39.8: the longer code comes from far away).
 constexpr int kPdManyParts = 8;
-// Codes: units begin at kPdLeastScale.  Where columns have their own, V's scales are kept times 2^kPdShift and weights over the
+// Codes: units begin at the least scale that an entry may have.  Where columns have their own, V's scales are kept times 2^kPdShift and weights over the
 // unit times 2^-kPdShift, so that neither a weight of 2^15 over the least unit nor a scale of 2^119 passes the largest fp32 number.
-constexpr float kPdLeastScale = 0x1p-100f;
+constexpr float kPdLeastScale = 0x1p-117f;
 constexpr int kPdShift = 6;
 
 template <class Src, int DH, int NT>

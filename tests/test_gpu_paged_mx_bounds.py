@@ -130,6 +130,37 @@ def test_values_of_many_magnitudes(vtlib, paged, dtype, code, d_head, group, cal
     check(vtlib, paged, c, call, q)
 
 
+@pytest.mark.parametrize("call", ["decode", "prefill"])
+@pytest.mark.parametrize("bits", [20.3, 25.6, 27.1])
+@pytest.mark.parametrize("dtype,code,value", [(*k, 1.0) for k in KINDS] + [("bf16", "e4m3", 2.0 ** -111), ("bf16", "int8", 2.0 ** -111),
+                                                                          ("bf16", "int8", 2.0 ** 100), ("f16", "e4m3", 2.0 ** -9)])
+def test_many_small_weights_add_up(vtlib, paged, dtype, code, value, bits, call):
+    """One key takes nearly all the weight and its value is 0; 40,000 others have 2^-bits of it each and one value, so that the output
+    is their sum alone.  A weight loses 2^-22 of itself or 2^-37 of the largest, and meets the value exactly or, as the bound has
+    it, twice.  Scores of up to 40 log2 units carry 2^-24 of that as fp32 values, two roundings each, 2^-17 of a weight; at most 2504
+    products are added in a row, 2^-23 of their sum each, and 1400 sums of weights, 2^-24 each: less than 2^-11."""
+    n, seqs = 40000, 38
+    c = MxCache(vtlib, [n], [1], code, dtype, 8, 64, 64)
+    live, at = c.live[:, None, :, None], entry(c, 0, 777)
+    k, v = torch.zeros_like(c.k, dtype=torch.float64), torch.zeros_like(c.v, dtype=torch.float64)
+    k[at[0], :, at[2], 0] = 1.0
+    v.masked_fill_(live, value)
+    v[at] = 0.0
+    set_values(c, 0, k)
+    set_values(c, 1, v)
+    assert (c.v.double() == v).masked_select(live.expand_as(v)).all() and (c.k.double() == k).masked_select(live.expand_as(k)).all()
+    # as many sequences, on the same pages, as leave each CTA whole histories
+    c.tables, c.lens, c.n_rows = c.tables.repeat(seqs, 1), c.lens.repeat(seqs), seqs
+    c.starts = torch.arange(seqs + 1, dtype=torch.int32, device="cuda")
+    q = torch.zeros(seqs, 16, 64, dtype=TYPE[dtype], device="cuda")
+    q[:, :, 0] = 1.0
+    out = torch.full_like(q, 7.0)
+    attend(vtlib, paged, c, call, q, out, bits * math.log(2.0), 0)
+    ref = n * 2.0 ** -bits / (1.0 + n * 2.0 ** -bits) * value
+    tol = (U[dtype] + 2.0 ** -11 + 2.0 ** -17 + 2.0 ** -22) * ref + n * 2.0 ** -36 * value + TINY[dtype]
+    assert ((out.double() - ref).abs() <= tol).all(), float(((out.double() - ref).abs() / tol).max())
+
+
 @pytest.mark.parametrize("d_head,heads", [(64, 4), (128, 4), (128, 12)])
 @pytest.mark.parametrize("each", [1, 3])
 @pytest.mark.parametrize("dtype,code", KINDS)
