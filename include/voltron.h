@@ -680,8 +680,8 @@ typedef enum { VT_ROPE_HALVES = 0, VT_ROPE_NEIGHBOURS = 1 } vt_rope_pairs; /* (i
  *   x = x / sqrt(mean(x^2) + eps) * gain     with a gain; NULL: x stays
  *   (a, b) = (a cos - b sin, b cos + a sin)  for each pair i of the first rotary_dim dimensions, with
  *                                            (cos, sin) = rope[position][i]; the others stay
- * The sum of squares has 32 bits: a bf16 head with magnitudes past 2^60 has no norm.  Values v are left as
- * they are.  Gains and rope are read by the kernels of each call. */
+ * A head of any finite magnitudes has its norm; one of zeros has none with eps 0 (NaN).  Values v are left
+ * as they are.  Gains and rope are read by the kernels of each call. */
 typedef struct {
     const void *q_gain, *k_gain; /* device [d_head] of the rows' dtype, 16-byte aligned, or NULL */
     const float* rope;           /* device fp32 [rope_len][rotary_dim / 2][2]; not used with rotary_dim 0 */

@@ -20,15 +20,32 @@ namespace vt {
 // shared memory and serve all its passes.
 //
 // What bounds it: for prompts bytes (as for the plain append), and behind them the registers, which leave 24 warps an SM.  7
-// prompts of 300 to 2500 rows, 32 query and 8 KV heads of 128, with norms and full rotation: 35.3 us, 5250 GB/s (16 bits) and
-// 35.3 us (e4m3); without either 32.  With a lane for 8 dimensions and the pairs' other halves by shuffles it took 50 and 53,
+// prompts of 300 to 2500 rows, 32 query and 8 KV heads of 128, with norms and full rotation: 35.8 us, 5180 GB/s (16 bits, bf16) and
+// 34.8 us (e4m3, fp16); without either 32.  With a lane for 8 dimensions and the pairs' other halves by shuffles it took 50 and 53,
 // with the four numbers in registers and 16 warps 36.8 and 37.1.  For single tokens the chain starts, lengths, table,
 // rotation.
 constexpr int kQkWarps = 8, kQkCtas = 3;
 
-// One row's queries, or its keys and values, from head `at` (of this lane) on: `batches` times PASSES passes.
-template <class T, int DH, int F, bool NEIGH, int PASSES, bool OF_Q>
-__device__ __forceinline__ void qk_heads(const PagedQkArgs& a, ulonglong2 (*coef)[DH / 16], int row, int at, int batches) {
+// Squares of bf16 values go past what 32 bits hold.  A head whose sum of squares is below kQkSquares, or above 1 over it, is far: its
+// values are multiplied by a power of two first, and eps by its square, which the norm takes out again.  That is done for all far
+// heads of a warp after its others (in line it cost the prompts 2.5 us more, by registers; as it is 1.2).
+constexpr float kQkSquares = 0x1p-40f;
+// The power that brings the larger of a far head's largest magnitude and eps's root to 1 .. 2 (or is 2^127, or 2^-126); 1 for what is
+// not finite.
+template <int LPH>
+__device__ __forceinline__ float qk_power(const float (&y)[16], float eps) {
+    uint32_t most = __float_as_uint(sqrtf(eps));
+#pragma unroll
+    for (int e = 0; e < 16; ++e) most = max(most, __float_as_uint(y[e]) & 0x7fffffffu);
+#pragma unroll
+    for (int o = LPH / 2; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+    return most < 0x7f800000u ? __uint_as_float((uint32_t)max(1, 254 - (int)(most >> 23)) << 23) : 1.f;
+}
+
+// One row's queries, or its keys and values, from head `at` (of this lane) on: `batches` times PASSES passes.  Those in which a
+// lane's head is far are left out and set in its word `far`; FAR: those alone.
+template <class T, int DH, int F, bool NEIGH, int PASSES, bool OF_Q, bool FAR>
+__device__ __forceinline__ void qk_heads(const PagedQkArgs& a, ulonglong2 (*coef)[DH / 16], uint32_t* far, int row, int at, int batches) {
     constexpr int LPH = DH / 16, HPW = 32 / LPH, NB = DH / kMxBlock;
     constexpr bool MX = F >= 0 && !OF_Q;
     using E = Elem<T>;
@@ -119,22 +136,39 @@ __device__ __forceinline__ void qk_heads(const PagedQkArgs& a, ulonglong2 (*coef
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) {  // (every lane takes part in the shuffles)
             const int h = h0 + i * HPW;
-            const bool formed = OF_Q || h < K, here = h < heads;
+            const bool formed = OF_Q || h < K;
+            bool here = h < heads;
             const int c0 = formed ? side : 2 * s, c1 = formed ? other : 2 * s + 1;
             float y[16];
             unpack(x[i][0], y);
             unpack(x[i][1], y + 8);
             float inv = 1.f;
             if (norm) {
-                uint64_t sum = f2_mul(f2_pack(y[0], y[1]), f2_pack(y[0], y[1]));
+                auto squares = [&]() {
+                    uint64_t sum = f2_mul(f2_pack(y[0], y[1]), f2_pack(y[0], y[1]));
 #pragma unroll
-                for (int e = 2; e < 16; e += 2) sum = f2_fma(f2_pack(y[e], y[e + 1]), f2_pack(y[e], y[e + 1]), sum);
-                float ss, s1;
-                f2_unpack(sum, ss, s1);
-                ss += s1;
+                    for (int e = 2; e < 16; e += 2) sum = f2_fma(f2_pack(y[e], y[e + 1]), f2_pack(y[e], y[e + 1]), sum);
+                    float ss, s1;
+                    f2_unpack(sum, ss, s1);
+                    ss += s1;
 #pragma unroll
-                for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-                const float ms = fmaf(ss, 1.f / DH, a.eps), r = rsqrtf(ms);
+                    for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+                    return ss;
+                };
+                float ss = squares(), eps = a.eps;
+                if (!FAR && std::is_same<T, __nv_bfloat16>::value && formed && here && !(ss >= kQkSquares && ss <= 1.f / kQkSquares)) {
+                    *far |= 1u << ((h - at) / HPW);
+                    here = false;
+                }
+                if (FAR) {
+                    here = (*far >> ((h - at) / HPW)) & 1u;
+                    const float f = qk_power<LPH>(y, eps);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) y[e] *= f;
+                    eps = eps * f * f;
+                    ss = squares();
+                }
+                const float ms = fmaf(ss, 1.f / DH, eps), r = rsqrtf(ms);
                 // one step of Newton's method: what the root is off by, all of the head's values are, next to borders of codes too
                 inv = ms < INFINITY ? fmaf(0.5f * r, fmaf(-ms * r, r, 1.f), r) : r;
             }
@@ -217,11 +251,25 @@ __device__ __forceinline__ void qk_heads(const PagedQkArgs& a, ulonglong2 (*coef
     }
 }
 
+template <class T, int DH, int F, bool NEIGH, bool OF_Q>
+__device__ __noinline__ void qk_far(const PagedQkArgs& a, ulonglong2 (*coef)[DH / 16], uint32_t* far, int row, int at, int passes) {
+    qk_heads<T, DH, F, NEIGH, 1, OF_Q, true>(a, coef, far, row, at, passes);
+}
+// All heads of a warp.
+template <class T, int DH, int F, bool NEIGH, int PASSES, bool OF_Q>
+__device__ __forceinline__ void qk_warp(const PagedQkArgs& a, ulonglong2 (*coef)[DH / 16], uint32_t* far, int row, int at, int batches) {
+    qk_heads<T, DH, F, NEIGH, PASSES, OF_Q, false>(a, coef, far, row, at, batches);
+    if constexpr (std::is_same<T, __nv_bfloat16>::value)
+        if (__any_sync(0xffffffffu, *far != 0u)) qk_far<T, DH, F, NEIGH, OF_Q>(a, coef, far, row, at, batches * PASSES);
+}
+
 // A row's warps: its queries', then its keys' and values', of `batches` times PASSES passes each at most.
 template <class T, int DH, int F, bool NEIGH, int PASSES>
 __global__ void __launch_bounds__(kQkWarps * 32, kQkCtas) k_paged_append_qk(const __grid_constant__ PagedQkArgs a) {
     constexpr int HPW = 32 / (DH / 16), HPB = HPW * PASSES;  // heads of a batch
     __shared__ ulonglong2 coef[kQkWarps][8][DH / 16];
+    __shared__ uint32_t far[kQkWarps * 32];
+    far[threadIdx.x] = 0u;
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31;
@@ -232,10 +280,10 @@ __global__ void __launch_bounds__(kQkWarps * 32, kQkCtas) k_paged_append_qk(cons
     const int w = (int)(gw - (int64_t)row * (q_warps + kv_warps)), sub = lane / (DH / 16);
     if (w < q_warps) {
         const int from = w * HPB * a.batches;
-        qk_heads<T, DH, F, NEIGH, PASSES, true>(a, coef[threadIdx.x >> 5], row, from + sub, min(a.batches, (a.n_heads - from + HPB - 1) / HPB));
+        qk_warp<T, DH, F, NEIGH, PASSES, true>(a, coef[threadIdx.x >> 5], &far[threadIdx.x], row, from + sub, min(a.batches, (a.n_heads - from + HPB - 1) / HPB));
     } else {
         const int from = (w - q_warps) * HPB * a.batches;
-        qk_heads<T, DH, F, NEIGH, PASSES, false>(a, coef[threadIdx.x >> 5], row, from + sub, min(a.batches, (2 * a.c.n_kv_heads - from + HPB - 1) / HPB));
+        qk_warp<T, DH, F, NEIGH, PASSES, false>(a, coef[threadIdx.x >> 5], &far[threadIdx.x], row, from + sub, min(a.batches, (2 * a.c.n_kv_heads - from + HPB - 1) / HPB));
     }
 }
 
