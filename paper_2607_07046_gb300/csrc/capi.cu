@@ -126,6 +126,7 @@ cudaError_t init_library() {
 // The paged kernels are set up by the first vt_paged_create: a process that has none does not load them.
 std::once_flag g_init_paged_once;
 cudaError_t g_init_paged_err = cudaSuccess;
+cudaError_t g_init_codes_err[2] = {cudaSuccess, cudaSuccess};  // by vt_mx_format: the calls over such pools say it
 
 cudaError_t init_paged() {
     std::call_once(g_init_paged_once, [] {
@@ -133,9 +134,10 @@ cudaError_t init_paged() {
         if (g_init_paged_err != cudaSuccess) return;
         g_init_paged_err = init_paged_decode();
         if (g_init_paged_err != cudaSuccess) return;
-        for (cudaError_t e : {init_paged_decode_e4m3(), init_paged_decode_int8()})
-            if (e != cudaSuccess) g_init_paged_err = e;
-        if (g_init_paged_err != cudaSuccess) return;
+        g_init_codes_err[VT_MX_E4M3] = init_paged_decode_e4m3();
+        g_init_codes_err[VT_MX_INT8] = init_paged_decode_int8();
+        for (cudaError_t e : g_init_codes_err)
+            if (e != cudaSuccess) cudaGetLastError();  // not the next call's
         init_paged_prefill();  // (the calls that need it say when it cannot run)
         init_paged_prefill_e4m3();
         init_paged_prefill_int8();
@@ -2600,6 +2602,7 @@ extern "C" vt_status vt_paged_decode_mx(vt_paged* g, const vt_paged_mx_pool* poo
     PagedAttnArgs a{};
     VT_TRY(paged_attn_mx(g, pool, batch, batch ? batch->n_seqs : 0, n_heads, q, q_ld, scale, window, out, out_ld, &a));
     if (a.n_rows == 0) return ok();
+    VT_CUDA(g_init_codes_err[pool->format]);
     VT_CUDA(launch_decode_mx(a, pool, (cudaStream_t)stream));
     return ok();
 }
@@ -2612,6 +2615,7 @@ extern "C" vt_status vt_paged_prefill_mx(vt_paged* g, const vt_paged_mx_pool* po
     if (a.n_rows == 0 || batch->n_seqs == 0) return ok();
     const PagedWay way = paged_way(&a, batch->n_seqs, g->over);
     const bool e4m3 = pool->format == VT_MX_E4M3;
+    if (way.tokens) VT_CUDA(g_init_codes_err[pool->format]);
     if (const char* e = !way.tiles ? nullptr : e4m3 ? paged_tiles_error_e4m3() : paged_tiles_error_int8()) return fail(VT_ERR_CUDA, "%s", e);
     cudaStream_t st = (cudaStream_t)stream;
     if (way.tokens) VT_CUDA(launch_decode_mx(a, pool, st));
