@@ -64,10 +64,15 @@ constexpr int kPdManyParts = 8;
 // unit times 2^-kPdShift, so that neither a weight of 2^15 over the least unit nor a scale of 2^119 passes the largest fp32 number.
 constexpr float kPdLeastScale = 0x1p-117f;
 constexpr int kPdShift = 6;
+// int8 codes of bf16 rows have scales up to 2^119, and a score's sum without its scales goes up to 2^25 (queries below 2^11, 128 codes
+// up to 127): the scales of K are then kept times 2^-kPdKeyShift, and the factor of the scores times 2^kPdKeyShift; not where a query is
+// past 2^kPdLargeQuery, whose factor is large itself.
+constexpr int kPdKeyShift = 17, kPdLargeQuery = 90;
 
 template <class Src, int DH, int NT>
 struct PdGeom {
     static constexpr bool kMx = Src::kMx;
+    static constexpr bool kWideKeys = Src::kWide;
     static constexpr int kCtas = 2;                                                // an SM
     static constexpr int kKeys = kMx ? 32 : 16;                                  // positions of a step
     static constexpr int kRow = DH * Src::kBytes;                                // bytes of a K or V row
@@ -486,6 +491,8 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
         float unit[NT], least = kPdLeastScale;
 #pragma unroll
         for (int x = 0; x < NT; ++x) unit[x] = kPdLeastScale;
+        float k_by = 1.f;  // codes: what K's scales are multiplied by
+        bool large = false;
         int last_key[NT];  // of this lane's columns, in the steps' keys
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -525,10 +532,17 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
                         }
                     // (not infinite: its product with a score of 0 is 0)
                     if (x < NT) qs[x] = fminf(a.scale_log2 * __uint_as_float((uint32_t)(127 - up) << 23), 3.4028235e38f);
+                    large |= -up >= kPdLargeQuery;
                 }
             }
             if (x < NT) last_key[x] = ROWS ? at.s.len + (c0 + g + 8 * x) / a.group : 0;
         }
+        if constexpr (G::kWideKeys)  // room for 2^25 times the largest scale, but not where a score's factor has none
+            if (!__any_sync(0xffffffffu, large)) {
+                k_by = pd_power(-kPdKeyShift);
+#pragma unroll
+                for (int x = 0; x < NT; ++x) qs[x] = fminf(qs[x] * pd_power(kPdKeyShift), 3.4028235e38f);
+            }
         float m[NT], l[NT], o[DH / 16][NT][4];
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
@@ -599,7 +613,7 @@ __global__ void __launch_bounds__(kPdThreads, PdGeom<Src, DH, NT>::kCtas) k_page
                 for (int j = 0; j < PASSES; ++j) {
                     const int i = (32 * j + lane) % WORDS, at = i % (WORDS / 2);
                     const bool of_v = i >= WORDS / 2;
-                    const float by = !of_v ? 1.f : ROWS ? pd_power(kPdShift) : pd_inverse(unit[0]);
+                    const float by = !of_v ? k_by : ROWS ? pd_power(kPdShift) : pd_inverse(unit[0]);
                     const uint32_t to = fs + (uint32_t)(of_v ? KEYS * NB * 4 : 0);
                     if (NB == 4) {
 #pragma unroll

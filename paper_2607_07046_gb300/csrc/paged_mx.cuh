@@ -103,7 +103,7 @@ __device__ __forceinline__ float mx_scale(uint32_t w, int b) {
 template <class E>
 struct PoolPlain {
     using T = E;
-    static constexpr bool kMx = false;
+    static constexpr bool kMx = false, kWide = false;
     static constexpr int kBytes = 2;  // of a value
 };
 template <class E, int F>
@@ -112,6 +112,7 @@ struct PoolMx {
     using C = MxCodes<E, F>;
     using H = MxCodes<__half, F>;
     static constexpr bool kMx = true;
+    static constexpr bool kWide = F == VT_MX_INT8 && std::is_same<E, __nv_bfloat16>::value;  // scales up to 2^119
     static constexpr int kBytes = 1;
 };
 

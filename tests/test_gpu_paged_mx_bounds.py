@@ -130,6 +130,20 @@ def test_values_of_many_magnitudes(vtlib, paged, dtype, code, d_head, group, cal
     check(vtlib, paged, c, call, q)
 
 
+@pytest.mark.parametrize("call,rows", [("decode", [1] * 4), ("prefill", [3, 1, 4, 2])])
+@pytest.mark.parametrize("d_head,group", [(64, 1), (128, 4), (128, 12)])
+@pytest.mark.parametrize("power", [-110, -60, 60, 100, 115, 122])
+def test_keys_and_queries_of_far_magnitudes(vtlib, paged, power, d_head, group, call, rows):
+    """bf16 keys in int8 far from 1, and queries as far on the other side: scores are what they are at 1, whatever a part of them is
+    on the way.  (Beside them a query of zeros, whose magnitude is the smallest.)"""
+    c = MxCache(vtlib, [0, 37, 700, 4000], rows, "int8", "bf16", 2, d_head, 16)
+    live = c.live[:, None, :, None]
+    set_values(c, 0, (c.k.double().masked_fill(~live, 0.0) * 2.0 ** power).clamp(-(2.0 ** 126), 2.0 ** 126))
+    q = c.rows(2 * group).mul_(2.0 ** -power)
+    q[-1, -1] = 0.0
+    check(vtlib, paged, c, call, q)
+
+
 @pytest.mark.parametrize("call", ["decode", "prefill"])
 @pytest.mark.parametrize("bits", [20.3, 25.6, 27.1])
 @pytest.mark.parametrize("dtype,code,value", [(*k, 1.0) for k in KINDS] + [("bf16", "e4m3", 2.0 ** -111), ("bf16", "int8", 2.0 ** -111),
