@@ -703,12 +703,13 @@ VT_API vt_status vt_paged_append_qk(vt_paged* paged, const vt_paged_pool* pool, 
  * stands for 2^(s - 127), and a value is code * 2^(s - 127).  Codes are e4m3 floats (largest 448) or
  * whole numbers in two's complement (-127 .. 127).
  * The append takes the least power of two with which the largest code is at least as large as every
- * magnitude of the 32, so nothing saturates, and rounds to the nearest code, ties to even.  Powers
- * stay where every value of an entry is one of the rows' type: in [-15, 7] (e4m3) and [-24, 9] (int8)
- * for fp16, [-117, 7] and [-117, 119] for bf16; magnitudes past the largest (57344; 65024 or 127 2^119)
- * become it.  32 dimensions with an infinity or a NaN are stored as NaN (s = 255, codes 0).  A pool
- * that another program fills may hold any codes but e4m3's NaN, any scales in those ranges, and 255
- * for NaN. */
+ * magnitude of the 32, and rounds to the nearest code, ties to even.  Powers stay in [-15, 7] (e4m3) and
+ * [-24, 9] (int8) for fp16 rows, [-117, 7] and [-117, 119] for bf16 rows: there every value of an entry is
+ * one of the rows' type.  e4m3 under bf16 rows could go further up by its format; the calls that read the
+ * pool do not.  So magnitudes past 57344 (e4m3), 65024 (int8, fp16) and 127 2^119 (int8, bf16) become that
+ * value, also where the rows' type has larger ones.  32 dimensions with an infinity or a NaN are stored as
+ * NaN (s = 255, codes 0).  A pool that another program fills may hold any codes but e4m3's NaN, any scales
+ * in those ranges, and 255 for NaN. */
 typedef enum { VT_MX_E4M3 = 0, VT_MX_INT8 = 1 } vt_mx_format;
 typedef struct {
     void *k, *v;                 /* codes, a byte each; entry (page, head, position) as in vt_paged_pool */
@@ -733,9 +734,10 @@ VT_API vt_status vt_paged_append_mx(vt_paged* paged, const vt_paged_mx_pool* poo
 
 /* vt_paged_decode_mx, vt_paged_prefill_mx (Section 2.1, decode and prefill phases): as vt_paged_decode and
  * vt_paged_prefill, over a pool in 8 bits.  K and V are the values that the entries stand for, exactly.
- * Weights of single tokens, and of a sequence's few rows, meet the codes in fp16 with the scale of their
- * value, as two terms (22 bits), and lose at most 2^-37 of the row's largest weight times twice the largest
- * value that it attends to; with more rows they are rounded to the rows' type as over a pool in 16 bits. */
+ * Single tokens, and a sequence's few rows, meet the codes in fp16.  Of a bf16 query each dimension loses at
+ * most 2^-35 of its head's largest.  Weights have two terms (22 bits) and lose at most 2^-37 of the row's
+ * largest weight times twice the largest value that it attends to.  Weights of more rows are rounded to the
+ * rows' type, as over a pool in 16 bits. */
 VT_API vt_status vt_paged_decode_mx(vt_paged* paged, const vt_paged_mx_pool* pool, const vt_paged_batch* batch,
                                     int32_t n_heads, const void* q, int64_t q_ld, float scale, int32_t window,
                                     void* out, int64_t out_ld, vt_stream stream);

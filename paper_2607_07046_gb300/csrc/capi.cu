@@ -2395,6 +2395,10 @@ PagedWay paged_way(PagedAttnArgs* a, int n_seqs, int* over) {
     // rows behind 4000 in one of 64 slots, group of 4, 238 and 66 us; 3000 rows in one of 128 slots, no group, 1245 and 138;
     // 300 rows behind 4000 beside 63 tokens, 346 and 248.  Where the second finds nothing it costs 2 to 5 us: 32 sequences
     // of 4 rows 56 and 59, 256 of one row 171 and 175.  With 64 columns altogether a prompt hides four tiles at most.)
+    // Pools in 8 bits go by the same rule, in the 16-bit kernel's steps.  (e4m3 and fp16, tokens' kernel and tiles: 24 rows of
+    // 32 heads behind 300, 16 sequences, 52 and 56 us; 12 rows of 8 KV heads of 4 behind 2000, 16 sequences, 72 and 55; 4 rows,
+    // 32 sequences, 54 and 97; one sequence: 50 rows behind 1000 21 and 30, 77 behind 300 18 and 20, 30 behind 5000 35 and 28;
+    // 150 behind 300, which the rule gives to the tiles, 18 and 32.  int8 and bf16 the same within 10%.)
     constexpr int kFewColumns = 24, kFewSteps = 32, kFewAltogether = 64;
     const int64_t columns = (int64_t)a->n_rows * a->group;
     const bool few = columns <= (int64_t)kFewColumns * n_seqs;

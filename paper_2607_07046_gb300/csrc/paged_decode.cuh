@@ -33,13 +33,13 @@
 // bf16 queries become fp16 times a power of two of their row.  Weights have two terms, 22 bits (one, for bf16 rows, left outputs
 // 9e-4 of their size off beside their own rounding, two 7e-5, for 1 us of 55 on the long history below).  m moves only when P would
 // pass 2^15, down to 2^12, so that a weight loses at most 2^-37 of the largest one, times the largest value.  What it costs beside
-// the 16-bit pool's kernel are the conversions: 350 instructions a 16 positions and warp, which fit beside the copies at the
+// the 16-bit pool's kernel are the conversions: 390 instructions a 16 positions and warp, which fit beside the copies at the
 // memory's rate.
 //
 // Measured: one history of 131,000 positions, 8 KV heads of 4, dh 128: 92 us, 5830 GB/s (86% of a copy's rate: the
 // start, the last steps and the join of 38 parts a head are the rest); 64 sequences of up to 8191, some idle: 47 us, 5310
 // GB/s; 16 of 500 to 4096 with 32 KV heads and a window of 1024: 46 us, 5290 GB/s; 128 positions of 8 heads: 5.6 us, all
-// of it latency (lengths, table, first rows, merge).  Codes: 55 us (e4m3, bf16), 39 and 38 us on the same three; from 131,000 to
+// of it latency (lengths, table, first rows, merge).  Codes: 56 us (e4m3, bf16), 39 and 40 us on the same three; from 131,000 to
 // 524,000 positions each further position comes at 7100 GB/s, and 18 us are start, merge and join.
 #pragma once
 
@@ -57,8 +57,9 @@ namespace vt {
 constexpr int kPdWarps = 4, kPdThreads = kPdWarps * 32;
 constexpr int kPdRing = 96 * 1024;           // bytes of the four warps' rings, at most
 constexpr int kPdSoloUnits = 2;              // (see kSoloSteps)
-// Codes: parts that are joined by several threads an item (131,000 positions, 38 parts a head, 57.7 us by one, 54.9 by several;
-// 64 ragged sequences, 2 to 3 parts, 38.3 and 39.8: the longer code comes from far away).
+// Codes: parts that are joined by several threads an item (fp16; 130,000 positions, 38 parts a head, 66.0 us by one, 63.1 by
+// several; 9 parts 56.7 and 56.3, 57.6 and 57.0; 5 parts 59.4 and 59.7; 64 ragged sequences, 2 to 3 parts, 40.9 and 41.9: the longer
+// code comes from far away).
 constexpr int kPdManyParts = 8;
 // Codes: units begin at the least scale that an entry may have.  Where columns have their own, V's scales are kept times 2^kPdShift and weights over the
 // unit times 2^-kPdShift, so that neither a weight of 2^15 over the least unit nor a scale of 2^119 passes the largest fp32 number.
@@ -88,12 +89,14 @@ struct PdGeom {
     static constexpr int kUnitCost = 256 / kKeys;
     // What a CTA takes at least: where the largest unit costs no more than kWhole (16 bits: 12 steps), that much, so that few
     // are split and joined (8 heads of 128 positions: 5.4 us, split 6.7; at 48, units of 20 to 30 steps lost up to 2 us);
-    // otherwise kMinSteps.
+    // otherwise kMinSteps.  (Codes, steps of 32: 8 heads of 128 positions 6.2 both ways, of 400 9.7 and 9.5 split, 30 sequences of 800
+    // 22.6 and 22.4: it does not count there.)
     static constexpr int kMinSteps = 256 / kKeys, kWhole = 448 / kKeys;
     // Where the largest unit has no more steps than kSoloSteps and there are kPdSoloUnits or more such units for every CTA,
     // each warp has units of its own: merging four warps would cost more than the steps.  Measured (16 bits), merged and alone:
     // 168 sequences of 1 to 3 positions, 32 heads, 38 and 15 us; 1024 sequences of 61 to 65 positions, 8 KV heads, 87 and 56;
     // 24 sequences of 201 to 251, 32 heads, 24 and 22.  At 32 steps 300 sequences of 21 to 501 positions lost (51 to 63).
+    // Codes (e4m3, fp16), merged and alone: the first three 58 and 21, 110 and 54, 24 and 21; at 16 steps the last 51 and 54.
     static constexpr int kSoloSteps = 256 / kKeys;
 };
 

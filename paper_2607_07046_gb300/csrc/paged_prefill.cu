@@ -14,7 +14,7 @@
 // tiles; the 2 x 128 x 128 exponentials take as long on the SM's special-function units.  In fact one tile's
 // chain, softmax (2200 cycles) and then P to V, S and its notice (2350), takes about 5000 cycles a block, of
 // which the two tiles hide half from each other.  Measured: 4096 rows, 32 heads, dh 128: 170 us, 810 TFLOP/s
-// (42% of what a matrix product reaches); 512 rows behind 16000, 8 KV heads of 4: 156 us, 870; 5 prompts of
+// (42% of what a matrix product reaches); 512 rows behind 16000, 8 KV heads of 4: 154 us, 885; 5 prompts of
 // 150 to 900 rows: 42 us, of which a CTA's start takes 7.  One tile a CTA with two threads a row
 // took 171 and 147 us on the first two, but 55 on the third; 64-key halves were slower throughout.
 //
@@ -38,7 +38,7 @@
 // A CTA of 512 threads has 128 registers a thread, and all roles share the instruction cache: the softmax reads S twice, in
 // halves, and what can be a loop is one.  (4096 rows of int8 codes, bf16: 462 us with the 12 warps and unrolled, 310 with the
 // roles apart, 221 with the conversions a loop, 181 with the softmax's parts loops too; the 16-bit pool takes 168.)
-// Measured: 512 rows behind 16000, e4m3 and fp16: 152 us, which is the 16-bit pool's time.
+// Measured: 512 rows behind 16000, e4m3 and fp16: 151 us (the 16-bit pool 154); 7 prompts of 300 to 2500 rows 165.
 //
 // The blocks of all units form one line, and CTA c (one an SM) takes its c-th equal part, so neither few
 // long histories nor ragged prompts leave SMs idle; lengths are known on the device only.  A unit that
@@ -74,7 +74,6 @@ constexpr int kPfJoinParts = 5;
 constexpr int kPfJoinChunk = 2;
 constexpr int kPfLag = 2;        // copy groups in flight behind the one just issued
 
-
 template <class Src, int DH>
 struct PfGeom {
     // Warps: 8 of softmax, those of the copies, then one MMA warp a tile.  Codes: four warps convert them, so that each of the
@@ -82,9 +81,9 @@ struct PfGeom {
     static constexpr int kCopyWarps = Src::kMx ? 4 : 2, kMma = 8 + kCopyWarps;
     static constexpr int kThreads = Src::kMx ? 512 : 384;
     // Registers a thread: at launch 65536 / threads, rounded down to 8; then 2 x 128 threads of softmax, and 128 of copies and
-    // MMAs, or 128 of each.
+    // MMAs, or (codes) 128 of conversions and 128 of MMAs and copies.
     static constexpr int kLaunchRegs = Src::kMx ? 128 : 168, kSoftmaxRegs = Src::kMx ? 176 : 208, kCopyRegs = Src::kMx ? 72 : 88;
-    static constexpr int kMmaRegs = Src::kMx ? 88 : 88;
+    static constexpr int kMmaRegs = 88;
     static_assert(256 * kSoftmaxRegs + 128 * kCopyRegs + (kThreads - 384) * kMmaRegs <= kThreads * kLaunchRegs,
                   "the register split must fit in the registers the block is launched with");
     static constexpr int kTile = kPfRows * DH * 2;         // bytes of a Q tile, of a K or V block
@@ -971,7 +970,8 @@ __global__ void __launch_bounds__(PfGeom<Src, DH>::kThreads, 1) k_paged_prefill(
                 for (int q = 0; q < 4; ++q) mw[q] = fa_range_bits(cb - 32 * q, ce - 32 * q) & vw[q];
                 const bool plain = __all_sync(0xffffffffu, (mw[0] & mw[1] & mw[2] & mw[3]) == 0xffffffffu);
                 if constexpr (Src::kMx) {
-                    if (!plain) {  // hidden scores become -inf where they lie (a loop: less code, see pf_convert)
+                    if (!plain) {  // hidden scores become -inf where they lie (a loop: less code, see pf_convert; its masks
+                                   // worked out again, as a loop's index would put mw into memory)
 #pragma unroll 1
                         for (int q = 0; q < 4; ++q) {
                             const uint32_t on = fa_range_bits(cb - 32 * q, ce - 32 * q) & vw[q];
@@ -986,16 +986,15 @@ __global__ void __launch_bounds__(PfGeom<Src, DH>::kThreads, 1) k_paged_prefill(
                     }
                 }
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                auto arrived = [&](uint32_t(&v)[32], int q) {  // keys 32 q ..
-                    tc::tmem_ld_wait_on(v);
-                    if (!plain)
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (!((mw[q] >> e) & 1u)) v[e] = 0xff800000u;  // -inf
-                };
                 if constexpr (!Src::kMx) {
 #pragma unroll
-                    for (int q = 0; q < KEPT; ++q) arrived(sv[q], q);
+                    for (int q = 0; q < KEPT; ++q) {
+                        tc::tmem_ld_wait_on(sv[q]);
+                        if (!plain)
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!((mw[q] >> e) & 1u)) sv[q][e] = 0xff800000u;  // -inf
+                    }
 #pragma unroll
                     for (int e = 0; e < 32; e += 2)
 #pragma unroll

@@ -20,10 +20,11 @@ namespace vt {
 // shared memory and serve all its passes.
 //
 // What bounds it: for prompts bytes (as for the plain append), and behind them the registers, which leave 24 warps an SM.  7
-// prompts of 300 to 2500 rows, 32 query and 8 KV heads of 128, with norms and full rotation: 35.8 us, 5180 GB/s (16 bits, bf16) and
-// 34.8 us (e4m3, fp16); without either 32.  With a lane for 8 dimensions and the pairs' other halves by shuffles it took 50 and 53,
-// with the four numbers in registers and 16 warps 36.8 and 37.1.  For single tokens the chain starts, lengths, table,
-// rotation.
+// prompts of 300 to 2500 rows, 32 query and 8 KV heads of 128, with norms and full rotation: fp16 rows 34.8 us (16 bits, 5330 GB/s),
+// 34.8 (e4m3) and 36.4 (int8), bf16 rows, whose far heads are looked for, 35.8, 37.4 and 38.8; without either 32.  With a lane for
+// 8 dimensions and the pairs' other halves by shuffles it took 50 and 53, with the four numbers in registers and 16 warps 36.8
+// and 37.1.  The 80 registers do not hold all of it: the forms for many rows spill 8 to 64 bytes a thread.  For single
+// tokens the chain starts, lengths, table, rotation.
 constexpr int kQkWarps = 8, kQkCtas = 3;
 
 // Squares of bf16 values go past what 32 bits hold.  A head whose sum of squares is below kQkSquares, or above 1 over it, is far: its
@@ -288,7 +289,8 @@ __global__ void __launch_bounds__(kQkWarps * 32, kQkCtas) k_paged_append_qk(cons
 }
 
 // Few rows: a warp a pass, so that all loads are in flight at once.  Many: several passes a warp share the rotation,
-// the gains and the search for the sequence.  (The prompts above, 16 bits and e4m3: 4 passes twice
+// the gains and the search for the sequence.  (32 query and 8 KV heads of 128, a pass a warp and several: 2048 rows 20 and 15 us, 1024
+// 10.8 and 8.2; at 512 and below both take the call's own time, 8.  The prompts above, 16 bits and e4m3: 4 passes twice
 // 35.3 and 35.3 us, 4 once 35.4 and 39.2, 3 three times 37.1 and 37.3; 2 passes and 4 CTAs an SM 34.1 and 36.4 twice, 37.6 and 36.5
 // four times; 2 CTAs 38.)
 constexpr int kQkPasses = 4, kQkBatches = 2, kQkManyRows = 512;
