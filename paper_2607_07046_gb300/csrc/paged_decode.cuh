@@ -40,7 +40,7 @@
 // start, the last steps and the join of 38 parts a head are the rest); 64 sequences of up to 8191, some idle: 47 us, 5310
 // GB/s; 16 of 500 to 4096 with 32 KV heads and a window of 1024: 46 us, 5290 GB/s; 128 positions of 8 heads: 5.6 us, all
 // of it latency (lengths, table, first rows, merge).  Codes: 56 us (e4m3, bf16), 39 and 40 us on the same three; from 131,000 to
-// 524,000 positions each further position comes at 7100 GB/s, and 18 us are start, merge and join.
+// 524,000 positions each further position comes at 6800 to 6900 GB/s, and 15 us are start, merge and join.
 #pragma once
 
 #include <cuda_runtime.h>
